@@ -453,6 +453,100 @@ int32_t mrl_schedule(const mrl_table* tab, const mrl_coord* goal,
  * (either pointer may be NULL). */
 int32_t mrl_copy_dense(const mrl_table* tab, uint64_t* cost_host, uint16_t* argmin_host);
 
+/* ---------------------------------------------------------------------------
+ * The operators that Specs name, on data: a Matmul with bias, activation,
+ * dropout and residual in its epilogue (the MATMUL and FUSED Specs), its
+ * gradients, and dropout alone.
+ *
+ *   z   = lhs rhs + bias                       b x m x n, the sum over k
+ *   out = residual + D f(z)
+ *
+ * f: identity, ReLU, GELU in its tanh form, z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2,
+ * or SiLU, z / (1 + e^-z).  D drops elements: it is 0 where an element's 16
+ * random bits are below `drop` and 65536 / (65536 - drop) elsewhere, so drop = 0
+ * is no dropout and drop = 65536 leaves the residual alone; a dropped element is 0
+ * even where f(z) is not finite.  The random bits of element (i, j), i the row
+ * counted over all batches, are a function of seed, offset, i and j alone and are
+ * never stored: half j % 2 (0: the low one) of word (j % 8) / 2 of the Philox4x32
+ * block of seven rounds (Salmon, Moraes, Dror, Shaw, 2011) with key (seed's low
+ * word, high word) and counter (j / 8, i, offset's low word, offset's high word).
+ * So a gradient finds the same elements dropped, and dropout alone after a
+ * mrl_linear without it gives what mrl_linear with it gives.
+ *
+ * All sums, activations and statistics are f32 or wider and rounded once, to
+ * the type of what is stored.  (A product of bf16 operands is exact in f32; dz
+ * of a gradient is rounded to the operands' type before the two Matmuls that read it.)
+ * Every call gives the same bits for the same arguments.
+ *
+ * Matrices are in device memory.  Sizes of zero are allowed: a sum over nothing
+ * is 0.  The calls queue work on hip_stream of the current device and return;
+ * they do not synchronise, allocate or keep anything.  The workspace may be used
+ * by one call at a time; it need not be initialised. */
+typedef enum { MRL_F32 = 0, MRL_BF16 = 1 } mrl_dtype;             /* as the dtype bit of a Spec  */
+typedef enum { MRL_ROW_MAJOR = 0, MRL_COLUMN_MAJOR = 1 } mrl_layout;   /* as its layout coordinate */
+typedef enum { MRL_ACT_NONE = 0, MRL_ACT_RELU = 1, MRL_ACT_GELU = 2, MRL_ACT_SILU = 3 } mrl_activation;
+
+/* data: device, aligned to its element; NULL where the matrix is optional and not
+ * wanted.  ld: elements from a row to the next (column-major: from a column to
+ * the next); batch: from a batch to the next.  What is read may overlap itself (ld or
+ * batch of 0: the same row or matrix again), what is written may not. */
+typedef struct { void* data; uint32_t dtype, layout; int64_t ld, batch; } mrl_matrix;
+
+typedef struct {
+  uint32_t b, m, k, n;           /* b * m, and each size, below 2^31                               */
+  mrl_matrix lhs, rhs;           /* b x m x k and b x k x n: one type, either layout               */
+  mrl_matrix bias;               /* n neighbouring elements; optional                              */
+  mrl_matrix residual;           /* b x m x n, row-major; optional.  May be `out` itself           */
+  mrl_matrix out;                /* b x m x n, row-major                                           */
+  mrl_matrix pre;                /* z, b x m x n, row-major; optional: what a gradient needs of f  */
+  uint32_t activation, drop;
+  uint64_t seed, offset;
+} mrl_linear_desc;
+
+/* Bytes of workspace that mrl_linear needs for these sizes (0: none). */
+int32_t mrl_linear_bytes(const mrl_linear_desc* desc, size_t* bytes);
+
+/* MRL_E_INVAL on a malformed descriptor, MRL_E_NOMEM if the workspace (device,
+ * aligned to 256 bytes) is smaller than mrl_linear_bytes says. */
+int32_t mrl_linear(const mrl_linear_desc* desc, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Gradients of a loss, given `grad`, its gradient by out:
+ *   dz = D f'(z) grad;  d_lhs = dz rhs^T;  d_rhs = lhs^T dz;  d_bias = the sum of dz over batches and rows
+ * (by the residual it is grad itself).  Each of the three is optional.  ReLU's slope at 0 is 0.
+ * Where d_rhs.batch is 0 and b is not 1 (batches that share rhs), d_rhs is k x n, the sum over the batches. */
+typedef struct {
+  uint32_t b, m, k, n;
+  mrl_matrix grad;               /* b x m x n, row-major, f32 or bf16                              */
+  mrl_matrix lhs, rhs;           /* as given to mrl_linear; lhs is read for d_rhs, rhs for d_lhs   */
+  mrl_matrix pre;                /* z as mrl_linear stored it; not read where f is the identity    */
+  mrl_matrix d_lhs;              /* b x m x k, row-major                                           */
+  mrl_matrix d_rhs;              /* k x n or b x k x n, either layout                              */
+  mrl_matrix d_bias;             /* n neighbouring elements                                        */
+  uint32_t activation, drop;
+  uint64_t seed, offset;         /* those of the mrl_linear call                                   */
+} mrl_linear_grad_desc;
+
+int32_t mrl_linear_grad_bytes(const mrl_linear_grad_desc* desc, size_t* bytes);
+int32_t mrl_linear_grad(const mrl_linear_grad_desc* desc, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* out = residual + D x, m x n, row-major.  Its gradient by x is the same call on the
+ * gradient by out, without a residual.  out may be x or residual itself. */
+typedef struct {
+  uint32_t m, n;
+  mrl_matrix x, residual, out;   /* residual optional; batch is ignored                            */
+  uint32_t drop;
+  uint64_t seed, offset;
+} mrl_dropout_desc;
+int32_t mrl_dropout(const mrl_dropout_desc* desc, void* hip_stream);
+
+/* The operator of the Spec at x: sizes, types and layouts, strides of matrices without
+ * gaps, bias and activation (data stays NULL; a FUSED Spec's bias is marked by its type
+ * and a stride of 1).  For tables of MATMUL_ACCUM, MATMUL_PARALLEL, MATMUL_BOUNDED,
+ * MATMUL_MOVES, FUSED_MM_ADD_RELU and FUSED_BOUNDED; MRL_E_INVAL for others, for packed
+ * layouts, and where mrl_linear has no such operands (lhs and rhs of two types, an output
+ * that is column-major).  An accumulating Matmul's output is also the residual. */
+int32_t mrl_spec_linear(const mrl_table* tab, const mrl_coord* x, mrl_linear_desc* out);
+
 const char* mrl_last_error(void);
 
 #ifdef __cplusplus

@@ -6,6 +6,7 @@ fallback: importing works without a GPU, calling `solve` does not.
 """
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -21,7 +22,8 @@ OK, E_INVAL, E_NOMEM, E_HIP, E_RANGE, E_BUFSZ, E_OVERFLOW = 0, -1, -2, -3, -4, -
 
 EXPORTS = ["mrl_target_create", "mrl_target_destroy", "mrl_geometry", "mrl_table_bytes", "mrl_solve", "mrl_solve_graph",
            "mrl_table_destroy", "mrl_query", "mrl_query_noalloc", "mrl_query_compressed", "mrl_rewrite_decode", "mrl_coord_of_spec",
-           "mrl_emit_compressed", "mrl_schedule", "mrl_copy_dense", "mrl_last_error"]
+           "mrl_emit_compressed", "mrl_schedule", "mrl_copy_dense", "mrl_linear_bytes", "mrl_linear", "mrl_linear_grad_bytes",
+           "mrl_linear_grad", "mrl_dropout", "mrl_spec_linear", "mrl_last_error"]
 
 
 class MorelloError(RuntimeError):
@@ -305,6 +307,32 @@ class Table:
         _check(lib().mrl_coord_of_spec(self._h, sh, lv, ly, dt, C.byref(out)))
         return list(out.x[:len(self.extents)])
 
+    def apply(self, coord, lhs, rhs, bias=None, out=None, workspace=None):
+        """The operator of the Spec at `coord` on torch tensors of its sizes, layouts and types: a FUSED
+        Spec gives relu(lhs rhs + bias), a Matmul lhs rhs, added to `out` if that is given.  Runs
+        binding.linear; the program that the table found for the Spec is not what is run."""
+        x = _Coord()
+        for a, v in enumerate(coord):
+            x.x[a] = int(v)
+        raw = C.create_string_buffer(_LINEAR.size)
+        _check(lib().mrl_spec_linear(self._h, C.byref(x), raw))
+        spec = _LINEAR.unpack(raw.raw)
+        b, m, k, n = spec[:4]
+        codes = _dtype_codes()
+        for name, t, at, shape in (("lhs", lhs, 4, (b, m, k)), ("rhs", rhs, 9, (b, k, n))):
+            if tuple(t.shape) not in (shape, shape[1:] if b == 1 else shape):
+                raise MorelloError(E_INVAL, "%s has shape %s, the Spec's is %s" % (name, tuple(t.shape), shape))
+            if codes.get(t.dtype) != spec[at + 1]:
+                raise MorelloError(E_INVAL, "%s is %s, the Spec's is another type" % (name, t.dtype))
+            if min(shape[1:]) > 1 and _matrix(name, t)[2] != spec[at + 2]:
+                raise MorelloError(E_INVAL, "%s has another layout than the Spec's" % name)
+        fused = spec[17] != 0                    # the bias's stride
+        if fused == (bias is None):
+            raise MorelloError(E_INVAL, "a FUSED Spec takes a bias, a Matmul none")
+        dtype = next(d for d, c in codes.items() if c == spec[25])
+        return linear(lhs, rhs, bias, None if fused else out, activation="relu" if fused else "none", dtype=dtype,
+                      out=out, workspace=workspace)
+
     def boxes(self, which):
         """which: 0 decisions, 1 costs.  numpy structured array (BOX_DTYPE), sorted by lo."""
         n = C.c_size_t()
@@ -437,3 +465,246 @@ def solve_config(cfg, scratch_bytes=None):
     """Solve every lattice of a workloads.config() dict.  Returns (Target, {label: Table})."""
     target = Target(cfg["target"])
     return target, solve_lattices(target, cfg["lattices"], scratch_bytes=scratch_bytes)
+
+
+# ---- the operators that Specs name, on torch tensors
+
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+
+# the C structs: b, m, k, n, then matrices of (data, dtype, layout, ld, batch), then what the operator adds
+_LINEAR = struct.Struct("=4I" + "QIIqq" * 6 + "2I2Q")
+_LINEAR_GRAD = struct.Struct("=4I" + "QIIqq" * 7 + "2I2Q")
+_DROPOUT = struct.Struct("=2I" + "QIIqq" * 3 + "I4x2Q")
+_ABSENT = (0, 0, 0, 0, 0)
+_codes = None
+
+
+def _dtype_codes():
+    global _codes
+    if _codes is None:
+        import torch
+        _codes = {torch.float32: 0, torch.bfloat16: 1}
+    return _codes
+
+
+def _dtype(name, t):
+    code = _dtype_codes().get(t.dtype)
+    if code is None:
+        raise MorelloError(E_INVAL, "%s is %s: float32 and bfloat16 are what there is" % (name, t.dtype))
+    return code
+
+
+def _matrix(name, t):
+    """(data, dtype, layout, ld, batch) of a tensor of two or three dimensions, either layout."""
+    st, sh = t.stride(), t.shape
+    if len(sh) == 2:
+        (r, c), (rows, columns), batch = st, sh, 0
+    elif len(sh) == 3:
+        batch, r, c = st
+        _, rows, columns = sh
+    else:
+        raise MorelloError(E_INVAL, "%s has %d dimensions: two, or three with a batch" % (name, len(sh)))
+    if c == 1 and not (columns == 1 and r == 1):
+        layout, ld = 0, r
+    elif r == 1:
+        layout, ld = 1, c
+    elif columns <= 1:
+        layout, ld = 0, r
+    elif rows <= 1:
+        layout, ld = 1, c
+    else:
+        raise MorelloError(E_INVAL, "%s: neither the elements of a row nor those of a column are adjacent (strides %s)" % (name, st))
+    return t.data_ptr(), _dtype(name, t), layout, ld, batch
+
+
+def _rows(name, t, shape):
+    """The same of a row-major tensor of this shape."""
+    if t.shape != shape:
+        raise MorelloError(E_INVAL, "%s has shape %s, not %s" % (name, tuple(t.shape), tuple(shape)))
+    st = t.stride()
+    if st[-1] != 1 and shape[-1] > 1:
+        raise MorelloError(E_INVAL, "%s: the elements of a row are not adjacent (strides %s)" % (name, st))
+    return t.data_ptr(), _dtype(name, t), 0, st[-2], st[0] if len(st) == 3 else 0
+
+
+def _vector(name, t, n):
+    if t.shape != (n,) or (n > 1 and t.stride(0) != 1):
+        raise MorelloError(E_INVAL, "%s has shape %s and strides %s, not %d neighbouring elements" % (name, tuple(t.shape), t.stride(), n))
+    return t.data_ptr(), _dtype(name, t), 0, 1, 0
+
+
+def drop_threshold(p):
+    """The `drop` of a probability: the nearest multiple of 2^-16, times 2^16."""
+    if not 0.0 <= p <= 1.0:
+        raise MorelloError(E_INVAL, "dropout of %r is no probability" % (p,))
+    return int(p * 65536 + 0.5)
+
+
+def _activation(name):
+    if name not in ACTIVATIONS:
+        raise MorelloError(E_INVAL, "activation %r is not one of %s" % (name, ", ".join(ACTIVATIONS)))
+    return ACTIVATIONS[name]
+
+
+def _word(name, v):
+    if not 0 <= v < 1 << 64:
+        raise MorelloError(E_INVAL, "%s %r does not fit 64 bits" % (name, v))
+    return v
+
+
+class _On:
+    """The device and stream of a call.  All tensors are on one device, which is current while the call queues
+    its work; with `stream` the outputs and the workspace belong to that stream, and torch is told that it
+    uses the inputs (the caller orders it after whatever makes them)."""
+
+    def __init__(self, first, tensors, stream):
+        import torch
+        if not first.is_cuda:
+            raise MorelloError(E_INVAL, "tensors on %s: there is no CPU path" % first.device)
+        index = first.get_device()
+        for t in tensors:
+            if t is not None and t.get_device() != index:
+                raise MorelloError(E_INVAL, "tensors on %s and %s" % (first.device, t.device))
+        self._within = []
+        if stream is not None:
+            if stream.device.index != index:
+                raise MorelloError(E_INVAL, "the stream is on %s, the tensors on %s" % (stream.device, first.device))
+            self._within.append(torch.cuda.stream(stream))
+            for t in (first,) + tensors:
+                if t is not None:
+                    t.record_stream(stream)
+            self.stream = stream.cuda_stream
+        else:
+            if torch.cuda.current_device() != index:
+                self._within.append(torch.cuda.device(index))
+            self.stream = torch.cuda.current_stream(index).cuda_stream
+
+    def __enter__(self):
+        for w in self._within:
+            w.__enter__()
+        return self
+
+    def __exit__(self, *what):
+        for w in reversed(self._within):
+            w.__exit__(*what)
+
+
+def _workspace(n, given, like):
+    import torch
+    if n == 0:
+        return 0
+    if given is None:
+        return torch.empty(n, dtype=torch.uint8, device=like.device)
+    return given
+
+
+def _queue(desc, size_of, run, given, like, on):
+    """Ask for the workspace, then queue the call; a workspace of torch's may be freed when this returns (work on
+    its stream that uses the memory next comes after the call's)."""
+    n = C.c_size_t()
+    _check(size_of(desc, C.byref(n)))
+    ws = _workspace(n.value, given, like) if n.value else None
+    _check(run(desc, C.c_void_p(ws.data_ptr() if ws is not None else None),
+               C.c_size_t(ws.numel() * ws.element_size() if ws is not None else 0), C.c_void_p(on.stream)))
+
+
+def _operands(lhs, rhs):
+    """b, m, k, n and the two matrices; rhs without a batch is shared by lhs's batches."""
+    ml, mr = _matrix("lhs", lhs), _matrix("rhs", rhs)
+    ls, rs = lhs.shape, rhs.shape
+    if ls[-1] != rs[-2] or (len(rs) == 3 and (len(ls) != 3 or ls[0] != rs[0])):
+        raise MorelloError(E_INVAL, "lhs of shape %s does not go with rhs of shape %s" % (tuple(ls), tuple(rs)))
+    return (ls[0] if len(ls) == 3 else 1, ls[-2], ls[-1], rs[-1]), ml, mr
+
+
+def linear(lhs, rhs, bias=None, residual=None, *, activation="none", dropout=0.0, seed=0, offset=0, dtype=None, pre=False,
+           out=None, workspace=None, stream=None):
+    """out = residual + D f(lhs rhs + bias) (mrl_linear); with pre=True also z = lhs rhs + bias: (out, z).
+
+    lhs: m x k or b x m x k, rhs: k x n or b x k x n, both float32 or both bfloat16, either one row- or
+    column-major with any stride between lines (a weight matrix stored n x k is given as its .t()).
+    bias: n elements; residual: of out's shape.  activation: none, relu, gelu (tanh form), silu.
+    dropout: the probability that an element is dropped; seed and offset (64 bits each) say which are, together with
+    the element's row and column.  dtype: out's and z's type (lhs's if None); out: a tensor to write to, which may be
+    `residual`.  workspace: a uint8 tensor the caller keeps (linear_bytes); stream: where the work
+    is queued (the current stream if None).
+    """
+    import torch
+    sizes, ml, mr = _operands(lhs, rhs)
+    shape = lhs.shape[:-1] + rhs.shape[-1:]
+    with _On(lhs, (rhs, bias, residual, out, workspace), stream) as on:
+        if out is None:
+            out = torch.empty(shape, dtype=lhs.dtype if dtype is None else dtype, device=lhs.device)
+        elif dtype is not None and out.dtype != dtype:
+            raise MorelloError(E_INVAL, "out is %s, not %s" % (out.dtype, dtype))
+        z = torch.empty(shape, dtype=out.dtype, device=lhs.device) if pre else None
+        desc = _LINEAR.pack(*sizes, *ml, *mr, *(_ABSENT if bias is None else _vector("bias", bias, sizes[3])),
+                            *(_ABSENT if residual is None else _rows("residual", residual, shape)), *_rows("out", out, shape),
+                            *(_ABSENT if z is None else _rows("pre", z, shape)),
+                            _activation(activation), drop_threshold(dropout), _word("seed", seed), _word("offset", offset))
+        _queue(desc, lib().mrl_linear_bytes, lib().mrl_linear, workspace, lhs, on)
+    return (out, z) if pre else out
+
+
+def linear_grad(grad, lhs, rhs, bias=None, pre=None, *, activation="none", dropout=0.0, seed=0, offset=0, need_lhs=True,
+                need_rhs=True, workspace=None, stream=None):
+    """(d_lhs, d_rhs, d_bias) of binding.linear with these arguments, given `grad`, the gradient by its out, and
+    `pre`, the z that it returned (not needed without an activation): mrl_linear_grad.  Each has its operand's type,
+    d_rhs also its layout; None for an operand that is not needed, or a bias that is None.  The gradient
+    by the residual is `grad`."""
+    import torch
+    sizes, ml, mr = _operands(lhs, rhs)
+    shape = lhs.shape[:-1] + rhs.shape[-1:]
+    act = _activation(activation)
+    if act and pre is None:
+        raise MorelloError(E_INVAL, "the gradient of %s needs pre" % activation)
+    with _On(lhs, (grad, rhs, bias, pre, workspace), stream) as on:
+        d_lhs = torch.empty(lhs.shape, dtype=lhs.dtype, device=lhs.device) if need_lhs else None
+        d_rhs = None
+        if need_rhs and mr[2]:
+            d_rhs = torch.empty(rhs.shape[:-2] + (rhs.shape[-1], rhs.shape[-2]), dtype=rhs.dtype, device=rhs.device).transpose(-1, -2)
+        elif need_rhs:
+            d_rhs = torch.empty(rhs.shape, dtype=rhs.dtype, device=rhs.device)
+        d_bias = torch.empty(bias.shape, dtype=bias.dtype, device=bias.device) if bias is not None else None
+        m_rhs = _ABSENT
+        if d_rhs is not None:       # (of one row or column d_rhs could be read either way: its layout is rhs's)
+            st = d_rhs.stride()
+            m_rhs = (d_rhs.data_ptr(), mr[1], mr[2], st[-1] if mr[2] else st[-2], st[0] if len(st) == 3 else 0)
+        desc = _LINEAR_GRAD.pack(*sizes, *_rows("grad", grad, shape), *ml, *mr, *(_rows("pre", pre, shape) if act else _ABSENT),
+                                 *(_ABSENT if d_lhs is None else _rows("d_lhs", d_lhs, lhs.shape)), *m_rhs,
+                                 *(_ABSENT if d_bias is None else _vector("d_bias", d_bias, sizes[3])),
+                                 act, drop_threshold(dropout), _word("seed", seed), _word("offset", offset))
+        _queue(desc, lib().mrl_linear_grad_bytes, lib().mrl_linear_grad, workspace, lhs, on)
+    return d_lhs, d_rhs, d_bias
+
+
+def dropout(x, residual=None, *, dropout, seed=0, offset=0, out=None, stream=None):
+    """residual + D x (mrl_dropout): x of m x n or b x m x n, rows without gaps between batches; see linear for the
+    other arguments."""
+    import torch
+    if x.dim() not in (2, 3):
+        raise MorelloError(E_INVAL, "x has %d dimensions: two, or three with a batch" % x.dim())
+    with _On(x, (residual, out), stream) as on:
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        matrices = []
+        for name, t in (("x", x), ("residual", residual), ("out", out)):
+            if t is None:
+                matrices += _ABSENT
+                continue
+            at = _rows(name, t, x.shape)
+            if x.dim() == 3 and x.shape[0] > 1 and at[4] != x.shape[1] * at[3]:
+                raise MorelloError(E_INVAL, "%s: its batches do not follow each other (strides %s)" % (name, t.stride()))
+            matrices += at
+        rows = x.shape[0] * x.shape[1] if x.dim() == 3 else x.shape[0]
+        desc = _DROPOUT.pack(rows, x.shape[-1], *matrices, drop_threshold(dropout), _word("seed", seed), _word("offset", offset))
+        _check(lib().mrl_dropout(desc, C.c_void_p(on.stream)))
+    return out
+
+
+def dropout_grad(grad, *, dropout, seed=0, offset=0, out=None, stream=None):
+    """The gradient of binding.dropout by x, given `grad`, that by its result: D grad."""
+    return _dropout(grad, dropout=dropout, seed=seed, offset=offset, out=out, stream=stream)
+
+
+_dropout = dropout

@@ -21,6 +21,7 @@
 #include "../../include/morello_mi355x.h"
 #include "compress.h"
 #include "dev_params.h"
+#include "operators.h"
 
 using namespace mrl;
 
@@ -33,6 +34,8 @@ static int32_t fail(int32_t code, const char* fmt, ...) {
   va_end(ap);
   return code;
 }
+
+int32_t mrl::fail_with(int32_t code, const char* message) { return fail(code, "%s", message); }
 
 #define HIP_TRY(expr)                                                                              \
   do {                                                                                             \
@@ -1923,6 +1926,49 @@ int32_t mrl_coord_of_spec(const mrl_table* tab, const uint32_t shape[4], const u
     if (c.lay_axis[i] >= 0) { if (!layouts || layouts[i] >= (1u << c.P.lay_w[i])) return fail(MRL_E_RANGE, "layout of operand %u", i); out->x[c.lay_axis[i]] = layouts[i]; }
     if (c.dt_axis[i] >= 0) { if (!dtypes || dtypes[i] > 1) return fail(MRL_E_RANGE, "dtype of operand %u", i); out->x[c.dt_axis[i]] = dtypes[i]; }
   }
+  return MRL_OK;
+  });
+}
+
+int32_t mrl_spec_linear(const mrl_table* tab, const mrl_coord* x, mrl_linear_desc* out) {
+  return guarded([&]() -> int32_t {
+  if (!tab || !x || !out) return fail(MRL_E_INVAL, "NULL argument");
+  memset(out, 0, sizeof *out);
+  const Compiled& c = *tab->cp;
+  const Geo& g = c.geo;
+  for (uint32_t a = 0; a < g.ndim; a++)
+    if (x->x[a] >= g.ext[a]) return fail(MRL_E_RANGE, "coordinate %u = %u outside [0, %u)", a, x->x[a], g.ext[a]);
+  const uint32_t kind = c.lat.kind;
+  const bool fused = kind == MRL_KIND_FUSED_MM_ADD_RELU || kind == MRL_KIND_FUSED_BOUNDED;
+  if (!fused && kind != MRL_KIND_MATMUL_ACCUM && kind != MRL_KIND_MATMUL_PARALLEL && kind != MRL_KIND_MATMUL_BOUNDED && kind != MRL_KIND_MATMUL_MOVES)
+    return fail(MRL_E_INVAL, "lattice kind %u has no Matmul Specs", kind);
+  mrl_linear_desc d{};
+  d.b = c.sizes[0][x->x[0]];
+  d.m = c.sizes[1][x->x[1]];
+  d.k = c.sizes[2][x->x[2]];
+  d.n = c.sizes[3][x->x[3]];
+  const auto matrix = [&](uint32_t operand, uint32_t rows, uint32_t columns, mrl_matrix* mat) -> int32_t {
+    mat->layout = c.lay_axis[operand] >= 0 ? x->x[c.lay_axis[operand]] : 0;
+    if (mat->layout > 1) return fail(MRL_E_INVAL, "operand %u is packed in strips", operand);
+    mat->dtype = c.dt_axis[operand] >= 0 ? x->x[c.dt_axis[operand]] : c.P.base_bf16[operand];
+    mat->ld = mat->layout ? rows : columns;
+    mat->batch = (int64_t)rows * columns;
+    return MRL_OK;
+  };
+  int32_t rc = matrix(0, d.m, d.k, &d.lhs);
+  if (!rc) rc = matrix(1, d.k, d.n, &d.rhs);
+  if (!rc && fused) rc = matrix(2, 1, d.n, &d.bias);
+  if (!rc) rc = matrix(fused ? 3 : 2, d.m, d.n, &d.out);
+  if (rc) return rc;
+  if (d.lhs.dtype != d.rhs.dtype) return fail(MRL_E_INVAL, "lhs and rhs of two types");
+  if (d.out.layout) return fail(MRL_E_INVAL, "the output is column-major");
+  if (fused) {
+    d.bias.ld = 1;
+    d.activation = MRL_ACT_RELU;
+  } else {
+    d.residual = d.out;
+  }
+  *out = d;
   return MRL_OK;
   });
 }

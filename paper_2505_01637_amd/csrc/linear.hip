@@ -1,0 +1,400 @@
+// The Matmul with bias, activation, dropout and residual in its epilogue, and the row passes of its gradient
+// (operators.h): kernels and launches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "operators.h"
+
+namespace mrl {
+namespace {
+
+constexpr uint32_t kLine = 128;            // bytes of a step along k: 64 bf16 or 32 f32
+constexpr uint32_t kLaunch = 1u << 22;     // workgroups of a launch
+
+// ---- tiles in shared memory
+//
+// A step holds 128 bytes along k of every row (column) of the tile, as chunks of 16 bytes.  KC: the operand's neighbours along k
+// are adjacent, a line of the tile is a row of A (column of B), 8 chunks.  Otherwise a line is one k with the W rows.
+// A chunk's place in its line is its number xor swizzle(line): without it the lines that one instruction reads lie in the same
+// banks.
+template <class T, bool KC, bool IS_B, int W>
+struct Tile {
+  static constexpr int E = 16 / sizeof(T);                           // elements of a chunk
+  static constexpr int kSteps = kLine / sizeof(T);                   // k of a step
+  static constexpr int kLineBytes = KC ? kLine : W * (int)sizeof(T);
+  static constexpr int kChunks = kLineBytes / 16;                    // of a line
+  __device__ static __forceinline__ uint32_t swizzle(uint32_t line) {
+    if (sizeof(T) == 2) {
+      if (KC) return IS_B ? (line & 3) | (line >> 1 & 4) : line & 7;
+      if (W == 64) return (line & 2) << 1 | (line >> 2 & 2);
+      return (line & 3) << 2 | (line >> 2 & 2);
+    }
+    return KC ? line >> 1 & 7 : (line & 4) << 1;
+  }
+  __device__ static __forceinline__ uint32_t at(uint32_t line, uint32_t chunk) { return line * kLineBytes + ((chunk ^ swizzle(line)) << 4); }
+};
+
+// A wave's operand for MFMA blocks of 16 x 16: rows (columns) `base` + 32 per pair of blocks.  q = lane % 16 names the row of a
+// block, g = lane / 16 a quarter of the instruction's k.  The rows of a block are chosen so that a lane ends up with eight
+// neighbouring columns of the result, and so that f32 reads take two blocks' rows at once:
+//   bf16, A:  block i, q -> 16 i + q
+//   bf16, B:  block i, q -> 32 (i / 2) + 8 (q / 4) + 4 (i % 2) + q % 4
+//   f32:      block i, q -> 32 (i / 2) + 2 q + i % 2
+template <class T, bool IS_B>
+__device__ __forceinline__ uint32_t row_of(uint32_t i, uint32_t q) {
+  if (sizeof(T) == 4) return 32 * (i >> 1) + 2 * q + (i & 1);
+  return IS_B ? 32 * (i >> 1) + 8 * (q >> 2) + 4 * (i & 1) + (q & 3) : 16 * i + q;
+}
+
+typedef __attribute__((address_space(3))) const char* lds_ptr;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+// bf16: block i's operand of the half step kk (32 k): a lane has k = 32 kk + 8 g .. + 7.
+template <bool KC, bool IS_B, int W>
+__device__ __forceinline__ bf16x8 read_block(lds_ptr tile, uint32_t base, uint32_t i, uint32_t kk, uint32_t q, uint32_t g) {
+  using Tl = Tile<bf16, KC, IS_B, W>;
+  if (KC) {
+    const uint32_t line = base + row_of<bf16, IS_B>(i, q);
+    return *(const __attribute__((address_space(3))) bf16x8*)(tile + Tl::at(line, kk * 4 + g));
+  }
+  // a transposing read: sixteen lanes give four lines of four times four neighbours and get a column of four k each
+  const uint32_t row = base + row_of<bf16, IS_B>(i, 4 * (q & 3));
+  union { s16x4 h[2]; bf16x8 v; } u;
+#pragma unroll
+  for (uint32_t h = 0; h < 2; h++) {
+    const uint32_t line = kk * 32 + 8 * g + 4 * h + (q >> 2);
+    u.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(tile + Tl::at(line, row >> 3) + (row & 7) * 2));
+  }
+  return u.v;
+}
+// f32: blocks 2 pair and 2 pair + 1 of the half step kk (16 k): v[s][j] is block 2 pair + s, k = 16 kk + 4 g + j.
+template <bool KC, bool IS_B, int W>
+__device__ __forceinline__ void read_pair(lds_ptr tile, uint32_t base, uint32_t pair, uint32_t kk, uint32_t q, uint32_t g, float (&v)[2][4]) {
+  using Tl = Tile<float, KC, IS_B, W>;
+  const uint32_t row = base + 32 * pair + 2 * q;
+  if (KC) {
+#pragma unroll
+    for (uint32_t s = 0; s < 2; s++) {
+      const f32x4 t = *(const __attribute__((address_space(3))) f32x4*)(tile + Tl::at(row + s, kk * 4 + g));
+#pragma unroll
+      for (int j = 0; j < 4; j++) v[s][j] = t[j];
+    }
+  } else {
+#pragma unroll
+    for (uint32_t j = 0; j < 4; j++) {
+      const uint32_t line = kk * 16 + 4 * g + j;
+      const f32x2 t = *(const __attribute__((address_space(3))) f32x2*)(tile + Tl::at(line, row >> 2) + (row & 3) * 4);
+      v[0][j] = t[0];
+      v[1][j] = t[1];
+    }
+  }
+}
+
+// The part of a tile that a thread brings from global memory: through registers, any address, zeros where there is nothing.
+template <class T, bool KC, bool IS_B, int W, int THREADS>
+struct Stage {
+  using Tl = Tile<T, KC, IS_B, W>;
+  static constexpr int N = W * 8 / THREADS;
+  u32x4 r[N];
+  // src: the tile's first row (column) at k = k0; rows and ks: how many there are from there on
+  __device__ __forceinline__ void load(const T* src, int64_t ld, uint32_t rows, uint32_t ks, uint32_t t) {
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+      const uint32_t c = t + i * THREADS, line = c / Tl::kChunks, at = c % Tl::kChunks * Tl::E;
+      const uint32_t lines = KC ? rows : ks, width = KC ? ks : rows;
+      const T* p = src + (int64_t)line * ld + at;
+      T v[Tl::E];
+      if (line < lines && at + Tl::E <= width) {
+        __builtin_memcpy(v, p, 16);
+      } else {
+#pragma unroll
+        for (int e = 0; e < Tl::E; e++) v[e] = line < lines && at + e < width ? p[e] : (T)0.0f;
+      }
+      __builtin_memcpy(&r[i], v, 16);
+    }
+  }
+  __device__ __forceinline__ void store(char* tile, uint32_t t) const {
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+      const uint32_t c = t + i * THREADS;
+      *(u32x4*)(tile + Tl::at(c / Tl::kChunks, c % Tl::kChunks)) = r[i];
+    }
+  }
+};
+
+// Where the sum of a workgroup stands: segment and k within it.
+struct Cursor { uint32_t seg, k; };
+
+// One tile of TM x TN, WAVES_M x WAVES_N waves, over a stretch of the steps along k.  The products are taken as B^T A^T: in the
+// MFMA result a lane has one column and four neighbouring rows, which are then one row of the result and neighbouring columns.
+template <class T, bool AKC, bool BKC, int TM, int TN, int WAVES_M, int WAVES_N>
+__global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void product_kernel(const Product p, uint32_t steps, uint32_t per_split, uint32_t splits,
+                                                                         uint32_t first, float* __restrict__ partial) {
+  constexpr int THREADS = 64 * WAVES_M * WAVES_N, WM = TM / WAVES_M, WN = TN / WAVES_N, BM = WM / 16, BN = WN / 16;
+  constexpr uint32_t KS = kLine / sizeof(T);
+  __shared__ __attribute__((aligned(16))) char lds[2][(TM + TN) * kLine];
+
+  const uint32_t tiles_m = (p.M + TM - 1) / TM, tiles_n = (p.N + TN - 1) / TN;
+  uint32_t id = first + blockIdx.x;
+  const uint32_t tn = id % tiles_n;
+  id /= tiles_n;
+  const uint32_t tm = id % tiles_m;
+  id /= tiles_m;
+  const uint32_t split = id % splits, batch = id / splits;
+  const uint32_t m0 = tm * TM, n0 = tn * TN;
+
+  const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6, q = lane & 15, g = lane >> 4;
+  const uint32_t wm = wave / WAVES_N * WM, wn = wave % WAVES_N * WN;
+
+  const T* a = (const T*)p.a + (int64_t)batch * p.batch_a + (AKC ? (int64_t)m0 * p.lda : (int64_t)m0);
+  const T* b = (const T*)p.b + (int64_t)batch * p.batch_b + (BKC ? (int64_t)n0 * p.ldb : (int64_t)n0);
+  const uint32_t seg_steps = (p.K + KS - 1) / KS;
+  const uint32_t begin = split * per_split, end = min(begin + per_split, steps);
+
+  Stage<T, AKC, false, TM, THREADS> sa;
+  Stage<T, BKC, true, TN, THREADS> sb;
+  const auto load = [&](uint32_t step) {
+    const uint32_t seg = step / seg_steps, k = (step - seg * seg_steps) * KS;
+    sa.load(a + (int64_t)seg * p.seg_a + (AKC ? (int64_t)k : (int64_t)k * p.lda), p.lda, p.M - m0, p.K - k, t);
+    sb.load(b + (int64_t)seg * p.seg_b + (BKC ? (int64_t)k : (int64_t)k * p.ldb), p.ldb, p.N - n0, p.K - k, t);
+  };
+
+  f32x4 acc[BM][BN];
+#pragma unroll
+  for (int i = 0; i < BM; i++)
+#pragma unroll
+    for (int j = 0; j < BN; j++) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+  if (begin < end) {
+    load(begin);
+    sa.store(lds[0], t);
+    sb.store(lds[0] + TM * kLine, t);
+  }
+  __syncthreads();
+  for (uint32_t step = begin; step < end; step++) {
+    const uint32_t cur = (step - begin) & 1;
+    if (step + 1 < end) load(step + 1);
+    const lds_ptr ta = (lds_ptr)lds[cur], tb = ta + TM * kLine;
+#pragma unroll
+    for (uint32_t kk = 0; kk < 2; kk++) {
+      if constexpr (sizeof(T) == 2) {
+        bf16x8 fa[BM], fb[BN];
+#pragma unroll
+        for (int i = 0; i < BM; i++) fa[i] = read_block<AKC, false, TM>(ta, wm, i, kk, q, g);
+#pragma unroll
+        for (int j = 0; j < BN; j++) fb[j] = read_block<BKC, true, TN>(tb, wn, j, kk, q, g);
+#pragma unroll
+        for (int i = 0; i < BM; i++)
+#pragma unroll
+          for (int j = 0; j < BN; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+      } else {
+        float fa[BM / 2][2][4], fb[BN / 2][2][4];
+#pragma unroll
+        for (int i = 0; i < BM / 2; i++) read_pair<AKC, false, TM>(ta, wm, i, kk, q, g, fa[i]);
+#pragma unroll
+        for (int j = 0; j < BN / 2; j++) read_pair<BKC, true, TN>(tb, wn, j, kk, q, g, fb[j]);
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+#pragma unroll
+          for (int i = 0; i < BM; i++)
+#pragma unroll
+            for (int j = 0; j < BN; j++)
+              acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[j >> 1][j & 1][e], fa[i >> 1][i & 1][e], acc[i][j], 0, 0, 0);
+      }
+    }
+    if (step + 1 < end) {
+      sa.store(lds[cur ^ 1], t);
+      sb.store(lds[cur ^ 1] + TM * kLine, t);
+    }
+    __syncthreads();
+  }
+
+  // a lane's results: row row_of(i, q); of the pair of blocks 2 j, 2 j + 1 the eight columns from 32 j + 8 g on
+  const uint32_t pitch = (p.N + 7) & ~7u;
+#pragma unroll
+  for (int i = 0; i < BM; i++) {
+    const uint32_t m = m0 + wm + row_of<T, false>(i, q);
+    if (m >= p.M) continue;
+#pragma unroll
+    for (int j = 0; j < BN / 2; j++) {
+      const uint32_t n = n0 + wn + 32 * j + 8 * g;
+      if (n >= p.N) continue;
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; e++) v[e] = sizeof(T) == 2 ? acc[i][2 * j + (e >> 2)][e & 3] : acc[i][2 * j + (e & 1)][e >> 1];
+      if (splits > 1) {
+        float* out = partial + (((uint64_t)split * p.batches + batch) * p.M + m) * pitch + n;
+#pragma unroll
+        for (int h = 0; h < 2; h++) *(f32x4*)(out + 4 * h) = f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+      } else {
+        finish8(p.e, batch, p.M, m, n, p.N - n, v);
+      }
+    }
+  }
+}
+
+// The sum over the splits, in their order, and the epilogue: eight columns a thread.
+__global__ __launch_bounds__(256) void join_kernel(const Product p, uint32_t splits, uint64_t first, const float* __restrict__ partial) {
+  const uint32_t groups = (p.N + 7) / 8;
+  const uint64_t id = first + (uint64_t)blockIdx.x * 256 + threadIdx.x, rows = (uint64_t)p.batches * p.M;
+  const uint64_t row = id / groups;
+  if (row >= rows) return;
+  const uint32_t n = (uint32_t)(id - row * groups) * 8;
+  const float* in = partial + row * (groups * 8) + n;
+  float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+  for (uint32_t s = 0; s < splits; s++) {
+    const f32x4 x = *(const f32x4*)in, y = *(const f32x4*)(in + 4);
+#pragma unroll
+    for (int e = 0; e < 4; e++) { v[e] += x[e]; v[4 + e] += y[e]; }
+    in += rows * (groups * 8);
+  }
+  const uint32_t batch = (uint32_t)(row / p.M);
+  finish8(p.e, batch, p.M, (uint32_t)(row - (uint64_t)batch * p.M), n, p.N - n, v);
+}
+
+// ---- rows
+
+constexpr uint32_t kGradRows = 64;         // rows of a workgroup of grad_rows_kernel
+
+// dz, and for dbias the column sums of the workgroup's rows before dz is rounded.  A workgroup: 256 columns, eight a thread, eight
+// rows at a time; grid: column blocks x row blocks.
+__global__ __launch_bounds__(256) void grad_rows_kernel(const GradRows p, uint32_t first, float* __restrict__ partial) {
+  __shared__ float sums[8][256];
+  const uint32_t blocks_n = (p.N + 255) / 256, id = first + blockIdx.x, bn = id % blocks_n, br = id / blocks_n;
+  const uint32_t c = threadIdx.x & 31, r = threadIdx.x >> 5, n = bn * 256 + c * 8, rows = p.batches * p.M;
+  float sum[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+  if (n < p.N) {
+    const uint32_t valid = p.N - n;
+    for (uint32_t i = 0; i < kGradRows / 8; i++) {
+      const uint64_t at = (uint64_t)br * kGradRows + i * 8 + r;
+      if (at >= rows) break;
+      const uint32_t row = (uint32_t)at, batch = row / p.M, m = row - batch * p.M;
+      float v[8];
+      load8(p.grad.data, p.grad.bf16, (int64_t)batch * p.grad.batch + (int64_t)m * p.grad.ld + n, valid, v);
+      if (p.drop.drop) drop8(p.drop, row, n, v);
+      if (p.pre.data) {
+        float z[8];
+        load8(p.pre.data, p.pre.bf16, (int64_t)batch * p.pre.batch + (int64_t)m * p.pre.ld + n, valid, z);
+#pragma unroll
+        for (int e = 0; e < 8; e++) v[e] *= slope(p.activation, z[e]);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; e++) sum[e] += v[e];
+      if (p.dz.data) store8(p.dz.data, p.dz.bf16, (int64_t)batch * p.dz.batch + (int64_t)m * p.dz.ld + n, valid, v);
+    }
+  }
+  if (!partial) return;
+#pragma unroll
+  for (int e = 0; e < 8; e++) sums[r][c * 8 + e] = sum[e];
+  __syncthreads();
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; i++) s += sums[i][threadIdx.x];
+  if (bn * 256 + threadIdx.x < p.N) partial[(uint64_t)br * p.N + bn * 256 + threadIdx.x] = s;
+}
+
+// dbias: the row blocks' sums added up, in an order that the sizes alone decide.
+__global__ __launch_bounds__(256) void grad_bias_kernel(const float* __restrict__ partial, uint32_t row_blocks, uint32_t N, void* dbias, uint32_t is_bf16) {
+  __shared__ float sums[8][32];
+  const uint32_t c = threadIdx.x & 31, r = threadIdx.x >> 5, n = blockIdx.x * 32 + c;
+  float s = 0.0f;
+  if (n < N) for (uint32_t i = r; i < row_blocks; i += 8) s += partial[(uint64_t)i * N + n];
+  sums[r][c] = s;
+  __syncthreads();
+  if (r || n >= N) return;
+  for (int i = 1; i < 8; i++) s += sums[i][c];
+  if (is_bf16) ((bf16*)dbias)[n] = (bf16)s;
+  else ((float*)dbias)[n] = s;
+}
+
+__global__ __launch_bounds__(256) void drop_kernel(const DropRows p, uint64_t first) {
+  const uint32_t groups = (p.N + 7) / 8;
+  const uint64_t id = first + (uint64_t)blockIdx.x * 256 + threadIdx.x, row = id / groups;
+  if (row >= p.M) return;
+  const uint32_t n = (uint32_t)(id - row * groups) * 8, valid = p.N - n;
+  float v[8];
+  load8(p.x.data, p.x.bf16, (int64_t)row * p.x.ld + n, valid, v);
+  if (p.drop.drop) drop8(p.drop, (uint32_t)row, n, v);
+  if (p.residual.data) {
+    float r[8];
+    load8(p.residual.data, p.residual.bf16, (int64_t)row * p.residual.ld + n, valid, r);
+#pragma unroll
+    for (int e = 0; e < 8; e++) v[e] += r[e];
+  }
+  store8(p.out.data, p.out.bf16, (int64_t)row * p.out.ld + n, valid, v);
+}
+
+// Work of `blocks` workgroups in launches of at most kLaunch: f(first, count)
+template <class F>
+hipError_t in_launches(uint64_t blocks, F&& f) {
+  for (uint64_t at = 0; at < blocks; at += kLaunch) {
+    f(at, (uint32_t)std::min<uint64_t>(kLaunch, blocks - at));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+template <class T, bool AKC, bool BKC>
+hipError_t launch_tiles(const Product& p, const ProductPlan& plan, float* partial, hipStream_t st) {
+  const uint64_t tiles = (uint64_t)((p.M + plan.tile - 1) / plan.tile) * ((p.N + plan.tile - 1) / plan.tile);
+  return in_launches(tiles * plan.splits * p.batches, [&](uint64_t first, uint32_t n) {
+    if (plan.tile == 128) product_kernel<T, AKC, BKC, 128, 128, 2, 2><<<n, 256, 0, st>>>(p, plan.steps, plan.per_split, plan.splits, (uint32_t)first, partial);
+    else product_kernel<T, AKC, BKC, 64, 64, 2, 2><<<n, 256, 0, st>>>(p, plan.steps, plan.per_split, plan.splits, (uint32_t)first, partial);
+  });
+}
+template <class T>
+hipError_t launch_layout(const Product& p, const ProductPlan& plan, float* partial, hipStream_t st) {
+  if (p.a_kc) return p.b_kc ? launch_tiles<T, true, true>(p, plan, partial, st) : launch_tiles<T, true, false>(p, plan, partial, st);
+  return p.b_kc ? launch_tiles<T, false, true>(p, plan, partial, st) : launch_tiles<T, false, false>(p, plan, partial, st);
+}
+
+}  // namespace
+
+ProductPlan plan_product(const Product& p) {
+  const uint32_t ks = kLine / (p.bf16 ? 2 : 4);
+  ProductPlan plan{};
+  plan.steps = (p.K + ks - 1) / ks * p.segs;
+  const auto tiles = [&](uint64_t t) { return (p.M + t - 1) / t * ((p.N + t - 1) / t) * p.batches; };
+  plan.tile = tiles(128) >= 256 ? 128 : 64;
+  // fewer tiles than compute units: several workgroups share a tile's sum, four steps each at least
+  const uint64_t n = tiles(plan.tile);
+  uint64_t splits = n && n < 256 ? std::min<uint64_t>({512 / n, plan.steps / 4, 64}) : 1;
+  splits = std::max<uint64_t>(splits, 1);
+  plan.per_split = (uint32_t)((plan.steps + splits - 1) / splits);
+  plan.splits = plan.per_split ? (plan.steps + plan.per_split - 1) / plan.per_split : 1;
+  plan.partial_bytes = plan.splits > 1 ? (uint64_t)plan.splits * p.batches * p.M * ((p.N + 7) / 8 * 8) * 4 : 0;
+  return plan;
+}
+
+hipError_t launch_product(const Product& p, const ProductPlan& plan, float* partial, hipStream_t st) {
+  if (!p.batches || !p.M || !p.N) return hipSuccess;
+  const hipError_t e = p.bf16 ? launch_layout<bf16>(p, plan, partial, st) : launch_layout<float>(p, plan, partial, st);
+  if (e != hipSuccess || plan.splits == 1) return e;
+  const uint64_t items = (uint64_t)p.batches * p.M * ((p.N + 7) / 8);
+  return in_launches((items + 255) / 256, [&](uint64_t first, uint32_t n) { join_kernel<<<n, 256, 0, st>>>(p, plan.splits, first * 256, partial); });
+}
+
+uint64_t grad_rows_bytes(uint32_t batches, uint32_t M, uint32_t N, bool dbias) {
+  return dbias ? ((uint64_t)batches * M + kGradRows - 1) / kGradRows * N * 4 : 0;
+}
+
+hipError_t launch_grad_rows(const GradRows& g, float* partial, hipStream_t st) {
+  if (!g.N) return hipSuccess;
+  const uint64_t row_blocks = ((uint64_t)g.batches * g.M + kGradRows - 1) / kGradRows;
+  const hipError_t e = in_launches(row_blocks * ((g.N + 255) / 256), [&](uint64_t first, uint32_t n) {
+    grad_rows_kernel<<<n, 256, 0, st>>>(g, (uint32_t)first, g.dbias ? partial : nullptr);
+  });
+  if (e != hipSuccess || !g.dbias) return e;
+  grad_bias_kernel<<<(g.N + 31) / 32, 256, 0, st>>>(partial, (uint32_t)row_blocks, g.N, g.dbias, g.dbias_bf16);
+  return hipGetLastError();
+}
+
+hipError_t launch_drop(const DropRows& d, hipStream_t st) {
+  if (!d.M || !d.N) return hipSuccess;
+  const uint64_t items = (uint64_t)d.M * ((d.N + 7) / 8);
+  return in_launches((items + 255) / 256, [&](uint64_t first, uint32_t n) { drop_kernel<<<n, 256, 0, st>>>(d, first * 256); });
+}
+
+}  // namespace mrl
