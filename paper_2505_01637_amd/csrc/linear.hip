@@ -123,11 +123,80 @@ struct Stage {
   }
 };
 
-// Where the sum of a workgroup stands: segment and k within it.
-struct Cursor { uint32_t seg, k; };
+// acc += the products of a step: a wave's WM x WN part of the tile at (wm, wn).  The products are taken as B^T A^T: in the MFMA result
+// a lane has one column and four neighbouring rows, which are then one row of the result and neighbouring columns.
+template <class T, bool AKC, bool BKC, int TM, int TN, int BM, int BN>
+__device__ __forceinline__ void multiply(lds_ptr ta, lds_ptr tb, uint32_t wm, uint32_t wn, uint32_t q, uint32_t g, f32x4 (&acc)[BM][BN]) {
+#pragma unroll
+  for (uint32_t kk = 0; kk < 2; kk++) {
+    if constexpr (sizeof(T) == 2) {
+      bf16x8 fa[BM], fb[BN];
+#pragma unroll
+      for (int i = 0; i < BM; i++) fa[i] = read_block<AKC, false, TM>(ta, wm, i, kk, q, g);
+#pragma unroll
+      for (int j = 0; j < BN; j++) fb[j] = read_block<BKC, true, TN>(tb, wn, j, kk, q, g);
+#pragma unroll
+      for (int i = 0; i < BM; i++)
+#pragma unroll
+        for (int j = 0; j < BN; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+    } else {
+      float fa[BM / 2][2][4], fb[BN / 2][2][4];
+#pragma unroll
+      for (int i = 0; i < BM / 2; i++) read_pair<AKC, false, TM>(ta, wm, i, kk, q, g, fa[i]);
+#pragma unroll
+      for (int j = 0; j < BN / 2; j++) read_pair<BKC, true, TN>(tb, wn, j, kk, q, g, fb[j]);
+#pragma unroll
+      for (int e = 0; e < 4; e++)
+#pragma unroll
+        for (int i = 0; i < BM; i++)
+#pragma unroll
+          for (int j = 0; j < BN; j++)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[j >> 1][j & 1][e], fa[i >> 1][i & 1][e], acc[i][j], 0, 0, 0);
+    }
+  }
+}
 
-// One tile of TM x TN, WAVES_M x WAVES_N waves, over a stretch of the steps along k.  The products are taken as B^T A^T: in the
-// MFMA result a lane has one column and four neighbouring rows, which are then one row of the result and neighbouring columns.
+// Where a workgroup's tile lies.
+struct Place { uint32_t tm, tn, split, batch; };
+__device__ __forceinline__ Place place(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, uint32_t splits) {
+  Place at;
+  at.tn = id % tiles_n;
+  id /= tiles_n;
+  at.tm = id % tiles_m;
+  id /= tiles_m;
+  at.split = id % splits;
+  at.batch = id / splits;
+  return at;
+}
+
+// A wave's results: a lane has row row_of(i, q) and, of the pair of blocks 2 j, 2 j + 1, the eight columns from 32 j + 8 g on.
+template <class T, int BM, int BN>
+__device__ __forceinline__ void write_out(const Product& p, const Place& at, uint32_t splits, uint32_t m0, uint32_t n0, uint32_t q, uint32_t g,
+                                          const f32x4 (&acc)[BM][BN], float* __restrict__ partial) {
+  const uint32_t pitch = (p.N + 7) & ~7u;
+#pragma unroll
+  for (int i = 0; i < BM; i++) {
+    const uint32_t m = m0 + row_of<T, false>(i, q);
+    if (m >= p.M) continue;
+#pragma unroll
+    for (int j = 0; j < BN / 2; j++) {
+      const uint32_t n = n0 + 32 * j + 8 * g;
+      if (n >= p.N) continue;
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; e++) v[e] = sizeof(T) == 2 ? acc[i][2 * j + (e >> 2)][e & 3] : acc[i][2 * j + (e & 1)][e >> 1];
+      if (splits > 1) {
+        float* out = partial + (((uint64_t)at.split * p.batches + at.batch) * p.M + m) * pitch + n;
+#pragma unroll
+        for (int h = 0; h < 2; h++) *(f32x4*)(out + 4 * h) = f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+      } else {
+        finish8(p.e, at.batch, p.M, m, n, p.N - n, v);
+      }
+    }
+  }
+}
+
+// One tile of TM x TN, WAVES_M x WAVES_N waves, over a stretch of the steps along k: operands of any stride and alignment.
 template <class T, bool AKC, bool BKC, int TM, int TN, int WAVES_M, int WAVES_N>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void product_kernel(const Product p, uint32_t steps, uint32_t per_split, uint32_t splits,
                                                                          uint32_t first, float* __restrict__ partial) {
@@ -135,22 +204,16 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void product_kernel(const P
   constexpr uint32_t KS = kLine / sizeof(T);
   __shared__ __attribute__((aligned(16))) char lds[2][(TM + TN) * kLine];
 
-  const uint32_t tiles_m = (p.M + TM - 1) / TM, tiles_n = (p.N + TN - 1) / TN;
-  uint32_t id = first + blockIdx.x;
-  const uint32_t tn = id % tiles_n;
-  id /= tiles_n;
-  const uint32_t tm = id % tiles_m;
-  id /= tiles_m;
-  const uint32_t split = id % splits, batch = id / splits;
-  const uint32_t m0 = tm * TM, n0 = tn * TN;
+  const Place at = place(first + blockIdx.x, (p.M + TM - 1) / TM, (p.N + TN - 1) / TN, splits);
+  const uint32_t m0 = at.tm * TM, n0 = at.tn * TN;
 
   const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6, q = lane & 15, g = lane >> 4;
   const uint32_t wm = wave / WAVES_N * WM, wn = wave % WAVES_N * WN;
 
-  const T* a = (const T*)p.a + (int64_t)batch * p.batch_a + (AKC ? (int64_t)m0 * p.lda : (int64_t)m0);
-  const T* b = (const T*)p.b + (int64_t)batch * p.batch_b + (BKC ? (int64_t)n0 * p.ldb : (int64_t)n0);
+  const T* a = (const T*)p.a + (int64_t)at.batch * p.batch_a + (AKC ? (int64_t)m0 * p.lda : (int64_t)m0);
+  const T* b = (const T*)p.b + (int64_t)at.batch * p.batch_b + (BKC ? (int64_t)n0 * p.ldb : (int64_t)n0);
   const uint32_t seg_steps = (p.K + KS - 1) / KS;
-  const uint32_t begin = split * per_split, end = min(begin + per_split, steps);
+  const uint32_t begin = at.split * per_split, end = min(begin + per_split, steps);
 
   Stage<T, AKC, false, TM, THREADS> sa;
   Stage<T, BKC, true, TN, THREADS> sb;
@@ -176,33 +239,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void product_kernel(const P
     const uint32_t cur = (step - begin) & 1;
     if (step + 1 < end) load(step + 1);
     const lds_ptr ta = (lds_ptr)lds[cur], tb = ta + TM * kLine;
-#pragma unroll
-    for (uint32_t kk = 0; kk < 2; kk++) {
-      if constexpr (sizeof(T) == 2) {
-        bf16x8 fa[BM], fb[BN];
-#pragma unroll
-        for (int i = 0; i < BM; i++) fa[i] = read_block<AKC, false, TM>(ta, wm, i, kk, q, g);
-#pragma unroll
-        for (int j = 0; j < BN; j++) fb[j] = read_block<BKC, true, TN>(tb, wn, j, kk, q, g);
-#pragma unroll
-        for (int i = 0; i < BM; i++)
-#pragma unroll
-          for (int j = 0; j < BN; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
-      } else {
-        float fa[BM / 2][2][4], fb[BN / 2][2][4];
-#pragma unroll
-        for (int i = 0; i < BM / 2; i++) read_pair<AKC, false, TM>(ta, wm, i, kk, q, g, fa[i]);
-#pragma unroll
-        for (int j = 0; j < BN / 2; j++) read_pair<BKC, true, TN>(tb, wn, j, kk, q, g, fb[j]);
-#pragma unroll
-        for (int e = 0; e < 4; e++)
-#pragma unroll
-          for (int i = 0; i < BM; i++)
-#pragma unroll
-            for (int j = 0; j < BN; j++)
-              acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[j >> 1][j & 1][e], fa[i >> 1][i & 1][e], acc[i][j], 0, 0, 0);
-      }
-    }
+    multiply<T, AKC, BKC, TM, TN, BM, BN>(ta, tb, wm, wn, q, g, acc);
     if (step + 1 < end) {
       sa.store(lds[cur ^ 1], t);
       sb.store(lds[cur ^ 1] + TM * kLine, t);
@@ -210,28 +247,120 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void product_kernel(const P
     __syncthreads();
   }
 
-  // a lane's results: row row_of(i, q); of the pair of blocks 2 j, 2 j + 1 the eight columns from 32 j + 8 g on
-  const uint32_t pitch = (p.N + 7) & ~7u;
+  write_out<T, BM, BN>(p, at, splits, m0 + wm, n0 + wn, q, g, acc, partial);
+}
+
+// ---- operands whose lines start at multiples of 16 bytes
+//
+// Loads go from memory to shared memory past the registers (a wave's load writes 1024 bytes in a row, a lane 16 of them, so the swizzle
+// is applied to the address that a lane reads), through a buffer descriptor whose range check gives 0 for what lies behind the operand.
+
+// Waits until at most LEFT of the wave's loads are under way and its reads of shared memory are done, then for the other waves.
+template <int LEFT>
+__device__ __forceinline__ void arrive() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory"); }
+
+// (The load is written out because the compiler, which cannot tell the stages apart, would wait for every load under way before any
+// read of shared memory.  It has no output register; its address registers are read as it is issued.)
+__device__ __forceinline__ void load_to_lds(uint32_t lds, uint32_t offset, u32x4 buffer) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(buffer) : "memory");
+}
+
+constexpr uint32_t kOutside = 0x80000000u;        // beyond any buffer's range
+
+template <class T, bool KC, bool IS_B, int W, int THREADS>
+struct Feed {
+  using Tl = Tile<T, KC, IS_B, W>;
+  static constexpr int N = W * 8 / THREADS;       // loads of a thread and step
+  uint32_t offset[N];                             // bytes from the tile's first element of a step
+  __device__ __forceinline__ void init(int64_t ld, uint32_t t) {
 #pragma unroll
-  for (int i = 0; i < BM; i++) {
-    const uint32_t m = m0 + wm + row_of<T, false>(i, q);
-    if (m >= p.M) continue;
-#pragma unroll
-    for (int j = 0; j < BN / 2; j++) {
-      const uint32_t n = n0 + wn + 32 * j + 8 * g;
-      if (n >= p.N) continue;
-      float v[8];
-#pragma unroll
-      for (int e = 0; e < 8; e++) v[e] = sizeof(T) == 2 ? acc[i][2 * j + (e >> 2)][e & 3] : acc[i][2 * j + (e & 1)][e >> 1];
-      if (splits > 1) {
-        float* out = partial + (((uint64_t)split * p.batches + batch) * p.M + m) * pitch + n;
-#pragma unroll
-        for (int h = 0; h < 2; h++) *(f32x4*)(out + 4 * h) = f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
-      } else {
-        finish8(p.e, batch, p.M, m, n, p.N - n, v);
-      }
+    for (int i = 0; i < N; i++) {
+      const uint32_t c = t + i * THREADS, line = c / Tl::kChunks, chunk = c % Tl::kChunks ^ Tl::swizzle(line);
+      offset[i] = line * (uint32_t)ld * (uint32_t)sizeof(T) + chunk * 16;
     }
   }
+  // from: the tile's first element of the step; left: bytes from there to the operand's end; ks: k that are left in the segment
+  __device__ __forceinline__ void load(const char* from, int64_t left, uint32_t ks, uint32_t lds, uint32_t t) const {
+    const uint64_t base = (uint64_t)from;
+    const u32x4 buffer = {(uint32_t)base, (uint32_t)(base >> 32) & 0xFFFFu, (uint32_t)(left < (int64_t)kOutside ? left : (int64_t)kOutside), 0x27000u};
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+      uint32_t at = offset[i];
+      if (KC && ks < Tl::kSteps) {                // chunks past the end of the sum would be the next line's
+        const uint32_t c = t + i * THREADS, line = c / Tl::kChunks, chunk = c % Tl::kChunks ^ Tl::swizzle(line);
+        if (chunk * Tl::E >= ks) at = kOutside;
+      }
+      load_to_lds(lds + (t & ~63u) * 16 + i * THREADS * 16, at, buffer);
+    }
+  }
+};
+
+template <class T, bool AKC, bool BKC, int TM, int TN, int WAVES_M, int WAVES_N, int STAGES>
+__global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void fast_kernel(const Product p, uint32_t steps, uint32_t per_split, uint32_t splits,
+                                                                      uint32_t first, float* __restrict__ partial) {
+  constexpr int THREADS = 64 * WAVES_M * WAVES_N, WM = TM / WAVES_M, WN = TN / WAVES_N, BM = WM / 16, BN = WN / 16;
+  constexpr uint32_t KS = kLine / sizeof(T), STAGE = (TM + TN) * kLine;
+  __shared__ __attribute__((aligned(1024))) char lds[STAGES * STAGE];
+
+  const Place at = place(first + blockIdx.x, (p.M + TM - 1) / TM, (p.N + TN - 1) / TN, splits);
+  const uint32_t m0 = at.tm * TM, n0 = at.tn * TN;
+  const uint32_t t = threadIdx.x, lane = t & 63, q = lane & 15, g = lane >> 4;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const uint32_t wm = wave / WAVES_N * WM, wn = wave % WAVES_N * WN;
+
+  Feed<T, AKC, false, TM, THREADS> fa;
+  Feed<T, BKC, true, TN, THREADS> fb;
+  fa.init(p.lda, t);
+  fb.init(p.ldb, t);
+  constexpr int LOADS = decltype(fa)::N + decltype(fb)::N;
+
+  const uint32_t seg_steps = (p.K + KS - 1) / KS;
+  const uint32_t begin = at.split * per_split, end = min(begin + per_split, steps);
+  // the next step to load: where it starts in either operand, and what is left behind that
+  const int64_t step_a = (AKC ? (int64_t)KS : KS * p.lda) * sizeof(T), step_b = (BKC ? (int64_t)KS : KS * p.ldb) * sizeof(T);
+  uint32_t seg = begin < end ? begin / seg_steps : 0, k = (begin - seg * seg_steps) * KS;
+  const char *a0 = (const char*)((const T*)p.a + (int64_t)at.batch * p.batch_a + (AKC ? (int64_t)m0 * p.lda : (int64_t)m0));
+  const char *b0 = (const char*)((const T*)p.b + (int64_t)at.batch * p.batch_b + (BKC ? (int64_t)n0 * p.ldb : (int64_t)n0));
+  const int64_t size_a = (AKC ? ((int64_t)(p.M - m0) - 1) * p.lda + p.K : ((int64_t)p.K - 1) * p.lda + (p.M - m0)) * (int64_t)sizeof(T);
+  const int64_t size_b = (BKC ? ((int64_t)(p.N - n0) - 1) * p.ldb + p.K : ((int64_t)p.K - 1) * p.ldb + (p.N - n0)) * (int64_t)sizeof(T);
+  int64_t off_a = (int64_t)(k / KS) * step_a, off_b = (int64_t)(k / KS) * step_b;
+  const char *sa = a0 + (int64_t)seg * p.seg_a * (int64_t)sizeof(T), *sb = b0 + (int64_t)seg * p.seg_b * (int64_t)sizeof(T);
+  const auto load = [&](uint32_t stage) {
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr)lds + stage * STAGE;
+    const uint32_t mine = __builtin_amdgcn_readfirstlane(lds0);
+    fa.load(sa + off_a, size_a - off_a, p.K - k, mine, wave * 64 + lane);
+    fb.load(sb + off_b, size_b - off_b, p.K - k, mine + TM * kLine, wave * 64 + lane);
+    k += KS;
+    off_a += step_a;
+    off_b += step_b;
+    if (k >= p.K) {
+      k = 0;
+      off_a = off_b = 0;
+      sa += p.seg_a * (int64_t)sizeof(T);
+      sb += p.seg_b * (int64_t)sizeof(T);
+    }
+  };
+
+  f32x4 acc[BM][BN];
+#pragma unroll
+  for (int i = 0; i < BM; i++)
+#pragma unroll
+    for (int j = 0; j < BN; j++) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+  const uint32_t n = end > begin ? end - begin : 0;
+#pragma unroll
+  for (int s = 0; s < STAGES - 1; s++) if (s < (int)n) load(s);
+  uint32_t cur = 0, next = STAGES - 1;
+  for (uint32_t s = 0; s < n; s++) {
+    if (s + STAGES - 1 <= n) arrive<(STAGES - 2) * LOADS>();      // the later stages' loads may still be under way
+    else arrive<0>();
+    if (s + STAGES - 1 < n) load(next);
+    const lds_ptr ta = (lds_ptr)lds + cur * STAGE;
+    multiply<T, AKC, BKC, TM, TN, BM, BN>(ta, ta + TM * kLine, wm, wn, q, g, acc);
+    cur = cur + 1 == STAGES ? 0 : cur + 1;
+    next = next + 1 == STAGES ? 0 : next + 1;
+  }
+  write_out<T, BM, BN>(p, at, splits, m0 + wm, n0 + wn, q, g, acc, partial);
 }
 
 // The sum over the splits, in their order, and the epilogue: eight columns a thread.
@@ -339,6 +468,11 @@ hipError_t in_launches(uint64_t blocks, F&& f) {
 template <class T, bool AKC, bool BKC>
 hipError_t launch_tiles(const Product& p, const ProductPlan& plan, float* partial, hipStream_t st) {
   const uint64_t tiles = (uint64_t)((p.M + plan.tile - 1) / plan.tile) * ((p.N + plan.tile - 1) / plan.tile);
+  if (plan.fast) return in_launches(tiles * plan.splits * p.batches, [&](uint64_t first, uint32_t n) {
+    if (plan.tile == 256) fast_kernel<T, AKC, BKC, 256, 256, 2, 4, 2><<<n, 512, 0, st>>>(p, plan.steps, plan.per_split, plan.splits, (uint32_t)first, partial);
+    else if (plan.tile == 128) fast_kernel<T, AKC, BKC, 128, 128, 2, 2, 2><<<n, 256, 0, st>>>(p, plan.steps, plan.per_split, plan.splits, (uint32_t)first, partial);
+    else fast_kernel<T, AKC, BKC, 64, 64, 2, 2, 4><<<n, 256, 0, st>>>(p, plan.steps, plan.per_split, plan.splits, (uint32_t)first, partial);
+  });
   return in_launches(tiles * plan.splits * p.batches, [&](uint64_t first, uint32_t n) {
     if (plan.tile == 128) product_kernel<T, AKC, BKC, 128, 128, 2, 2><<<n, 256, 0, st>>>(p, plan.steps, plan.per_split, plan.splits, (uint32_t)first, partial);
     else product_kernel<T, AKC, BKC, 64, 64, 2, 2><<<n, 256, 0, st>>>(p, plan.steps, plan.per_split, plan.splits, (uint32_t)first, partial);
@@ -350,6 +484,15 @@ hipError_t launch_layout(const Product& p, const ProductPlan& plan, float* parti
   return p.b_kc ? launch_tiles<T, false, true>(p, plan, partial, st) : launch_tiles<T, false, false>(p, plan, partial, st);
 }
 
+// Whether every line that is read starts at a multiple of 16 bytes, ends at one, and follows the one before; offsets within a tile fit 31 bits.
+bool aligned(const Product& p) {
+  const int64_t e = p.bf16 ? 8 : 4;
+  const auto whole = [&](const void* data, int64_t ld, int64_t batch, int64_t seg, int64_t width) {
+    return (uintptr_t)data % 16 == 0 && ld % e == 0 && batch % e == 0 && seg % e == 0 && width % e == 0 && ld >= width && ld < (int64_t)1 << 21;
+  };
+  return whole(p.a, p.lda, p.batch_a, p.segs > 1 ? p.seg_a : 0, p.a_kc ? p.K : p.M) && whole(p.b, p.ldb, p.batch_b, p.segs > 1 ? p.seg_b : 0, p.b_kc ? p.K : p.N);
+}
+
 }  // namespace
 
 ProductPlan plan_product(const Product& p) {
@@ -357,7 +500,8 @@ ProductPlan plan_product(const Product& p) {
   ProductPlan plan{};
   plan.steps = (p.K + ks - 1) / ks * p.segs;
   const auto tiles = [&](uint64_t t) { return (p.M + t - 1) / t * ((p.N + t - 1) / t) * p.batches; };
-  plan.tile = tiles(128) >= 256 ? 128 : 64;
+  plan.fast = aligned(p);
+  plan.tile = plan.fast && tiles(256) >= 256 ? 256 : tiles(128) >= 256 ? 128 : 64;
   // fewer tiles than compute units: several workgroups share a tile's sum, four steps each at least
   const uint64_t n = tiles(plan.tile);
   uint64_t splits = n && n < 256 ? std::min<uint64_t>({512 / n, plan.steps / 4, 64}) : 1;

@@ -168,6 +168,7 @@ struct Product {
 
 // How it is launched.
 struct ProductPlan {
+  bool fast;                     // both operands aligned to 16 bytes throughout
   uint32_t tile;                 // rows and columns of a workgroup's tile
   uint32_t splits;               // workgroups along k
   uint32_t steps, per_split;     // steps of 128 bytes along k: in all, per split
