@@ -476,19 +476,19 @@ _LINEAR = struct.Struct("=4I" + "QIIqq" * 6 + "2I2Q")
 _LINEAR_GRAD = struct.Struct("=4I" + "QIIqq" * 7 + "2I2Q")
 _DROPOUT = struct.Struct("=2I" + "QIIqq" * 3 + "I4x2Q")
 _ABSENT = (0, 0, 0, 0, 0)
-_codes = None
+_codes = _uint8 = None
 
 
 def _dtype_codes():
-    global _codes
+    global _codes, _uint8
     if _codes is None:
         import torch
-        _codes = {torch.float32: 0, torch.bfloat16: 1}
+        _codes, _uint8 = {torch.float32: 0, torch.bfloat16: 1}, torch.uint8
     return _codes
 
 
 def _dtype(name, t):
-    code = _dtype_codes().get(t.dtype)
+    code = (_codes or _dtype_codes()).get(t.dtype)
     if code is None:
         raise MorelloError(E_INVAL, "%s is %s: float32 and bfloat16 are what there is" % (name, t.dtype))
     return code
@@ -553,68 +553,90 @@ def _word(name, v):
 
 
 class _On:
-    """The device and stream of a call.  All tensors are on one device, which is current while the call queues
-    its work; with `stream` the outputs and the workspace belong to that stream, and torch is told that it
-    uses the inputs (the caller orders it after whatever makes them)."""
+    """Device and stream of a call that are not the current ones: with `stream` the outputs and the workspace belong
+    to that stream, and torch is told that it uses the inputs (the caller orders it after whatever makes them)."""
 
-    def __init__(self, first, tensors, stream):
+    def __init__(self, index, tensors, stream):
         import torch
-        if not first.is_cuda:
-            raise MorelloError(E_INVAL, "tensors on %s: there is no CPU path" % first.device)
-        index = first.get_device()
-        for t in tensors:
-            if t is not None and t.get_device() != index:
-                raise MorelloError(E_INVAL, "tensors on %s and %s" % (first.device, t.device))
-        self._within = []
-        if stream is not None:
-            if stream.device.index != index:
-                raise MorelloError(E_INVAL, "the stream is on %s, the tensors on %s" % (stream.device, first.device))
-            self._within.append(torch.cuda.stream(stream))
-            for t in (first,) + tensors:
-                if t is not None:
-                    t.record_stream(stream)
-            self.stream = stream.cuda_stream
-        else:
-            if torch.cuda.current_device() != index:
-                self._within.append(torch.cuda.device(index))
+        if stream is None:
+            self._within = torch.cuda.device(index)
             self.stream = torch.cuda.current_stream(index).cuda_stream
+            return
+        if stream.device.index != index:
+            raise MorelloError(E_INVAL, "the stream is on %s, the tensors on cuda:%d" % (stream.device, index))
+        self._within = torch.cuda.stream(stream)
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+        self.stream = stream.cuda_stream
 
     def __enter__(self):
-        for w in self._within:
-            w.__enter__()
-        return self
+        self._within.__enter__()
+        return self.stream
 
     def __exit__(self, *what):
-        for w in reversed(self._within):
-            w.__exit__(*what)
+        self._within.__exit__(*what)
 
 
-def _workspace(n, given, like):
-    import torch
-    if n == 0:
-        return 0
-    if given is None:
-        return torch.empty(n, dtype=torch.uint8, device=like.device)
-    return given
+class _Current:
+    """The current device and stream: nothing to change."""
+
+    def __init__(self, stream):
+        self.stream = stream
+
+    def __enter__(self):
+        return self.stream
+
+    def __exit__(self, *what):
+        pass
 
 
-def _queue(desc, size_of, run, given, like, on):
+_raw_stream = _current_device = None
+
+
+def _on(tensors, stream):
+    """All tensors (None: not given) are on one device, which is current while the call queues its work."""
+    global _raw_stream, _current_device
+    if _raw_stream is None:
+        import torch
+        # (what torch's own generated code asks; torch.cuda.current_stream makes a Stream object first, 1 us)
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+        _current_device = torch.cuda.current_device
+    index = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != index:
+            raise MorelloError(E_INVAL, "tensors on %s and %s" % (tensors[0].device, t.device))
+    if index < 0:
+        raise MorelloError(E_INVAL, "tensors on %s: there is no CPU path" % tensors[0].device)
+    if stream is None and index == _current_device():
+        return _Current(_raw_stream(index))
+    return _On(index, tensors, stream)
+
+
+def _queue(desc, size_of, run, given, like, stream):
     """Ask for the workspace, then queue the call; a workspace of torch's may be freed when this returns (work on
     its stream that uses the memory next comes after the call's)."""
     n = C.c_size_t()
-    _check(size_of(desc, C.byref(n)))
-    ws = _workspace(n.value, given, like) if n.value else None
-    _check(run(desc, C.c_void_p(ws.data_ptr() if ws is not None else None),
-               C.c_size_t(ws.numel() * ws.element_size() if ws is not None else 0), C.c_void_p(on.stream)))
+    rc = size_of(desc, C.byref(n))
+    if rc == 0:
+        if n.value == 0:
+            rc = run(desc, None, C.c_size_t(0), C.c_void_p(stream))
+        else:
+            if given is None:
+                given = like.new_empty(n.value, dtype=_uint8)
+            rc = run(desc, C.c_void_p(given.data_ptr()), C.c_size_t(given.numel() * given.element_size()), C.c_void_p(stream))
+    _check(rc)
 
 
 def _operands(lhs, rhs):
-    """b, m, k, n and the two matrices; rhs without a batch is shared by lhs's batches."""
+    """(b, m, k, n), the two matrices and out's shape; rhs without a batch is shared by lhs's batches."""
     ml, mr = _matrix("lhs", lhs), _matrix("rhs", rhs)
     ls, rs = lhs.shape, rhs.shape
     if ls[-1] != rs[-2] or (len(rs) == 3 and (len(ls) != 3 or ls[0] != rs[0])):
         raise MorelloError(E_INVAL, "lhs of shape %s does not go with rhs of shape %s" % (tuple(ls), tuple(rs)))
-    return (ls[0] if len(ls) == 3 else 1, ls[-2], ls[-1], rs[-1]), ml, mr
+    if len(ls) == 2:
+        return (1, ls[0], ls[1], rs[-1]), ml, mr, (ls[0], rs[-1])
+    return (ls[0], ls[1], ls[2], rs[-1]), ml, mr, (ls[0], ls[1], rs[-1])
 
 
 def linear(lhs, rhs, bias=None, residual=None, *, activation="none", dropout=0.0, seed=0, offset=0, dtype=None, pre=False,
@@ -629,15 +651,13 @@ def linear(lhs, rhs, bias=None, residual=None, *, activation="none", dropout=0.0
     `residual`.  workspace: a uint8 tensor the caller keeps (linear_bytes); stream: where the work
     is queued (the current stream if None).
     """
-    import torch
-    sizes, ml, mr = _operands(lhs, rhs)
-    shape = lhs.shape[:-1] + rhs.shape[-1:]
-    with _On(lhs, (rhs, bias, residual, out, workspace), stream) as on:
+    sizes, ml, mr, shape = _operands(lhs, rhs)
+    with _on((lhs, rhs, bias, residual, out, workspace), stream) as on:
         if out is None:
-            out = torch.empty(shape, dtype=lhs.dtype if dtype is None else dtype, device=lhs.device)
+            out = lhs.new_empty(shape) if dtype is None or dtype == lhs.dtype else lhs.new_empty(shape, dtype=dtype)
         elif dtype is not None and out.dtype != dtype:
             raise MorelloError(E_INVAL, "out is %s, not %s" % (out.dtype, dtype))
-        z = torch.empty(shape, dtype=out.dtype, device=lhs.device) if pre else None
+        z = out.new_empty(shape) if pre else None
         desc = _LINEAR.pack(*sizes, *ml, *mr, *(_ABSENT if bias is None else _vector("bias", bias, sizes[3])),
                             *(_ABSENT if residual is None else _rows("residual", residual, shape)), *_rows("out", out, shape),
                             *(_ABSENT if z is None else _rows("pre", z, shape)),
@@ -652,20 +672,18 @@ def linear_grad(grad, lhs, rhs, bias=None, pre=None, *, activation="none", dropo
     `pre`, the z that it returned (not needed without an activation): mrl_linear_grad.  Each has its operand's type,
     d_rhs also its layout; None for an operand that is not needed, or a bias that is None.  The gradient
     by the residual is `grad`."""
-    import torch
-    sizes, ml, mr = _operands(lhs, rhs)
-    shape = lhs.shape[:-1] + rhs.shape[-1:]
+    sizes, ml, mr, shape = _operands(lhs, rhs)
     act = _activation(activation)
     if act and pre is None:
         raise MorelloError(E_INVAL, "the gradient of %s needs pre" % activation)
-    with _On(lhs, (grad, rhs, bias, pre, workspace), stream) as on:
-        d_lhs = torch.empty(lhs.shape, dtype=lhs.dtype, device=lhs.device) if need_lhs else None
+    with _on((lhs, grad, rhs, bias, pre, workspace), stream) as on:
+        d_lhs = lhs.new_empty(lhs.shape) if need_lhs else None
         d_rhs = None
         if need_rhs and mr[2]:
-            d_rhs = torch.empty(rhs.shape[:-2] + (rhs.shape[-1], rhs.shape[-2]), dtype=rhs.dtype, device=rhs.device).transpose(-1, -2)
+            d_rhs = rhs.new_empty(rhs.shape[:-2] + (rhs.shape[-1], rhs.shape[-2])).transpose(-1, -2)
         elif need_rhs:
-            d_rhs = torch.empty(rhs.shape, dtype=rhs.dtype, device=rhs.device)
-        d_bias = torch.empty(bias.shape, dtype=bias.dtype, device=bias.device) if bias is not None else None
+            d_rhs = rhs.new_empty(rhs.shape)
+        d_bias = bias.new_empty(bias.shape) if bias is not None else None
         m_rhs = _ABSENT
         if d_rhs is not None:       # (of one row or column d_rhs could be read either way: its layout is rhs's)
             st = d_rhs.stride()
@@ -681,12 +699,11 @@ def linear_grad(grad, lhs, rhs, bias=None, pre=None, *, activation="none", dropo
 def dropout(x, residual=None, *, dropout, seed=0, offset=0, out=None, stream=None):
     """residual + D x (mrl_dropout): x of m x n or b x m x n, rows without gaps between batches; see linear for the
     other arguments."""
-    import torch
     if x.dim() not in (2, 3):
         raise MorelloError(E_INVAL, "x has %d dimensions: two, or three with a batch" % x.dim())
-    with _On(x, (residual, out), stream) as on:
+    with _on((x, residual, out), stream) as on:
         if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            out = x.new_empty(x.shape)
         matrices = []
         for name, t in (("x", x), ("residual", residual), ("out", out)):
             if t is None:
@@ -698,7 +715,7 @@ def dropout(x, residual=None, *, dropout, seed=0, offset=0, out=None, stream=Non
             matrices += at
         rows = x.shape[0] * x.shape[1] if x.dim() == 3 else x.shape[0]
         desc = _DROPOUT.pack(rows, x.shape[-1], *matrices, drop_threshold(dropout), _word("seed", seed), _word("offset", offset))
-        _check(lib().mrl_dropout(desc, C.c_void_p(on.stream)))
+        _check(lib().mrl_dropout(desc, C.c_void_p(on)))
     return out
 
 

@@ -9,22 +9,23 @@
 namespace mrl {
 namespace {
 
-constexpr uint32_t kLine = 128;            // bytes of a step along k: 64 bf16 or 32 f32
+constexpr int kStep = 128;                 // bytes of a step along k: 64 bf16 or 32 f32
 constexpr uint32_t kLaunch = 1u << 22;     // workgroups of a launch
 
 // ---- tiles in shared memory
 //
-// A step holds 128 bytes along k of every row (column) of the tile, as chunks of 16 bytes.  KC: the operand's neighbours along k
-// are adjacent, a line of the tile is a row of A (column of B), 8 chunks.  Otherwise a line is one k with the W rows.
+// A step holds LB bytes along k of every row (column) of the tile, as chunks of 16 bytes.  KC: the operand's neighbours along k
+// are adjacent, a line of the tile is a row of A (column of B), 4 or 8 chunks.  Otherwise a line is one k with the W rows.
 // A chunk's place in its line is its number xor swizzle(line): without it the lines that one instruction reads lie in the same
 // banks.
-template <class T, bool KC, bool IS_B, int W>
+template <class T, bool KC, bool IS_B, int W, int LB>
 struct Tile {
   static constexpr int E = 16 / sizeof(T);                           // elements of a chunk
-  static constexpr int kSteps = kLine / sizeof(T);                   // k of a step
-  static constexpr int kLineBytes = KC ? kLine : W * (int)sizeof(T);
+  static constexpr int kSteps = LB / sizeof(T);                      // k of a step
+  static constexpr int kLineBytes = KC ? LB : W * (int)sizeof(T);
   static constexpr int kChunks = kLineBytes / 16;                    // of a line
   __device__ static __forceinline__ uint32_t swizzle(uint32_t line) {
+    if (KC && LB == 64) return (sizeof(T) == 2 && IS_B ? line >> 3 : line >> 2) & 3;
     if (sizeof(T) == 2) {
       if (KC) return IS_B ? (line & 3) | (line >> 1 & 4) : line & 7;
       if (W == 64) return (line & 2) << 1 | (line >> 2 & 2);
@@ -51,9 +52,9 @@ typedef __attribute__((address_space(3))) const char* lds_ptr;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 // bf16: block i's operand of the half step kk (32 k): a lane has k = 32 kk + 8 g .. + 7.
-template <bool KC, bool IS_B, int W>
+template <bool KC, bool IS_B, int W, int LB>
 __device__ __forceinline__ bf16x8 read_block(lds_ptr tile, uint32_t base, uint32_t i, uint32_t kk, uint32_t q, uint32_t g) {
-  using Tl = Tile<bf16, KC, IS_B, W>;
+  using Tl = Tile<bf16, KC, IS_B, W, LB>;
   if (KC) {
     const uint32_t line = base + row_of<bf16, IS_B>(i, q);
     return *(const __attribute__((address_space(3))) bf16x8*)(tile + Tl::at(line, kk * 4 + g));
@@ -68,33 +69,63 @@ __device__ __forceinline__ bf16x8 read_block(lds_ptr tile, uint32_t base, uint32
   }
   return u.v;
 }
-// f32: blocks 2 pair and 2 pair + 1 of the half step kk (16 k): v[s][j] is block 2 pair + s, k = 16 kk + 4 g + j.
-template <bool KC, bool IS_B, int W>
-__device__ __forceinline__ void read_pair(lds_ptr tile, uint32_t base, uint32_t pair, uint32_t kk, uint32_t q, uint32_t g, float (&v)[2][4]) {
-  using Tl = Tile<float, KC, IS_B, W>;
-  const uint32_t row = base + 32 * pair + 2 * q;
+// f32: blocks i and i + 1 (i even) of the half step kk (16 k): element j is k = 16 kk + 4 g + j.
+template <bool KC, bool IS_B, int W, int LB>
+__device__ __forceinline__ void read_pair(lds_ptr tile, uint32_t base, uint32_t i, uint32_t kk, uint32_t q, uint32_t g, f32x4& v0, f32x4& v1) {
+  using Tl = Tile<float, KC, IS_B, W, LB>;
+  const uint32_t row = base + row_of<float, IS_B>(i, q);
   if (KC) {
-#pragma unroll
-    for (uint32_t s = 0; s < 2; s++) {
-      const f32x4 t = *(const __attribute__((address_space(3))) f32x4*)(tile + Tl::at(row + s, kk * 4 + g));
-#pragma unroll
-      for (int j = 0; j < 4; j++) v[s][j] = t[j];
-    }
+    v0 = *(const __attribute__((address_space(3))) f32x4*)(tile + Tl::at(row, kk * 4 + g));
+    v1 = *(const __attribute__((address_space(3))) f32x4*)(tile + Tl::at(row + 1, kk * 4 + g));
   } else {
 #pragma unroll
     for (uint32_t j = 0; j < 4; j++) {
       const uint32_t line = kk * 16 + 4 * g + j;
       const f32x2 t = *(const __attribute__((address_space(3))) f32x2*)(tile + Tl::at(line, row >> 2) + (row & 3) * 4);
-      v[0][j] = t[0];
-      v[1][j] = t[1];
+      v0[j] = t[0];
+      v1[j] = t[1];
     }
   }
+}
+
+// What a lane holds of N blocks for a half step.
+template <class T> struct Operand { using Type = bf16x8; };
+template <> struct Operand<float> { using Type = f32x4; };
+
+template <class T, bool KC, bool IS_B, int W, int LB, int N>
+__device__ __forceinline__ void read_blocks(lds_ptr tile, uint32_t base, uint32_t first, uint32_t kk, uint32_t q, uint32_t g, typename Operand<T>::Type (&v)[N]) {
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int i = 0; i < N; i++) v[i] = read_block<KC, IS_B, W, LB>(tile, base, first + i, kk, q, g);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i += 2) read_pair<KC, IS_B, W, LB>(tile, base, first + i, kk, q, g, v[i], v[i + 1]);
+  }
+}
+
+// acc[first + i][j] += the products of A's block i and B's block j over a half step.  The products are taken as B^T A^T: in the MFMA
+// result a lane has one column and four neighbouring rows, which are then one row of the result and neighbouring columns.
+template <int NM, int BN, int BM>
+__device__ __forceinline__ void multiply(const bf16x8 (&a)[NM], const bf16x8 (&b)[BN], uint32_t first, f32x4 (&acc)[BM][BN]) {
+#pragma unroll
+  for (int i = 0; i < NM; i++)
+#pragma unroll
+    for (int j = 0; j < BN; j++) acc[first + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], a[i], acc[first + i][j], 0, 0, 0);
+}
+template <int NM, int BN, int BM>
+__device__ __forceinline__ void multiply(const f32x4 (&a)[NM], const f32x4 (&b)[BN], uint32_t first, f32x4 (&acc)[BM][BN]) {
+#pragma unroll
+  for (int e = 0; e < 4; e++)
+#pragma unroll
+    for (int i = 0; i < NM; i++)
+#pragma unroll
+      for (int j = 0; j < BN; j++) acc[first + i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(b[j][e], a[i][e], acc[first + i][j], 0, 0, 0);
 }
 
 // The part of a tile that a thread brings from global memory: through registers, any address, zeros where there is nothing.
 template <class T, bool KC, bool IS_B, int W, int THREADS>
 struct Stage {
-  using Tl = Tile<T, KC, IS_B, W>;
+  using Tl = Tile<T, KC, IS_B, W, kStep>;
   static constexpr int N = W * 8 / THREADS;
   u32x4 r[N];
   // src: the tile's first row (column) at k = k0; rows and ks: how many there are from there on
@@ -123,76 +154,76 @@ struct Stage {
   }
 };
 
-// acc += the products of a step: a wave's WM x WN part of the tile at (wm, wn).  The products are taken as B^T A^T: in the MFMA result
-// a lane has one column and four neighbouring rows, which are then one row of the result and neighbouring columns.
-template <class T, bool AKC, bool BKC, int TM, int TN, int BM, int BN>
-__device__ __forceinline__ void multiply(lds_ptr ta, lds_ptr tb, uint32_t wm, uint32_t wn, uint32_t q, uint32_t g, f32x4 (&acc)[BM][BN]) {
-#pragma unroll
-  for (uint32_t kk = 0; kk < 2; kk++) {
-    if constexpr (sizeof(T) == 2) {
-      bf16x8 fa[BM], fb[BN];
-#pragma unroll
-      for (int i = 0; i < BM; i++) fa[i] = read_block<AKC, false, TM>(ta, wm, i, kk, q, g);
-#pragma unroll
-      for (int j = 0; j < BN; j++) fb[j] = read_block<BKC, true, TN>(tb, wn, j, kk, q, g);
-#pragma unroll
-      for (int i = 0; i < BM; i++)
-#pragma unroll
-        for (int j = 0; j < BN; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
-    } else {
-      float fa[BM / 2][2][4], fb[BN / 2][2][4];
-#pragma unroll
-      for (int i = 0; i < BM / 2; i++) read_pair<AKC, false, TM>(ta, wm, i, kk, q, g, fa[i]);
-#pragma unroll
-      for (int j = 0; j < BN / 2; j++) read_pair<BKC, true, TN>(tb, wn, j, kk, q, g, fb[j]);
-#pragma unroll
-      for (int e = 0; e < 4; e++)
-#pragma unroll
-        for (int i = 0; i < BM; i++)
-#pragma unroll
-          for (int j = 0; j < BN; j++)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[j >> 1][j & 1][e], fa[i >> 1][i & 1][e], acc[i][j], 0, 0, 0);
-    }
-  }
-}
-
 // Where a workgroup's tile lies.
 struct Place { uint32_t tm, tn, split, batch; };
-__device__ __forceinline__ Place place(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, uint32_t splits) {
+// Workgroups go to the eight dies in turn, each with an L2 of its own: a die gets a stretch of consecutive tiles, and
+// consecutive tiles are kGroup rows of tiles high, so that the tiles that are worked on at once share rows and columns there.
+constexpr uint32_t kDies = 8, kGroup = 8;
+__device__ __forceinline__ Place place(uint32_t first, uint32_t tiles_m, uint32_t tiles_n, uint32_t splits) {
+  const uint32_t i = blockIdx.x, die = i % kDies, each = gridDim.x / kDies, rest = gridDim.x % kDies;
+  uint32_t id = first + die * each + min(die, rest) + i / kDies;
+  const uint32_t tiles = tiles_m * tiles_n, outer = id / tiles;
+  id -= outer * tiles;
   Place at;
-  at.tn = id % tiles_n;
-  id /= tiles_n;
-  at.tm = id % tiles_m;
-  id /= tiles_m;
-  at.split = id % splits;
-  at.batch = id / splits;
+  at.split = outer % splits;
+  at.batch = outer / splits;
+  const uint32_t band = id / (kGroup * tiles_n), top = band * kGroup, high = min(kGroup, tiles_m - top);
+  id -= band * kGroup * tiles_n;
+  at.tm = top + id % high;
+  at.tn = id / high;
   return at;
 }
 
-// A wave's results: a lane has row row_of(i, q) and, of the pair of blocks 2 j, 2 j + 1, the eight columns from 32 j + 8 g on.
+// A wave's results: a lane has row row_of(i, q) and, of the pair of blocks 2 j, 2 j + 1, the eight columns from 32 j + 8 g on.  They go
+// through shared memory that is the wave's own, four blocks of rows at a time at most, so that a row's results are
+// stored side by side (lines of 128 bytes and more) and the epilogue is a short loop: unrolled over the registers it is as long as
+// the instruction cache.  The 16-byte chunks of a row lie at their number xor the row's, against bank conflicts.
 template <class T, int BM, int BN>
-__device__ __forceinline__ void write_out(const Product& p, const Place& at, uint32_t splits, uint32_t m0, uint32_t n0, uint32_t q, uint32_t g,
-                                          const f32x4 (&acc)[BM][BN], float* __restrict__ partial) {
-  const uint32_t pitch = (p.N + 7) & ~7u;
+__device__ __forceinline__ void write_out(const Product& p, const Place& at, uint32_t splits, uint32_t m0, uint32_t n0, uint32_t lane,
+                                          const f32x4 (&acc)[BM][BN], char* mine, float* __restrict__ partial) {
+  constexpr uint32_t CHUNKS = BN * 4, GROUPS = BN * 2, ROWS = 64 / GROUPS;      // chunks and groups of 8 columns of a row; rows at a time
+  constexpr int PASS = BM > 4 ? BM / 2 : BM;                                    // blocks of rows that go through at once
+  const uint32_t q = lane & 15, g = lane >> 4, pitch = (p.N + 7) & ~7u;
+  const uint32_t c = lane % GROUPS, n = n0 + c * 8;
+  float bias[8];
+  bias8(p.e, n, n < p.N ? p.N - n : 0, bias);
 #pragma unroll
-  for (int i = 0; i < BM; i++) {
-    const uint32_t m = m0 + row_of<T, false>(i, q);
-    if (m >= p.M) continue;
+  for (int h = 0; h < BM; h += PASS) {
 #pragma unroll
-    for (int j = 0; j < BN / 2; j++) {
-      const uint32_t n = n0 + 32 * j + 8 * g;
-      if (n >= p.N) continue;
-      float v[8];
+    for (int i = 0; i < PASS; i++) {
+      const uint32_t r = row_of<T, false>(i, q);
 #pragma unroll
-      for (int e = 0; e < 8; e++) v[e] = sizeof(T) == 2 ? acc[i][2 * j + (e >> 2)][e & 3] : acc[i][2 * j + (e & 1)][e >> 1];
-      if (splits > 1) {
-        float* out = partial + (((uint64_t)at.split * p.batches + at.batch) * p.M + m) * pitch + n;
+      for (int j = 0; j < BN / 2; j++)
 #pragma unroll
-        for (int h = 0; h < 2; h++) *(f32x4*)(out + 4 * h) = f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
-      } else {
-        finish8(p.e, at.batch, p.M, m, n, p.N - n, v);
+        for (int x = 0; x < 2; x++) {
+          const f32x4 &lo = acc[h + i][2 * j], &hi = acc[h + i][2 * j + 1];
+          *(f32x4*)(mine + (r * CHUNKS + ((8 * j + 2 * g + x) ^ (r & (CHUNKS - 1)))) * 16) =
+              sizeof(T) == 2 ? (x ? hi : lo) : f32x4{lo[2 * x], hi[2 * x], lo[2 * x + 1], hi[2 * x + 1]};
+        }
+    }
+    asm volatile("" ::: "memory");         // (a wave's accesses to shared memory are done in their order)
+    if (n < p.N) {
+#pragma unroll 2
+      for (uint32_t r = lane / GROUPS; r < 16 * PASS; r += ROWS) {
+        const uint32_t m = m0 + h * 16 + r;
+        if (m >= p.M) break;
+        float v[8];
+#pragma unroll
+        for (int x = 0; x < 2; x++) {
+          const f32x4 t = *(const f32x4*)(mine + (r * CHUNKS + ((2 * c + x) ^ (r & (CHUNKS - 1)))) * 16);
+#pragma unroll
+          for (int e = 0; e < 4; e++) v[4 * x + e] = t[e];
+        }
+        if (splits > 1) {
+          float* out = partial + (((uint64_t)at.split * p.batches + at.batch) * p.M + m) * pitch + n;
+#pragma unroll
+          for (int x = 0; x < 2; x++) *(f32x4*)(out + 4 * x) = f32x4{v[4 * x], v[4 * x + 1], v[4 * x + 2], v[4 * x + 3]};
+        } else {
+          finish8(p.e, at.batch, p.M, m, n, p.N - n, bias, v);
+        }
       }
     }
+    asm volatile("" ::: "memory");
   }
 }
 
@@ -201,10 +232,10 @@ template <class T, bool AKC, bool BKC, int TM, int TN, int WAVES_M, int WAVES_N>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void product_kernel(const Product p, uint32_t steps, uint32_t per_split, uint32_t splits,
                                                                          uint32_t first, float* __restrict__ partial) {
   constexpr int THREADS = 64 * WAVES_M * WAVES_N, WM = TM / WAVES_M, WN = TN / WAVES_N, BM = WM / 16, BN = WN / 16;
-  constexpr uint32_t KS = kLine / sizeof(T);
-  __shared__ __attribute__((aligned(16))) char lds[2][(TM + TN) * kLine];
+  constexpr uint32_t KS = kStep / sizeof(T);
+  __shared__ __attribute__((aligned(16))) char lds[2][(TM + TN) * kStep];
 
-  const Place at = place(first + blockIdx.x, (p.M + TM - 1) / TM, (p.N + TN - 1) / TN, splits);
+  const Place at = place(first, (p.M + TM - 1) / TM, (p.N + TN - 1) / TN, splits);
   const uint32_t m0 = at.tm * TM, n0 = at.tn * TN;
 
   const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6, q = lane & 15, g = lane >> 4;
@@ -232,22 +263,28 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void product_kernel(const P
   if (begin < end) {
     load(begin);
     sa.store(lds[0], t);
-    sb.store(lds[0] + TM * kLine, t);
+    sb.store(lds[0] + TM * kStep, t);
   }
   __syncthreads();
   for (uint32_t step = begin; step < end; step++) {
     const uint32_t cur = (step - begin) & 1;
     if (step + 1 < end) load(step + 1);
-    const lds_ptr ta = (lds_ptr)lds[cur], tb = ta + TM * kLine;
-    multiply<T, AKC, BKC, TM, TN, BM, BN>(ta, tb, wm, wn, q, g, acc);
+    const lds_ptr ta = (lds_ptr)lds[cur], tb = ta + TM * kStep;
+#pragma unroll
+    for (uint32_t kk = 0; kk < 2; kk++) {
+      typename Operand<T>::Type fa[BM], fb[BN];
+      read_blocks<T, AKC, false, TM, kStep>(ta, wm, 0, kk, q, g, fa);
+      read_blocks<T, BKC, true, TN, kStep>(tb, wn, 0, kk, q, g, fb);
+      multiply(fa, fb, 0, acc);
+    }
     if (step + 1 < end) {
       sa.store(lds[cur ^ 1], t);
-      sb.store(lds[cur ^ 1] + TM * kLine, t);
+      sb.store(lds[cur ^ 1] + TM * kStep, t);
     }
     __syncthreads();
   }
 
-  write_out<T, BM, BN>(p, at, splits, m0 + wm, n0 + wn, q, g, acc, partial);
+  write_out<T, BM, BN>(p, at, splits, m0 + wm, n0 + wn, lane, acc, &lds[0][0] + wave * (WM * WN * 4), partial);
 }
 
 // ---- operands whose lines start at multiples of 16 bytes
@@ -267,10 +304,10 @@ __device__ __forceinline__ void load_to_lds(uint32_t lds, uint32_t offset, u32x4
 
 constexpr uint32_t kOutside = 0x80000000u;        // beyond any buffer's range
 
-template <class T, bool KC, bool IS_B, int W, int THREADS>
+template <class T, bool KC, bool IS_B, int W, int LB, int THREADS>
 struct Feed {
-  using Tl = Tile<T, KC, IS_B, W>;
-  static constexpr int N = W * 8 / THREADS;       // loads of a thread and step
+  using Tl = Tile<T, KC, IS_B, W, LB>;
+  static constexpr int N = W * (LB / 16) / THREADS;       // loads of a thread and step
   uint32_t offset[N];                             // bytes from the tile's first element of a step
   __device__ __forceinline__ void init(int64_t ld, uint32_t t) {
 #pragma unroll
@@ -282,7 +319,9 @@ struct Feed {
   // from: the tile's first element of the step; left: bytes from there to the operand's end; ks: k that are left in the segment
   __device__ __forceinline__ void load(const char* from, int64_t left, uint32_t ks, uint32_t lds, uint32_t t) const {
     const uint64_t base = (uint64_t)from;
-    const u32x4 buffer = {(uint32_t)base, (uint32_t)(base >> 32) & 0xFFFFu, (uint32_t)(left < (int64_t)kOutside ? left : (int64_t)kOutside), 0x27000u};
+    const uint32_t low = (uint32_t)left, range = (uint32_t)(left >> 32) | low >> 31 ? kOutside : low;      // (scalar units have no 64-bit minimum)
+    const u32x4 buffer = {(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)base), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(base >> 32) & 0xFFFFu),
+                          (uint32_t)__builtin_amdgcn_readfirstlane(range), 0x27000u};
 #pragma unroll
     for (int i = 0; i < N; i++) {
       uint32_t at = offset[i];
@@ -295,21 +334,21 @@ struct Feed {
   }
 };
 
-template <class T, bool AKC, bool BKC, int TM, int TN, int WAVES_M, int WAVES_N, int STAGES>
-__global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void fast_kernel(const Product p, uint32_t steps, uint32_t per_split, uint32_t splits,
+template <class T, bool AKC, bool BKC, int TM, int TN, int WAVES_M, int WAVES_N, int LB, int STAGES>
+__global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void fast_kernel(const Product p, uint32_t steps, uint32_t per_split, uint32_t splits,
                                                                       uint32_t first, float* __restrict__ partial) {
   constexpr int THREADS = 64 * WAVES_M * WAVES_N, WM = TM / WAVES_M, WN = TN / WAVES_N, BM = WM / 16, BN = WN / 16;
-  constexpr uint32_t KS = kLine / sizeof(T), STAGE = (TM + TN) * kLine;
+  constexpr uint32_t KS = LB / sizeof(T), STAGE = (TM + TN) * LB;
   __shared__ __attribute__((aligned(1024))) char lds[STAGES * STAGE];
 
-  const Place at = place(first + blockIdx.x, (p.M + TM - 1) / TM, (p.N + TN - 1) / TN, splits);
+  const Place at = place(first, (p.M + TM - 1) / TM, (p.N + TN - 1) / TN, splits);
   const uint32_t m0 = at.tm * TM, n0 = at.tn * TN;
   const uint32_t t = threadIdx.x, lane = t & 63, q = lane & 15, g = lane >> 4;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const uint32_t wm = wave / WAVES_N * WM, wn = wave % WAVES_N * WN;
 
-  Feed<T, AKC, false, TM, THREADS> fa;
-  Feed<T, BKC, true, TN, THREADS> fb;
+  Feed<T, AKC, false, TM, LB, THREADS> fa;
+  Feed<T, BKC, true, TN, LB, THREADS> fb;
   fa.init(p.lda, t);
   fb.init(p.ldb, t);
   constexpr int LOADS = decltype(fa)::N + decltype(fb)::N;
@@ -325,11 +364,15 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void fast_kernel(const Prod
   const int64_t size_b = (BKC ? ((int64_t)(p.N - n0) - 1) * p.ldb + p.K : ((int64_t)p.K - 1) * p.ldb + (p.N - n0)) * (int64_t)sizeof(T);
   int64_t off_a = (int64_t)(k / KS) * step_a, off_b = (int64_t)(k / KS) * step_b;
   const char *sa = a0 + (int64_t)seg * p.seg_a * (int64_t)sizeof(T), *sb = b0 + (int64_t)seg * p.seg_b * (int64_t)sizeof(T);
+  const uint32_t n = end > begin ? end - begin : 0;
+  uint32_t loaded = 0;
+  // (behind the last step the buffers have no bytes: zeros are written that nothing uses, and every step has the same loads under way)
   const auto load = [&](uint32_t stage) {
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_ptr)lds + stage * STAGE;
-    const uint32_t mine = __builtin_amdgcn_readfirstlane(lds0);
-    fa.load(sa + off_a, size_a - off_a, p.K - k, mine, wave * 64 + lane);
-    fb.load(sb + off_b, size_b - off_b, p.K - k, mine + TM * kLine, wave * 64 + lane);
+    const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr)lds + stage * STAGE);
+    const bool more = loaded++ < n;
+    fa.load(sa + off_a, more ? size_a - off_a : 0, p.K - k, to, wave * 64 + lane);
+    fb.load(sb + off_b, more ? size_b - off_b : 0, p.K - k, to + TM * LB, wave * 64 + lane);
+    if (!more) return;
     k += KS;
     off_a += step_a;
     off_b += step_b;
@@ -347,20 +390,46 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void fast_kernel(const Prod
 #pragma unroll
     for (int j = 0; j < BN; j++) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-  const uint32_t n = end > begin ? end - begin : 0;
+  // A half step of 64 bytes along k is one or two phases of NM blocks of rows each.  A phase first reads the operands of the next one, then
+  // multiplies, so that the reads' latency lies under the products.  Before the last phase of a step everything of it has been read and
+  // the next step's tile must be there: the one barrier of a step; behind it this step's place is free for the step STAGES ahead.
+  constexpr int NM = BM > 4 ? BM / 2 : BM, PHASES = BM / NM;
+  typename Operand<T>::Type oa[2][NM], ob[2][BN];
+  if (n) {
 #pragma unroll
-  for (int s = 0; s < STAGES - 1; s++) if (s < (int)n) load(s);
-  uint32_t cur = 0, next = STAGES - 1;
-  for (uint32_t s = 0; s < n; s++) {
-    if (s + STAGES - 1 <= n) arrive<(STAGES - 2) * LOADS>();      // the later stages' loads may still be under way
-    else arrive<0>();
-    if (s + STAGES - 1 < n) load(next);
-    const lds_ptr ta = (lds_ptr)lds + cur * STAGE;
-    multiply<T, AKC, BKC, TM, TN, BM, BN>(ta, ta + TM * kLine, wm, wn, q, g, acc);
-    cur = cur + 1 == STAGES ? 0 : cur + 1;
-    next = next + 1 == STAGES ? 0 : next + 1;
+    for (int s = 0; s < STAGES; s++) load(s);
+    arrive<(STAGES - 1) * LOADS>();
+    read_blocks<T, AKC, false, TM, LB>((lds_ptr)lds, wm, 0, 0, q, g, oa[0]);
+    read_blocks<T, BKC, true, TN, LB>((lds_ptr)lds + TM * LB, wn, 0, 0, q, g, ob[0]);
+    uint32_t cur = 0;
+    for (uint32_t s = 0; s < n; s += 128 / LB) {  // (two half steps a turn, as the operands' registers alternate; one too many adds zeros)
+#pragma unroll
+      for (int h = 0; h < 2; h++) {
+        const bool ends = LB == 64 || h == 1;
+        const uint32_t next = cur + 1 == STAGES ? 0 : cur + 1;
+#pragma unroll
+        for (int ph = 0; ph < PHASES; ph++) {
+          const int now = (h * PHASES + ph) & 1;
+          if (ph == PHASES - 1) {
+            if (ends) {
+              arrive<(STAGES - 2) * LOADS>();
+              load(cur);
+            }
+            const lds_ptr tile = (lds_ptr)lds + (ends ? next : cur) * STAGE;
+            read_blocks<T, AKC, false, TM, LB>(tile, wm, 0, ends ? 0 : 1, q, g, oa[now ^ 1]);
+            read_blocks<T, BKC, true, TN, LB>(tile + TM * LB, wn, 0, ends ? 0 : 1, q, g, ob[h ^ 1]);
+          } else {
+            read_blocks<T, AKC, false, TM, LB>((lds_ptr)lds + cur * STAGE, wm, NM, LB == 64 ? 0 : h, q, g, oa[now ^ 1]);
+          }
+          multiply(oa[now], ob[h], ph * NM, acc);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (ends) cur = next;
+      }
+    }
+    arrive<0>();                  // nothing is under way to shared memory when the workgroup gives it up
   }
-  write_out<T, BM, BN>(p, at, splits, m0 + wm, n0 + wn, q, g, acc, partial);
+  write_out<T, BM, BN>(p, at, splits, m0 + wm, n0 + wn, lane, acc, lds + wave * (sizeof lds / (WAVES_M * WAVES_N)), partial);
 }
 
 // The sum over the splits, in their order, and the epilogue: eight columns a thread.
@@ -379,7 +448,9 @@ __global__ __launch_bounds__(256) void join_kernel(const Product p, uint32_t spl
     in += rows * (groups * 8);
   }
   const uint32_t batch = (uint32_t)(row / p.M);
-  finish8(p.e, batch, p.M, (uint32_t)(row - (uint64_t)batch * p.M), n, p.N - n, v);
+  float bias[8];
+  bias8(p.e, n, p.N - n, bias);
+  finish8(p.e, batch, p.M, (uint32_t)(row - (uint64_t)batch * p.M), n, p.N - n, bias, v);
 }
 
 // ---- rows
@@ -405,8 +476,7 @@ __global__ __launch_bounds__(256) void grad_rows_kernel(const GradRows p, uint32
       if (p.pre.data) {
         float z[8];
         load8(p.pre.data, p.pre.bf16, (int64_t)batch * p.pre.batch + (int64_t)m * p.pre.ld + n, valid, z);
-#pragma unroll
-        for (int e = 0; e < 8; e++) v[e] *= slope(p.activation, z[e]);
+        slope8(p.activation, z, v);
       }
 #pragma unroll
       for (int e = 0; e < 8; e++) sum[e] += v[e];
@@ -467,15 +537,17 @@ hipError_t in_launches(uint64_t blocks, F&& f) {
 
 template <class T, bool AKC, bool BKC>
 hipError_t launch_tiles(const Product& p, const ProductPlan& plan, float* partial, hipStream_t st) {
-  const uint64_t tiles = (uint64_t)((p.M + plan.tile - 1) / plan.tile) * ((p.N + plan.tile - 1) / plan.tile);
-  if (plan.fast) return in_launches(tiles * plan.splits * p.batches, [&](uint64_t first, uint32_t n) {
-    if (plan.tile == 256) fast_kernel<T, AKC, BKC, 256, 256, 2, 4, 2><<<n, 512, 0, st>>>(p, plan.steps, plan.per_split, plan.splits, (uint32_t)first, partial);
-    else if (plan.tile == 128) fast_kernel<T, AKC, BKC, 128, 128, 2, 2, 2><<<n, 256, 0, st>>>(p, plan.steps, plan.per_split, plan.splits, (uint32_t)first, partial);
-    else fast_kernel<T, AKC, BKC, 64, 64, 2, 2, 4><<<n, 256, 0, st>>>(p, plan.steps, plan.per_split, plan.splits, (uint32_t)first, partial);
-  });
-  return in_launches(tiles * plan.splits * p.batches, [&](uint64_t first, uint32_t n) {
-    if (plan.tile == 128) product_kernel<T, AKC, BKC, 128, 128, 2, 2><<<n, 256, 0, st>>>(p, plan.steps, plan.per_split, plan.splits, (uint32_t)first, partial);
-    else product_kernel<T, AKC, BKC, 64, 64, 2, 2><<<n, 256, 0, st>>>(p, plan.steps, plan.per_split, plan.splits, (uint32_t)first, partial);
+  return in_launches(plan.blocks, [&](uint64_t first, uint32_t n) {
+    const auto go = [&](auto kernel, uint32_t threads) { kernel<<<n, threads, 0, st>>>(p, plan.steps, plan.per_split, plan.splits, (uint32_t)first, partial); };
+    switch (plan.kernel) {
+      case kFast256: return go(fast_kernel<T, AKC, BKC, 256, 256, 2, 4, 128, 2>, 512);
+      case kFast256x128: return go(fast_kernel<T, AKC, BKC, 256, 128, 4, 2, 128, 3>, 512);
+      case kFast128: return go(fast_kernel<T, AKC, BKC, 128, 128, 2, 4, 128, 2>, 512);
+      case kFast128Alone: return go(fast_kernel<T, AKC, BKC, 128, 128, 2, 4, 128, 4>, 512);
+      case kFast64: return go(fast_kernel<T, AKC, BKC, 64, 64, 2, 2, 128, 4>, 256);
+      case kAny128: return go(product_kernel<T, AKC, BKC, 128, 128, 2, 2>, 256);
+      case kAny64: return go(product_kernel<T, AKC, BKC, 64, 64, 2, 2>, 256);
+    }
   });
 }
 template <class T>
@@ -495,25 +567,59 @@ bool aligned(const Product& p) {
 
 }  // namespace
 
+// How long a kernel takes, in us: a round of workgroups on the 256 compute units, one each or two at once, is `fixed` and a
+// step's time for each step along k.  Measured on products whose tiles are one whole round, 2048 and 8192 long along k:
+//                      step bf16 (one, two)   step f32 (one, two)
+//   256 x 256               1.52     -          7.33     -
+//   256 x 128               0.87     -          3.81     -
+//   128 x 128, 4 stages     0.50     -          1.99     -        (2 stages alone: 0.56; four fill the shared memory)
+//   128 x 128, 2 stages       -     0.93          -     3.78
+//   64 x 64                 0.25    0.37        0.62    1.07
+// So a large tile does more per time (16 units of 64 x 64 in 1.52 against 1 in 0.25) and a small one leaves fewer compute units
+// without work; where the tiles are few, workgroups share a tile's sum and a second launch adds up: its time, and the partial sums
+// written and read at 4.5 TB/s.
+struct Kernel { uint32_t id, tm, tn; bool fast; float fixed, one[2], two[2]; };
+constexpr Kernel kKernels[] = {
+    {kFast256, 256, 256, true, 11, {1.52f, 7.33f}, {0, 0}},
+    {kFast256x128, 256, 128, true, 6, {0.87f, 3.81f}, {0, 0}},
+    {kFast128, 128, 128, true, 4, {0.50f, 1.99f}, {0.93f, 3.78f}},
+    {kFast64, 64, 64, true, 2, {0.25f, 0.62f}, {0.37f, 1.07f}},
+    {kAny128, 128, 128, false, 4, {1.90f, 2.60f}, {2.60f, 4.20f}},
+    {kAny64, 64, 64, false, 2, {0.70f, 0.90f}, {0.90f, 1.40f}},
+};
+constexpr float kJoin = 4, kJoinBytes = 4.5e6f;
+
 ProductPlan plan_product(const Product& p) {
-  const uint32_t ks = kLine / (p.bf16 ? 2 : 4);
   ProductPlan plan{};
+  const uint32_t ks = kStep / (p.bf16 ? 2 : 4), f32 = !p.bf16;
+  const bool fast = aligned(p);
   plan.steps = (p.K + ks - 1) / ks * p.segs;
-  const auto tiles = [&](uint64_t t) { return (p.M + t - 1) / t * ((p.N + t - 1) / t) * p.batches; };
-  plan.fast = aligned(p);
-  plan.tile = plan.fast && tiles(256) >= 256 ? 256 : tiles(128) >= 256 ? 128 : 64;
-  // fewer tiles than compute units: several workgroups share a tile's sum, four steps each at least
-  const uint64_t n = tiles(plan.tile);
-  uint64_t splits = n && n < 256 ? std::min<uint64_t>({512 / n, plan.steps / 4, 64}) : 1;
-  splits = std::max<uint64_t>(splits, 1);
-  plan.per_split = (uint32_t)((plan.steps + splits - 1) / splits);
-  plan.splits = plan.per_split ? (plan.steps + plan.per_split - 1) / plan.per_split : 1;
+  const float out = (float)p.batches * p.M * p.N * 4;
+  float best = 0;
+  for (const Kernel& k : kKernels) {
+    if (k.fast != fast) continue;
+    const uint64_t tiles = (uint64_t)((p.M + k.tm - 1) / k.tm) * ((p.N + k.tn - 1) / k.tn) * p.batches;
+    for (uint32_t splits = 1; splits <= 64; splits = splits == 1 ? 2 : splits & splits - 1 ? splits / 3 * 4 : splits / 2 * 3) {
+      const uint32_t per = (plan.steps + splits - 1) / splits;
+      if (splits > 1 && (per < 4 || tiles * splits > 1024)) break;
+      const float one = k.fixed + per * k.one[f32], two = k.two[0] ? k.fixed + per * k.two[f32] : 2 * one;
+      const uint64_t blocks = tiles * splits, rounds = blocks / 512, rest = blocks % 512;
+      float t = rounds * two + (rest > 256 ? two : rest ? one : 0);
+      if (splits > 1) t += kJoin + (splits + 1) * out / kJoinBytes;
+      if (best && t >= best) continue;
+      best = t;
+      plan.kernel = k.id == kFast128 && blocks <= 256 ? kFast128Alone : k.id;
+      plan.per_split = per;
+      plan.splits = per ? (plan.steps + per - 1) / per : 1;
+      plan.blocks = tiles * plan.splits;
+    }
+  }
   plan.partial_bytes = plan.splits > 1 ? (uint64_t)plan.splits * p.batches * p.M * ((p.N + 7) / 8 * 8) * 4 : 0;
   return plan;
 }
 
 hipError_t launch_product(const Product& p, const ProductPlan& plan, float* partial, hipStream_t st) {
-  if (!p.batches || !p.M || !p.N) return hipSuccess;
+  if (!plan.blocks) return hipSuccess;
   const hipError_t e = p.bf16 ? launch_layout<bf16>(p, plan, partial, st) : launch_layout<float>(p, plan, partial, st);
   if (e != hipSuccess || plan.splits == 1) return e;
   const uint64_t items = (uint64_t)p.batches * p.M * ((p.N + 7) / 8);

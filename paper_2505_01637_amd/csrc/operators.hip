@@ -70,11 +70,9 @@ int32_t check_common(uint32_t b, uint32_t m, uint32_t k, uint32_t n, uint32_t ac
 // An operand of a product over k: lines along the other index where its neighbours along k are adjacent.
 struct Side { const void* data; uint32_t kc; int64_t ld, batch; };
 
-// A launch counts its workgroups in 32 bits.
+// Workgroups and steps are counted in 32 bits.
 int32_t check_product(const Product& p, const ProductPlan& plan) {
-  const uint64_t tiles_m = (p.M + plan.tile - 1) / plan.tile, tiles_n = (p.N + plan.tile - 1) / plan.tile;
-  const double blocks = (double)tiles_m * (double)tiles_n * plan.splits * p.batches;
-  CHECK(blocks < 4294967296.0 && (double)p.segs * ((p.K + 31) / 32) < 4294967296.0, "the product is too large for one call");
+  CHECK(plan.blocks <= UINT32_MAX && (uint64_t)p.segs * ((p.K + 31ull) / 32) <= UINT32_MAX, "the product is too large for one call");
   return MRL_OK;
 }
 
