@@ -122,35 +122,55 @@ __device__ __forceinline__ void multiply(const f32x4 (&a)[NM], const f32x4 (&b)[
       for (int j = 0; j < BN; j++) acc[first + i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(b[j][e], a[i][e], acc[first + i][j], 0, 0, 0);
 }
 
-// The part of a tile that a thread brings from global memory: through registers, any address, zeros where there is nothing.
-template <class T, bool KC, bool IS_B, int W, int THREADS>
+// The part of a tile that a thread brings from global memory through registers, from any address.
+//
+// WIDE: every line has at least a chunk's elements.  Then every chunk is one load of 16 bytes whatever the edge: a chunk that ends past its line
+// is read from the line's last 16 bytes, a line that is not there at the last one, and both are put right (shifted, zeroed) on the way
+// to shared memory, so that no load waits for a branch.  Otherwise element by element.
+template <class T, bool KC, bool IS_B, int W, int THREADS, bool WIDE>
 struct Stage {
   using Tl = Tile<T, KC, IS_B, W, kStep>;
-  static constexpr int N = W * 8 / THREADS;
+  static constexpr int N = W * 8 / THREADS, E = Tl::E;
   u32x4 r[N];
-  // src: the tile's first row (column) at k = k0; rows and ks: how many there are from there on
-  __device__ __forceinline__ void load(const T* src, int64_t ld, uint32_t rows, uint32_t ks, uint32_t t) {
+  uint32_t ks;                     // k that are left where r was read
+  __device__ static __forceinline__ uint32_t line(int i, uint32_t t) { return (t + i * THREADS) / Tl::kChunks; }
+  __device__ static __forceinline__ int32_t at(int i, uint32_t t) { return (t + i * THREADS) % Tl::kChunks * E; }
+
+  // src: the tile's first row (column) at k = k0; rows and left: how many rows (columns) and k there are from there on
+  __device__ __forceinline__ void load(const T* src, int64_t ld, uint32_t rows, uint32_t left, uint32_t t) {
+    ks = left;
+    const uint32_t lines = KC ? rows : left, width = KC ? left : rows;
 #pragma unroll
     for (int i = 0; i < N; i++) {
-      const uint32_t c = t + i * THREADS, line = c / Tl::kChunks, at = c % Tl::kChunks * Tl::E;
-      const uint32_t lines = KC ? rows : ks, width = KC ? ks : rows;
-      const T* p = src + (int64_t)line * ld + at;
-      T v[Tl::E];
-      if (line < lines && at + Tl::E <= width) {
-        __builtin_memcpy(v, p, 16);
+      const uint32_t l = line(i, t);
+      if constexpr (WIDE) {
+        const int32_t from = min(at(i, t), (int32_t)min(width, 1u << 30) - E);
+        __builtin_memcpy(&r[i], src + (int64_t)min(l, lines - 1) * ld + from, 16);
       } else {
+        const T* p = src + (int64_t)l * ld;
+        T v[E];
 #pragma unroll
-        for (int e = 0; e < Tl::E; e++) v[e] = line < lines && at + e < width ? p[e] : (T)0.0f;
+        for (int e = 0; e < E; e++) v[e] = l < lines && (uint32_t)at(i, t) + e < width ? p[at(i, t) + e] : (T)0.0f;
+        __builtin_memcpy(&r[i], v, 16);
       }
-      __builtin_memcpy(&r[i], v, 16);
     }
   }
-  __device__ __forceinline__ void store(char* tile, uint32_t t) const {
+  __device__ __forceinline__ void store(char* tile, uint32_t rows, uint32_t t) {
+    if (WIDE && (ks < (uint32_t)Tl::kSteps || (!KC && rows < W))) {
+      const uint32_t width = KC ? ks : rows;
 #pragma unroll
-    for (int i = 0; i < N; i++) {
-      const uint32_t c = t + i * THREADS;
-      *(u32x4*)(tile + Tl::at(c / Tl::kChunks, c % Tl::kChunks)) = r[i];
+      for (int i = 0; i < N; i++) {
+        // (behind the end of the sum zeros; rows and columns that are not there may hold anything, as nothing of them is stored)
+        const int32_t past = max(at(i, t) + E - (int32_t)min(width, 1u << 30), 0);
+        const bool none = past >= E || (!KC && line(i, t) >= ks);
+        const uint32_t s = past * 8 * sizeof(T) & 127;
+        const uint64_t lo = (uint64_t)r[i][1] << 32 | r[i][0], hi = (uint64_t)r[i][3] << 32 | r[i][2];
+        const uint64_t l = s >= 64 ? hi >> (s - 64) : s ? lo >> s | hi << (64 - s) : lo, h = s >= 64 ? 0 : hi >> s;
+        r[i] = none ? u32x4{0, 0, 0, 0} : u32x4{(uint32_t)l, (uint32_t)(l >> 32), (uint32_t)h, (uint32_t)(h >> 32)};
+      }
     }
+#pragma unroll
+    for (int i = 0; i < N; i++) *(u32x4*)(tile + Tl::at(line(i, t), (uint32_t)at(i, t) / E)) = r[i];
   }
 };
 
@@ -228,7 +248,7 @@ __device__ __forceinline__ void write_out(const Product& p, const Place& at, uin
 }
 
 // One tile of TM x TN, WAVES_M x WAVES_N waves, over a stretch of the steps along k: operands of any stride and alignment.
-template <class T, bool AKC, bool BKC, int TM, int TN, int WAVES_M, int WAVES_N>
+template <class T, bool AKC, bool BKC, int TM, int TN, int WAVES_M, int WAVES_N, bool WIDE>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void product_kernel(const Product p, uint32_t steps, uint32_t per_split, uint32_t splits,
                                                                          uint32_t first, float* __restrict__ partial) {
   constexpr int THREADS = 64 * WAVES_M * WAVES_N, WM = TM / WAVES_M, WN = TN / WAVES_N, BM = WM / 16, BN = WN / 16;
@@ -237,21 +257,26 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void product_kernel(const P
 
   const Place at = place(first, (p.M + TM - 1) / TM, (p.N + TN - 1) / TN, splits);
   const uint32_t m0 = at.tm * TM, n0 = at.tn * TN;
-
   const uint32_t t = threadIdx.x, lane = t & 63, wave = t >> 6, q = lane & 15, g = lane >> 4;
   const uint32_t wm = wave / WAVES_N * WM, wn = wave % WAVES_N * WN;
-
-  const T* a = (const T*)p.a + (int64_t)at.batch * p.batch_a + (AKC ? (int64_t)m0 * p.lda : (int64_t)m0);
-  const T* b = (const T*)p.b + (int64_t)at.batch * p.batch_b + (BKC ? (int64_t)n0 * p.ldb : (int64_t)n0);
-  const uint32_t seg_steps = (p.K + KS - 1) / KS;
   const uint32_t begin = at.split * per_split, end = min(begin + per_split, steps);
 
-  Stage<T, AKC, false, TM, THREADS> sa;
-  Stage<T, BKC, true, TN, THREADS> sb;
-  const auto load = [&](uint32_t step) {
-    const uint32_t seg = step / seg_steps, k = (step - seg * seg_steps) * KS;
+  // the next step to load
+  const uint32_t seg_steps = (p.K + KS - 1) / KS;
+  uint32_t seg = begin < end ? begin / seg_steps : 0, k = (begin - seg * seg_steps) * KS;
+  const T* a = (const T*)p.a + (int64_t)at.batch * p.batch_a + (AKC ? (int64_t)m0 * p.lda : (int64_t)m0);
+  const T* b = (const T*)p.b + (int64_t)at.batch * p.batch_b + (BKC ? (int64_t)n0 * p.ldb : (int64_t)n0);
+  Stage<T, AKC, false, TM, THREADS, WIDE> sa;
+  Stage<T, BKC, true, TN, THREADS, WIDE> sb;
+  const auto load = [&] {
     sa.load(a + (int64_t)seg * p.seg_a + (AKC ? (int64_t)k : (int64_t)k * p.lda), p.lda, p.M - m0, p.K - k, t);
     sb.load(b + (int64_t)seg * p.seg_b + (BKC ? (int64_t)k : (int64_t)k * p.ldb), p.ldb, p.N - n0, p.K - k, t);
+    k += KS;
+    if (k >= p.K) { k = 0; seg++; }
+  };
+  const auto store = [&](char* stage) {
+    sa.store(stage, p.M - m0, t);
+    sb.store(stage + TM * kStep, p.N - n0, t);
   };
 
   f32x4 acc[BM][BN];
@@ -261,14 +286,13 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void product_kernel(const P
     for (int j = 0; j < BN; j++) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
   if (begin < end) {
-    load(begin);
-    sa.store(lds[0], t);
-    sb.store(lds[0] + TM * kStep, t);
+    load();
+    store(lds[0]);
   }
   __syncthreads();
   for (uint32_t step = begin; step < end; step++) {
     const uint32_t cur = (step - begin) & 1;
-    if (step + 1 < end) load(step + 1);
+    if (step + 1 < end) load();
     const lds_ptr ta = (lds_ptr)lds[cur], tb = ta + TM * kStep;
 #pragma unroll
     for (uint32_t kk = 0; kk < 2; kk++) {
@@ -277,13 +301,9 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void product_kernel(const P
       read_blocks<T, BKC, true, TN, kStep>(tb, wn, 0, kk, q, g, fb);
       multiply(fa, fb, 0, acc);
     }
-    if (step + 1 < end) {
-      sa.store(lds[cur ^ 1], t);
-      sb.store(lds[cur ^ 1] + TM * kStep, t);
-    }
+    if (step + 1 < end) store(lds[cur ^ 1]);
     __syncthreads();
   }
-
   write_out<T, BM, BN>(p, at, splits, m0 + wm, n0 + wn, lane, acc, &lds[0][0] + wave * (WM * WN * 4), partial);
 }
 
@@ -455,19 +475,26 @@ __global__ __launch_bounds__(256) void join_kernel(const Product p, uint32_t spl
 
 // ---- rows
 
-constexpr uint32_t kGradRows = 64;         // rows of a workgroup of grad_rows_kernel
+// Rows of a workgroup of grad_rows_kernel: 8 to 64, fewer where there would not be a thousand workgroups (1000 x 777 in f32: 64 rows
+// 21 us, 8 rows 6 us; of many rows, more of them leave fewer partial sums).
+uint32_t grad_rows(uint64_t rows, uint32_t N) {
+  const uint64_t blocks_n = (N + 255) / 256;
+  uint32_t each = 64;
+  while (each > 8 && (rows + each - 1) / each * blocks_n < 1024) each /= 2;
+  return each;
+}
 
 // dz, and for dbias the column sums of the workgroup's rows before dz is rounded.  A workgroup: 256 columns, eight a thread, eight
 // rows at a time; grid: column blocks x row blocks.
-__global__ __launch_bounds__(256) void grad_rows_kernel(const GradRows p, uint32_t first, float* __restrict__ partial) {
+__global__ __launch_bounds__(256) void grad_rows_kernel(const GradRows p, uint32_t each, uint32_t first, float* __restrict__ partial) {
   __shared__ float sums[8][256];
   const uint32_t blocks_n = (p.N + 255) / 256, id = first + blockIdx.x, bn = id % blocks_n, br = id / blocks_n;
   const uint32_t c = threadIdx.x & 31, r = threadIdx.x >> 5, n = bn * 256 + c * 8, rows = p.batches * p.M;
   float sum[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
   if (n < p.N) {
     const uint32_t valid = p.N - n;
-    for (uint32_t i = 0; i < kGradRows / 8; i++) {
-      const uint64_t at = (uint64_t)br * kGradRows + i * 8 + r;
+    for (uint32_t i = 0; i < each / 8; i++) {
+      const uint64_t at = (uint64_t)br * each + i * 8 + r;
       if (at >= rows) break;
       const uint32_t row = (uint32_t)at, batch = row / p.M, m = row - batch * p.M;
       float v[8];
@@ -545,8 +572,9 @@ hipError_t launch_tiles(const Product& p, const ProductPlan& plan, float* partia
       case kFast128: return go(fast_kernel<T, AKC, BKC, 128, 128, 2, 4, 128, 2>, 512);
       case kFast128Alone: return go(fast_kernel<T, AKC, BKC, 128, 128, 2, 4, 128, 4>, 512);
       case kFast64: return go(fast_kernel<T, AKC, BKC, 64, 64, 2, 2, 128, 4>, 256);
-      case kAny128: return go(product_kernel<T, AKC, BKC, 128, 128, 2, 2>, 256);
-      case kAny64: return go(product_kernel<T, AKC, BKC, 64, 64, 2, 2>, 256);
+      case kWide128: return go(product_kernel<T, AKC, BKC, 128, 128, 2, 2, true>, 256);
+      case kWide64: return go(product_kernel<T, AKC, BKC, 64, 64, 2, 2, true>, 256);
+      case kAny64: return go(product_kernel<T, AKC, BKC, 64, 64, 2, 2, false>, 256);
     }
   });
 }
@@ -556,13 +584,17 @@ hipError_t launch_layout(const Product& p, const ProductPlan& plan, float* parti
   return p.b_kc ? launch_tiles<T, false, true>(p, plan, partial, st) : launch_tiles<T, false, false>(p, plan, partial, st);
 }
 
-// Whether every line that is read starts at a multiple of 16 bytes, ends at one, and follows the one before; offsets within a tile fit 31 bits.
-bool aligned(const Product& p) {
+// What a product's operands allow.  kAligned: every line that is read starts at a multiple of 16 bytes, ends at one, and follows the one before,
+// and offsets within a tile fit 31 bits.  kWide: every line holds 16 bytes at least.
+enum Access { kAligned, kWide, kAny };
+Access access_of(const Product& p) {
   const int64_t e = p.bf16 ? 8 : 4;
-  const auto whole = [&](const void* data, int64_t ld, int64_t batch, int64_t seg, int64_t width) {
+  const auto aligned = [&](const void* data, int64_t ld, int64_t batch, int64_t seg, int64_t width) {
     return (uintptr_t)data % 16 == 0 && ld % e == 0 && batch % e == 0 && seg % e == 0 && width % e == 0 && ld >= width && ld < (int64_t)1 << 21;
   };
-  return whole(p.a, p.lda, p.batch_a, p.segs > 1 ? p.seg_a : 0, p.a_kc ? p.K : p.M) && whole(p.b, p.ldb, p.batch_b, p.segs > 1 ? p.seg_b : 0, p.b_kc ? p.K : p.N);
+  const int64_t wa = p.a_kc ? p.K : p.M, wb = p.b_kc ? p.K : p.N;
+  if (aligned(p.a, p.lda, p.batches > 1 ? p.batch_a : 0, p.segs > 1 ? p.seg_a : 0, wa) && aligned(p.b, p.ldb, p.batches > 1 ? p.batch_b : 0, p.segs > 1 ? p.seg_b : 0, wb)) return kAligned;
+  return wa >= e && wb >= e ? kWide : kAny;
 }
 
 }  // namespace
@@ -578,26 +610,27 @@ bool aligned(const Product& p) {
 // So a large tile does more per time (16 units of 64 x 64 in 1.52 against 1 in 0.25) and a small one leaves fewer compute units
 // without work; where the tiles are few, workgroups share a tile's sum and a second launch adds up: its time, and the partial sums
 // written and read at 4.5 TB/s.
-struct Kernel { uint32_t id, tm, tn; bool fast; float fixed, one[2], two[2]; };
+struct Kernel { uint32_t id, tm, tn; Access access; float fixed, one[2], two[2]; };
 constexpr Kernel kKernels[] = {
-    {kFast256, 256, 256, true, 11, {1.52f, 7.33f}, {0, 0}},
-    {kFast256x128, 256, 128, true, 6, {0.87f, 3.81f}, {0, 0}},
-    {kFast128, 128, 128, true, 4, {0.50f, 1.99f}, {0.93f, 3.78f}},
-    {kFast64, 64, 64, true, 2, {0.25f, 0.62f}, {0.37f, 1.07f}},
-    {kAny128, 128, 128, false, 4, {1.90f, 2.60f}, {2.60f, 4.20f}},
-    {kAny64, 64, 64, false, 2, {0.70f, 0.90f}, {0.90f, 1.40f}},
+    {kFast256, 256, 256, kAligned, 11, {1.52f, 7.33f}, {0, 0}},
+    {kFast256x128, 256, 128, kAligned, 6, {0.87f, 3.81f}, {0, 0}},
+    {kFast128, 128, 128, kAligned, 4, {0.50f, 1.99f}, {0.93f, 3.78f}},
+    {kFast64, 64, 64, kAligned, 2, {0.25f, 0.62f}, {0.37f, 1.07f}},
+    {kWide128, 128, 128, kWide, 4, {1.90f, 2.60f}, {2.60f, 4.20f}},
+    {kWide64, 64, 64, kWide, 2, {0.70f, 0.90f}, {0.90f, 1.40f}},
+    {kAny64, 64, 64, kAny, 2, {2.0f, 2.0f}, {3.0f, 3.0f}},
 };
 constexpr float kJoin = 4, kJoinBytes = 4.5e6f;
 
 ProductPlan plan_product(const Product& p) {
   ProductPlan plan{};
   const uint32_t ks = kStep / (p.bf16 ? 2 : 4), f32 = !p.bf16;
-  const bool fast = aligned(p);
+  const Access access = access_of(p);
   plan.steps = (p.K + ks - 1) / ks * p.segs;
   const float out = (float)p.batches * p.M * p.N * 4;
   float best = 0;
   for (const Kernel& k : kKernels) {
-    if (k.fast != fast) continue;
+    if (k.access != access) continue;
     const uint64_t tiles = (uint64_t)((p.M + k.tm - 1) / k.tm) * ((p.N + k.tn - 1) / k.tn) * p.batches;
     for (uint32_t splits = 1; splits <= 64; splits = splits == 1 ? 2 : splits & splits - 1 ? splits / 3 * 4 : splits / 2 * 3) {
       const uint32_t per = (plan.steps + splits - 1) / splits;
@@ -627,14 +660,18 @@ hipError_t launch_product(const Product& p, const ProductPlan& plan, float* part
 }
 
 uint64_t grad_rows_bytes(uint32_t batches, uint32_t M, uint32_t N, bool dbias) {
-  return dbias ? ((uint64_t)batches * M + kGradRows - 1) / kGradRows * N * 4 : 0;
+  const uint64_t rows = (uint64_t)batches * M;
+  const uint32_t each = grad_rows(rows, N);
+  return dbias ? (rows + each - 1) / each * N * 4 : 0;
 }
 
 hipError_t launch_grad_rows(const GradRows& g, float* partial, hipStream_t st) {
   if (!g.N) return hipSuccess;
-  const uint64_t row_blocks = ((uint64_t)g.batches * g.M + kGradRows - 1) / kGradRows;
+  const uint64_t rows = (uint64_t)g.batches * g.M;
+  const uint32_t each = grad_rows(rows, g.N);
+  const uint64_t row_blocks = (rows + each - 1) / each;
   const hipError_t e = in_launches(row_blocks * ((g.N + 255) / 256), [&](uint64_t first, uint32_t n) {
-    grad_rows_kernel<<<n, 256, 0, st>>>(g, (uint32_t)first, g.dbias ? partial : nullptr);
+    grad_rows_kernel<<<n, 256, 0, st>>>(g, each, (uint32_t)first, g.dbias ? partial : nullptr);
   });
   if (e != hipSuccess || !g.dbias) return e;
   grad_bias_kernel<<<(g.N + 31) / 32, 256, 0, st>>>(partial, (uint32_t)row_blocks, g.N, g.dbias, g.dbias_bf16);
