@@ -28,10 +28,12 @@ struct Tile {
     if (KC && LB == 64) return (sizeof(T) == 2 && IS_B ? line >> 3 : line >> 2) & 3;
     if (sizeof(T) == 2) {
       if (KC) return IS_B ? (line & 3) | (line >> 1 & 4) : line & 7;
+      if (W < 64) return 0;
       if (W == 64) return (line & 2) << 1 | (line >> 2 & 2);
       return (line & 3) << 2 | (line >> 2 & 2);
     }
-    return KC ? line >> 1 & 7 : (line & 4) << 1;
+    if (KC) return line >> 1 & 7;
+    return W < 64 ? line & 4 : (line & 4) << 1;
   }
   __device__ static __forceinline__ uint32_t at(uint32_t line, uint32_t chunk) { return line * kLineBytes + ((chunk ^ swizzle(line)) << 4); }
 };
@@ -194,6 +196,23 @@ __device__ __forceinline__ Place place(uint32_t first, uint32_t tiles_m, uint32_
   return at;
 }
 
+// Four neighbouring columns of a pair of blocks' results, the first (x = 0) or last of the eight that a lane has.
+template <class T>
+__device__ __forceinline__ f32x4 chunk_of(const f32x4& lo, const f32x4& hi, int x) {
+  return sizeof(T) == 2 ? (x ? hi : lo) : f32x4{lo[2 * x], hi[2 * x], lo[2 * x + 1], hi[2 * x + 1]};
+}
+
+// Eight sums: the epilogue, or where others share them into the workspace.
+__device__ __forceinline__ void put8(const Product& p, const Place& at, uint32_t splits, uint32_t m, uint32_t n, const float (&bias)[8], float (&v)[8], float* partial) {
+  if (splits > 1) {
+    float* out = partial + (((uint64_t)at.split * p.batches + at.batch) * p.M + m) * ((p.N + 7) & ~7u) + n;
+#pragma unroll
+    for (int x = 0; x < 2; x++) *(f32x4*)(out + 4 * x) = f32x4{v[4 * x], v[4 * x + 1], v[4 * x + 2], v[4 * x + 3]};
+  } else {
+    finish8(p.e, at.batch, p.M, m, n, p.N - n, bias, v);
+  }
+}
+
 // A wave's results: a lane has row row_of(i, q) and, of the pair of blocks 2 j, 2 j + 1, the eight columns from 32 j + 8 g on.  They go
 // through shared memory that is the wave's own, four blocks of rows at a time at most, so that a row's results are
 // stored side by side (lines of 128 bytes and more) and the epilogue is a short loop: unrolled over the registers it is as long as
@@ -203,7 +222,7 @@ __device__ __forceinline__ void write_out(const Product& p, const Place& at, uin
                                           const f32x4 (&acc)[BM][BN], char* mine, float* __restrict__ partial) {
   constexpr uint32_t CHUNKS = BN * 4, GROUPS = BN * 2, ROWS = 64 / GROUPS;      // chunks and groups of 8 columns of a row; rows at a time
   constexpr int PASS = BM > 4 ? BM / 2 : BM;                                    // blocks of rows that go through at once
-  const uint32_t q = lane & 15, g = lane >> 4, pitch = (p.N + 7) & ~7u;
+  const uint32_t q = lane & 15, g = lane >> 4;
   const uint32_t c = lane % GROUPS, n = n0 + c * 8;
   float bias[8];
   bias8(p.e, n, n < p.N ? p.N - n : 0, bias);
@@ -216,9 +235,7 @@ __device__ __forceinline__ void write_out(const Product& p, const Place& at, uin
       for (int j = 0; j < BN / 2; j++)
 #pragma unroll
         for (int x = 0; x < 2; x++) {
-          const f32x4 &lo = acc[h + i][2 * j], &hi = acc[h + i][2 * j + 1];
-          *(f32x4*)(mine + (r * CHUNKS + ((8 * j + 2 * g + x) ^ (r & (CHUNKS - 1)))) * 16) =
-              sizeof(T) == 2 ? (x ? hi : lo) : f32x4{lo[2 * x], hi[2 * x], lo[2 * x + 1], hi[2 * x + 1]};
+          *(f32x4*)(mine + (r * CHUNKS + ((8 * j + 2 * g + x) ^ (r & (CHUNKS - 1)))) * 16) = chunk_of<T>(acc[h + i][2 * j], acc[h + i][2 * j + 1], x);
         }
     }
     asm volatile("" ::: "memory");         // (a wave's accesses to shared memory are done in their order)
@@ -234,13 +251,7 @@ __device__ __forceinline__ void write_out(const Product& p, const Place& at, uin
 #pragma unroll
           for (int e = 0; e < 4; e++) v[4 * x + e] = t[e];
         }
-        if (splits > 1) {
-          float* out = partial + (((uint64_t)at.split * p.batches + at.batch) * p.M + m) * pitch + n;
-#pragma unroll
-          for (int x = 0; x < 2; x++) *(f32x4*)(out + 4 * x) = f32x4{v[4 * x], v[4 * x + 1], v[4 * x + 2], v[4 * x + 3]};
-        } else {
-          finish8(p.e, at.batch, p.M, m, n, p.N - n, bias, v);
-        }
+        put8(p, at, splits, m, n, bias, v, partial);
       }
     }
     asm volatile("" ::: "memory");
@@ -452,6 +463,102 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void fast_kernel(const P
   write_out<T, BM, BN>(p, at, splits, m0 + wm, n0 + wn, lane, acc, lds + wave * (sizeof lds / (WAVES_M * WAVES_N)), partial);
 }
 
+// Few rows: the sum is split among the waves of a workgroup, each with a ring of STAGES steps of its own in shared memory and no barrier
+// until their sums are added up.  A tile of 16 rows (f32: 32, as its operands are read two blocks at a time) and 64 columns; wave w takes the
+// steps w, w + WAVES, ...  Bound by the read of the columns: 1 x 2048 x 16384 in bf16 keeps 96 KB under way on every compute unit.
+template <class T, bool AKC, bool BKC, int WAVES, int STAGES>
+__global__ __launch_bounds__(64 * WAVES) void rows_kernel(const Product p, uint32_t steps, uint32_t per_split, uint32_t splits, uint32_t first,
+                                                          float* __restrict__ partial) {
+  constexpr int TM = sizeof(T) == 2 ? 16 : 32, TN = 64, BM = TM / 16, BN = TN / 16;
+  constexpr uint32_t KS = kStep / sizeof(T), STAGE = (TM + TN) * kStep;
+  __shared__ __attribute__((aligned(1024))) char lds[WAVES][STAGES * STAGE];
+
+  const Place at = place(first, (p.M + TM - 1) / TM, (p.N + TN - 1) / TN, splits);
+  const uint32_t m0 = at.tm * TM, n0 = at.tn * TN;
+  const uint32_t t = threadIdx.x, lane = t & 63, q = lane & 15, g = lane >> 4;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(t >> 6);
+
+  Feed<T, AKC, false, TM, kStep, 64> fa;
+  Feed<T, BKC, true, TN, kStep, 64> fb;
+  fa.init(p.lda, lane);
+  fb.init(p.ldb, lane);
+  constexpr int LOADS = decltype(fa)::N + decltype(fb)::N;
+
+  const uint32_t seg_steps = (p.K + KS - 1) / KS;
+  const uint32_t begin = at.split * per_split, end = min(begin + per_split, steps);
+  uint32_t step = begin + wave;                   // the next one to load
+  const uint32_t n = end > step ? (end - step + WAVES - 1) / WAVES : 0;
+  const char *a0 = (const char*)((const T*)p.a + (int64_t)at.batch * p.batch_a + (AKC ? (int64_t)m0 * p.lda : (int64_t)m0));
+  const char *b0 = (const char*)((const T*)p.b + (int64_t)at.batch * p.batch_b + (BKC ? (int64_t)n0 * p.ldb : (int64_t)n0));
+  const int64_t size_a = (AKC ? ((int64_t)(p.M - m0) - 1) * p.lda + p.K : ((int64_t)p.K - 1) * p.lda + (p.M - m0)) * (int64_t)sizeof(T);
+  const int64_t size_b = (BKC ? ((int64_t)(p.N - n0) - 1) * p.ldb + p.K : ((int64_t)p.K - 1) * p.ldb + (p.N - n0)) * (int64_t)sizeof(T);
+  char* const ring = lds[wave];
+  const auto load = [&](uint32_t stage) {
+    const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr)ring + stage * STAGE);
+    const bool more = step < end;
+    const uint32_t seg = more ? step / seg_steps : 0, k = more ? (step - seg * seg_steps) * KS : 0;
+    const int64_t off_a = (AKC ? (int64_t)k : (int64_t)k * p.lda) * (int64_t)sizeof(T), off_b = (BKC ? (int64_t)k : (int64_t)k * p.ldb) * (int64_t)sizeof(T);
+    fa.load(a0 + (int64_t)seg * p.seg_a * (int64_t)sizeof(T) + off_a, more ? size_a - off_a : 0, p.K - k, to, lane);
+    fb.load(b0 + (int64_t)seg * p.seg_b * (int64_t)sizeof(T) + off_b, more ? size_b - off_b : 0, p.K - k, to + TM * kStep, lane);
+    step += WAVES;
+  };
+
+  f32x4 acc[BM][BN];
+#pragma unroll
+  for (int i = 0; i < BM; i++)
+#pragma unroll
+    for (int j = 0; j < BN; j++) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+  if (n) {
+#pragma unroll
+    for (int s = 0; s < STAGES; s++) load(s);
+    uint32_t cur = 0;
+    for (uint32_t s = 0; s < n; s++) {
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 1) * LOADS) : "memory");
+      const lds_ptr tile = (lds_ptr)ring + cur * STAGE;
+      typename Operand<T>::Type oa[2][BM], ob[2][BN];
+#pragma unroll
+      for (uint32_t kk = 0; kk < 2; kk++) {
+        read_blocks<T, AKC, false, TM, kStep>(tile, 0, 0, kk, q, g, oa[kk]);
+        read_blocks<T, BKC, true, TN, kStep>(tile + TM * kStep, 0, 0, kk, q, g, ob[kk]);
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // read before the place is loaded again
+      load(cur);
+      multiply(oa[0], ob[0], 0, acc);
+      multiply(oa[1], ob[1], 0, acc);
+      cur = cur + 1 == STAGES ? 0 : cur + 1;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  }
+
+  // the waves' sums, added in their order: rows of 64, the 16-byte chunks of a row at their number xor the row's
+#pragma unroll
+  for (int i = 0; i < BM; i++) {
+    const uint32_t r = row_of<T, false>(i, q);
+#pragma unroll
+    for (int j = 0; j < BN / 2; j++)
+#pragma unroll
+      for (int x = 0; x < 2; x++) *(f32x4*)(ring + (r * 16 + ((8 * j + 2 * g + x) ^ (r & 15))) * 16) = chunk_of<T>(acc[i][2 * j], acc[i][2 * j + 1], x);
+  }
+  __syncthreads();
+  for (uint32_t id = t; id < TM * 8; id += 64 * WAVES) {
+    const uint32_t r = id / 8, c = id % 8, m = m0 + r, col = n0 + c * 8;
+    if (m >= p.M || col >= p.N) continue;
+    float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int w = 0; w < WAVES; w++)
+#pragma unroll
+      for (int x = 0; x < 2; x++) {
+        const f32x4 y = *(const f32x4*)(lds[w] + (r * 16 + ((2 * c + x) ^ (r & 15))) * 16);
+#pragma unroll
+        for (int e = 0; e < 4; e++) v[4 * x + e] += y[e];
+      }
+    float bias[8];
+    bias8(p.e, col, p.N - col, bias);
+    put8(p, at, splits, m, col, bias, v, partial);
+  }
+}
+
 // The sum over the splits, in their order, and the epilogue: eight columns a thread.
 __global__ __launch_bounds__(256) void join_kernel(const Product p, uint32_t splits, uint64_t first, const float* __restrict__ partial) {
   const uint32_t groups = (p.N + 7) / 8;
@@ -461,6 +568,7 @@ __global__ __launch_bounds__(256) void join_kernel(const Product p, uint32_t spl
   const uint32_t n = (uint32_t)(id - row * groups) * 8;
   const float* in = partial + row * (groups * 8) + n;
   float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
   for (uint32_t s = 0; s < splits; s++) {
     const f32x4 x = *(const f32x4*)in, y = *(const f32x4*)(in + 4);
 #pragma unroll
@@ -521,15 +629,16 @@ __global__ __launch_bounds__(256) void grad_rows_kernel(const GradRows p, uint32
 }
 
 // dbias: the row blocks' sums added up, in an order that the sizes alone decide.
-__global__ __launch_bounds__(256) void grad_bias_kernel(const float* __restrict__ partial, uint32_t row_blocks, uint32_t N, void* dbias, uint32_t is_bf16) {
-  __shared__ float sums[8][32];
+__global__ __launch_bounds__(1024) void grad_bias_kernel(const float* __restrict__ partial, uint32_t row_blocks, uint32_t N, void* dbias, uint32_t is_bf16) {
+  __shared__ float sums[32][33];
   const uint32_t c = threadIdx.x & 31, r = threadIdx.x >> 5, n = blockIdx.x * 32 + c;
   float s = 0.0f;
-  if (n < N) for (uint32_t i = r; i < row_blocks; i += 8) s += partial[(uint64_t)i * N + n];
+  if (n < N) for (uint32_t i = r; i < row_blocks; i += 32) s += partial[(uint64_t)i * N + n];
   sums[r][c] = s;
   __syncthreads();
   if (r || n >= N) return;
-  for (int i = 1; i < 8; i++) s += sums[i][c];
+#pragma unroll
+  for (int i = 1; i < 32; i++) s += sums[i][c];
   if (is_bf16) ((bf16*)dbias)[n] = (bf16)s;
   else ((float*)dbias)[n] = s;
 }
@@ -571,6 +680,7 @@ hipError_t launch_tiles(const Product& p, const ProductPlan& plan, float* partia
       case kFast256x128: return go(fast_kernel<T, AKC, BKC, 256, 128, 4, 2, 128, 3>, 512);
       case kFast128: return go(fast_kernel<T, AKC, BKC, 128, 128, 2, 4, 128, 2>, 512);
       case kFast128Alone: return go(fast_kernel<T, AKC, BKC, 128, 128, 2, 4, 128, 4>, 512);
+      case kRows: return go(rows_kernel<T, AKC, BKC, 4, 3>, 256);
       case kFast64: return go(fast_kernel<T, AKC, BKC, 64, 64, 2, 2, 128, 4>, 256);
       case kWide128: return go(product_kernel<T, AKC, BKC, 128, 128, 2, 2, true>, 256);
       case kWide64: return go(product_kernel<T, AKC, BKC, 64, 64, 2, 2, true>, 256);
@@ -616,8 +726,9 @@ constexpr Kernel kKernels[] = {
     {kFast256x128, 256, 128, kAligned, 6, {0.87f, 3.81f}, {0, 0}},
     {kFast128, 128, 128, kAligned, 4, {0.50f, 1.99f}, {0.93f, 3.78f}},
     {kFast64, 64, 64, kAligned, 2, {0.25f, 0.62f}, {0.37f, 1.07f}},
-    {kWide128, 128, 128, kWide, 4, {1.90f, 2.60f}, {2.60f, 4.20f}},
-    {kWide64, 64, 64, kWide, 2, {0.70f, 0.90f}, {0.90f, 1.40f}},
+    {kRows, 0, 64, kAligned, 3, {0.12f, 0.27f}, {0, 0}},
+    {kWide128, 128, 128, kWide, 4, {0.97f, 2.38f}, {1.69f, 4.76f}},
+    {kWide64, 64, 64, kWide, 2, {0.36f, 0.62f}, {0.60f, 1.10f}},
     {kAny64, 64, 64, kAny, 2, {2.0f, 2.0f}, {3.0f, 3.0f}},
 };
 constexpr float kJoin = 4, kJoinBytes = 4.5e6f;
@@ -631,7 +742,8 @@ ProductPlan plan_product(const Product& p) {
   float best = 0;
   for (const Kernel& k : kKernels) {
     if (k.access != access) continue;
-    const uint64_t tiles = (uint64_t)((p.M + k.tm - 1) / k.tm) * ((p.N + k.tn - 1) / k.tn) * p.batches;
+    const uint32_t tm = k.id == kRows ? (f32 ? 32 : 16) : k.tm;
+    const uint64_t tiles = (uint64_t)((p.M + tm - 1) / tm) * ((p.N + k.tn - 1) / k.tn) * p.batches;
     for (uint32_t splits = 1; splits <= 64; splits = splits == 1 ? 2 : splits & splits - 1 ? splits / 3 * 4 : splits / 2 * 3) {
       const uint32_t per = (plan.steps + splits - 1) / splits;
       if (splits > 1 && (per < 4 || tiles * splits > 1024)) break;
@@ -674,7 +786,7 @@ hipError_t launch_grad_rows(const GradRows& g, float* partial, hipStream_t st) {
     grad_rows_kernel<<<n, 256, 0, st>>>(g, each, (uint32_t)first, g.dbias ? partial : nullptr);
   });
   if (e != hipSuccess || !g.dbias) return e;
-  grad_bias_kernel<<<(g.N + 31) / 32, 256, 0, st>>>(partial, (uint32_t)row_blocks, g.N, g.dbias, g.dbias_bf16);
+  grad_bias_kernel<<<(g.N + 31) / 32, 1024, 0, st>>>(partial, (uint32_t)row_blocks, g.N, g.dbias, g.dbias_bf16);
   return hipGetLastError();
 }
 

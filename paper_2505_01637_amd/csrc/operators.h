@@ -192,7 +192,7 @@ struct Product {
 };
 
 // How it is launched.
-enum : uint32_t { kFast256, kFast256x128, kFast128, kFast128Alone, kFast64, kWide128, kWide64, kAny64 };
+enum : uint32_t { kFast256, kFast256x128, kFast128, kFast128Alone, kFast64, kRows, kWide128, kWide64, kAny64 };
 struct ProductPlan {
   uint32_t kernel;
   uint32_t splits;               // workgroups along k
