@@ -111,6 +111,11 @@ def lib():
         _lib.mrl_last_error.restype = C.c_char_p
         _lib.mrl_target_destroy.restype = None
         _lib.mrl_table_destroy.restype = None
+        # (the operators' calls are short: with these, plain integers and bytes go in without an object each)
+        for name in ("mrl_linear", "mrl_linear_grad"):
+            getattr(_lib, name).argtypes = [C.c_char_p, C.c_void_p, C.c_size_t, C.c_void_p]
+            getattr(_lib, name + "_bytes").argtypes = [C.c_char_p, C.c_void_p]
+        _lib.mrl_dropout.argtypes = [C.c_char_p, C.c_void_p]
     return _lib
 
 
@@ -560,7 +565,6 @@ class _On:
         import torch
         if stream is None:
             self._within = torch.cuda.device(index)
-            self.stream = torch.cuda.current_stream(index).cuda_stream
             return
         if stream.device.index != index:
             raise MorelloError(E_INVAL, "the stream is on %s, the tensors on cuda:%d" % (stream.device, index))
@@ -568,40 +572,26 @@ class _On:
         for t in tensors:
             if t is not None:
                 t.record_stream(stream)
-        self.stream = stream.cuda_stream
 
     def __enter__(self):
         self._within.__enter__()
-        return self.stream
 
     def __exit__(self, *what):
         self._within.__exit__(*what)
 
 
-class _Current:
-    """The current device and stream: nothing to change."""
-
-    def __init__(self, stream):
-        self.stream = stream
-
-    def __enter__(self):
-        return self.stream
-
-    def __exit__(self, *what):
-        pass
-
-
 _raw_stream = _current_device = None
 
 
-def _on(tensors, stream):
-    """All tensors (None: not given) are on one device, which is current while the call queues its work."""
+def _elsewhere(tensors, stream):
+    """Checks that all tensors (None: not given) are on one GPU.  Returns None where that is the current device and no stream
+    is given, else the _On to be entered."""
     global _raw_stream, _current_device
     if _raw_stream is None:
         import torch
         # (what torch's own generated code asks; torch.cuda.current_stream makes a Stream object first, 1 us)
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
-        _current_device = torch.cuda.current_device
+        _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
     index = tensors[0].get_device()
     for t in tensors:
         if t is not None and t.get_device() != index:
@@ -609,23 +599,27 @@ def _on(tensors, stream):
     if index < 0:
         raise MorelloError(E_INVAL, "tensors on %s: there is no CPU path" % tensors[0].device)
     if stream is None and index == _current_device():
-        return _Current(_raw_stream(index))
+        return None
     return _On(index, tensors, stream)
 
 
-def _queue(desc, size_of, run, given, like, stream):
-    """Ask for the workspace, then queue the call; a workspace of torch's may be freed when this returns (work on
-    its stream that uses the memory next comes after the call's)."""
+def _queue(desc, size_of, run, given, like):
+    """Ask for the workspace, then queue the call on the current stream; a workspace of torch's may be freed when this
+    returns (work on its stream that uses the memory next comes after the call's)."""
     n = C.c_size_t()
-    rc = size_of(desc, C.byref(n))
+    rc = size_of(desc, C.addressof(n))
     if rc == 0:
+        stream = _raw_stream(like.get_device())
         if n.value == 0:
-            rc = run(desc, None, C.c_size_t(0), C.c_void_p(stream))
+            rc = run(desc, None, 0, stream)
         else:
             if given is None:
                 given = like.new_empty(n.value, dtype=_uint8)
-            rc = run(desc, C.c_void_p(given.data_ptr()), C.c_size_t(given.numel() * given.element_size()), C.c_void_p(stream))
-    _check(rc)
+            elif not given.is_contiguous():
+                raise MorelloError(E_INVAL, "the workspace is not contiguous")
+            rc = run(desc, given.data_ptr(), given.numel() * given.element_size(), stream)
+    if rc:
+        _check(rc)
 
 
 def _operands(lhs, rhs):
@@ -648,21 +642,25 @@ def linear(lhs, rhs, bias=None, residual=None, *, activation="none", dropout=0.0
     bias: n elements; residual: of out's shape.  activation: none, relu, gelu (tanh form), silu.
     dropout: the probability that an element is dropped; seed and offset (64 bits each) say which are, together with
     the element's row and column.  dtype: out's and z's type (lhs's if None); out: a tensor to write to, which may be
-    `residual`.  workspace: a uint8 tensor the caller keeps (linear_bytes); stream: where the work
-    is queued (the current stream if None).
+    `residual`.  workspace: device memory that the caller keeps, a contiguous tensor (one that is too small is refused
+    with E_NOMEM and what is needed); stream: where the work is queued (the current stream if None).
     """
+    on = _elsewhere((lhs, rhs, bias, residual, out, workspace), stream)
+    if on is not None:
+        with on:
+            return linear(lhs, rhs, bias, residual, activation=activation, dropout=dropout, seed=seed, offset=offset, dtype=dtype, pre=pre,
+                          out=out, workspace=workspace)
     sizes, ml, mr, shape = _operands(lhs, rhs)
-    with _on((lhs, rhs, bias, residual, out, workspace), stream) as on:
-        if out is None:
-            out = lhs.new_empty(shape) if dtype is None or dtype == lhs.dtype else lhs.new_empty(shape, dtype=dtype)
-        elif dtype is not None and out.dtype != dtype:
-            raise MorelloError(E_INVAL, "out is %s, not %s" % (out.dtype, dtype))
-        z = out.new_empty(shape) if pre else None
-        desc = _LINEAR.pack(*sizes, *ml, *mr, *(_ABSENT if bias is None else _vector("bias", bias, sizes[3])),
-                            *(_ABSENT if residual is None else _rows("residual", residual, shape)), *_rows("out", out, shape),
-                            *(_ABSENT if z is None else _rows("pre", z, shape)),
-                            _activation(activation), drop_threshold(dropout), _word("seed", seed), _word("offset", offset))
-        _queue(desc, lib().mrl_linear_bytes, lib().mrl_linear, workspace, lhs, on)
+    if out is None:
+        out = lhs.new_empty(shape) if dtype is None or dtype == lhs.dtype else lhs.new_empty(shape, dtype=dtype)
+    elif dtype is not None and out.dtype != dtype:
+        raise MorelloError(E_INVAL, "out is %s, not %s" % (out.dtype, dtype))
+    z = out.new_empty(shape) if pre else None
+    desc = _LINEAR.pack(*sizes, *ml, *mr, *(_ABSENT if bias is None else _vector("bias", bias, sizes[3])),
+                        *(_ABSENT if residual is None else _rows("residual", residual, shape)), *_rows("out", out, shape),
+                        *(_ABSENT if z is None else _rows("pre", z, shape)),
+                        _activation(activation), drop_threshold(dropout), _word("seed", seed), _word("offset", offset))
+    _queue(desc, lib().mrl_linear_bytes, lib().mrl_linear, workspace, lhs)
     return (out, z) if pre else out
 
 
@@ -672,27 +670,31 @@ def linear_grad(grad, lhs, rhs, bias=None, pre=None, *, activation="none", dropo
     `pre`, the z that it returned (not needed without an activation): mrl_linear_grad.  Each has its operand's type,
     d_rhs also its layout; None for an operand that is not needed, or a bias that is None.  The gradient
     by the residual is `grad`."""
+    on = _elsewhere((lhs, grad, rhs, bias, pre, workspace), stream)
+    if on is not None:
+        with on:
+            return linear_grad(grad, lhs, rhs, bias, pre, activation=activation, dropout=dropout, seed=seed, offset=offset,
+                               need_lhs=need_lhs, need_rhs=need_rhs, workspace=workspace)
     sizes, ml, mr, shape = _operands(lhs, rhs)
     act = _activation(activation)
     if act and pre is None:
         raise MorelloError(E_INVAL, "the gradient of %s needs pre" % activation)
-    with _on((lhs, grad, rhs, bias, pre, workspace), stream) as on:
-        d_lhs = lhs.new_empty(lhs.shape) if need_lhs else None
-        d_rhs = None
-        if need_rhs and mr[2]:
-            d_rhs = rhs.new_empty(rhs.shape[:-2] + (rhs.shape[-1], rhs.shape[-2])).transpose(-1, -2)
-        elif need_rhs:
-            d_rhs = rhs.new_empty(rhs.shape)
-        d_bias = bias.new_empty(bias.shape) if bias is not None else None
-        m_rhs = _ABSENT
-        if d_rhs is not None:       # (of one row or column d_rhs could be read either way: its layout is rhs's)
-            st = d_rhs.stride()
-            m_rhs = (d_rhs.data_ptr(), mr[1], mr[2], st[-1] if mr[2] else st[-2], st[0] if len(st) == 3 else 0)
-        desc = _LINEAR_GRAD.pack(*sizes, *_rows("grad", grad, shape), *ml, *mr, *(_rows("pre", pre, shape) if act else _ABSENT),
-                                 *(_ABSENT if d_lhs is None else _rows("d_lhs", d_lhs, lhs.shape)), *m_rhs,
-                                 *(_ABSENT if d_bias is None else _vector("d_bias", d_bias, sizes[3])),
-                                 act, drop_threshold(dropout), _word("seed", seed), _word("offset", offset))
-        _queue(desc, lib().mrl_linear_grad_bytes, lib().mrl_linear_grad, workspace, lhs, on)
+    d_lhs = lhs.new_empty(lhs.shape) if need_lhs else None
+    d_rhs = None
+    if need_rhs and mr[2]:
+        d_rhs = rhs.new_empty(rhs.shape[:-2] + (rhs.shape[-1], rhs.shape[-2])).transpose(-1, -2)
+    elif need_rhs:
+        d_rhs = rhs.new_empty(rhs.shape)
+    d_bias = bias.new_empty(bias.shape) if bias is not None else None
+    m_rhs = _ABSENT
+    if d_rhs is not None:       # (of one row or column d_rhs could be read either way: its layout is rhs's)
+        st = d_rhs.stride()
+        m_rhs = (d_rhs.data_ptr(), mr[1], mr[2], st[-1] if mr[2] else st[-2], st[0] if len(st) == 3 else 0)
+    desc = _LINEAR_GRAD.pack(*sizes, *_rows("grad", grad, shape), *ml, *mr, *(_rows("pre", pre, shape) if act else _ABSENT),
+                             *(_ABSENT if d_lhs is None else _rows("d_lhs", d_lhs, lhs.shape)), *m_rhs,
+                             *(_ABSENT if d_bias is None else _vector("d_bias", d_bias, sizes[3])),
+                             act, drop_threshold(dropout), _word("seed", seed), _word("offset", offset))
+    _queue(desc, lib().mrl_linear_grad_bytes, lib().mrl_linear_grad, workspace, lhs)
     return d_lhs, d_rhs, d_bias
 
 
@@ -701,21 +703,26 @@ def dropout(x, residual=None, *, dropout, seed=0, offset=0, out=None, stream=Non
     other arguments."""
     if x.dim() not in (2, 3):
         raise MorelloError(E_INVAL, "x has %d dimensions: two, or three with a batch" % x.dim())
-    with _on((x, residual, out), stream) as on:
-        if out is None:
-            out = x.new_empty(x.shape)
-        matrices = []
-        for name, t in (("x", x), ("residual", residual), ("out", out)):
-            if t is None:
-                matrices += _ABSENT
-                continue
-            at = _rows(name, t, x.shape)
-            if x.dim() == 3 and x.shape[0] > 1 and at[4] != x.shape[1] * at[3]:
-                raise MorelloError(E_INVAL, "%s: its batches do not follow each other (strides %s)" % (name, t.stride()))
-            matrices += at
-        rows = x.shape[0] * x.shape[1] if x.dim() == 3 else x.shape[0]
-        desc = _DROPOUT.pack(rows, x.shape[-1], *matrices, drop_threshold(dropout), _word("seed", seed), _word("offset", offset))
-        _check(lib().mrl_dropout(desc, C.c_void_p(on)))
+    on = _elsewhere((x, residual, out), stream)
+    if on is not None:
+        with on:
+            return _dropout(x, residual, dropout=dropout, seed=seed, offset=offset, out=out)
+    if out is None:
+        out = x.new_empty(x.shape)
+    matrices = []
+    for name, t in (("x", x), ("residual", residual), ("out", out)):
+        if t is None:
+            matrices += _ABSENT
+            continue
+        at = _rows(name, t, x.shape)
+        if x.dim() == 3 and x.shape[0] > 1 and at[4] != x.shape[1] * at[3]:
+            raise MorelloError(E_INVAL, "%s: its batches do not follow each other (strides %s)" % (name, t.stride()))
+        matrices += at
+    rows = x.shape[0] * x.shape[1] if x.dim() == 3 else x.shape[0]
+    desc = _DROPOUT.pack(rows, x.shape[-1], *matrices, drop_threshold(dropout), _word("seed", seed), _word("offset", offset))
+    rc = lib().mrl_dropout(desc, _raw_stream(x.get_device()))
+    if rc:
+        _check(rc)
     return out
 
 
