@@ -14,18 +14,17 @@ constexpr uint32_t kLaunch = 1u << 22;     // workgroups of a launch
 
 // ---- tiles in shared memory
 //
-// A step holds LB bytes along k of every row (column) of the tile, as chunks of 16 bytes.  KC: the operand's neighbours along k
-// are adjacent, a line of the tile is a row of A (column of B), 4 or 8 chunks.  Otherwise a line is one k with the W rows.
+// A step holds 128 bytes along k of every row (column) of the tile, as chunks of 16 bytes.  KC: the operand's neighbours along k
+// are adjacent, a line of the tile is a row of A (column of B), 8 chunks.  Otherwise a line is one k with the W rows.
 // A chunk's place in its line is its number xor swizzle(line): without it the lines that one instruction reads lie in the same
 // banks.
-template <class T, bool KC, bool IS_B, int W, int LB>
+template <class T, bool KC, bool IS_B, int W>
 struct Tile {
   static constexpr int E = 16 / sizeof(T);                           // elements of a chunk
-  static constexpr int kSteps = LB / sizeof(T);                      // k of a step
-  static constexpr int kLineBytes = KC ? LB : W * (int)sizeof(T);
+  static constexpr int kSteps = kStep / sizeof(T);                      // k of a step
+  static constexpr int kLineBytes = KC ? kStep : W * (int)sizeof(T);
   static constexpr int kChunks = kLineBytes / 16;                    // of a line
   __device__ static __forceinline__ uint32_t swizzle(uint32_t line) {
-    if (KC && LB == 64) return (sizeof(T) == 2 && IS_B ? line >> 3 : line >> 2) & 3;
     if (sizeof(T) == 2) {
       if (KC) return IS_B ? (line & 3) | (line >> 1 & 4) : line & 7;
       if (W < 64) return 0;
@@ -54,9 +53,9 @@ typedef __attribute__((address_space(3))) const char* lds_ptr;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 // bf16: block i's operand of the half step kk (32 k): a lane has k = 32 kk + 8 g .. + 7.
-template <bool KC, bool IS_B, int W, int LB>
+template <bool KC, bool IS_B, int W>
 __device__ __forceinline__ bf16x8 read_block(lds_ptr tile, uint32_t base, uint32_t i, uint32_t kk, uint32_t q, uint32_t g) {
-  using Tl = Tile<bf16, KC, IS_B, W, LB>;
+  using Tl = Tile<bf16, KC, IS_B, W>;
   if (KC) {
     const uint32_t line = base + row_of<bf16, IS_B>(i, q);
     return *(const __attribute__((address_space(3))) bf16x8*)(tile + Tl::at(line, kk * 4 + g));
@@ -72,9 +71,9 @@ __device__ __forceinline__ bf16x8 read_block(lds_ptr tile, uint32_t base, uint32
   return u.v;
 }
 // f32: blocks i and i + 1 (i even) of the half step kk (16 k): element j is k = 16 kk + 4 g + j.
-template <bool KC, bool IS_B, int W, int LB>
+template <bool KC, bool IS_B, int W>
 __device__ __forceinline__ void read_pair(lds_ptr tile, uint32_t base, uint32_t i, uint32_t kk, uint32_t q, uint32_t g, f32x4& v0, f32x4& v1) {
-  using Tl = Tile<float, KC, IS_B, W, LB>;
+  using Tl = Tile<float, KC, IS_B, W>;
   const uint32_t row = base + row_of<float, IS_B>(i, q);
   if (KC) {
     v0 = *(const __attribute__((address_space(3))) f32x4*)(tile + Tl::at(row, kk * 4 + g));
@@ -94,34 +93,31 @@ __device__ __forceinline__ void read_pair(lds_ptr tile, uint32_t base, uint32_t 
 template <class T> struct Operand { using Type = bf16x8; };
 template <> struct Operand<float> { using Type = f32x4; };
 
-template <class T, bool KC, bool IS_B, int W, int LB, int N>
+template <class T, bool KC, bool IS_B, int W, int N>
 __device__ __forceinline__ void read_blocks(lds_ptr tile, uint32_t base, uint32_t first, uint32_t kk, uint32_t q, uint32_t g, typename Operand<T>::Type (&v)[N]) {
   if constexpr (sizeof(T) == 2) {
 #pragma unroll
-    for (int i = 0; i < N; i++) v[i] = read_block<KC, IS_B, W, LB>(tile, base, first + i, kk, q, g);
+    for (int i = 0; i < N; i++) v[i] = read_block<KC, IS_B, W>(tile, base, first + i, kk, q, g);
   } else {
 #pragma unroll
-    for (int i = 0; i < N; i += 2) read_pair<KC, IS_B, W, LB>(tile, base, first + i, kk, q, g, v[i], v[i + 1]);
+    for (int i = 0; i < N; i += 2) read_pair<KC, IS_B, W>(tile, base, first + i, kk, q, g, v[i], v[i + 1]);
   }
 }
 
-// acc[first + i][j] += the products of A's block i and B's block j over a half step.  The products are taken as B^T A^T: in the MFMA
-// result a lane has one column and four neighbouring rows, which are then one row of the result and neighbouring columns.
+// acc[first + i][j] += the products of A's block i and B's block j over a half step, one of kParts parts.  The products are taken as B^T A^T: in the
+// MFMA result a lane has one column and four neighbouring rows, which are then one row of the result and neighbouring columns.
+template <class T, int NM> constexpr int kParts = sizeof(T) == 2 ? NM : 4;
 template <int NM, int BN, int BM>
-__device__ __forceinline__ void multiply(const bf16x8 (&a)[NM], const bf16x8 (&b)[BN], uint32_t first, f32x4 (&acc)[BM][BN]) {
+__device__ __forceinline__ void multiply(const bf16x8 (&a)[NM], const bf16x8 (&b)[BN], uint32_t first, int part, f32x4 (&acc)[BM][BN]) {
+#pragma unroll
+  for (int j = 0; j < BN; j++) acc[first + part][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], a[part], acc[first + part][j], 0, 0, 0);
+}
+template <int NM, int BN, int BM>
+__device__ __forceinline__ void multiply(const f32x4 (&a)[NM], const f32x4 (&b)[BN], uint32_t first, int part, f32x4 (&acc)[BM][BN]) {
 #pragma unroll
   for (int i = 0; i < NM; i++)
 #pragma unroll
-    for (int j = 0; j < BN; j++) acc[first + i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], a[i], acc[first + i][j], 0, 0, 0);
-}
-template <int NM, int BN, int BM>
-__device__ __forceinline__ void multiply(const f32x4 (&a)[NM], const f32x4 (&b)[BN], uint32_t first, f32x4 (&acc)[BM][BN]) {
-#pragma unroll
-  for (int e = 0; e < 4; e++)
-#pragma unroll
-    for (int i = 0; i < NM; i++)
-#pragma unroll
-      for (int j = 0; j < BN; j++) acc[first + i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(b[j][e], a[i][e], acc[first + i][j], 0, 0, 0);
+    for (int j = 0; j < BN; j++) acc[first + i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(b[j][part], a[i][part], acc[first + i][j], 0, 0, 0);
 }
 
 // The part of a tile that a thread brings from global memory through registers, from any address.
@@ -131,7 +127,7 @@ __device__ __forceinline__ void multiply(const f32x4 (&a)[NM], const f32x4 (&b)[
 // to shared memory, so that no load waits for a branch.  Otherwise element by element.
 template <class T, bool KC, bool IS_B, int W, int THREADS, bool WIDE>
 struct Stage {
-  using Tl = Tile<T, KC, IS_B, W, kStep>;
+  using Tl = Tile<T, KC, IS_B, W>;
   static constexpr int N = W * 8 / THREADS, E = Tl::E;
   u32x4 r[N];
   uint32_t ks;                     // k that are left where r was read
@@ -308,9 +304,10 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void product_kernel(const P
 #pragma unroll
     for (uint32_t kk = 0; kk < 2; kk++) {
       typename Operand<T>::Type fa[BM], fb[BN];
-      read_blocks<T, AKC, false, TM, kStep>(ta, wm, 0, kk, q, g, fa);
-      read_blocks<T, BKC, true, TN, kStep>(tb, wn, 0, kk, q, g, fb);
-      multiply(fa, fb, 0, acc);
+      read_blocks<T, AKC, false, TM>(ta, wm, 0, kk, q, g, fa);
+      read_blocks<T, BKC, true, TN>(tb, wn, 0, kk, q, g, fb);
+#pragma unroll
+      for (int part = 0; part < kParts<T, BM>; part++) multiply(fa, fb, 0, part, acc);
     }
     if (step + 1 < end) store(lds[cur ^ 1]);
     __syncthreads();
@@ -335,10 +332,10 @@ __device__ __forceinline__ void load_to_lds(uint32_t lds, uint32_t offset, u32x4
 
 constexpr uint32_t kOutside = 0x80000000u;        // beyond any buffer's range
 
-template <class T, bool KC, bool IS_B, int W, int LB, int THREADS>
+template <class T, bool KC, bool IS_B, int W, int THREADS>
 struct Feed {
-  using Tl = Tile<T, KC, IS_B, W, LB>;
-  static constexpr int N = W * (LB / 16) / THREADS;       // loads of a thread and step
+  using Tl = Tile<T, KC, IS_B, W>;
+  static constexpr int N = W * 8 / THREADS;       // loads of a thread and step
   uint32_t offset[N];                             // bytes from the tile's first element of a step
   __device__ __forceinline__ void init(int64_t ld, uint32_t t) {
 #pragma unroll
@@ -347,29 +344,29 @@ struct Feed {
       offset[i] = line * (uint32_t)ld * (uint32_t)sizeof(T) + chunk * 16;
     }
   }
-  // from: the tile's first element of the step; left: bytes from there to the operand's end; ks: k that are left in the segment
-  __device__ __forceinline__ void load(const char* from, int64_t left, uint32_t ks, uint32_t lds, uint32_t t) const {
+  // Descriptor of what lies behind the tile's first element of a step; left: bytes to the operand's end.
+  __device__ static __forceinline__ u32x4 buffer(const char* from, int64_t left) {
     const uint64_t base = (uint64_t)from;
     const uint32_t low = (uint32_t)left, range = (uint32_t)(left >> 32) | low >> 31 ? kOutside : low;      // (scalar units have no 64-bit minimum)
-    const u32x4 buffer = {(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)base), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(base >> 32) & 0xFFFFu),
-                          (uint32_t)__builtin_amdgcn_readfirstlane(range), 0x27000u};
-#pragma unroll
-    for (int i = 0; i < N; i++) {
-      uint32_t at = offset[i];
-      if (KC && ks < Tl::kSteps) {                // chunks past the end of the sum would be the next line's
-        const uint32_t c = t + i * THREADS, line = c / Tl::kChunks, chunk = c % Tl::kChunks ^ Tl::swizzle(line);
-        if (chunk * Tl::E >= ks) at = kOutside;
-      }
-      load_to_lds(lds + (t & ~63u) * 16 + i * THREADS * 16, at, buffer);
+    return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)base), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(base >> 32) & 0xFFFFu),
+                 (uint32_t)__builtin_amdgcn_readfirstlane(range), 0x27000u};
+  }
+  // The thread's i-th load of a step; ks: k that are left in the segment.
+  __device__ __forceinline__ void load(int i, const u32x4& buffer, uint32_t ks, uint32_t lds, uint32_t t) const {
+    uint32_t at = offset[i];
+    if (KC && ks < Tl::kSteps) {                  // chunks past the end of the sum would be the next line's
+      const uint32_t c = t + i * THREADS, line = c / Tl::kChunks, chunk = c % Tl::kChunks ^ Tl::swizzle(line);
+      if (chunk * Tl::E >= ks) at = kOutside;
     }
+    load_to_lds(lds + (t & ~63u) * 16 + i * THREADS * 16, at, buffer);
   }
 };
 
-template <class T, bool AKC, bool BKC, int TM, int TN, int WAVES_M, int WAVES_N, int LB, int STAGES>
+template <class T, bool AKC, bool BKC, int TM, int TN, int WAVES_M, int WAVES_N, int STAGES>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void fast_kernel(const Product p, uint32_t steps, uint32_t per_split, uint32_t splits,
                                                                       uint32_t first, float* __restrict__ partial) {
   constexpr int THREADS = 64 * WAVES_M * WAVES_N, WM = TM / WAVES_M, WN = TN / WAVES_N, BM = WM / 16, BN = WN / 16;
-  constexpr uint32_t KS = LB / sizeof(T), STAGE = (TM + TN) * LB;
+  constexpr uint32_t KS = kStep / sizeof(T), STAGE = (TM + TN) * kStep;
   __shared__ __attribute__((aligned(1024))) char lds[STAGES * STAGE];
 
   const Place at = place(first, (p.M + TM - 1) / TM, (p.N + TN - 1) / TN, splits);
@@ -378,8 +375,8 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void fast_kernel(const P
   const uint32_t wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const uint32_t wm = wave / WAVES_N * WM, wn = wave % WAVES_N * WN;
 
-  Feed<T, AKC, false, TM, LB, THREADS> fa;
-  Feed<T, BKC, true, TN, LB, THREADS> fb;
+  Feed<T, AKC, false, TM, THREADS> fa;
+  Feed<T, BKC, true, TN, THREADS> fb;
   fa.init(p.lda, t);
   fb.init(p.ldb, t);
   constexpr int LOADS = decltype(fa)::N + decltype(fb)::N;
@@ -398,11 +395,14 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void fast_kernel(const P
   const uint32_t n = end > begin ? end - begin : 0;
   uint32_t loaded = 0;
   // (behind the last step the buffers have no bytes: zeros are written that nothing uses, and every step has the same loads under way)
-  const auto load = [&](uint32_t stage) {
-    const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr)lds + stage * STAGE);
+  u32x4 buf_a, buf_b;
+  uint32_t to, ks;
+  const auto aim = [&](uint32_t stage) {          // at the next step, to be put into `stage`
     const bool more = loaded++ < n;
-    fa.load(sa + off_a, more ? size_a - off_a : 0, p.K - k, to, wave * 64 + lane);
-    fb.load(sb + off_b, more ? size_b - off_b : 0, p.K - k, to + TM * LB, wave * 64 + lane);
+    to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr)lds + stage * STAGE);
+    ks = p.K - k;
+    buf_a = fa.buffer(sa + off_a, more ? size_a - off_a : 0);
+    buf_b = fb.buffer(sb + off_b, more ? size_b - off_b : 0);
     if (!more) return;
     k += KS;
     off_a += step_a;
@@ -414,6 +414,10 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void fast_kernel(const P
       sb += p.seg_b * (int64_t)sizeof(T);
     }
   };
+  const auto load = [&](int i) {
+    if (i < fa.N) fa.load(i, buf_a, ks, to, wave * 64 + lane);
+    else fb.load(i - fa.N, buf_b, ks, to + TM * kStep, wave * 64 + lane);
+  };
 
   f32x4 acc[BM][BN];
 #pragma unroll
@@ -421,46 +425,89 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void fast_kernel(const P
 #pragma unroll
     for (int j = 0; j < BN; j++) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-  // A half step of 64 bytes along k is one or two phases of NM blocks of rows each.  A phase first reads the operands of the next one, then
-  // multiplies, so that the reads' latency lies under the products.  Before the last phase of a step everything of it has been read and
-  // the next step's tile must be there: the one barrier of a step; behind it this step's place is free for the step STAGES ahead.
-  constexpr int NM = BM > 4 ? BM / 2 : BM, PHASES = BM / NM;
+  // A step is two half steps of one or two phases, of NM blocks of rows each.  A phase first reads the operands of the next one, then
+  // multiplies, so that the reads' latency lies under the products.  Before the last phase everything of the step has been read and
+  // the next step's tile must be there: the one barrier of a step; behind it this step's place is free for the step STAGES ahead.  Its
+  // loads go out one by one between the products from there on: all at once they fill the queue to memory, and the wave stands still
+  // before its products until the queue has room (8192-cube 850 us, spread 820).
+  constexpr int NM = BM > 4 ? BM / 2 : BM, PHASES = 2 * BM / NM, PARTS = kParts<T, NM>;
+  constexpr bool SPREAD = BM > 4;
+  static_assert(LOADS <= PHASES * PARTS, "one load at most beside a part of the products");
   typename Operand<T>::Type oa[2][NM], ob[2][BN];
   if (n) {
 #pragma unroll
-    for (int s = 0; s < STAGES; s++) load(s);
+    for (int s = 0; s < STAGES; s++) {
+      aim(s);
+#pragma unroll
+      for (int i = 0; i < LOADS; i++) load(i);
+    }
     arrive<(STAGES - 1) * LOADS>();
-    read_blocks<T, AKC, false, TM, LB>((lds_ptr)lds, wm, 0, 0, q, g, oa[0]);
-    read_blocks<T, BKC, true, TN, LB>((lds_ptr)lds + TM * LB, wn, 0, 0, q, g, ob[0]);
+    read_blocks<T, AKC, false, TM>((lds_ptr)lds, wm, 0, 0, q, g, oa[0]);
+    read_blocks<T, BKC, true, TN>((lds_ptr)lds + TM * kStep, wn, 0, 0, q, g, ob[0]);
     uint32_t cur = 0;
-    for (uint32_t s = 0; s < n; s += 128 / LB) {  // (two half steps a turn, as the operands' registers alternate; one too many adds zeros)
+    for (uint32_t s = 0; s < n; s++) {
+      const uint32_t next = cur + 1 == STAGES ? 0 : cur + 1;
 #pragma unroll
-      for (int h = 0; h < 2; h++) {
-        const bool ends = LB == 64 || h == 1;
-        const uint32_t next = cur + 1 == STAGES ? 0 : cur + 1;
+      for (int ph = 0; ph < PHASES; ph++) {
+        const int then = (ph + 1) % PHASES, kk = then / (PHASES / 2), m = then % (PHASES / 2) * NM;
+        if (ph == PHASES - 1) {
+          arrive<(STAGES - 2) * LOADS>();
+          aim(cur);
 #pragma unroll
-        for (int ph = 0; ph < PHASES; ph++) {
-          const int now = (h * PHASES + ph) & 1;
-          if (ph == PHASES - 1) {
-            if (ends) {
-              arrive<(STAGES - 2) * LOADS>();
-              load(cur);
-            }
-            const lds_ptr tile = (lds_ptr)lds + (ends ? next : cur) * STAGE;
-            read_blocks<T, AKC, false, TM, LB>(tile, wm, 0, ends ? 0 : 1, q, g, oa[now ^ 1]);
-            read_blocks<T, BKC, true, TN, LB>(tile + TM * LB, wn, 0, ends ? 0 : 1, q, g, ob[h ^ 1]);
-          } else {
-            read_blocks<T, AKC, false, TM, LB>((lds_ptr)lds + cur * STAGE, wm, NM, LB == 64 ? 0 : h, q, g, oa[now ^ 1]);
-          }
-          multiply(oa[now], ob[h], ph * NM, acc);
-          __builtin_amdgcn_sched_barrier(0);
+          for (int i = 0; i < (SPREAD ? 0 : LOADS); i++) load(i);
         }
-        if (ends) cur = next;
+        const lds_ptr tile = (lds_ptr)lds + (ph == PHASES - 1 ? next : cur) * STAGE;
+        read_blocks<T, AKC, false, TM>(tile, wm, m, kk, q, g, oa[then & 1]);
+        if (m == 0) read_blocks<T, BKC, true, TN>(tile + TM * kStep, wn, 0, kk, q, g, ob[kk]);
+#pragma unroll
+        for (int part = 0; part < PARTS; part++) {
+          multiply(oa[ph & 1], ob[ph / (PHASES / 2)], ph % (PHASES / 2) * NM, part, acc);
+          // (in the first step, before its barrier, the last stage's loads again: the same bytes to the same place)
+          if (SPREAD && then * PARTS + part < LOADS) {
+            load(then * PARTS + part);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
+      cur = next;
     }
     arrive<0>();                  // nothing is under way to shared memory when the workgroup gives it up
   }
   write_out<T, BM, BN>(p, at, splits, m0 + wm, n0 + wn, lane, acc, lds + wave * (sizeof lds / (WAVES_M * WAVES_N)), partial);
+}
+
+// The sums of a workgroup's waves over one tile of few rows and 64 columns, added in their order: each wave's in shared memory of its own, `each`
+// bytes apart, rows of 64 with the 16-byte chunks of a row at their number xor the row's.
+template <class T, int WAVES, int BM>
+__device__ __forceinline__ void add_waves(const Product& p, const Place& at, uint32_t splits, uint32_t m0, uint32_t n0, uint32_t t, const f32x4 (&acc)[BM][4],
+                                          char* lds, uint32_t each, float* __restrict__ partial) {
+  const uint32_t q = t & 15, g = t >> 4 & 3;
+  char* const mine = lds + (t >> 6) * each;
+#pragma unroll
+  for (int i = 0; i < BM; i++) {
+    const uint32_t r = row_of<T, false>(i, q);
+#pragma unroll
+    for (int j = 0; j < 2; j++)
+#pragma unroll
+      for (int x = 0; x < 2; x++) *(f32x4*)(mine + (r * 16 + ((8 * j + 2 * g + x) ^ (r & 15))) * 16) = chunk_of<T>(acc[i][2 * j], acc[i][2 * j + 1], x);
+  }
+  __syncthreads();
+  for (uint32_t id = t; id < BM * 16 * 8; id += 64 * WAVES) {
+    const uint32_t r = id / 8, c = id % 8, m = m0 + r, col = n0 + c * 8;
+    if (m >= p.M || col >= p.N) continue;
+    float bias[8], v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    bias8(p.e, col, p.N - col, bias);
+#pragma unroll
+    for (int w = 0; w < WAVES; w++)
+#pragma unroll
+      for (int x = 0; x < 2; x++) {
+        const f32x4 y = *(const f32x4*)(lds + w * each + (r * 16 + ((2 * c + x) ^ (r & 15))) * 16);
+#pragma unroll
+        for (int e = 0; e < 4; e++) v[4 * x + e] += y[e];
+      }
+    put8(p, at, splits, m, col, bias, v, partial);
+  }
 }
 
 // Few rows: the sum is split among the waves of a workgroup, each with a ring of STAGES steps of its own in shared memory and no barrier
@@ -478,8 +525,8 @@ __global__ __launch_bounds__(64 * WAVES) void rows_kernel(const Product p, uint3
   const uint32_t t = threadIdx.x, lane = t & 63, q = lane & 15, g = lane >> 4;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(t >> 6);
 
-  Feed<T, AKC, false, TM, kStep, 64> fa;
-  Feed<T, BKC, true, TN, kStep, 64> fb;
+  Feed<T, AKC, false, TM, 64> fa;
+  Feed<T, BKC, true, TN, 64> fb;
   fa.init(p.lda, lane);
   fb.init(p.ldb, lane);
   constexpr int LOADS = decltype(fa)::N + decltype(fb)::N;
@@ -498,8 +545,12 @@ __global__ __launch_bounds__(64 * WAVES) void rows_kernel(const Product p, uint3
     const bool more = step < end;
     const uint32_t seg = more ? step / seg_steps : 0, k = more ? (step - seg * seg_steps) * KS : 0;
     const int64_t off_a = (AKC ? (int64_t)k : (int64_t)k * p.lda) * (int64_t)sizeof(T), off_b = (BKC ? (int64_t)k : (int64_t)k * p.ldb) * (int64_t)sizeof(T);
-    fa.load(a0 + (int64_t)seg * p.seg_a * (int64_t)sizeof(T) + off_a, more ? size_a - off_a : 0, p.K - k, to, lane);
-    fb.load(b0 + (int64_t)seg * p.seg_b * (int64_t)sizeof(T) + off_b, more ? size_b - off_b : 0, p.K - k, to + TM * kStep, lane);
+    const u32x4 buf_a = fa.buffer(a0 + (int64_t)seg * p.seg_a * (int64_t)sizeof(T) + off_a, more ? size_a - off_a : 0);
+    const u32x4 buf_b = fb.buffer(b0 + (int64_t)seg * p.seg_b * (int64_t)sizeof(T) + off_b, more ? size_b - off_b : 0);
+#pragma unroll
+    for (int i = 0; i < fa.N; i++) fa.load(i, buf_a, p.K - k, to, lane);
+#pragma unroll
+    for (int i = 0; i < fb.N; i++) fb.load(i, buf_b, p.K - k, to + TM * kStep, lane);
     step += WAVES;
   };
 
@@ -519,55 +570,96 @@ __global__ __launch_bounds__(64 * WAVES) void rows_kernel(const Product p, uint3
       typename Operand<T>::Type oa[2][BM], ob[2][BN];
 #pragma unroll
       for (uint32_t kk = 0; kk < 2; kk++) {
-        read_blocks<T, AKC, false, TM, kStep>(tile, 0, 0, kk, q, g, oa[kk]);
-        read_blocks<T, BKC, true, TN, kStep>(tile + TM * kStep, 0, 0, kk, q, g, ob[kk]);
+        read_blocks<T, AKC, false, TM>(tile, 0, 0, kk, q, g, oa[kk]);
+        read_blocks<T, BKC, true, TN>(tile + TM * kStep, 0, 0, kk, q, g, ob[kk]);
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // read before the place is loaded again
       load(cur);
-      multiply(oa[0], ob[0], 0, acc);
-      multiply(oa[1], ob[1], 0, acc);
+#pragma unroll
+      for (int kk = 0; kk < 2; kk++)
+#pragma unroll
+        for (int part = 0; part < kParts<T, BM>; part++) multiply(oa[kk], ob[kk], 0, part, acc);
       cur = cur + 1 == STAGES ? 0 : cur + 1;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   }
 
-  // the waves' sums, added in their order: rows of 64, the 16-byte chunks of a row at their number xor the row's
-#pragma unroll
-  for (int i = 0; i < BM; i++) {
-    const uint32_t r = row_of<T, false>(i, q);
-#pragma unroll
-    for (int j = 0; j < BN / 2; j++)
-#pragma unroll
-      for (int x = 0; x < 2; x++) *(f32x4*)(ring + (r * 16 + ((8 * j + 2 * g + x) ^ (r & 15))) * 16) = chunk_of<T>(acc[i][2 * j], acc[i][2 * j + 1], x);
-  }
-  __syncthreads();
-  for (uint32_t id = t; id < TM * 8; id += 64 * WAVES) {
-    const uint32_t r = id / 8, c = id % 8, m = m0 + r, col = n0 + c * 8;
-    if (m >= p.M || col >= p.N) continue;
-    float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int w = 0; w < WAVES; w++)
-#pragma unroll
-      for (int x = 0; x < 2; x++) {
-        const f32x4 y = *(const f32x4*)(lds[w] + (r * 16 + ((2 * c + x) ^ (r & 15))) * 16);
-#pragma unroll
-        for (int e = 0; e < 4; e++) v[4 * x + e] += y[e];
-      }
-    float bias[8];
-    bias8(p.e, col, p.N - col, bias);
-    put8(p, at, splits, m, col, bias, v, partial);
-  }
+  add_waves<T, WAVES>(p, at, splits, m0, n0, t, acc, &lds[0][0], sizeof lds[0], partial);
 }
 
-// The sum over the splits, in their order, and the epilogue: eight columns a thread.
-__global__ __launch_bounds__(256) void join_kernel(const Product p, uint32_t splits, uint64_t first, const float* __restrict__ partial) {
+// The same for operands of any alignment: through registers, the next step's loads under way while this one is multiplied.
+template <class T, bool AKC, bool BKC, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void rows_wide_kernel(const Product p, uint32_t steps, uint32_t per_split, uint32_t splits, uint32_t first,
+                                                               float* __restrict__ partial) {
+  constexpr int TM = sizeof(T) == 2 ? 16 : 32, TN = 64, BM = TM / 16, BN = TN / 16;
+  constexpr uint32_t KS = kStep / sizeof(T);
+  __shared__ __attribute__((aligned(16))) char lds[WAVES][(TM + TN) * kStep];
+
+  const Place at = place(first, (p.M + TM - 1) / TM, (p.N + TN - 1) / TN, splits);
+  const uint32_t m0 = at.tm * TM, n0 = at.tn * TN;
+  const uint32_t t = threadIdx.x, lane = t & 63, q = lane & 15, g = lane >> 4;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(t >> 6);
+
+  const uint32_t seg_steps = (p.K + KS - 1) / KS;
+  const uint32_t begin = at.split * per_split, end = min(begin + per_split, steps);
+  const T* a = (const T*)p.a + (int64_t)at.batch * p.batch_a + (AKC ? (int64_t)m0 * p.lda : (int64_t)m0);
+  const T* b = (const T*)p.b + (int64_t)at.batch * p.batch_b + (BKC ? (int64_t)n0 * p.ldb : (int64_t)n0);
+  Stage<T, AKC, false, TM, 64, true> sa;
+  Stage<T, BKC, true, TN, 64, true> sb;
+  const auto load = [&](uint32_t step) {
+    const uint32_t seg = step / seg_steps, k = (step - seg * seg_steps) * KS;
+    sa.load(a + (int64_t)seg * p.seg_a + (AKC ? (int64_t)k : (int64_t)k * p.lda), p.lda, p.M - m0, p.K - k, lane);
+    sb.load(b + (int64_t)seg * p.seg_b + (BKC ? (int64_t)k : (int64_t)k * p.ldb), p.ldb, p.N - n0, p.K - k, lane);
+  };
+
+  f32x4 acc[BM][BN];
+#pragma unroll
+  for (int i = 0; i < BM; i++)
+#pragma unroll
+    for (int j = 0; j < BN; j++) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+  char* const mine = lds[wave];
+  if (begin + wave < end) load(begin + wave);
+  for (uint32_t step = begin + wave; step < end; step += WAVES) {
+    asm volatile("" ::: "memory");         // (a wave's accesses to shared memory are done in their order)
+    sa.store(mine, p.M - m0, lane);
+    sb.store(mine + TM * kStep, p.N - n0, lane);
+    asm volatile("" ::: "memory");
+    if (step + WAVES < end) load(step + WAVES);
+#pragma unroll
+    for (uint32_t kk = 0; kk < 2; kk++) {
+      typename Operand<T>::Type oa[BM], ob[BN];
+      read_blocks<T, AKC, false, TM>((lds_ptr)mine, 0, 0, kk, q, g, oa);
+      read_blocks<T, BKC, true, TN>((lds_ptr)mine + TM * kStep, 0, 0, kk, q, g, ob);
+#pragma unroll
+      for (int part = 0; part < kParts<T, BM>; part++) multiply(oa, ob, 0, part, acc);
+    }
+  }
+  asm volatile("" ::: "memory");
+  add_waves<T, WAVES>(p, at, splits, m0, n0, t, acc, &lds[0][0], sizeof lds[0], partial);
+}
+
+// What is left to do when a call's products and rows are through, in one launch: the sums over splits of up to two products with their
+// epilogues, and the column sums of dz.  All are added in an order that the sizes alone decide.
+struct Rest {
+  Product p[2];
+  uint32_t splits[2];              // 1: nothing to join
+  const float* partial[2];
+  uint64_t blocks[2];
+  const float* sums;               // the row blocks' column sums, nullptr: none
+  uint32_t row_blocks, N, dbias_bf16, bias_blocks;
+  void* dbias;
+};
+
+// Eight columns a thread.
+__device__ __forceinline__ void join(const Product& p, uint32_t splits, const float* __restrict__ partial, uint64_t id) {
   const uint32_t groups = (p.N + 7) / 8;
-  const uint64_t id = first + (uint64_t)blockIdx.x * 256 + threadIdx.x, rows = (uint64_t)p.batches * p.M;
-  const uint64_t row = id / groups;
+  const uint64_t rows = (uint64_t)p.batches * p.M, row = id / groups;
   if (row >= rows) return;
   const uint32_t n = (uint32_t)(id - row * groups) * 8;
   const float* in = partial + row * (groups * 8) + n;
-  float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+  float bias[8], v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+  bias8(p.e, n, p.N - n, bias);
 #pragma unroll 4
   for (uint32_t s = 0; s < splits; s++) {
     const f32x4 x = *(const f32x4*)in, y = *(const f32x4*)(in + 4);
@@ -576,9 +668,30 @@ __global__ __launch_bounds__(256) void join_kernel(const Product p, uint32_t spl
     in += rows * (groups * 8);
   }
   const uint32_t batch = (uint32_t)(row / p.M);
-  float bias[8];
-  bias8(p.e, n, p.N - n, bias);
   finish8(p.e, batch, p.M, (uint32_t)(row - (uint64_t)batch * p.M), n, p.N - n, bias, v);
+}
+
+__global__ __launch_bounds__(256) void rest_kernel(const Rest r, uint64_t first) {
+  __shared__ float sums[8][32];
+  uint64_t block = first + blockIdx.x;
+  if (block < r.bias_blocks) {     // 32 columns, eight rows of sums at a time
+    const uint32_t c = threadIdx.x & 31, l = threadIdx.x >> 5, n = (uint32_t)block * 32 + c;
+    float s = 0.0f;
+    if (n < r.N) {
+#pragma unroll 8
+      for (uint32_t i = l; i < r.row_blocks; i += 8) s += r.sums[(uint64_t)i * r.N + n];
+    }
+    sums[l][c] = s;
+    __syncthreads();
+    if (l || n >= r.N) return;
+    for (int i = 1; i < 8; i++) s += sums[i][c];
+    if (r.dbias_bf16) ((bf16*)r.dbias)[n] = (bf16)s;
+    else ((float*)r.dbias)[n] = s;
+    return;
+  }
+  block -= r.bias_blocks;
+  if (block < r.blocks[0]) join(r.p[0], r.splits[0], r.partial[0], block * 256 + threadIdx.x);
+  else join(r.p[1], r.splits[1], r.partial[1], (block - r.blocks[0]) * 256 + threadIdx.x);
 }
 
 // ---- rows
@@ -628,21 +741,6 @@ __global__ __launch_bounds__(256) void grad_rows_kernel(const GradRows p, uint32
   if (bn * 256 + threadIdx.x < p.N) partial[(uint64_t)br * p.N + bn * 256 + threadIdx.x] = s;
 }
 
-// dbias: the row blocks' sums added up, in an order that the sizes alone decide.
-__global__ __launch_bounds__(1024) void grad_bias_kernel(const float* __restrict__ partial, uint32_t row_blocks, uint32_t N, void* dbias, uint32_t is_bf16) {
-  __shared__ float sums[32][33];
-  const uint32_t c = threadIdx.x & 31, r = threadIdx.x >> 5, n = blockIdx.x * 32 + c;
-  float s = 0.0f;
-  if (n < N) for (uint32_t i = r; i < row_blocks; i += 32) s += partial[(uint64_t)i * N + n];
-  sums[r][c] = s;
-  __syncthreads();
-  if (r || n >= N) return;
-#pragma unroll
-  for (int i = 1; i < 32; i++) s += sums[i][c];
-  if (is_bf16) ((bf16*)dbias)[n] = (bf16)s;
-  else ((float*)dbias)[n] = s;
-}
-
 __global__ __launch_bounds__(256) void drop_kernel(const DropRows p, uint64_t first) {
   const uint32_t groups = (p.N + 7) / 8;
   const uint64_t id = first + (uint64_t)blockIdx.x * 256 + threadIdx.x, row = id / groups;
@@ -676,12 +774,13 @@ hipError_t launch_tiles(const Product& p, const ProductPlan& plan, float* partia
   return in_launches(plan.blocks, [&](uint64_t first, uint32_t n) {
     const auto go = [&](auto kernel, uint32_t threads) { kernel<<<n, threads, 0, st>>>(p, plan.steps, plan.per_split, plan.splits, (uint32_t)first, partial); };
     switch (plan.kernel) {
-      case kFast256: return go(fast_kernel<T, AKC, BKC, 256, 256, 2, 4, 128, 2>, 512);
-      case kFast256x128: return go(fast_kernel<T, AKC, BKC, 256, 128, 4, 2, 128, 3>, 512);
-      case kFast128: return go(fast_kernel<T, AKC, BKC, 128, 128, 2, 4, 128, 2>, 512);
-      case kFast128Alone: return go(fast_kernel<T, AKC, BKC, 128, 128, 2, 4, 128, 4>, 512);
+      case kFast256: return go(fast_kernel<T, AKC, BKC, 256, 256, 2, 4, 2>, 512);
+      case kFast256x128: return go(fast_kernel<T, AKC, BKC, 256, 128, 4, 2, 3>, 512);
+      case kFast128: return go(fast_kernel<T, AKC, BKC, 128, 128, 2, 4, 2>, 512);
+      case kFast128Alone: return go(fast_kernel<T, AKC, BKC, 128, 128, 2, 4, 4>, 512);
       case kRows: return go(rows_kernel<T, AKC, BKC, 4, 3>, 256);
-      case kFast64: return go(fast_kernel<T, AKC, BKC, 64, 64, 2, 2, 128, 4>, 256);
+      case kFast64: return go(fast_kernel<T, AKC, BKC, 64, 64, 2, 2, 4>, 256);
+      case kRowsWide: return go(rows_wide_kernel<T, AKC, BKC, 8>, 512);
       case kWide128: return go(product_kernel<T, AKC, BKC, 128, 128, 2, 2, true>, 256);
       case kWide64: return go(product_kernel<T, AKC, BKC, 64, 64, 2, 2, true>, 256);
       case kAny64: return go(product_kernel<T, AKC, BKC, 64, 64, 2, 2, false>, 256);
@@ -727,6 +826,7 @@ constexpr Kernel kKernels[] = {
     {kFast128, 128, 128, kAligned, 4, {0.50f, 1.99f}, {0.93f, 3.78f}},
     {kFast64, 64, 64, kAligned, 2, {0.25f, 0.62f}, {0.37f, 1.07f}},
     {kRows, 0, 64, kAligned, 3, {0.12f, 0.27f}, {0, 0}},
+    {kRowsWide, 0, 64, kWide, 3, {0.08f, 0.14f}, {0, 0}},
     {kWide128, 128, 128, kWide, 4, {0.97f, 2.38f}, {1.69f, 4.76f}},
     {kWide64, 64, 64, kWide, 2, {0.36f, 0.62f}, {0.60f, 1.10f}},
     {kAny64, 64, 64, kAny, 2, {2.0f, 2.0f}, {3.0f, 3.0f}},
@@ -742,7 +842,7 @@ ProductPlan plan_product(const Product& p) {
   float best = 0;
   for (const Kernel& k : kKernels) {
     if (k.access != access) continue;
-    const uint32_t tm = k.id == kRows ? (f32 ? 32 : 16) : k.tm;
+    const uint32_t tm = k.tm ? k.tm : f32 ? 32 : 16;
     const uint64_t tiles = (uint64_t)((p.M + tm - 1) / tm) * ((p.N + k.tn - 1) / k.tn) * p.batches;
     for (uint32_t splits = 1; splits <= 64; splits = splits == 1 ? 2 : splits & splits - 1 ? splits / 3 * 4 : splits / 2 * 3) {
       const uint32_t per = (plan.steps + splits - 1) / splits;
@@ -764,11 +864,32 @@ ProductPlan plan_product(const Product& p) {
 }
 
 hipError_t launch_product(const Product& p, const ProductPlan& plan, float* partial, hipStream_t st) {
-  if (!plan.blocks) return hipSuccess;
-  const hipError_t e = p.bf16 ? launch_layout<bf16>(p, plan, partial, st) : launch_layout<float>(p, plan, partial, st);
-  if (e != hipSuccess || plan.splits == 1) return e;
-  const uint64_t items = (uint64_t)p.batches * p.M * ((p.N + 7) / 8);
-  return in_launches((items + 255) / 256, [&](uint64_t first, uint32_t n) { join_kernel<<<n, 256, 0, st>>>(p, plan.splits, first * 256, partial); });
+  return p.bf16 ? launch_layout<bf16>(p, plan, partial, st) : launch_layout<float>(p, plan, partial, st);
+}
+
+hipError_t launch_rest(const Product* const p[2], const ProductPlan* const plan[2], const float* const partial[2], const GradRows* rows, const float* sums, hipStream_t st) {
+  Rest r{};
+  uint64_t blocks = 0;
+  for (int i = 0; i < 2; i++) {
+    if (!p[i] || plan[i]->splits < 2) continue;
+    r.p[i] = *p[i];
+    r.splits[i] = plan[i]->splits;
+    r.partial[i] = partial[i];
+    r.blocks[i] = ((uint64_t)p[i]->batches * p[i]->M * ((p[i]->N + 7) / 8) + 255) / 256;
+    blocks += r.blocks[i];
+  }
+  if (rows && rows->dbias && rows->N) {
+    const uint64_t n = (uint64_t)rows->batches * rows->M;
+    const uint32_t each = grad_rows(n, rows->N);
+    r.sums = sums;
+    r.row_blocks = (uint32_t)((n + each - 1) / each);
+    r.N = rows->N;
+    r.dbias = rows->dbias;
+    r.dbias_bf16 = rows->dbias_bf16;
+    r.bias_blocks = (rows->N + 31) / 32;
+    blocks += r.bias_blocks;
+  }
+  return in_launches(blocks, [&](uint64_t first, uint32_t n) { rest_kernel<<<n, 256, 0, st>>>(r, first); });
 }
 
 uint64_t grad_rows_bytes(uint32_t batches, uint32_t M, uint32_t N, bool dbias) {
@@ -782,12 +903,9 @@ hipError_t launch_grad_rows(const GradRows& g, float* partial, hipStream_t st) {
   const uint64_t rows = (uint64_t)g.batches * g.M;
   const uint32_t each = grad_rows(rows, g.N);
   const uint64_t row_blocks = (rows + each - 1) / each;
-  const hipError_t e = in_launches(row_blocks * ((g.N + 255) / 256), [&](uint64_t first, uint32_t n) {
+  return in_launches(row_blocks * ((g.N + 255) / 256), [&](uint64_t first, uint32_t n) {
     grad_rows_kernel<<<n, 256, 0, st>>>(g, each, (uint32_t)first, g.dbias ? partial : nullptr);
   });
-  if (e != hipSuccess || !g.dbias) return e;
-  grad_bias_kernel<<<(g.N + 31) / 32, 1024, 0, st>>>(partial, (uint32_t)row_blocks, g.N, g.dbias, g.dbias_bf16);
-  return hipGetLastError();
 }
 
 hipError_t launch_drop(const DropRows& d, hipStream_t st) {

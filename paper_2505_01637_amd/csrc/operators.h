@@ -192,7 +192,7 @@ struct Product {
 };
 
 // How it is launched.
-enum : uint32_t { kFast256, kFast256x128, kFast128, kFast128Alone, kFast64, kRows, kWide128, kWide64, kAny64 };
+enum : uint32_t { kFast256, kFast256x128, kFast128, kFast128Alone, kFast64, kRows, kRowsWide, kWide128, kWide64, kAny64 };
 struct ProductPlan {
   uint32_t kernel;
   uint32_t splits;               // workgroups along k
@@ -201,7 +201,7 @@ struct ProductPlan {
   uint64_t partial_bytes;        // workspace
 };
 ProductPlan plan_product(const Product& p);
-hipError_t launch_product(const Product& p, const ProductPlan& plan, float* partial, hipStream_t st);
+hipError_t launch_product(const Product& p, const ProductPlan& plan, float* partial, hipStream_t st);      // without the sum over splits
 
 // dz = D f'(z) grad of `rows` x N elements (rows over all batches of M) and its column sums.
 struct GradRows {
@@ -212,7 +212,9 @@ struct GradRows {
   uint32_t dbias_bf16;
 };
 uint64_t grad_rows_bytes(uint32_t batches, uint32_t M, uint32_t N, bool dbias);
-hipError_t launch_grad_rows(const GradRows& g, float* partial, hipStream_t st);
+hipError_t launch_grad_rows(const GradRows& g, float* sums, hipStream_t st);       // dz, and the column sums of blocks of rows
+// What is left, in one launch: the products' sums over splits (nullptr: no such product), dbias from the blocks' sums.
+hipError_t launch_rest(const Product* const p[2], const ProductPlan* const plan[2], const float* const partial[2], const GradRows* rows, const float* sums, hipStream_t st);
 
 // out = residual + D x
 struct DropRows {

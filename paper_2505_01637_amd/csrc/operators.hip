@@ -127,7 +127,8 @@ struct GradPlan {
   GradRows rows;
   Product by_lhs, by_rhs;
   ProductPlan plan_lhs, plan_rhs;
-  size_t dz_bytes, partial_bytes;
+  size_t dz_bytes, sums_bytes, lhs_bytes, rhs_bytes;      // workspace, in this order
+  size_t bytes() const { return dz_bytes + sums_bytes + lhs_bytes + rhs_bytes; }
 };
 
 int32_t plan_grad(const mrl_linear_grad_desc& d, GradPlan* out) {
@@ -165,7 +166,7 @@ int32_t plan_grad(const mrl_linear_grad_desc& d, GradPlan* out) {
   g.rows.drop = drop;
   g.rows.dbias = d.d_bias.data;
   g.rows.dbias_bf16 = d.d_bias.dtype == MRL_BF16;
-  g.partial_bytes = grad_rows_bytes(d.b, d.m, d.n, d.d_bias.data);
+  g.sums_bytes = align_up(grad_rows_bytes(d.b, d.m, d.n, d.d_bias.data));
 
   if (g.lhs) {                     // d_lhs = dz rhs^T: m x k, the sum over n
     Product& p = g.by_lhs;
@@ -190,7 +191,7 @@ int32_t plan_grad(const mrl_linear_grad_desc& d, GradPlan* out) {
     }
     g.plan_lhs = plan_product(p);
     if ((rc = check_product(p, g.plan_lhs))) return rc;
-    g.partial_bytes = std::max<size_t>(g.partial_bytes, g.plan_lhs.partial_bytes);
+    g.lhs_bytes = align_up(g.plan_lhs.partial_bytes);
   }
   if (g.rhs) {                     // d_rhs = lhs^T dz: k x n (column-major: its transpose, dz^T lhs), the sum over m
     Product& p = g.by_rhs;
@@ -219,7 +220,7 @@ int32_t plan_grad(const mrl_linear_grad_desc& d, GradPlan* out) {
     }
     g.plan_rhs = plan_product(p);
     if ((rc = check_product(p, g.plan_rhs))) return rc;
-    g.partial_bytes = std::max<size_t>(g.partial_bytes, g.plan_rhs.partial_bytes);
+    g.rhs_bytes = align_up(g.plan_rhs.partial_bytes);
   }
   *out = g;
   return MRL_OK;
@@ -253,7 +254,13 @@ int32_t mrl_linear(const mrl_linear_desc* desc, void* d_workspace, size_t worksp
   const ProductPlan plan = plan_product(p);
   if ((rc = check_product(p, plan))) return rc;
   if ((rc = check_workspace(d_workspace, workspace_bytes, plan.partial_bytes))) return rc;
-  return hip_status(launch_product(p, plan, (float*)d_workspace, (hipStream_t)hip_stream));
+  const hipStream_t st = (hipStream_t)hip_stream;
+  hipError_t e = launch_product(p, plan, (float*)d_workspace, st);
+  const Product* const products[2] = {&p, nullptr};
+  const ProductPlan* const plans[2] = {&plan, nullptr};
+  const float* const partials[2] = {(const float*)d_workspace, nullptr};
+  if (e == hipSuccess && plan.splits > 1) e = launch_rest(products, plans, partials, nullptr, nullptr, st);
+  return hip_status(e);
 }
 
 int32_t mrl_linear_grad_bytes(const mrl_linear_grad_desc* desc, size_t* bytes) {
@@ -261,7 +268,7 @@ int32_t mrl_linear_grad_bytes(const mrl_linear_grad_desc* desc, size_t* bytes) {
   GradPlan g;
   const int32_t rc = plan_grad(*desc, &g);
   if (rc) return rc;
-  *bytes = g.dz_bytes + g.partial_bytes;
+  *bytes = g.bytes();
   return MRL_OK;
 }
 
@@ -270,8 +277,10 @@ int32_t mrl_linear_grad(const mrl_linear_grad_desc* desc, void* d_workspace, siz
   GradPlan g;
   int32_t rc = plan_grad(*desc, &g);
   if (rc) return rc;
-  if ((rc = check_workspace(d_workspace, workspace_bytes, g.dz_bytes + g.partial_bytes))) return rc;
-  float* partial = (float*)((char*)d_workspace + g.dz_bytes);
+  if ((rc = check_workspace(d_workspace, workspace_bytes, g.bytes()))) return rc;
+  float* const sums = (float*)((char*)d_workspace + g.dz_bytes);
+  float* const partial_lhs = (float*)((char*)sums + g.sums_bytes);
+  float* const partial_rhs = (float*)((char*)partial_lhs + g.lhs_bytes);
   const hipStream_t st = (hipStream_t)hip_stream;
   if (g.pass) {
     g.rows.dz.data = d_workspace;
@@ -281,9 +290,13 @@ int32_t mrl_linear_grad(const mrl_linear_grad_desc* desc, void* d_workspace, siz
     g.rows.dz.data = nullptr;      // grad is dz
   }
   hipError_t e = hipSuccess;
-  if (g.pass || g.rows.dbias) e = launch_grad_rows(g.rows, partial, st);
-  if (e == hipSuccess && g.lhs) e = launch_product(g.by_lhs, g.plan_lhs, partial, st);
-  if (e == hipSuccess && g.rhs) e = launch_product(g.by_rhs, g.plan_rhs, partial, st);
+  if (g.pass || g.rows.dbias) e = launch_grad_rows(g.rows, sums, st);
+  if (e == hipSuccess && g.lhs) e = launch_product(g.by_lhs, g.plan_lhs, partial_lhs, st);
+  if (e == hipSuccess && g.rhs) e = launch_product(g.by_rhs, g.plan_rhs, partial_rhs, st);
+  const Product* const products[2] = {g.lhs ? &g.by_lhs : nullptr, g.rhs ? &g.by_rhs : nullptr};
+  const ProductPlan* const plans[2] = {&g.plan_lhs, &g.plan_rhs};
+  const float* const partials[2] = {partial_lhs, partial_rhs};
+  if (e == hipSuccess) e = launch_rest(products, plans, partials, &g.rows, sums, st);
   return hip_status(e);
 }
 
