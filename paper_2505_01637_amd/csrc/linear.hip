@@ -388,8 +388,8 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void fast_kernel(const P
   uint32_t seg = begin < end ? begin / seg_steps : 0, k = (begin - seg * seg_steps) * KS;
   const char *a0 = (const char*)((const T*)p.a + (int64_t)at.batch * p.batch_a + (AKC ? (int64_t)m0 * p.lda : (int64_t)m0));
   const char *b0 = (const char*)((const T*)p.b + (int64_t)at.batch * p.batch_b + (BKC ? (int64_t)n0 * p.ldb : (int64_t)n0));
-  const int64_t size_a = (AKC ? ((int64_t)(p.M - m0) - 1) * p.lda + p.K : ((int64_t)p.K - 1) * p.lda + (p.M - m0)) * (int64_t)sizeof(T);
-  const int64_t size_b = (BKC ? ((int64_t)(p.N - n0) - 1) * p.ldb + p.K : ((int64_t)p.K - 1) * p.ldb + (p.N - n0)) * (int64_t)sizeof(T);
+  const int64_t size_a = (AKC ? ((int64_t)(p.M - m0) - 1) * p.lda + p.wa : ((int64_t)p.K - 1) * p.lda + (p.wa - m0)) * (int64_t)sizeof(T);
+  const int64_t size_b = (BKC ? ((int64_t)(p.N - n0) - 1) * p.ldb + p.wb : ((int64_t)p.K - 1) * p.ldb + (p.wb - n0)) * (int64_t)sizeof(T);
   int64_t off_a = (int64_t)(k / KS) * step_a, off_b = (int64_t)(k / KS) * step_b;
   const char *sa = a0 + (int64_t)seg * p.seg_a * (int64_t)sizeof(T), *sb = b0 + (int64_t)seg * p.seg_b * (int64_t)sizeof(T);
   const uint32_t n = end > begin ? end - begin : 0;
@@ -537,8 +537,8 @@ __global__ __launch_bounds__(64 * WAVES) void rows_kernel(const Product p, uint3
   const uint32_t n = end > step ? (end - step + WAVES - 1) / WAVES : 0;
   const char *a0 = (const char*)((const T*)p.a + (int64_t)at.batch * p.batch_a + (AKC ? (int64_t)m0 * p.lda : (int64_t)m0));
   const char *b0 = (const char*)((const T*)p.b + (int64_t)at.batch * p.batch_b + (BKC ? (int64_t)n0 * p.ldb : (int64_t)n0));
-  const int64_t size_a = (AKC ? ((int64_t)(p.M - m0) - 1) * p.lda + p.K : ((int64_t)p.K - 1) * p.lda + (p.M - m0)) * (int64_t)sizeof(T);
-  const int64_t size_b = (BKC ? ((int64_t)(p.N - n0) - 1) * p.ldb + p.K : ((int64_t)p.K - 1) * p.ldb + (p.N - n0)) * (int64_t)sizeof(T);
+  const int64_t size_a = (AKC ? ((int64_t)(p.M - m0) - 1) * p.lda + p.wa : ((int64_t)p.K - 1) * p.lda + (p.wa - m0)) * (int64_t)sizeof(T);
+  const int64_t size_b = (BKC ? ((int64_t)(p.N - n0) - 1) * p.ldb + p.wb : ((int64_t)p.K - 1) * p.ldb + (p.wb - n0)) * (int64_t)sizeof(T);
   char* const ring = lds[wave];
   const auto load = [&](uint32_t stage) {
     const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr)ring + stage * STAGE);
@@ -701,6 +701,7 @@ __global__ __launch_bounds__(256) void rest_kernel(const Rest r, uint64_t first)
 uint32_t grad_rows(uint64_t rows, uint32_t N) {
   const uint64_t blocks_n = (N + 255) / 256;
   uint32_t each = 64;
+  if (rows <= each) return each;         // one block of rows: its sums are dbias, and no launch follows to add them up
   while (each > 8 && (rows + each - 1) / each * blocks_n < 1024) each /= 2;
   return each;
 }
@@ -728,17 +729,21 @@ __global__ __launch_bounds__(256) void grad_rows_kernel(const GradRows p, uint32
       }
 #pragma unroll
       for (int e = 0; e < 8; e++) sum[e] += v[e];
-      if (p.dz.data) store8(p.dz.data, p.dz.bf16, (int64_t)batch * p.dz.batch + (int64_t)m * p.dz.ld + n, valid, v);
+      if (p.dz.data) store8(p.dz.data, p.dz.bf16, (int64_t)batch * p.dz.batch + (int64_t)m * p.dz.ld + n, 8, v);     // (zeros up to a multiple of 8)
     }
   }
-  if (!partial) return;
+  if (!p.dbias) return;
 #pragma unroll
   for (int e = 0; e < 8; e++) sums[r][c * 8 + e] = sum[e];
   __syncthreads();
   float s = 0.0f;
 #pragma unroll
   for (int i = 0; i < 8; i++) s += sums[i][threadIdx.x];
-  if (bn * 256 + threadIdx.x < p.N) partial[(uint64_t)br * p.N + bn * 256 + threadIdx.x] = s;
+  const uint32_t at = bn * 256 + threadIdx.x;
+  if (at >= p.N) return;
+  if (partial) partial[(uint64_t)br * p.N + at] = s;
+  else if (p.dbias_bf16) ((bf16*)p.dbias)[at] = (bf16)s;
+  else ((float*)p.dbias)[at] = s;
 }
 
 __global__ __launch_bounds__(256) void drop_kernel(const DropRows p, uint64_t first) {
@@ -793,18 +798,53 @@ hipError_t launch_layout(const Product& p, const ProductPlan& plan, float* parti
   return p.b_kc ? launch_tiles<T, false, true>(p, plan, partial, st) : launch_tiles<T, false, false>(p, plan, partial, st);
 }
 
-// What a product's operands allow.  kAligned: every line that is read starts at a multiple of 16 bytes, ends at one, and follows the one before,
-// and offsets within a tile fit 31 bits.  kWide: every line holds 16 bytes at least.
+// What an operand allows.  kAligned: every line that is read starts at a multiple of 16 bytes, ends at one, and follows the one before, and
+// offsets within a tile fit 31 bits.  kWide: every line holds 16 bytes at least.
 enum Access { kAligned, kWide, kAny };
-Access access_of(const Product& p) {
-  const int64_t e = p.bf16 ? 8 : 4;
-  const auto aligned = [&](const void* data, int64_t ld, int64_t batch, int64_t seg, int64_t width) {
-    return (uintptr_t)data % 16 == 0 && ld % e == 0 && batch % e == 0 && seg % e == 0 && width % e == 0 && ld >= width && ld < (int64_t)1 << 21;
-  };
-  const int64_t wa = p.a_kc ? p.K : p.M, wb = p.b_kc ? p.K : p.N;
-  if (aligned(p.a, p.lda, p.batches > 1 ? p.batch_a : 0, p.segs > 1 ? p.seg_a : 0, wa) && aligned(p.b, p.ldb, p.batches > 1 ? p.batch_b : 0, p.segs > 1 ? p.seg_b : 0, wb)) return kAligned;
-  return wa >= e && wb >= e ? kWide : kAny;
+Access access_of(const void* data, int64_t ld, int64_t batch, int64_t seg, int64_t width, int64_t e) {
+  if ((uintptr_t)data % 16 == 0 && ld % e == 0 && batch % e == 0 && seg % e == 0 && width % e == 0 && ld >= width && ld < (int64_t)1 << 21) return kAligned;
+  return width >= e ? kWide : kAny;
 }
+
+// Matrices of `lines` lines of `width` elements, copied to lines of `pitch` elements (a multiple of 16 bytes), zeros behind the width.
+struct Copy {
+  const void* from;
+  void* to;
+  int64_t ld, step;                // from a line to the next, from a matrix to the next
+  uint32_t matrices, lines, width, pitch;
+  uint64_t chunks() const { return (uint64_t)matrices * lines * pitch; }        // (times the elements of a chunk)
+};
+
+// 16 bytes a thread, first of a's copy, then of b's.
+template <class T>
+__global__ __launch_bounds__(256) void copy_kernel(const Copy a, const Copy b, uint64_t chunks_a, uint64_t chunks, uint64_t first) {
+  constexpr uint32_t E = 16 / sizeof(T);
+  uint64_t id = (first + blockIdx.x) * 256 + threadIdx.x;
+  if (id >= chunks) return;
+  const Copy& c = id < chunks_a ? a : b;
+  if (id >= chunks_a) id -= chunks_a;
+  const uint32_t per = c.pitch / E;
+  const uint64_t line = id / per, matrix = line / c.lines;
+  const uint32_t at = (uint32_t)(id - line * per) * E;
+  const T* from = (const T*)c.from + (int64_t)matrix * c.step + (int64_t)(line - matrix * c.lines) * c.ld + at;
+  T v[E];
+  if (at + E <= c.width) {
+    __builtin_memcpy(v, from, 16);
+  } else {
+#pragma unroll
+    for (uint32_t e = 0; e < E; e++) v[e] = at + e < c.width ? from[e] : (T)0.0f;
+  }
+  *(u32x4*)((T*)c.to + line * c.pitch + at) = *(const u32x4*)v;
+}
+
+// The copy of an operand: as many matrices as it has, lines along the other index than its own.
+Copy copy_of(const void* from, uint32_t kc, int64_t ld, int64_t batch, int64_t seg, uint32_t width, const Product& p, uint32_t others) {
+  const uint32_t e = p.bf16 ? 8 : 4;
+  const bool batched = p.batches > 1 && batch, segmented = p.segs > 1 && seg;       // (never both)
+  return Copy{from, nullptr, ld, batched ? batch : seg, batched ? p.batches : segmented ? p.segs : 1, kc ? others : p.K, width, (width + e - 1) / e * e};
+}
+Copy copy_a(const Product& p) { return copy_of(p.a, p.a_kc, p.lda, p.batch_a, p.seg_a, p.a_kc ? p.K : p.M, p, p.M); }
+Copy copy_b(const Product& p) { return copy_of(p.b, p.b_kc, p.ldb, p.batch_b, p.seg_b, p.b_kc ? p.K : p.N, p, p.N); }
 
 }  // namespace
 
@@ -825,23 +865,30 @@ constexpr Kernel kKernels[] = {
     {kFast256x128, 256, 128, kAligned, 6, {0.87f, 3.81f}, {0, 0}},
     {kFast128, 128, 128, kAligned, 4, {0.50f, 1.99f}, {0.93f, 3.78f}},
     {kFast64, 64, 64, kAligned, 2, {0.25f, 0.62f}, {0.37f, 1.07f}},
-    {kRows, 0, 64, kAligned, 3, {0.12f, 0.27f}, {0, 0}},
-    {kRowsWide, 0, 64, kWide, 3, {0.08f, 0.14f}, {0, 0}},
-    {kWide128, 128, 128, kWide, 4, {0.97f, 2.38f}, {1.69f, 4.76f}},
-    {kWide64, 64, 64, kWide, 2, {0.36f, 0.62f}, {0.60f, 1.10f}},
+    {kRows, 0, 64, kAligned, 3, {0.12f, 0.27f}, {0.24f, 0.54f}},
+    {kRowsWide, 0, 64, kWide, 3, {0.11f, 0.20f}, {0.42f, 0.70f}},
+    {kWide128, 128, 128, kWide, 4, {1.25f, 2.50f}, {1.70f, 4.80f}},
+    {kWide64, 64, 64, kWide, 2, {0.80f, 0.72f}, {0.86f, 1.15f}},
     {kAny64, 64, 64, kAny, 2, {2.0f, 2.0f}, {3.0f, 3.0f}},
 };
-constexpr float kJoin = 4, kJoinBytes = 4.5e6f;
+constexpr float kLaunch1 = 5, kBytes = 4.5e6f;                     // a further launch, us; bytes a us
 
 ProductPlan plan_product(const Product& p) {
   ProductPlan plan{};
-  const uint32_t ks = kStep / (p.bf16 ? 2 : 4), f32 = !p.bf16;
-  const Access access = access_of(p);
+  const uint32_t size = p.bf16 ? 2 : 4, ks = kStep / size, f32 = !p.bf16;
+  const Access a = access_of(p.a, p.lda, p.batches > 1 ? p.batch_a : 0, p.segs > 1 ? p.seg_a : 0, p.wa, 16 / size);
+  const Access b = access_of(p.b, p.ldb, p.batches > 1 ? p.batch_b : 0, p.segs > 1 ? p.seg_b : 0, p.wb, 16 / size);
+  const Access both = a > b ? a : b;
   plan.steps = (p.K + ks - 1) / ks * p.segs;
   const float out = (float)p.batches * p.M * p.N * 4;
+  // operands that are not aligned may be copied so that they are
+  const Copy ca = copy_a(p), cb = copy_b(p);
+  const uint64_t bytes_a = a == kAligned ? 0 : (ca.chunks() * size + 255) / 256 * 256, bytes_b = b == kAligned ? 0 : (cb.chunks() * size + 255) / 256 * 256;
+  const bool copies = both != kAligned && ca.pitch < 1u << 21 && cb.pitch < 1u << 21;
   float best = 0;
   for (const Kernel& k : kKernels) {
-    if (k.access != access) continue;
+    const bool copied = k.access == kAligned && both != kAligned;
+    if (copied ? !copies : k.access != both) continue;
     const uint32_t tm = k.tm ? k.tm : f32 ? 32 : 16;
     const uint64_t tiles = (uint64_t)((p.M + tm - 1) / tm) * ((p.N + k.tn - 1) / k.tn) * p.batches;
     for (uint32_t splits = 1; splits <= 64; splits = splits == 1 ? 2 : splits & splits - 1 ? splits / 3 * 4 : splits / 2 * 3) {
@@ -850,20 +897,49 @@ ProductPlan plan_product(const Product& p) {
       const float one = k.fixed + per * k.one[f32], two = k.two[0] ? k.fixed + per * k.two[f32] : 2 * one;
       const uint64_t blocks = tiles * splits, rounds = blocks / 512, rest = blocks % 512;
       float t = rounds * two + (rest > 256 ? two : rest ? one : 0);
-      if (splits > 1) t += kJoin + (splits + 1) * out / kJoinBytes;
+      if (splits > 1) t += kLaunch1 + (splits + 1) * out / kBytes;
+      if (copied) t += kLaunch1 + 2 * (bytes_a + bytes_b) / kBytes;
       if (best && t >= best) continue;
       best = t;
       plan.kernel = k.id == kFast128 && blocks <= 256 ? kFast128Alone : k.id;
       plan.per_split = per;
       plan.splits = per ? (plan.steps + per - 1) / per : 1;
       plan.blocks = tiles * plan.splits;
+      plan.copy_a_bytes = copied ? bytes_a : 0;
+      plan.copy_b_bytes = copied ? bytes_b : 0;
     }
   }
   plan.partial_bytes = plan.splits > 1 ? (uint64_t)plan.splits * p.batches * p.M * ((p.N + 7) / 8 * 8) * 4 : 0;
   return plan;
 }
 
-hipError_t launch_product(const Product& p, const ProductPlan& plan, float* partial, hipStream_t st) {
+hipError_t launch_product(const Product& given, const ProductPlan& plan, void* workspace, hipStream_t st) {
+  Product p = given;
+  if (plan.blocks && plan.copy_a_bytes + plan.copy_b_bytes) {
+    Copy a = copy_a(p), b = copy_b(p);
+    a.to = workspace;
+    b.to = (char*)workspace + plan.copy_a_bytes;
+    const uint32_t e = p.bf16 ? 8 : 4;
+    const uint64_t chunks_a = plan.copy_a_bytes ? a.chunks() / e : 0, chunks = chunks_a + (plan.copy_b_bytes ? b.chunks() / e : 0);
+    const hipError_t err = in_launches((chunks + 255) / 256, [&](uint64_t first, uint32_t n) {
+      if (p.bf16) copy_kernel<bf16><<<n, 256, 0, st>>>(a, b, chunks_a, chunks, first);
+      else copy_kernel<float><<<n, 256, 0, st>>>(a, b, chunks_a, chunks, first);
+    });
+    if (err != hipSuccess) return err;
+    if (plan.copy_a_bytes) {
+      p.a = a.to;
+      p.lda = p.wa = a.pitch;
+      if (p.batch_a) p.batch_a = (int64_t)a.lines * a.pitch;
+      if (p.seg_a) p.seg_a = (int64_t)a.lines * a.pitch;
+    }
+    if (plan.copy_b_bytes) {
+      p.b = b.to;
+      p.ldb = p.wb = b.pitch;
+      if (p.batch_b) p.batch_b = (int64_t)b.lines * b.pitch;
+      if (p.seg_b) p.seg_b = (int64_t)b.lines * b.pitch;
+    }
+  }
+  float* const partial = plan.partial(workspace);
   return p.bf16 ? launch_layout<bf16>(p, plan, partial, st) : launch_layout<float>(p, plan, partial, st);
 }
 
@@ -878,9 +954,9 @@ hipError_t launch_rest(const Product* const p[2], const ProductPlan* const plan[
     r.blocks[i] = ((uint64_t)p[i]->batches * p[i]->M * ((p[i]->N + 7) / 8) + 255) / 256;
     blocks += r.blocks[i];
   }
-  if (rows && rows->dbias && rows->N) {
-    const uint64_t n = (uint64_t)rows->batches * rows->M;
-    const uint32_t each = grad_rows(n, rows->N);
+  const uint64_t n = rows ? (uint64_t)rows->batches * rows->M : 0;
+  const uint32_t each = rows ? grad_rows(n, rows->N) : 0;
+  if (rows && rows->dbias && n > each) {
     r.sums = sums;
     r.row_blocks = (uint32_t)((n + each - 1) / each);
     r.N = rows->N;
@@ -895,16 +971,16 @@ hipError_t launch_rest(const Product* const p[2], const ProductPlan* const plan[
 uint64_t grad_rows_bytes(uint32_t batches, uint32_t M, uint32_t N, bool dbias) {
   const uint64_t rows = (uint64_t)batches * M;
   const uint32_t each = grad_rows(rows, N);
-  return dbias ? (rows + each - 1) / each * N * 4 : 0;
+  return dbias && rows > each ? (rows + each - 1) / each * N * 4 : 0;
 }
 
 hipError_t launch_grad_rows(const GradRows& g, float* partial, hipStream_t st) {
   if (!g.N) return hipSuccess;
   const uint64_t rows = (uint64_t)g.batches * g.M;
   const uint32_t each = grad_rows(rows, g.N);
-  const uint64_t row_blocks = (rows + each - 1) / each;
+  const uint64_t row_blocks = rows ? (rows + each - 1) / each : 1;       // (of no rows: dbias is 0)
   return in_launches(row_blocks * ((g.N + 255) / 256), [&](uint64_t first, uint32_t n) {
-    grad_rows_kernel<<<n, 256, 0, st>>>(g, each, (uint32_t)first, g.dbias ? partial : nullptr);
+    grad_rows_kernel<<<n, 256, 0, st>>>(g, each, (uint32_t)first, rows > each ? partial : nullptr);
   });
 }
 

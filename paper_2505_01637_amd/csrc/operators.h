@@ -188,6 +188,7 @@ struct Product {
   int64_t batch_a, batch_b;      // elements between batches
   int64_t seg_a, seg_b;          // and between segments
   uint32_t batches, segs, M, N, K;
+  uint32_t wa, wb;               // elements of a line that are there: K, or M (N); more where a line is followed by zeros
   Epilogue e;
 };
 
@@ -198,10 +199,13 @@ struct ProductPlan {
   uint32_t splits;               // workgroups along k
   uint32_t steps, per_split;     // steps of 128 bytes along k: in all, per split
   uint64_t blocks;               // workgroups
-  uint64_t partial_bytes;        // workspace
+  bool copy_a, copy_b;           // the operand is first copied to lines that start at multiples of 16 bytes
+  uint64_t copy_a_bytes, copy_b_bytes, partial_bytes;        // workspace, in this order
+  uint64_t bytes() const { return copy_a_bytes + copy_b_bytes + partial_bytes; }
+  float* partial(void* workspace) const { return (float*)((char*)workspace + copy_a_bytes + copy_b_bytes); }
 };
 ProductPlan plan_product(const Product& p);
-hipError_t launch_product(const Product& p, const ProductPlan& plan, float* partial, hipStream_t st);      // without the sum over splits
+hipError_t launch_product(const Product& p, const ProductPlan& plan, void* workspace, hipStream_t st);     // without the sum over splits
 
 // dz = D f'(z) grad of `rows` x N elements (rows over all batches of M) and its column sums.
 struct GradRows {

@@ -116,6 +116,8 @@ int32_t linear_product(const mrl_linear_desc& d, Product* out) {
     p.M = d.b * d.m;
     p.batches = 1;
   }
+  p.wa = p.a_kc ? p.K : p.M;
+  p.wb = p.b_kc ? p.K : p.N;
   *out = p;
   return MRL_OK;
 }
@@ -189,9 +191,11 @@ int32_t plan_grad(const mrl_linear_grad_desc& d, GradPlan* out) {
       p.M = d.b * d.m;
       p.batches = 1;
     }
+    p.wa = g.pass ? pitch : p.K;
+    p.wb = p.b_kc ? p.K : p.N;
     g.plan_lhs = plan_product(p);
     if ((rc = check_product(p, g.plan_lhs))) return rc;
-    g.lhs_bytes = align_up(g.plan_lhs.partial_bytes);
+    g.lhs_bytes = align_up(g.plan_lhs.bytes());
   }
   if (g.rhs) {                     // d_rhs = lhs^T dz: k x n (column-major: its transpose, dz^T lhs), the sum over m
     Product& p = g.by_rhs;
@@ -218,9 +222,12 @@ int32_t plan_grad(const mrl_linear_grad_desc& d, GradPlan* out) {
       p.K = d.b * d.m;
       p.segs = 1;
     }
+    const uint32_t width_lhs = lhs.kc ? p.K : d.k, width_z = g.pass ? pitch : d.n;
+    p.wa = turned ? width_z : width_lhs;
+    p.wb = turned ? width_lhs : width_z;
     g.plan_rhs = plan_product(p);
     if ((rc = check_product(p, g.plan_rhs))) return rc;
-    g.rhs_bytes = align_up(g.plan_rhs.partial_bytes);
+    g.rhs_bytes = align_up(g.plan_rhs.bytes());
   }
   *out = g;
   return MRL_OK;
@@ -242,7 +249,7 @@ int32_t mrl_linear_bytes(const mrl_linear_desc* desc, size_t* bytes) {
   Product p;
   const int32_t rc = linear_product(*desc, &p);
   if (rc) return rc;
-  *bytes = plan_product(p).partial_bytes;
+  *bytes = plan_product(p).bytes();
   return MRL_OK;
 }
 
@@ -253,12 +260,12 @@ int32_t mrl_linear(const mrl_linear_desc* desc, void* d_workspace, size_t worksp
   if (rc) return rc;
   const ProductPlan plan = plan_product(p);
   if ((rc = check_product(p, plan))) return rc;
-  if ((rc = check_workspace(d_workspace, workspace_bytes, plan.partial_bytes))) return rc;
+  if ((rc = check_workspace(d_workspace, workspace_bytes, plan.bytes()))) return rc;
   const hipStream_t st = (hipStream_t)hip_stream;
-  hipError_t e = launch_product(p, plan, (float*)d_workspace, st);
+  hipError_t e = launch_product(p, plan, d_workspace, st);
   const Product* const products[2] = {&p, nullptr};
   const ProductPlan* const plans[2] = {&plan, nullptr};
-  const float* const partials[2] = {(const float*)d_workspace, nullptr};
+  const float* const partials[2] = {plan.partial(d_workspace), nullptr};
   if (e == hipSuccess && plan.splits > 1) e = launch_rest(products, plans, partials, nullptr, nullptr, st);
   return hip_status(e);
 }
@@ -279,8 +286,8 @@ int32_t mrl_linear_grad(const mrl_linear_grad_desc* desc, void* d_workspace, siz
   if (rc) return rc;
   if ((rc = check_workspace(d_workspace, workspace_bytes, g.bytes()))) return rc;
   float* const sums = (float*)((char*)d_workspace + g.dz_bytes);
-  float* const partial_lhs = (float*)((char*)sums + g.sums_bytes);
-  float* const partial_rhs = (float*)((char*)partial_lhs + g.lhs_bytes);
+  char* const for_lhs = (char*)sums + g.sums_bytes;
+  char* const for_rhs = for_lhs + g.lhs_bytes;
   const hipStream_t st = (hipStream_t)hip_stream;
   if (g.pass) {
     g.rows.dz.data = d_workspace;
@@ -291,11 +298,11 @@ int32_t mrl_linear_grad(const mrl_linear_grad_desc* desc, void* d_workspace, siz
   }
   hipError_t e = hipSuccess;
   if (g.pass || g.rows.dbias) e = launch_grad_rows(g.rows, sums, st);
-  if (e == hipSuccess && g.lhs) e = launch_product(g.by_lhs, g.plan_lhs, partial_lhs, st);
-  if (e == hipSuccess && g.rhs) e = launch_product(g.by_rhs, g.plan_rhs, partial_rhs, st);
+  if (e == hipSuccess && g.lhs) e = launch_product(g.by_lhs, g.plan_lhs, for_lhs, st);
+  if (e == hipSuccess && g.rhs) e = launch_product(g.by_rhs, g.plan_rhs, for_rhs, st);
   const Product* const products[2] = {g.lhs ? &g.by_lhs : nullptr, g.rhs ? &g.by_rhs : nullptr};
   const ProductPlan* const plans[2] = {&g.plan_lhs, &g.plan_rhs};
-  const float* const partials[2] = {partial_lhs, partial_rhs};
+  const float* const partials[2] = {g.plan_lhs.partial(for_lhs), g.plan_rhs.partial(for_rhs)};
   if (e == hipSuccess) e = launch_rest(products, plans, partials, &g.rows, sums, st);
   return hip_status(e);
 }

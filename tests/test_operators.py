@@ -28,20 +28,18 @@ def _torch():
 # ---- 64 bits
 
 def random_bits(rows, cols, seed, offset):
-    """The 16 bits of every element, block by block in Python's integers."""
-    out = np.empty((rows, cols), dtype=np.int64)
-    M = 0xFFFFFFFF
-    for i in range(rows):
-        for j in range(0, cols, 8):
-            c = [j // 8, i, offset & M, offset >> 32]
-            k = [seed & M, seed >> 32]
-            for _ in range(7):
-                p0, p1 = 0xD2511F53 * c[0], 0xCD9E8D57 * c[2]
-                c = [(p1 >> 32) ^ c[1] ^ k[0], p1 & M, (p0 >> 32) ^ c[3] ^ k[1], p0 & M]
-                k = [(k[0] + 0x9E3779B9) & M, (k[1] + 0xBB67AE85) & M]
-            half = [w >> s & 0xFFFF for w in c for s in (0, 16)]
-            out[i, j:j + 8] = half[:min(8, cols - j)]
-    return out
+    """The 16 bits of every element: the block function in 64-bit unsigned integers, for all blocks at once."""
+    U64, M = np.uint64, np.uint64(0xFFFFFFFF)
+    groups = (cols + 7) // 8
+    c = [np.broadcast_to(np.arange(groups, dtype=U64), (rows, groups)), np.broadcast_to(np.arange(rows, dtype=U64)[:, None], (rows, groups)),
+         np.full((rows, groups), offset & 0xFFFFFFFF, dtype=U64), np.full((rows, groups), offset >> 32, dtype=U64)]
+    k = [seed & 0xFFFFFFFF, seed >> 32]
+    for _ in range(7):
+        p0, p1 = U64(0xD2511F53) * c[0], U64(0xCD9E8D57) * c[2]         # (factors below 2^32: the products fit)
+        c = [(p1 >> U64(32)) ^ c[1] ^ U64(k[0]), p1 & M, (p0 >> U64(32)) ^ c[3] ^ U64(k[1]), p0 & M]
+        k = [(k[0] + 0x9E3779B9) & 0xFFFFFFFF, (k[1] + 0xBB67AE85) & 0xFFFFFFFF]
+    halves = np.stack([w >> U64(s) & U64(0xFFFF) for w in c for s in (0, 16)], axis=-1)
+    return halves.reshape(rows, groups * 8)[:, :cols].astype(np.int64)
 
 
 def scale_of(shape, p, seed, offset):
@@ -174,6 +172,17 @@ def test_linear_sizes_of_every_path(dtype, m, k, n, rhs_columns):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lhs_columns,rhs_columns", [(False, False), (False, True), (True, False), (True, True)])
+@pytest.mark.parametrize("b,batched,m,k,n,gap", [(None, False, 1029, 1543, 1031, 0), (None, False, 2057, 263, 3001, 3), (None, False, 1024, 1001, 2048, 0),
+                                                 (None, False, 1001, 1024, 2056, 0), (3, True, 515, 1030, 777, 0), (3, False, 515, 1030, 777, 8),
+                                                 (None, False, 2000, 3, 2000, 0), (None, False, 3, 2000, 2000, 5)])
+def test_large_operands_of_any_alignment(dtype, lhs_columns, rhs_columns, b, batched, m, k, n, gap):
+    """Large products with one operand or both at odd strides or sizes (NaN in the gaps)."""
+    case_linear(b, m, k, n, dtype, batched=batched, lhs_columns=lhs_columns, rhs_columns=rhs_columns, gap=gap, activation="silu", residual=False, pre=False)
+
+
+@gpu
 @pytest.mark.parametrize("m,k,n", [(0, 8, 8), (8, 0, 8), (8, 8, 0), (0, 0, 0)])
 @pytest.mark.parametrize("b", [None, 0, 2])
 def test_sizes_of_zero(b, m, k, n):
@@ -197,7 +206,7 @@ def plain_grad(grad, lhs, rhs, z, act, d):
 @pytest.mark.parametrize("lhs_columns,rhs_columns", [(False, False), (False, True), (True, False), (True, True)])
 @pytest.mark.parametrize("activation,p", [("none", 0.0), ("none", 0.4), ("relu", 0.0), ("gelu", 0.25), ("silu", 0.0)])
 @pytest.mark.parametrize("b,batched,m,k,n,gap", [(None, False, 1, 64, 40, 0), (None, False, 70, 33, 90, 1), (None, False, 130, 136, 264, 8), (3, False, 33, 40, 24, 0),
-                                                 (3, False, 33, 40, 24, 8), (3, True, 33, 40, 24, 0), (2, True, 65, 17, 9, 3)])
+                                                 (3, False, 33, 40, 24, 8), (3, True, 33, 40, 24, 0), (2, True, 65, 17, 9, 3), (None, False, 131, 1027, 1501, 0)])
 def test_gradients_of_the_formula(dtype, lhs_columns, rhs_columns, activation, p, b, batched, m, k, n, gap):
     torch, _ = _torch()
     rng = np.random.default_rng(11)
