@@ -210,14 +210,13 @@ __device__ __forceinline__ void put8(const Product& p, const Place& at, uint32_t
 }
 
 // A wave's results: a lane has row row_of(i, q) and, of the pair of blocks 2 j, 2 j + 1, the eight columns from 32 j + 8 g on.  They go
-// through shared memory that is the wave's own, four blocks of rows at a time at most, so that a row's results are
-// stored side by side (lines of 128 bytes and more) and the epilogue is a short loop: unrolled over the registers it is as long as
-// the instruction cache.  The 16-byte chunks of a row lie at their number xor the row's, against bank conflicts.
-template <class T, int BM, int BN>
+// through shared memory that is the wave's own, PASS blocks of 16 rows at a time, so that a row's results are stored side by side (lines of
+// 128 bytes and more) and the epilogue is a short loop: unrolled over the registers it is as long as the instruction cache.  The 16-byte chunks of a
+// row lie at their number xor the row's, against bank conflicts.
+template <class T, int PASS, int BM, int BN>
 __device__ __forceinline__ void write_out(const Product& p, const Place& at, uint32_t splits, uint32_t m0, uint32_t n0, uint32_t lane,
                                           const f32x4 (&acc)[BM][BN], char* mine, float* __restrict__ partial) {
   constexpr uint32_t CHUNKS = BN * 4, GROUPS = BN * 2, ROWS = 64 / GROUPS;      // chunks and groups of 8 columns of a row; rows at a time
-  constexpr int PASS = BM > 4 ? BM / 2 : BM;                                    // blocks of rows that go through at once
   const uint32_t q = lane & 15, g = lane >> 4;
   const uint32_t c = lane % GROUPS, n = n0 + c * 8;
   float bias[8];
@@ -226,20 +225,19 @@ __device__ __forceinline__ void write_out(const Product& p, const Place& at, uin
   for (int h = 0; h < BM; h += PASS) {
 #pragma unroll
     for (int i = 0; i < PASS; i++) {
-      const uint32_t r = row_of<T, false>(i, q);
+      const uint32_t r = 16 * i + q;
 #pragma unroll
       for (int j = 0; j < BN / 2; j++)
 #pragma unroll
-        for (int x = 0; x < 2; x++) {
+        for (int x = 0; x < 2; x++)
           *(f32x4*)(mine + (r * CHUNKS + ((8 * j + 2 * g + x) ^ (r & (CHUNKS - 1)))) * 16) = chunk_of<T>(acc[h + i][2 * j], acc[h + i][2 * j + 1], x);
-        }
     }
     asm volatile("" ::: "memory");         // (a wave's accesses to shared memory are done in their order)
     if (n < p.N) {
 #pragma unroll 2
       for (uint32_t r = lane / GROUPS; r < 16 * PASS; r += ROWS) {
-        const uint32_t m = m0 + h * 16 + r;
-        if (m >= p.M) break;
+        const uint32_t m = m0 + row_of<T, false>(h + (r >> 4), r & 15);
+        if (m >= p.M) continue;
         float v[8];
 #pragma unroll
         for (int x = 0; x < 2; x++) {
@@ -312,7 +310,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void product_kernel(const P
     if (step + 1 < end) store(lds[cur ^ 1]);
     __syncthreads();
   }
-  write_out<T, BM, BN>(p, at, splits, m0 + wm, n0 + wn, lane, acc, &lds[0][0] + wave * (WM * WN * 4), partial);
+  write_out<T, BM, BM, BN>(p, at, splits, m0 + wm, n0 + wn, lane, acc, &lds[0][0] + wave * (WM * WN * 4), partial);
 }
 
 // ---- operands whose lines start at multiples of 16 bytes
@@ -327,7 +325,7 @@ __device__ __forceinline__ void arrive() { asm volatile("s_waitcnt vmcnt(%0) lgk
 // (The load is written out because the compiler, which cannot tell the stages apart, would wait for every load under way before any
 // read of shared memory.  It has no output register; its address registers are read as it is issued.)
 __device__ __forceinline__ void load_to_lds(uint32_t lds, uint32_t offset, u32x4 buffer) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(offset), "s"(buffer) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(buffer) : "memory");
 }
 
 constexpr uint32_t kOutside = 0x80000000u;        // beyond any buffer's range
@@ -351,23 +349,26 @@ struct Feed {
     return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)base), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(base >> 32) & 0xFFFFu),
                  (uint32_t)__builtin_amdgcn_readfirstlane(range), 0x27000u};
   }
-  // The thread's i-th load of a step; ks: k that are left in the segment.
+  // The thread's i-th load of a step; ks: k that are left in the segment; lds: where the wave's first load goes.
   __device__ __forceinline__ void load(int i, const u32x4& buffer, uint32_t ks, uint32_t lds, uint32_t t) const {
     uint32_t at = offset[i];
     if (KC && ks < Tl::kSteps) {                  // chunks past the end of the sum would be the next line's
       const uint32_t c = t + i * THREADS, line = c / Tl::kChunks, chunk = c % Tl::kChunks ^ Tl::swizzle(line);
       if (chunk * Tl::E >= ks) at = kOutside;
     }
-    load_to_lds(lds + (t & ~63u) * 16 + i * THREADS * 16, at, buffer);
+    load_to_lds(lds + i * THREADS * 16, at, buffer);
   }
 };
 
+// One tile of TM x TN, WAVES_M x WAVES_N waves, STAGES steps in shared memory.
 template <class T, bool AKC, bool BKC, int TM, int TN, int WAVES_M, int WAVES_N, int STAGES>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void fast_kernel(const Product p, uint32_t steps, uint32_t per_split, uint32_t splits,
                                                                       uint32_t first, float* __restrict__ partial) {
   constexpr int THREADS = 64 * WAVES_M * WAVES_N, WM = TM / WAVES_M, WN = TN / WAVES_N, BM = WM / 16, BN = WN / 16;
-  constexpr uint32_t KS = kStep / sizeof(T), STAGE = (TM + TN) * kStep;
+  constexpr int PASS = BM > 4 ? BM / 2 : BM;
+  constexpr uint32_t KS = kStep / sizeof(T), STAGE = (TM + TN) * kStep, OUT = 16 * PASS * WN * 4;
   __shared__ __attribute__((aligned(1024))) char lds[STAGES * STAGE];
+  static_assert(WAVES_M * WAVES_N * OUT <= sizeof lds, "the results go where the stages were");
 
   const Place at = place(first, (p.M + TM - 1) / TM, (p.N + TN - 1) / TN, splits);
   const uint32_t m0 = at.tm * TM, n0 = at.tn * TN;
@@ -380,45 +381,45 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void fast_kernel(const P
   fa.init(p.lda, t);
   fb.init(p.ldb, t);
   constexpr int LOADS = decltype(fa)::N + decltype(fb)::N;
-
   const uint32_t seg_steps = (p.K + KS - 1) / KS;
-  const uint32_t begin = at.split * per_split, end = min(begin + per_split, steps);
-  // the next step to load: where it starts in either operand, and what is left behind that
   const int64_t step_a = (AKC ? (int64_t)KS : KS * p.lda) * sizeof(T), step_b = (BKC ? (int64_t)KS : KS * p.ldb) * sizeof(T);
-  uint32_t seg = begin < end ? begin / seg_steps : 0, k = (begin - seg * seg_steps) * KS;
-  const char *a0 = (const char*)((const T*)p.a + (int64_t)at.batch * p.batch_a + (AKC ? (int64_t)m0 * p.lda : (int64_t)m0));
-  const char *b0 = (const char*)((const T*)p.b + (int64_t)at.batch * p.batch_b + (BKC ? (int64_t)n0 * p.ldb : (int64_t)n0));
-  const int64_t size_a = (AKC ? ((int64_t)(p.M - m0) - 1) * p.lda + p.wa : ((int64_t)p.K - 1) * p.lda + (p.wa - m0)) * (int64_t)sizeof(T);
-  const int64_t size_b = (BKC ? ((int64_t)(p.N - n0) - 1) * p.ldb + p.wb : ((int64_t)p.K - 1) * p.ldb + (p.wb - n0)) * (int64_t)sizeof(T);
-  int64_t off_a = (int64_t)(k / KS) * step_a, off_b = (int64_t)(k / KS) * step_b;
-  const char *sa = a0 + (int64_t)seg * p.seg_a * (int64_t)sizeof(T), *sb = b0 + (int64_t)seg * p.seg_b * (int64_t)sizeof(T);
-  const uint32_t n = end > begin ? end - begin : 0;
-  uint32_t loaded = 0;
+
+  const uint32_t from = at.split * per_split, end = min(from + per_split, steps), n = end > from ? end - from : 0;
+
+  // the next step to load: where it starts in either operand, the bytes that are left behind that, the k
+  const uint32_t seg = n ? from / seg_steps : 0, step0 = from - seg * seg_steps;
+  uint32_t k = step0 * KS, loaded = 0;
+  const char* sa = (const char*)((const T*)p.a + (int64_t)at.batch * p.batch_a + (int64_t)seg * p.seg_a + (AKC ? (int64_t)m0 * p.lda : (int64_t)m0)) + step0 * step_a;
+  const char* sb = (const char*)((const T*)p.b + (int64_t)at.batch * p.batch_b + (int64_t)seg * p.seg_b + (BKC ? (int64_t)n0 * p.ldb : (int64_t)n0)) + step0 * step_b;
+  int64_t left_a = (AKC ? ((int64_t)(p.M - m0) - 1) * p.lda + p.wa : ((int64_t)p.K - 1) * p.lda + (p.wa - m0)) * (int64_t)sizeof(T) - step0 * step_a;
+  int64_t left_b = (BKC ? ((int64_t)(p.N - n0) - 1) * p.ldb + p.wb : ((int64_t)p.K - 1) * p.ldb + (p.wb - n0)) * (int64_t)sizeof(T) - step0 * step_b;
   // (behind the last step the buffers have no bytes: zeros are written that nothing uses, and every step has the same loads under way)
   u32x4 buf_a, buf_b;
   uint32_t to, ks;
   const auto aim = [&](uint32_t stage) {          // at the next step, to be put into `stage`
     const bool more = loaded++ < n;
-    to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr)lds + stage * STAGE);
+    to = (uint32_t)(uintptr_t)(lds_ptr)lds + stage * STAGE + wave * 1024;
     ks = p.K - k;
-    buf_a = fa.buffer(sa + off_a, more ? size_a - off_a : 0);
-    buf_b = fb.buffer(sb + off_b, more ? size_b - off_b : 0);
+    buf_a = fa.buffer(sa, more ? left_a : 0);
+    buf_b = fb.buffer(sb, more ? left_b : 0);
     if (!more) return;
     k += KS;
-    off_a += step_a;
-    off_b += step_b;
-    if (k >= p.K) {
+    sa += step_a;
+    sb += step_b;
+    left_a -= step_a;
+    left_b -= step_b;
+    if (k >= p.K) {                               // the next segment
       k = 0;
-      off_a = off_b = 0;
-      sa += p.seg_a * (int64_t)sizeof(T);
-      sb += p.seg_b * (int64_t)sizeof(T);
+      sa += p.seg_a * (int64_t)sizeof(T) - seg_steps * step_a;
+      sb += p.seg_b * (int64_t)sizeof(T) - seg_steps * step_b;
+      left_a += seg_steps * step_a;
+      left_b += seg_steps * step_b;
     }
   };
   const auto load = [&](int i) {
-    if (i < fa.N) fa.load(i, buf_a, ks, to, wave * 64 + lane);
-    else fb.load(i - fa.N, buf_b, ks, to + TM * kStep, wave * 64 + lane);
+    if (i < fa.N) fa.load(i, buf_a, ks, to, t);
+    else fb.load(i - fa.N, buf_b, ks, to + TM * kStep, t);
   };
-
   f32x4 acc[BM][BN];
 #pragma unroll
   for (int i = 0; i < BM; i++)
@@ -456,9 +457,9 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void fast_kernel(const P
 #pragma unroll
           for (int i = 0; i < (SPREAD ? 0 : LOADS); i++) load(i);
         }
-        const lds_ptr tile = (lds_ptr)lds + (ph == PHASES - 1 ? next : cur) * STAGE;
-        read_blocks<T, AKC, false, TM>(tile, wm, m, kk, q, g, oa[then & 1]);
-        if (m == 0) read_blocks<T, BKC, true, TN>(tile + TM * kStep, wn, 0, kk, q, g, ob[kk]);
+        const lds_ptr stage = (lds_ptr)lds + (ph == PHASES - 1 ? next : cur) * STAGE;
+        read_blocks<T, AKC, false, TM>(stage, wm, m, kk, q, g, oa[then & 1]);
+        if (m == 0) read_blocks<T, BKC, true, TN>(stage + TM * kStep, wn, 0, kk, q, g, ob[kk]);
 #pragma unroll
         for (int part = 0; part < PARTS; part++) {
           multiply(oa[ph & 1], ob[ph / (PHASES / 2)], ph % (PHASES / 2) * NM, part, acc);
@@ -472,9 +473,9 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void fast_kernel(const P
       }
       cur = next;
     }
-    arrive<0>();                  // nothing is under way to shared memory when the workgroup gives it up
+    arrive<0>();                  // nothing is under way to shared memory when it is given up
   }
-  write_out<T, BM, BN>(p, at, splits, m0 + wm, n0 + wn, lane, acc, lds + wave * (sizeof lds / (WAVES_M * WAVES_N)), partial);
+  write_out<T, PASS, BM, BN>(p, at, splits, m0 + wm, n0 + wn, lane, acc, lds + wave * OUT, partial);
 }
 
 // The sums of a workgroup's waves over one tile of few rows and 64 columns, added in their order: each wave's in shared memory of its own, `each`
@@ -783,8 +784,8 @@ hipError_t launch_tiles(const Product& p, const ProductPlan& plan, float* partia
       case kFast256x128: return go(fast_kernel<T, AKC, BKC, 256, 128, 4, 2, 3>, 512);
       case kFast128: return go(fast_kernel<T, AKC, BKC, 128, 128, 2, 4, 2>, 512);
       case kFast128Alone: return go(fast_kernel<T, AKC, BKC, 128, 128, 2, 4, 4>, 512);
-      case kRows: return go(rows_kernel<T, AKC, BKC, 4, 3>, 256);
       case kFast64: return go(fast_kernel<T, AKC, BKC, 64, 64, 2, 2, 4>, 256);
+      case kRows: return go(rows_kernel<T, AKC, BKC, 4, 3>, 256);
       case kRowsWide: return go(rows_wide_kernel<T, AKC, BKC, 8>, 512);
       case kWide128: return go(product_kernel<T, AKC, BKC, 128, 128, 2, 2, true>, 256);
       case kWide64: return go(product_kernel<T, AKC, BKC, 64, 64, 2, 2, true>, 256);
