@@ -23,13 +23,14 @@ HBM_PEAK_GBS = 8000.0          # MI355X published HBM3E peak
 
 
 def source_hash():
-    """Hash of the kernel sources: a committed counter summary names the sources it was taken
-    with, so that a stale one is not passed off as this build's traffic."""
+    """Hash of the solver's sources: a committed counter summary names the sources it was taken
+    with, so that a stale one is not passed off as this build's traffic.  (The operators that Specs
+    name are no part of a solve.)"""
     import hashlib
     h = hashlib.sha256()
     d = os.path.join(ROOT, "paper_2505_01637_amd", "csrc")
     for name in sorted(os.listdir(d)):
-        if name.endswith((".hip", ".h")):
+        if name.endswith((".hip", ".h")) and name not in ("operators.h", "operators.hip", "linear.hip"):
             with open(os.path.join(d, name), "rb") as f:
                 h.update(name.encode() + b"\0" + f.read())
     return h.hexdigest()[:16]

@@ -21,7 +21,7 @@ constexpr uint32_t kLaunch = 1u << 22;     // workgroups of a launch
 template <class T, bool KC, bool IS_B, int W>
 struct Tile {
   static constexpr int E = 16 / sizeof(T);                           // elements of a chunk
-  static constexpr int kSteps = kStep / sizeof(T);                      // k of a step
+  static constexpr int kSteps = kStep / sizeof(T);                          // k of a step
   static constexpr int kLineBytes = KC ? kStep : W * (int)sizeof(T);
   static constexpr int kChunks = kLineBytes / 16;                    // of a line
   __device__ static __forceinline__ uint32_t swizzle(uint32_t line) {
@@ -361,6 +361,11 @@ struct Feed {
 };
 
 // One tile of TM x TN, WAVES_M x WAVES_N waves, STAGES steps in shared memory.
+//
+// A wave of the 256 tile has 128 x 64 of it: 24 KB read from shared memory for 64 MFMA of a step, 192 KB and 64 KB written by all eight
+// waves in 2048 cycles of products.  8192-cube in bf16 805 us, 1360 TFLOP/s: 577 us without loads and reads of shared memory, 650 without the loads, 770
+// without the reads, 755 with every step's operands in L2; so what bounds it is the way of the operands to shared memory, then their
+// reads.  2048-cube in f32 (128 x 128, eight waves) 133 us, of which the products take 117 at the clock it runs at.
 template <class T, bool AKC, bool BKC, int TM, int TN, int WAVES_M, int WAVES_N, int STAGES>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void fast_kernel(const Product p, uint32_t steps, uint32_t per_split, uint32_t splits,
                                                                       uint32_t first, float* __restrict__ partial) {
@@ -851,15 +856,20 @@ Copy copy_b(const Product& p) { return copy_of(p.b, p.b_kc, p.ldb, p.batch_b, p.
 
 // How long a kernel takes, in us: a round of workgroups on the 256 compute units, one each or two at once, is `fixed` and a
 // step's time for each step along k.  Measured on products whose tiles are one whole round, 2048 and 8192 long along k:
-//                      step bf16 (one, two)   step f32 (one, two)
-//   256 x 256               1.52     -          7.33     -
-//   256 x 128               0.87     -          3.81     -
-//   128 x 128, 4 stages     0.50     -          1.99     -        (2 stages alone: 0.56; four fill the shared memory)
-//   128 x 128, 2 stages       -     0.93          -     3.78
-//   64 x 64                 0.25    0.37        0.62    1.07
+//                           step bf16 (one, two)   step f32 (one, two)
+//   256 x 256                    1.52     -          7.33     -
+//   256 x 128                    0.87     -          3.81     -
+//   128 x 128, 4 stages          0.50     -          1.99     -        (2 stages alone: 0.56; four fill the shared memory)
+//   128 x 128, 2 stages            -     0.93          -     3.78
+//   64 x 64                      0.25    0.37        0.62    1.07
+//   few rows                     0.12    0.24        0.27    0.54
+//   few rows, any alignment      0.11    0.42        0.20    0.70
+//   128 x 128, any alignment     1.25    1.70        2.50    4.80
+//   64 x 64, any alignment       0.80    0.86        0.72    1.15
 // So a large tile does more per time (16 units of 64 x 64 in 1.52 against 1 in 0.25) and a small one leaves fewer compute units
-// without work; where the tiles are few, workgroups share a tile's sum and a second launch adds up: its time, and the partial sums
-// written and read at 4.5 TB/s.
+// without work.  Where the tiles are few, workgroups share a tile's sum and a second launch adds up: its time, and the partial sums
+// written and read at 4.5 TB/s (bf16: 1 x 16384 x 2048 17 us split and 31 whole, 4096 x 16384 x 1024 131 and 165).  Operands that are
+// not aligned may be copied first, at the same rates (bf16: 4750 x 2297 x 4096 121 us copied and 158 through registers, 7 x 2047 x 1001 15 and 11).
 struct Kernel { uint32_t id, tm, tn; Access access; float fixed, one[2], two[2]; };
 constexpr Kernel kKernels[] = {
     {kFast256, 256, 256, kAligned, 11, {1.52f, 7.33f}, {0, 0}},
@@ -872,7 +882,7 @@ constexpr Kernel kKernels[] = {
     {kWide64, 64, 64, kWide, 2, {0.80f, 0.72f}, {0.86f, 1.15f}},
     {kAny64, 64, 64, kAny, 2, {2.0f, 2.0f}, {3.0f, 3.0f}},
 };
-constexpr float kLaunch1 = 5, kBytes = 4.5e6f;                     // a further launch, us; bytes a us
+constexpr float kLaunch1 = 6, kBytes = 4.5e6f;                     // a further launch, us; bytes a us
 
 ProductPlan plan_product(const Product& p) {
   ProductPlan plan{};

@@ -27,11 +27,11 @@ def _torch():
 
 # ---- 64 bits
 
-def random_bits(rows, cols, seed, offset):
+def random_bits(rows, cols, seed, offset, first_row=0):
     """The 16 bits of every element: the block function in 64-bit unsigned integers, for all blocks at once."""
     U64, M = np.uint64, np.uint64(0xFFFFFFFF)
     groups = (cols + 7) // 8
-    c = [np.broadcast_to(np.arange(groups, dtype=U64), (rows, groups)), np.broadcast_to(np.arange(rows, dtype=U64)[:, None], (rows, groups)),
+    c = [np.broadcast_to(np.arange(groups, dtype=U64), (rows, groups)), np.broadcast_to(np.arange(first_row, first_row + rows, dtype=U64)[:, None], (rows, groups)),
          np.full((rows, groups), offset & 0xFFFFFFFF, dtype=U64), np.full((rows, groups), offset >> 32, dtype=U64)]
     k = [seed & 0xFFFFFFFF, seed >> 32]
     for _ in range(7):
