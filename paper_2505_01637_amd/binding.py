@@ -603,23 +603,56 @@ def _elsewhere(tensors, stream):
     return _On(index, tensors, stream)
 
 
-def _queue(desc, size_of, run, given, like):
-    """Ask for the workspace, then queue the call on the current stream; a workspace of torch's may be freed when this
-    returns (work on its stream that uses the memory next comes after the call's)."""
-    n = C.c_size_t()
-    rc = size_of(desc, C.addressof(n))
-    if rc == 0:
-        stream = _raw_stream(like.get_device())
-        if n.value == 0:
-            rc = run(desc, None, 0, stream)
-        else:
-            if given is None:
-                given = like.new_empty(n.value, dtype=_uint8)
-            elif not given.is_contiguous():
-                raise MorelloError(E_INVAL, "the workspace is not contiguous")
-            rc = run(desc, given.data_ptr(), given.numel() * given.element_size(), stream)
+def _run(desc, run, need, given, like):
+    """Queue a call on the current stream; a workspace of torch's may be freed when this returns (work on its stream
+    that uses the memory next comes after the call's)."""
+    stream = _raw_stream(like.get_device())
+    if need == 0:
+        rc = run(desc, None, 0, stream)
+    else:
+        if given is None:
+            given = like.new_empty(need, dtype=_uint8)
+        elif not given.is_contiguous():
+            raise MorelloError(E_INVAL, "the workspace is not contiguous")
+        rc = run(desc, given.data_ptr(), given.numel() * given.element_size(), stream)
     if rc:
         _check(rc)
+
+
+def _queue(desc, size_of, run, given, like):
+    """The same after asking for the workspace."""
+    n = C.c_size_t()
+    rc = size_of(desc, C.addressof(n))
+    if rc:
+        _check(rc)
+    _run(desc, run, n.value, given, like)
+
+
+# What a call of linear with these sizes, strides, types and alignments comes to (no addresses, no values), worked out once: that takes
+# 3 us of a call's 10.  As many as a program with many layers has.
+_FORMS_MOST = 1024
+_WORD_END = 1 << 64
+_forms = {}
+
+
+def _form_linear(key, lhs, rhs, bias, residual, out, dtype, pre, activation, dropout):
+    sizes, ml, mr, shape = _operands(lhs, rhs)
+    made = out is None
+    if made:
+        out = lhs.new_empty(shape, dtype=lhs.dtype if dtype is None else dtype)
+    elif dtype is not None and out.dtype != dtype:
+        raise MorelloError(E_INVAL, "out is %s, not %s" % (out.dtype, dtype))
+    z = out.new_empty(shape) if pre else None
+    mats = [ml, mr, _ABSENT if bias is None else _vector("bias", bias, sizes[3]), _ABSENT if residual is None else _rows("residual", residual, shape),
+            _rows("out", out, shape), _ABSENT if z is None else _rows("pre", z, shape)]
+    act, drop = _activation(activation), drop_threshold(dropout)
+    n = C.c_size_t()
+    _check(lib().mrl_linear_bytes(_LINEAR.pack(*sizes, *(v for m in mats for v in m), act, drop, 0, 0), C.addressof(n)))
+    form = (shape, out.dtype, sizes, *(m[1:] for m in mats), act, drop, n.value)
+    if len(_forms) >= _FORMS_MOST:
+        _forms.clear()
+    _forms[key] = form
+    return form
 
 
 def _operands(lhs, rhs):
@@ -650,17 +683,23 @@ def linear(lhs, rhs, bias=None, residual=None, *, activation="none", dropout=0.0
         with on:
             return linear(lhs, rhs, bias, residual, activation=activation, dropout=dropout, seed=seed, offset=offset, dtype=dtype, pre=pre,
                           out=out, workspace=workspace)
-    sizes, ml, mr, shape = _operands(lhs, rhs)
+    pl, pr = lhs.data_ptr(), rhs.data_ptr()
+    key = (lhs.shape, lhs.stride(), lhs.dtype, rhs.shape, rhs.stride(), rhs.dtype, (pl | pr) & 15,
+           None if bias is None else (bias.shape, bias.stride(), bias.dtype),
+           None if residual is None else (residual.shape, residual.stride(), residual.dtype),
+           None if out is None else (out.shape, out.stride(), out.dtype), dtype, pre, activation, dropout)
+    form = _forms.get(key)
+    if form is None:
+        form = _form_linear(key, lhs, rhs, bias, residual, out, dtype, pre, activation, dropout)
+    shape, dtype, sizes, ml, mr, mb, ms, mo, mz, act, drop, need = form
     if out is None:
-        out = lhs.new_empty(shape) if dtype is None or dtype == lhs.dtype else lhs.new_empty(shape, dtype=dtype)
-    elif dtype is not None and out.dtype != dtype:
-        raise MorelloError(E_INVAL, "out is %s, not %s" % (out.dtype, dtype))
+        out = lhs.new_empty(shape, dtype=dtype)
     z = out.new_empty(shape) if pre else None
-    desc = _LINEAR.pack(*sizes, *ml, *mr, *(_ABSENT if bias is None else _vector("bias", bias, sizes[3])),
-                        *(_ABSENT if residual is None else _rows("residual", residual, shape)), *_rows("out", out, shape),
-                        *(_ABSENT if z is None else _rows("pre", z, shape)),
-                        _activation(activation), drop_threshold(dropout), _word("seed", seed), _word("offset", offset))
-    _queue(desc, lib().mrl_linear_bytes, lib().mrl_linear, workspace, lhs)
+    if not (0 <= seed < _WORD_END and 0 <= offset < _WORD_END):
+        raise MorelloError(E_INVAL, "seed %r or offset %r does not fit 64 bits" % (seed, offset))
+    desc = _LINEAR.pack(*sizes, pl, *ml, pr, *mr, 0 if bias is None else bias.data_ptr(), *mb, 0 if residual is None else residual.data_ptr(), *ms,
+                        out.data_ptr(), *mo, z.data_ptr() if pre else 0, *mz, act, drop, seed, offset)
+    _run(desc, _lib.mrl_linear, need, workspace, lhs)
     return (out, z) if pre else out
 
 
