@@ -131,26 +131,41 @@ struct Stage {
   static constexpr int N = W * 8 / THREADS, E = Tl::E;
   u32x4 r[N];
   uint32_t ks;                     // k that are left where r was read
+  int64_t offset[N];               // bytes from a whole step's first element (worked out once: a 64-bit product per load and step costs more than the load)
   __device__ static __forceinline__ uint32_t line(int i, uint32_t t) { return (t + i * THREADS) / Tl::kChunks; }
   __device__ static __forceinline__ int32_t at(int i, uint32_t t) { return (t + i * THREADS) % Tl::kChunks * E; }
+  __device__ static __forceinline__ int64_t place(int i, uint32_t t, int64_t ld, uint32_t rows, uint32_t left) {
+    const uint32_t lines = KC ? rows : left, width = KC ? left : rows;
+    return ((int64_t)min(line(i, t), lines - 1) * ld + min(at(i, t), (int32_t)min(width, 1u << 30) - E)) * (int64_t)sizeof(T);
+  }
+  __device__ __forceinline__ void init(int64_t ld, uint32_t rows, uint32_t t) {
+    if constexpr (WIDE)
+#pragma unroll
+      for (int i = 0; i < N; i++) offset[i] = place(i, t, ld, rows, Tl::kSteps);
+  }
 
   // src: the tile's first row (column) at k = k0; rows and left: how many rows (columns) and k there are from there on
   __device__ __forceinline__ void load(const T* src, int64_t ld, uint32_t rows, uint32_t left, uint32_t t) {
     ks = left;
+    if constexpr (WIDE) {
+      if (left >= (uint32_t)Tl::kSteps) {
+#pragma unroll
+        for (int i = 0; i < N; i++) __builtin_memcpy(&r[i], (const char*)src + offset[i], 16);
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; i++) __builtin_memcpy(&r[i], (const char*)src + place(i, t, ld, rows, left), 16);
+      }
+      return;
+    }
     const uint32_t lines = KC ? rows : left, width = KC ? left : rows;
 #pragma unroll
     for (int i = 0; i < N; i++) {
       const uint32_t l = line(i, t);
-      if constexpr (WIDE) {
-        const int32_t from = min(at(i, t), (int32_t)min(width, 1u << 30) - E);
-        __builtin_memcpy(&r[i], src + (int64_t)min(l, lines - 1) * ld + from, 16);
-      } else {
-        const T* p = src + (int64_t)l * ld;
-        T v[E];
+      const T* p = src + (int64_t)l * ld;
+      T v[E];
 #pragma unroll
-        for (int e = 0; e < E; e++) v[e] = l < lines && (uint32_t)at(i, t) + e < width ? p[at(i, t) + e] : (T)0.0f;
-        __builtin_memcpy(&r[i], v, 16);
-      }
+      for (int e = 0; e < E; e++) v[e] = l < lines && (uint32_t)at(i, t) + e < width ? p[at(i, t) + e] : (T)0.0f;
+      __builtin_memcpy(&r[i], v, 16);
     }
   }
   __device__ __forceinline__ void store(char* tile, uint32_t rows, uint32_t t) {
@@ -273,6 +288,8 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N) void product_kernel(const P
   const T* b = (const T*)p.b + (int64_t)at.batch * p.batch_b + (BKC ? (int64_t)n0 * p.ldb : (int64_t)n0);
   Stage<T, AKC, false, TM, THREADS, WIDE> sa;
   Stage<T, BKC, true, TN, THREADS, WIDE> sb;
+  sa.init(p.lda, p.M - m0, t);
+  sb.init(p.ldb, p.N - n0, t);
   const auto load = [&] {
     sa.load(a + (int64_t)seg * p.seg_a + (AKC ? (int64_t)k : (int64_t)k * p.lda), p.lda, p.M - m0, p.K - k, t);
     sb.load(b + (int64_t)seg * p.seg_b + (BKC ? (int64_t)k : (int64_t)k * p.ldb), p.ldb, p.N - n0, p.K - k, t);
@@ -485,9 +502,11 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void fast_kernel(const P
 
 // The sums of a workgroup's waves over one tile of few rows and 64 columns, added in their order: each wave's in shared memory of its own, `each`
 // bytes apart, rows of 64 with the 16-byte chunks of a row at their number xor the row's.
+// bias: of the eight columns that the thread stores, asked for before the sums are made.
 template <class T, int WAVES, int BM>
-__device__ __forceinline__ void add_waves(const Product& p, const Place& at, uint32_t splits, uint32_t m0, uint32_t n0, uint32_t t, const f32x4 (&acc)[BM][4],
-                                          char* lds, uint32_t each, float* __restrict__ partial) {
+__device__ __forceinline__ void add_waves(const Product& p, const Place& at, uint32_t splits, uint32_t m0, uint32_t n0, uint32_t t, const float (&bias)[8],
+                                          const f32x4 (&acc)[BM][4], char* lds, uint32_t each, float* __restrict__ partial) {
+  static_assert(BM * 16 * 8 <= 64 * WAVES, "eight columns a thread");
   const uint32_t q = t & 15, g = t >> 4 & 3;
   char* const mine = lds + (t >> 6) * each;
 #pragma unroll
@@ -499,21 +518,18 @@ __device__ __forceinline__ void add_waves(const Product& p, const Place& at, uin
       for (int x = 0; x < 2; x++) *(f32x4*)(mine + (r * 16 + ((8 * j + 2 * g + x) ^ (r & 15))) * 16) = chunk_of<T>(acc[i][2 * j], acc[i][2 * j + 1], x);
   }
   __syncthreads();
-  for (uint32_t id = t; id < BM * 16 * 8; id += 64 * WAVES) {
-    const uint32_t r = id / 8, c = id % 8, m = m0 + r, col = n0 + c * 8;
-    if (m >= p.M || col >= p.N) continue;
-    float bias[8], v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-    bias8(p.e, col, p.N - col, bias);
+  const uint32_t r = t / 8, c = t % 8, m = m0 + r, col = n0 + c * 8;
+  if (r >= BM * 16 || m >= p.M || col >= p.N) return;
+  float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int w = 0; w < WAVES; w++)
+  for (int w = 0; w < WAVES; w++)
 #pragma unroll
-      for (int x = 0; x < 2; x++) {
-        const f32x4 y = *(const f32x4*)(lds + w * each + (r * 16 + ((2 * c + x) ^ (r & 15))) * 16);
+    for (int x = 0; x < 2; x++) {
+      const f32x4 y = *(const f32x4*)(lds + w * each + (r * 16 + ((2 * c + x) ^ (r & 15))) * 16);
 #pragma unroll
-        for (int e = 0; e < 4; e++) v[4 * x + e] += y[e];
-      }
-    put8(p, at, splits, m, col, bias, v, partial);
-  }
+      for (int e = 0; e < 4; e++) v[4 * x + e] += y[e];
+    }
+  put8(p, at, splits, m, col, bias, v, partial);
 }
 
 // Few rows: the sum is split among the waves of a workgroup, each with a ring of STAGES steps of its own in shared memory and no barrier
@@ -531,6 +547,8 @@ __global__ __launch_bounds__(64 * WAVES) void rows_kernel(const Product p, uint3
   const uint32_t t = threadIdx.x, lane = t & 63, q = lane & 15, g = lane >> 4;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(t >> 6);
 
+  float bias[8];
+  bias8(p.e, n0 + t % 8 * 8, n0 + t % 8 * 8 < p.N ? p.N - (n0 + t % 8 * 8) : 0, bias);
   Feed<T, AKC, false, TM, 64> fa;
   Feed<T, BKC, true, TN, 64> fb;
   fa.init(p.lda, lane);
@@ -590,7 +608,7 @@ __global__ __launch_bounds__(64 * WAVES) void rows_kernel(const Product p, uint3
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   }
 
-  add_waves<T, WAVES>(p, at, splits, m0, n0, t, acc, &lds[0][0], sizeof lds[0], partial);
+  add_waves<T, WAVES>(p, at, splits, m0, n0, t, bias, acc, &lds[0][0], sizeof lds[0], partial);
 }
 
 // The same for operands of any alignment: through registers, the next step's loads under way while this one is multiplied.
@@ -610,8 +628,12 @@ __global__ __launch_bounds__(64 * WAVES) void rows_wide_kernel(const Product p, 
   const uint32_t begin = at.split * per_split, end = min(begin + per_split, steps);
   const T* a = (const T*)p.a + (int64_t)at.batch * p.batch_a + (AKC ? (int64_t)m0 * p.lda : (int64_t)m0);
   const T* b = (const T*)p.b + (int64_t)at.batch * p.batch_b + (BKC ? (int64_t)n0 * p.ldb : (int64_t)n0);
+  float bias[8];
+  bias8(p.e, n0 + t % 8 * 8, n0 + t % 8 * 8 < p.N ? p.N - (n0 + t % 8 * 8) : 0, bias);
   Stage<T, AKC, false, TM, 64, true> sa;
   Stage<T, BKC, true, TN, 64, true> sb;
+  sa.init(p.lda, p.M - m0, lane);
+  sb.init(p.ldb, p.N - n0, lane);
   const auto load = [&](uint32_t step) {
     const uint32_t seg = step / seg_steps, k = (step - seg * seg_steps) * KS;
     sa.load(a + (int64_t)seg * p.seg_a + (AKC ? (int64_t)k : (int64_t)k * p.lda), p.lda, p.M - m0, p.K - k, lane);
@@ -642,7 +664,7 @@ __global__ __launch_bounds__(64 * WAVES) void rows_wide_kernel(const Product p, 
     }
   }
   asm volatile("" ::: "memory");
-  add_waves<T, WAVES>(p, at, splits, m0, n0, t, acc, &lds[0][0], sizeof lds[0], partial);
+  add_waves<T, WAVES>(p, at, splits, m0, n0, t, bias, acc, &lds[0][0], sizeof lds[0], partial);
 }
 
 // What is left to do when a call's products and rows are through, in one launch: the sums over splits of up to two products with their
