@@ -619,26 +619,49 @@ def _run(desc, run, need, given, like):
         _check(rc)
 
 
-def _queue(desc, size_of, run, given, like):
-    """The same after asking for the workspace."""
-    n = C.c_size_t()
-    rc = size_of(desc, C.addressof(n))
-    if rc:
-        _check(rc)
-    _run(desc, run, n.value, given, like)
-
-
-# What a call of linear with these sizes, strides, types and alignments comes to (no addresses, no values), worked out once: that takes
-# 3 us of a call's 10.  As many as a program with many layers has.
+# What a call of linear or linear_grad with these sizes, strides, types and alignments comes to (no addresses, no values), worked
+# out once: that takes 3 us of a call's 10.  As many as a program with many layers has.
 _FORMS_MOST = 1024
 _WORD_END = 1 << 64
 _forms = {}
 
 
+def _keep_form(key, form):
+    if len(_forms) >= _FORMS_MOST:
+        _forms.clear()
+    _forms[key] = form
+    return form
+
+
+def _like(rhs, layout):
+    """A tensor without gaps of rhs's shape and layout."""
+    if layout:
+        return rhs.new_empty(rhs.shape[:-2] + (rhs.shape[-1], rhs.shape[-2])).transpose(-1, -2)
+    return rhs.new_empty(rhs.shape)
+
+
+def _form_grad(key, grad, lhs, rhs, bias, pre, activation, dropout, need_lhs, need_rhs):
+    sizes, ml, mr, shape = _operands(lhs, rhs)
+    act, drop = _activation(activation), drop_threshold(dropout)
+    if act and pre is None:
+        raise MorelloError(E_INVAL, "the gradient of %s needs pre" % activation)
+    m_lhs = m_rhs = _ABSENT
+    if need_lhs:
+        m_lhs = _rows("d_lhs", lhs.new_empty(lhs.shape), lhs.shape)
+    if need_rhs:                # (of one row or column d_rhs could be read either way: its layout is rhs's)
+        d_rhs = _like(rhs, mr[2])
+        st = d_rhs.stride()
+        m_rhs = (d_rhs.data_ptr(), mr[1], mr[2], st[-1] if mr[2] else st[-2], st[0] if len(st) == 3 else 0)
+    mats = [_rows("grad", grad, shape), ml, mr, _rows("pre", pre, shape) if act else _ABSENT, m_lhs, m_rhs,
+            _ABSENT if bias is None else _vector("bias", bias, sizes[3])]
+    n = C.c_size_t()
+    _check(lib().mrl_linear_grad_bytes(_LINEAR_GRAD.pack(*sizes, *(v for m in mats for v in m), act, drop, 0, 0), C.addressof(n)))
+    return _keep_form(key, (sizes, *(m[1:] for m in mats), act, drop, n.value))
+
+
 def _form_linear(key, lhs, rhs, bias, residual, out, dtype, pre, activation, dropout):
     sizes, ml, mr, shape = _operands(lhs, rhs)
-    made = out is None
-    if made:
+    if out is None:
         out = lhs.new_empty(shape, dtype=lhs.dtype if dtype is None else dtype)
     elif dtype is not None and out.dtype != dtype:
         raise MorelloError(E_INVAL, "out is %s, not %s" % (out.dtype, dtype))
@@ -648,11 +671,7 @@ def _form_linear(key, lhs, rhs, bias, residual, out, dtype, pre, activation, dro
     act, drop = _activation(activation), drop_threshold(dropout)
     n = C.c_size_t()
     _check(lib().mrl_linear_bytes(_LINEAR.pack(*sizes, *(v for m in mats for v in m), act, drop, 0, 0), C.addressof(n)))
-    form = (shape, out.dtype, sizes, *(m[1:] for m in mats), act, drop, n.value)
-    if len(_forms) >= _FORMS_MOST:
-        _forms.clear()
-    _forms[key] = form
-    return form
+    return _keep_form(key, (shape, out.dtype, sizes, *(m[1:] for m in mats), act, drop, n.value))
 
 
 def _operands(lhs, rhs):
@@ -676,7 +695,8 @@ def linear(lhs, rhs, bias=None, residual=None, *, activation="none", dropout=0.0
     dropout: the probability that an element is dropped; seed and offset (64 bits each) say which are, together with
     the element's row and column.  dtype: out's and z's type (lhs's if None); out: a tensor to write to, which may be
     `residual`.  workspace: device memory that the caller keeps, a contiguous tensor (one that is too small is refused
-    with E_NOMEM and what is needed); stream: where the work is queued (the current stream if None).
+    with E_NOMEM and what is needed); stream: where the work is queued (the current stream if None).  Autograd
+    does not record the call: linear_grad is its gradient.
     """
     on = _elsewhere((lhs, rhs, bias, residual, out, workspace), stream)
     if on is not None:
@@ -714,26 +734,22 @@ def linear_grad(grad, lhs, rhs, bias=None, pre=None, *, activation="none", dropo
         with on:
             return linear_grad(grad, lhs, rhs, bias, pre, activation=activation, dropout=dropout, seed=seed, offset=offset,
                                need_lhs=need_lhs, need_rhs=need_rhs, workspace=workspace)
-    sizes, ml, mr, shape = _operands(lhs, rhs)
-    act = _activation(activation)
-    if act and pre is None:
-        raise MorelloError(E_INVAL, "the gradient of %s needs pre" % activation)
+    pg, pl, pr = grad.data_ptr(), lhs.data_ptr(), rhs.data_ptr()
+    key = (grad.shape, grad.stride(), grad.dtype, lhs.shape, lhs.stride(), lhs.dtype, rhs.shape, rhs.stride(), rhs.dtype, (pg | pl | pr) & 15,
+           None if bias is None else (bias.shape, bias.stride(), bias.dtype), None if pre is None else (pre.shape, pre.stride(), pre.dtype),
+           activation, dropout, need_lhs, need_rhs)
+    form = _forms.get(key)
+    if form is None:
+        form = _form_grad(key, grad, lhs, rhs, bias, pre, activation, dropout, need_lhs, need_rhs)
+    sizes, mg, ml, mr, mz, m_lhs, m_rhs, m_bias, act, drop, need = form
     d_lhs = lhs.new_empty(lhs.shape) if need_lhs else None
-    d_rhs = None
-    if need_rhs and mr[2]:
-        d_rhs = rhs.new_empty(rhs.shape[:-2] + (rhs.shape[-1], rhs.shape[-2])).transpose(-1, -2)
-    elif need_rhs:
-        d_rhs = rhs.new_empty(rhs.shape)
+    d_rhs = _like(rhs, mr[1]) if need_rhs else None
     d_bias = bias.new_empty(bias.shape) if bias is not None else None
-    m_rhs = _ABSENT
-    if d_rhs is not None:       # (of one row or column d_rhs could be read either way: its layout is rhs's)
-        st = d_rhs.stride()
-        m_rhs = (d_rhs.data_ptr(), mr[1], mr[2], st[-1] if mr[2] else st[-2], st[0] if len(st) == 3 else 0)
-    desc = _LINEAR_GRAD.pack(*sizes, *_rows("grad", grad, shape), *ml, *mr, *(_rows("pre", pre, shape) if act else _ABSENT),
-                             *(_ABSENT if d_lhs is None else _rows("d_lhs", d_lhs, lhs.shape)), *m_rhs,
-                             *(_ABSENT if d_bias is None else _vector("d_bias", d_bias, sizes[3])),
-                             act, drop_threshold(dropout), _word("seed", seed), _word("offset", offset))
-    _queue(desc, lib().mrl_linear_grad_bytes, lib().mrl_linear_grad, workspace, lhs)
+    if not (0 <= seed < _WORD_END and 0 <= offset < _WORD_END):
+        raise MorelloError(E_INVAL, "seed %r or offset %r does not fit 64 bits" % (seed, offset))
+    desc = _LINEAR_GRAD.pack(*sizes, pg, *mg, pl, *ml, pr, *mr, pre.data_ptr() if act else 0, *mz, d_lhs.data_ptr() if need_lhs else 0, *m_lhs,
+                             d_rhs.data_ptr() if need_rhs else 0, *m_rhs, 0 if bias is None else d_bias.data_ptr(), *m_bias, act, drop, seed, offset)
+    _run(desc, _lib.mrl_linear_grad, need, workspace, lhs)
     return d_lhs, d_rhs, d_bias
 
 
