@@ -724,12 +724,13 @@ __global__ __launch_bounds__(256) void rest_kernel(const Rest r, uint64_t first)
 
 // ---- rows
 
-// Rows of a workgroup of grad_rows_kernel: 8 to 64, fewer where there would not be a thousand workgroups (1000 x 777 in f32: 64 rows
-// 21 us, 8 rows 6 us; of many rows, more of them leave fewer partial sums).
+// Rows of a workgroup of grad_rows_kernel: 8 to 32, fewer where there would not be a thousand workgroups (1000 x 777 in f32: 64 rows
+// 21 us, 8 rows 7 us; 4096 x 16384 in bf16 with ReLU and the sums: 128 rows 136 us, 64 rows 122, 32 rows 115, 16 rows 115 and more partial sums to read).
+// Up to 64 rows are one block: its sums are dbias, and no launch follows to add them up.
 uint32_t grad_rows(uint64_t rows, uint32_t N) {
   const uint64_t blocks_n = (N + 255) / 256;
-  uint32_t each = 64;
-  if (rows <= each) return each;         // one block of rows: its sums are dbias, and no launch follows to add them up
+  if (rows <= 64) return 64;
+  uint32_t each = 32;
   while (each > 8 && (rows + each - 1) / each * blocks_n < 1024) each /= 2;
   return each;
 }
