@@ -668,7 +668,7 @@ __global__ __launch_bounds__(64 * WAVES) void rows_wide_kernel(const Product p, 
 }
 
 // What is left to do when a call's products and rows are through, in one launch: the sums over splits of up to two products with their
-// epilogues, and the column sums of dz.  All are added in an order that the sizes alone decide.
+// epilogues, and the column sums of dz.  All are added in an order that sizes, types and alignments alone decide.
 struct Rest {
   Product p[2];
   uint32_t splits[2];              // 1: nothing to join

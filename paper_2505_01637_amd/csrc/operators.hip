@@ -122,7 +122,9 @@ int32_t linear_product(const mrl_linear_desc& d, Product* out) {
   return MRL_OK;
 }
 
-// What a gradient is made of: dz (rows without gaps, starting at multiples of 8 elements), then the two products.
+// What a gradient is made of: dz (rows without gaps, starting at multiples of 8 elements), then the two products.  dz is rounded to the
+// operands' type, which both products need it in: a bf16 gradient is then within 0.0024 of its norm, where one rounding at the end leaves 0.0017,
+// and a dz in f32 (or in two bf16 parts) would double what is written, read and multiplied.
 struct GradPlan {
   bool pass;                       // dz differs from grad (or has another type): a pass over the rows makes it
   bool lhs, rhs;                   // wanted

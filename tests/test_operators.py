@@ -322,6 +322,35 @@ def test_linear_with_dropout_is_linear_then_dropout(dtype):
 
 
 @gpu
+def test_operands_beyond_32_bits():
+    """Offsets past 4 GB: the last rows of a product over 4.6 GB, a gradient that sums over them, a dropout of as much; every part
+    against 64 bits.  (d_rhs adds 1,130,000 products: u times their number times the sum of magnitudes bounds it.)"""
+    torch, _ = _torch()
+    m, k, n = 1130000, 2048, 24
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    lhs = torch.empty((m, k), device="cuda", dtype=torch.bfloat16).normal_(generator=gen)
+    rhs = torch.randn((k, n), generator=gen, device="cuda").bfloat16()
+    grad = torch.randn((m, n), generator=gen, device="cuda").bfloat16()
+    print("linear beyond 4 GB", flush=True)
+    out = B.linear(lhs, rhs, dtype=torch.float32)
+    for at in (0, 524288 - 50, 1048576 - 50, m - 100):          # around 2 GB, around 4 GB, the end
+        L, R = f64(lhs[at:at + 100]), f64(rhs)
+        check(out[at:at + 100], L @ R, (k + 2) * U * (np.abs(L) @ np.abs(R)), "f32", at)
+    _, d_rhs, _ = B.linear_grad(grad, lhs, rhs, need_lhs=False)
+    want = sum(a.double().t() @ g.double() for a, g in zip(lhs.split(100000), grad.split(100000)))
+    size = sum(a.abs().double().t() @ g.abs().double() for a, g in zip(lhs.split(100000), grad.split(100000)))
+    check(d_rhs, f64(want), f64(size) * (m + 2) * U, "bf16", "d_rhs")
+    assert (d_rhs.double() - want).norm() <= 2.0 ** -8 * want.norm()
+    d_lhs, _, _ = B.linear_grad(grad, lhs, rhs, need_rhs=False)
+    G = f64(grad[-100:])
+    check(d_lhs[-100:], G @ f64(rhs).T, (n + 2) * U * (np.abs(G) @ np.abs(f64(rhs)).T), "bf16", "d_lhs")
+    dropped = B.dropout(lhs, dropout=0.25, seed=9)
+    bits = random_bits(3, k, 9, 0, first_row=m - 3)
+    want = np.where(bits < 16384, 0.0, f64(lhs[-3:]) * 65536 / 49152)
+    check(dropped[-3:], want, 2 * U * np.abs(want), "bf16", "dropout")
+
+
+@gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_values_that_are_not_finite(dtype):
     """Infinities and NaN go where the formula takes them; where an element is dropped there is the residual, whatever was dropped."""
