@@ -8,7 +8,6 @@
 namespace mrl {
 
 using bf16 = __bf16;
-typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -199,8 +198,8 @@ struct ProductPlan {
   uint32_t splits;               // workgroups along k
   uint32_t steps, per_split;     // steps of 128 bytes along k: in all, per split
   uint64_t blocks;               // workgroups
-  bool copy_a, copy_b;           // the operand is first copied to lines that start at multiples of 16 bytes
-  uint64_t copy_a_bytes, copy_b_bytes, partial_bytes;        // workspace, in this order
+  // workspace, in this order: the operands' copies to lines that start at multiples of 16 bytes (0: not copied), the sums over splits
+  uint64_t copy_a_bytes, copy_b_bytes, partial_bytes;
   uint64_t bytes() const { return copy_a_bytes + copy_b_bytes + partial_bytes; }
   float* partial(void* workspace) const { return (float*)((char*)workspace + copy_a_bytes + copy_b_bytes); }
 };
