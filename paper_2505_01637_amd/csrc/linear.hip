@@ -827,12 +827,12 @@ hipError_t launch_layout(const Product& p, const ProductPlan& plan, float* parti
   return p.b_kc ? launch_tiles<T, false, true>(p, plan, partial, st) : launch_tiles<T, false, false>(p, plan, partial, st);
 }
 
-// What an operand allows.  kAligned: every line that is read starts at a multiple of 16 bytes, ends at one, and follows the one before, and
-// offsets within a tile fit 31 bits.  kWide: every line holds 16 bytes at least.
+// What operands allow.  kAligned: every line that is read starts at a multiple of 16 bytes, ends at one, and follows the one before, and
+// offsets within a tile fit 31 bits.  kWide: every line holds 16 bytes at least, of the elements that the sum is over or the tile has (Stage moves a
+// load that ends past those back by as much, and zeros that follow a shorter line do not keep it from starting before the line).
 enum Access { kAligned, kWide, kAny };
-Access access_of(const void* data, int64_t ld, int64_t batch, int64_t seg, int64_t width, int64_t e) {
-  if ((uintptr_t)data % 16 == 0 && ld % e == 0 && batch % e == 0 && seg % e == 0 && width % e == 0 && ld >= width && ld < (int64_t)1 << 21) return kAligned;
-  return width >= e ? kWide : kAny;
+bool aligned(const void* data, int64_t ld, int64_t batch, int64_t seg, int64_t width, int64_t e) {
+  return (uintptr_t)data % 16 == 0 && ld % e == 0 && batch % e == 0 && seg % e == 0 && width % e == 0 && ld >= width && ld < (int64_t)1 << 21;
 }
 
 // Matrices of `lines` lines of `width` elements, copied to lines of `pitch` elements (a multiple of 16 bytes), zeros behind the width.
@@ -910,14 +910,15 @@ constexpr float kLaunch1 = 6, kBytes = 4.5e6f;                     // a further 
 ProductPlan plan_product(const Product& p) {
   ProductPlan plan{};
   const uint32_t size = p.bf16 ? 2 : 4, ks = kStep / size, f32 = !p.bf16;
-  const Access a = access_of(p.a, p.lda, p.batches > 1 ? p.batch_a : 0, p.segs > 1 ? p.seg_a : 0, p.wa, 16 / size);
-  const Access b = access_of(p.b, p.ldb, p.batches > 1 ? p.batch_b : 0, p.segs > 1 ? p.seg_b : 0, p.wb, 16 / size);
-  const Access both = a > b ? a : b;
+  const uint32_t e = 16 / size;
+  const bool a = aligned(p.a, p.lda, p.batches > 1 ? p.batch_a : 0, p.segs > 1 ? p.seg_a : 0, p.wa, e);
+  const bool b = aligned(p.b, p.ldb, p.batches > 1 ? p.batch_b : 0, p.segs > 1 ? p.seg_b : 0, p.wb, e);
+  const Access both = a && b ? kAligned : (p.a_kc ? p.K : p.M) >= e && (p.b_kc ? p.K : p.N) >= e ? kWide : kAny;
   plan.steps = (p.K + ks - 1) / ks * p.segs;
   const float out = (float)p.batches * p.M * p.N * 4;
   // operands that are not aligned may be copied so that they are
   const Copy ca = copy_a(p), cb = copy_b(p);
-  const uint64_t bytes_a = a == kAligned ? 0 : (ca.chunks() * size + 255) / 256 * 256, bytes_b = b == kAligned ? 0 : (cb.chunks() * size + 255) / 256 * 256;
+  const uint64_t bytes_a = a ? 0 : (ca.chunks() * size + 255) / 256 * 256, bytes_b = b ? 0 : (cb.chunks() * size + 255) / 256 * 256;
   const bool copies = both != kAligned && ca.pitch < 1u << 21 && cb.pitch < 1u << 21;
   float best = 0;
   for (const Kernel& k : kKernels) {

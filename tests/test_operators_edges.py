@@ -1,0 +1,104 @@
+"""Edges of the operators that Specs name, on data: what the library's host part launches there (on the CPU, on a runtime
+that launches nothing but counts: fake_hip.c), and values against 64 bits on a GPU."""
+import numpy as np
+import pytest
+
+from test_host_part import run_on_fake_hip
+from test_operators import U, UNIT, check, f64, plain_grad, scale_of, strided
+
+gpu = pytest.mark.gpu
+
+# what the programs below begin with: descriptors by what a matrix is, and the (mangled) names of what they launched
+HOST = r"""
+import ctypes as C, sys
+sys.path.insert(0, sys.argv[2])
+sys.modules["torch"] = None                       # (its own runtime would be loaded first)
+hip = C.CDLL(sys.argv[1], mode=C.RTLD_GLOBAL)
+from paper_2505_01637_amd import binding as B
+lib = B.lib()
+NONE, P = (0, 0, 0, 0, 0), 1 << 20                # (addresses that nothing reads)
+
+def mat(rows, columns, dtype, layout=0, at=0, ld=0, shared=False):
+    ld = ld or (rows if layout else columns)
+    return P + at, dtype, layout, ld, 0 if shared else ld * (columns if layout else rows)
+
+def grad(m, k, n, dtype=1, b=1, act=0, drop=0, lhs=0, rhs=0, d_rhs=None, shared=True, at=0, need_lhs=True, need_rhs=True, d_bias=False):
+    mats = (mat(m, n, dtype, at=at), mat(m, k, dtype, lhs), mat(k, n, dtype, rhs, shared=shared), mat(m, n, dtype) if act else NONE,
+            mat(m, k, dtype) if need_lhs else NONE, mat(k, n, dtype, rhs if d_rhs is None else d_rhs, shared=shared) if need_rhs else NONE,
+            mat(1, n, 0) if d_bias else NONE)
+    return B._LINEAR_GRAD.pack(b, m, k, n, *(v for x in mats for v in x), act, drop, 0, 0)
+
+def linear(m, k, n, dtype=1, b=1, lhs=0, rhs=0, shared=True, at_lhs=0, at_rhs=0, out=None):
+    mats = (mat(m, k, dtype, lhs, at_lhs), mat(k, n, dtype, rhs, at_rhs, shared=shared), NONE, NONE, mat(m, n, dtype if out is None else out), NONE)
+    return B._LINEAR.pack(b, m, k, n, *(v for x in mats for v in x), 0, 0, 0, 0)
+
+def took(*names):
+    # how often each was launched (counting takes what it counts: a part of a longer name comes after it)
+    n = {k: hip.fake_launches_of(k.encode()) for k in names}
+    return {k: v for k, v in n.items() if v}
+
+def run(name, desc):
+    size = C.c_size_t()
+    assert getattr(lib, name + "_bytes")(desc, C.addressof(size)) == 0, lib.mrl_last_error()
+    assert getattr(lib, name)(desc, P, size.value, None) == 0, lib.mrl_last_error()
+    return size.value
+"""
+
+NARROW = HOST + r"""
+# lines of dz are padded, but a line that holds less than 16 bytes of elements must not be read as 16 bytes of them
+def wide():
+    n = took("rows_wide_kernel")
+    # (the last template argument of product_kernel: loads of 16 bytes)
+    for t in ("DF16b", "f"):
+        for a in "01":
+            for b in "01":
+                for tile in ("Li128ELi128ELi2ELi2E", "Li64ELi64ELi2ELi2E"):
+                    n.update(took("product_kernelI%sLb%sELb%sE%sLb1E" % (t, a, b, tile)))
+    return n
+seen = 0
+for dtype, narrow in ((1, range(1, 8)), (0, range(1, 4))):
+    for n in narrow:
+        for m, k in ((100, 33), (3, 7), (1, 1001), (2000, 511), (9, 40)):
+            for act, drop in ((1, 0), (0, 6554), (2, 100)):
+                for lhs in (0, 1):
+                    for rhs in (0, 1):
+                        for d_rhs in (0, 1):
+                            for need_lhs, need_rhs in ((True, False), (False, True), (True, True)):
+                                wide()
+                                run("mrl_linear_grad", grad(m, k, n, dtype, 1, act, drop, lhs, rhs, d_rhs, need_lhs=need_lhs, need_rhs=need_rhs))
+                                assert not wide(), (dtype, m, k, n, act, lhs, rhs, d_rhs, need_lhs, need_rhs)
+                                seen += bool(took("product_kernel"))
+assert seen
+# of eight (four) and more they are
+run("mrl_linear_grad", grad(100, 33, 9, 1, act=1, need_lhs=False))
+assert wide()
+print("done")
+"""
+
+
+def test_narrow_gradients_take_no_loads_of_16_bytes(tmp_path):
+    run_on_fake_hip(tmp_path, NARROW)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [1, 2, 3, 4, 5, 6, 7])
+@pytest.mark.parametrize("lhs_columns,rhs_columns", [(False, False), (False, True), (True, False), (True, True)])
+@pytest.mark.parametrize("m,k", [(100, 33), (65, 72), (1, 129)])
+def test_gradients_of_narrow_outputs(dtype, n, lhs_columns, rhs_columns, m, k):
+    """Few columns of out, dz made by a pass.  The bounds are those of the formula's other shapes: dz before it is rounded within two products
+    of f32 (ReLU, D), rounded to the operands' type, then a sum over n or m."""
+    from paper_2505_01637_amd import binding as B
+    rng = np.random.default_rng(n)
+    lhs, rhs = strided(rng.standard_normal((m, k)), dtype, lhs_columns), strided(rng.standard_normal((k, n)), dtype, rhs_columns)
+    bias = strided(rng.standard_normal((1, n)), "f32")[0]
+    grad, z = strided(rng.standard_normal((m, n)), dtype), strided(rng.standard_normal((m, n)), dtype)
+    print("linear_grad", m, k, n, dtype, lhs_columns, rhs_columns, flush=True)
+    d_lhs, d_rhs, d_bias = B.linear_grad(grad, lhs, rhs, bias, z, activation="relu", dropout=0.25, seed=9, offset=2)
+    G, L, R, Z = f64(grad), f64(lhs), f64(rhs), f64(z)
+    dz, want_l, want_r = plain_grad(G, L, R, Z, "relu", scale_of(G.shape, 0.25, 9, 2))
+    db = 2 * U * np.abs(dz)
+    rounded = db + UNIT[dtype] * (np.abs(dz) + db)
+    check(d_lhs, want_l, rounded @ np.abs(R).T + (n + 2) * U * (np.abs(dz) @ np.abs(R).T), dtype, "d_lhs")
+    check(d_rhs, want_r, np.abs(L).T @ rounded + (m + 2) * U * (np.abs(L).T @ np.abs(dz)), dtype, "d_rhs")
+    check(d_bias, dz.sum(0), db.sum(0) + (m + 2) * U * np.abs(dz).sum(0), "f32", "d_bias")
