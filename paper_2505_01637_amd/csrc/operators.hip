@@ -217,7 +217,7 @@ int32_t plan_grad(const mrl_linear_grad_desc& d, GradPlan* out) {
     p.batch_b = p.seg_b = b.batch;
     p.M = turned ? d.n : d.k;
     p.N = turned ? d.k : d.n;
-    p.K = d.m;
+    p.K = d.b ? d.m : 0;           // (of no batches there is nothing to sum, nor to copy)
     p.e.out = RowsOf{d.d_rhs.data, d.d_rhs.ld, d.d_rhs.batch, d.d_rhs.dtype == MRL_BF16};
     // batches whose rows follow each other are one sum
     if (sum && !lhs.kc && (uint64_t)lhs.batch == (uint64_t)d.m * (uint64_t)lhs.ld && (uint64_t)z.batch == (uint64_t)d.m * (uint64_t)z.ld) {

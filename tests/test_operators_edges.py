@@ -102,3 +102,45 @@ def test_gradients_of_narrow_outputs(dtype, n, lhs_columns, rhs_columns, m, k):
     check(d_lhs, want_l, rounded @ np.abs(R).T + (n + 2) * U * (np.abs(dz) @ np.abs(R).T), dtype, "d_lhs")
     check(d_rhs, want_r, np.abs(L).T @ rounded + (m + 2) * U * (np.abs(L).T @ np.abs(dz)), dtype, "d_rhs")
     check(d_bias, dz.sum(0), db.sum(0) + (m + 2) * U * np.abs(dz).sum(0), "f32", "d_bias")
+
+
+NO_BATCHES = HOST + r"""
+# d_rhs of batches that share rhs, of which there are none: zeros, and lhs, of which there is nothing, is not copied
+took("copy_kernel")
+seen = []
+for dtype in (0, 1):
+    for m, k, n in ((3, 8192, 8192), (5, 4000, 9000), (100, 33, 70), (1001, 511, 777), (8, 64, 64), (1, 1, 1)):
+        for lhs in (0, 1):
+            for d_rhs in (0, 1):
+                for act in (0, 1):
+                    took("_kernel")
+                    run("mrl_linear_grad", grad(m, k, n, dtype, 0, act, 0, lhs, 0, d_rhs, need_lhs=False))
+                    n_copies = took("copy_kernel")
+                    if n_copies: seen.append((dtype, m, k, n, lhs, d_rhs, act))
+                    assert took("_kernel"), "zeros are stored"
+assert not seen, seen
+print("done")
+"""
+
+
+def test_no_copies_of_batches_that_are_not_there(tmp_path):
+    run_on_fake_hip(tmp_path, NO_BATCHES)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,k,n", [(3, 8192, 8192), (100, 33, 70), (8, 64, 64)])
+@pytest.mark.parametrize("activation", ["none", "silu"])
+def test_gradient_of_no_batches_is_zero(dtype, m, k, n, activation):
+    """rhs shared by the batches, of which there are none; lhs column-major."""
+    import torch
+    from paper_2505_01637_amd import binding as B
+    t = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    lhs = torch.empty((0, k, m), device="cuda", dtype=t).transpose(-1, -2)
+    rhs = torch.ones((k, n), device="cuda", dtype=t)
+    grad = torch.empty((0, m, n), device="cuda", dtype=t)
+    print("linear_grad of no batches", m, k, n, dtype, activation, flush=True)
+    for _ in range(2):
+        torch.full((k, n), float("nan"), device="cuda", dtype=t)        # (what the result's memory held)
+        d_lhs, d_rhs, d_bias = B.linear_grad(grad, lhs, rhs, torch.ones(n, device="cuda"), grad, activation=activation)
+        assert d_lhs.shape == lhs.shape and d_rhs.shape == rhs.shape and not d_rhs.any() and not d_bias.any()
