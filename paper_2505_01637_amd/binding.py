@@ -620,7 +620,8 @@ def _run(desc, run, need, given, like):
 
 
 # What a call of linear or linear_grad with these sizes, strides, types and alignments comes to (no addresses, no values), worked
-# out once: that takes 3 us of a call's 10.  As many as a program with many layers has.
+# out once: that takes 3 us of a call's 10.  As many as a program with many layers has.  (Of an address only whether it is a multiple of 16
+# counts, of each operand by itself: one that is not may be copied into the workspace.)
 _FORMS_MOST = 1024
 _WORD_END = 1 << 64
 _forms = {}
@@ -704,7 +705,7 @@ def linear(lhs, rhs, bias=None, residual=None, *, activation="none", dropout=0.0
             return linear(lhs, rhs, bias, residual, activation=activation, dropout=dropout, seed=seed, offset=offset, dtype=dtype, pre=pre,
                           out=out, workspace=workspace)
     pl, pr = lhs.data_ptr(), rhs.data_ptr()
-    key = (lhs.shape, lhs.stride(), lhs.dtype, rhs.shape, rhs.stride(), rhs.dtype, (pl | pr) & 15,
+    key = (lhs.shape, lhs.stride(), lhs.dtype, rhs.shape, rhs.stride(), rhs.dtype, pl & 15 == 0, pr & 15 == 0,
            None if bias is None else (bias.shape, bias.stride(), bias.dtype),
            None if residual is None else (residual.shape, residual.stride(), residual.dtype),
            None if out is None else (out.shape, out.stride(), out.dtype), dtype, pre, activation, dropout)
@@ -735,7 +736,7 @@ def linear_grad(grad, lhs, rhs, bias=None, pre=None, *, activation="none", dropo
             return linear_grad(grad, lhs, rhs, bias, pre, activation=activation, dropout=dropout, seed=seed, offset=offset,
                                need_lhs=need_lhs, need_rhs=need_rhs, workspace=workspace)
     pg, pl, pr = grad.data_ptr(), lhs.data_ptr(), rhs.data_ptr()
-    key = (grad.shape, grad.stride(), grad.dtype, lhs.shape, lhs.stride(), lhs.dtype, rhs.shape, rhs.stride(), rhs.dtype, (pg | pl | pr) & 15,
+    key = (grad.shape, grad.stride(), grad.dtype, lhs.shape, lhs.stride(), lhs.dtype, rhs.shape, rhs.stride(), rhs.dtype, pg & 15 == 0, pl & 15 == 0, pr & 15 == 0,
            None if bias is None else (bias.shape, bias.stride(), bias.dtype), None if pre is None else (pre.shape, pre.stride(), pre.dtype),
            activation, dropout, need_lhs, need_rhs)
     form = _forms.get(key)

@@ -144,3 +144,78 @@ def test_gradient_of_no_batches_is_zero(dtype, m, k, n, activation):
         torch.full((k, n), float("nan"), device="cuda", dtype=t)        # (what the result's memory held)
         d_lhs, d_rhs, d_bias = B.linear_grad(grad, lhs, rhs, torch.ones(n, device="cuda"), grad, activation=activation)
         assert d_lhs.shape == lhs.shape and d_rhs.shape == rhs.shape and not d_rhs.any() and not d_bias.any()
+
+
+FORMS = HOST + r"""
+class Device:
+    index = 0
+
+class Tensor:
+    # what the binding asks of a tensor
+    def __init__(self, shape, strides, dtype, at):
+        self.shape, self.strides, self.dtype, self.at, self.device = tuple(shape), tuple(strides), dtype, at, Device
+    def data_ptr(self): return self.at
+    def stride(self, i=None): return self.strides if i is None else self.strides[i]
+    def get_device(self): return 0
+    def is_contiguous(self): return True
+    def numel(self):
+        n = 1
+        for s in self.shape: n *= s
+        return n
+    def element_size(self): return {"f32": 4, "bf16": 2, "u8": 1}[self.dtype]
+    def new_empty(self, shape, dtype=None):
+        return row_major(shape if isinstance(shape, tuple) else (shape,), dtype or self.dtype)
+    def transpose(self, a, b):
+        return Tensor(self.shape[:-2] + self.shape[:-3:-1], self.strides[:-2] + self.strides[:-3:-1], self.dtype, self.at)
+
+def row_major(shape, dtype, at=P):
+    strides = [1]
+    for s in shape[:0:-1]: strides.insert(0, strides[0] * s)
+    return Tensor(shape, strides, dtype, at)
+
+B._codes, B._uint8, B._raw_stream, B._current_device = {"f32": 0, "bf16": 1}, "u8", lambda i: None, lambda: 0
+off = {"f32": (0, 4, 8), "bf16": (0, 2, 8)}
+for dtype in ("bf16", "f32"):
+    for m, k, n in ((4096, 4096, 1024), (8192, 1024, 1024), (4096, 2048, 8192), (1, 16384, 256), (300, 301, 302)):
+        shifts = [(a, b, c) for a in off[dtype] for b in off[dtype] for c in off[dtype]]
+        for order in (shifts, shifts[::-1]):
+            B._forms.clear()
+            for a, b, c in order:
+                lhs, rhs, g = row_major((m, k), dtype, P + a), row_major((k, n), dtype, P + b), row_major((m, n), dtype, P + c)
+                B.linear(lhs, rhs)                     # (a workspace that is too small is refused)
+                B.linear_grad(g, lhs, rhs)
+            assert len(B._forms) <= 4 + 8, "as many forms as there are plans, not one an address"
+print("done")
+"""
+
+
+def test_operands_at_different_alignments_in_turn(tmp_path):
+    """The same sizes and strides with now one operand and now another off a multiple of 16 bytes: each call has the workspace
+    that it needs, whatever was called before."""
+    run_on_fake_hip(tmp_path, FORMS)
+
+
+@gpu
+@pytest.mark.parametrize("shifts", [((0, 0), (0, 4), (4, 0), (4, 4)), ((4, 0), (0, 4), (0, 0), (4, 4))])
+def test_values_at_different_alignments_in_turn(shifts):
+    """And the results are the same: 8192 x 1024 x 1024 in bf16, where only an operand that is off is copied."""
+    import torch
+    from paper_2505_01637_amd import binding as B
+    B._forms.clear()
+    m, k, n = 8192, 1024, 1024
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    flat = [torch.randn(r * c + 8, generator=gen, device="cuda").bfloat16() for r, c in ((m, k), (k, n), (m, n))]
+    values = [f[:r * c].clone().view(r, c) for f, (r, c) in zip(flat, ((m, k), (k, n), (m, n)))]
+    want = values[0].double() @ values[1].double()
+    bound = (k + 2) * U * (values[0].double().abs() @ values[1].double().abs())
+    grads = values[2].double() @ values[1].double().t(), values[0].double().t() @ values[2].double()
+    bounds = (n + 2) * U * (values[2].double().abs() @ values[1].double().abs().t()), (m + 2) * U * (values[0].double().abs().t() @ values[2].double().abs())
+    for a, b in shifts:
+        lhs, rhs = (f[s:s + v.numel()].view(v.shape) for f, v, s in zip(flat, values, (a, b)))
+        lhs.copy_(values[0])
+        rhs.copy_(values[1])
+        print("linear", m, k, n, a, b, flush=True)
+        out = B.linear(lhs, rhs, dtype=torch.float32)
+        assert ((out.double() - want).abs() <= bound + U * want.abs()).all()
+        for got, w, e in zip(B.linear_grad(values[2], lhs, rhs), grads, bounds):
+            assert ((got.double() - w).abs() <= e + UNIT["bf16"] * (w.abs() + e)).all()
