@@ -621,7 +621,8 @@ def _run(desc, run, need, given, like):
 
 # What a call of linear or linear_grad with these sizes, strides, types and alignments comes to (no addresses, no values), worked
 # out once: that takes 3 us of a call's 10.  As many as a program with many layers has.  (Of an address only whether it is a multiple of 16
-# counts, of each operand by itself: one that is not may be copied into the workspace.)
+# counts, of each operand by itself: one that is not may be copied into the workspace.  Of a probability its value now: it may come as an
+# object that changes.)
 _FORMS_MOST = 1024
 _WORD_END = 1 << 64
 _forms = {}
@@ -641,9 +642,9 @@ def _like(rhs, layout):
     return rhs.new_empty(rhs.shape)
 
 
-def _form_grad(key, grad, lhs, rhs, bias, pre, activation, dropout, need_lhs, need_rhs):
+def _form_grad(key, grad, lhs, rhs, bias, pre, activation, drop, need_lhs, need_rhs):
     sizes, ml, mr, shape = _operands(lhs, rhs)
-    act, drop = _activation(activation), drop_threshold(dropout)
+    act = _activation(activation)
     if act and pre is None:
         raise MorelloError(E_INVAL, "the gradient of %s needs pre" % activation)
     m_lhs = m_rhs = _ABSENT
@@ -657,10 +658,10 @@ def _form_grad(key, grad, lhs, rhs, bias, pre, activation, dropout, need_lhs, ne
             _ABSENT if bias is None else _vector("bias", bias, sizes[3])]
     n = C.c_size_t()
     _check(lib().mrl_linear_grad_bytes(_LINEAR_GRAD.pack(*sizes, *(v for m in mats for v in m), act, drop, 0, 0), C.addressof(n)))
-    return _keep_form(key, (sizes, *(m[1:] for m in mats), act, drop, n.value))
+    return _keep_form(key, (sizes, *(m[1:] for m in mats), act, n.value))
 
 
-def _form_linear(key, lhs, rhs, bias, residual, out, dtype, pre, activation, dropout):
+def _form_linear(key, lhs, rhs, bias, residual, out, dtype, pre, activation, drop):
     sizes, ml, mr, shape = _operands(lhs, rhs)
     if out is None:
         out = lhs.new_empty(shape, dtype=lhs.dtype if dtype is None else dtype)
@@ -669,10 +670,10 @@ def _form_linear(key, lhs, rhs, bias, residual, out, dtype, pre, activation, dro
     z = out.new_empty(shape) if pre else None
     mats = [ml, mr, _ABSENT if bias is None else _vector("bias", bias, sizes[3]), _ABSENT if residual is None else _rows("residual", residual, shape),
             _rows("out", out, shape), _ABSENT if z is None else _rows("pre", z, shape)]
-    act, drop = _activation(activation), drop_threshold(dropout)
+    act = _activation(activation)
     n = C.c_size_t()
     _check(lib().mrl_linear_bytes(_LINEAR.pack(*sizes, *(v for m in mats for v in m), act, drop, 0, 0), C.addressof(n)))
-    return _keep_form(key, (shape, out.dtype, sizes, *(m[1:] for m in mats), act, drop, n.value))
+    return _keep_form(key, (shape, out.dtype, sizes, *(m[1:] for m in mats), act, n.value))
 
 
 def _operands(lhs, rhs):
@@ -704,15 +705,15 @@ def linear(lhs, rhs, bias=None, residual=None, *, activation="none", dropout=0.0
         with on:
             return linear(lhs, rhs, bias, residual, activation=activation, dropout=dropout, seed=seed, offset=offset, dtype=dtype, pre=pre,
                           out=out, workspace=workspace)
-    pl, pr = lhs.data_ptr(), rhs.data_ptr()
+    pl, pr, drop = lhs.data_ptr(), rhs.data_ptr(), drop_threshold(dropout)
     key = (lhs.shape, lhs.stride(), lhs.dtype, rhs.shape, rhs.stride(), rhs.dtype, pl & 15 == 0, pr & 15 == 0,
            None if bias is None else (bias.shape, bias.stride(), bias.dtype),
            None if residual is None else (residual.shape, residual.stride(), residual.dtype),
-           None if out is None else (out.shape, out.stride(), out.dtype), dtype, pre, activation, dropout)
+           None if out is None else (out.shape, out.stride(), out.dtype), dtype, pre, activation, drop)
     form = _forms.get(key)
     if form is None:
-        form = _form_linear(key, lhs, rhs, bias, residual, out, dtype, pre, activation, dropout)
-    shape, dtype, sizes, ml, mr, mb, ms, mo, mz, act, drop, need = form
+        form = _form_linear(key, lhs, rhs, bias, residual, out, dtype, pre, activation, drop)
+    shape, dtype, sizes, ml, mr, mb, ms, mo, mz, act, need = form
     if out is None:
         out = lhs.new_empty(shape, dtype=dtype)
     z = out.new_empty(shape) if pre else None
@@ -735,14 +736,14 @@ def linear_grad(grad, lhs, rhs, bias=None, pre=None, *, activation="none", dropo
         with on:
             return linear_grad(grad, lhs, rhs, bias, pre, activation=activation, dropout=dropout, seed=seed, offset=offset,
                                need_lhs=need_lhs, need_rhs=need_rhs, workspace=workspace)
-    pg, pl, pr = grad.data_ptr(), lhs.data_ptr(), rhs.data_ptr()
+    pg, pl, pr, drop = grad.data_ptr(), lhs.data_ptr(), rhs.data_ptr(), drop_threshold(dropout)
     key = (grad.shape, grad.stride(), grad.dtype, lhs.shape, lhs.stride(), lhs.dtype, rhs.shape, rhs.stride(), rhs.dtype, pg & 15 == 0, pl & 15 == 0, pr & 15 == 0,
            None if bias is None else (bias.shape, bias.stride(), bias.dtype), None if pre is None else (pre.shape, pre.stride(), pre.dtype),
-           activation, dropout, need_lhs, need_rhs)
+           activation, drop, need_lhs, need_rhs)
     form = _forms.get(key)
     if form is None:
-        form = _form_grad(key, grad, lhs, rhs, bias, pre, activation, dropout, need_lhs, need_rhs)
-    sizes, mg, ml, mr, mz, m_lhs, m_rhs, m_bias, act, drop, need = form
+        form = _form_grad(key, grad, lhs, rhs, bias, pre, activation, drop, need_lhs, need_rhs)
+    sizes, mg, ml, mr, mz, m_lhs, m_rhs, m_bias, act, need = form
     d_lhs = lhs.new_empty(lhs.shape) if need_lhs else None
     d_rhs = _like(rhs, mr[1]) if need_rhs else None
     d_bias = bias.new_empty(bias.shape) if bias is not None else None

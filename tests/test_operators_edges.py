@@ -146,7 +146,7 @@ def test_gradient_of_no_batches_is_zero(dtype, m, k, n, activation):
         assert d_lhs.shape == lhs.shape and d_rhs.shape == rhs.shape and not d_rhs.any() and not d_bias.any()
 
 
-FORMS = HOST + r"""
+TENSORS = HOST + r"""
 class Device:
     index = 0
 
@@ -174,6 +174,9 @@ def row_major(shape, dtype, at=P):
     return Tensor(shape, strides, dtype, at)
 
 B._codes, B._uint8, B._raw_stream, B._current_device = {"f32": 0, "bf16": 1}, "u8", lambda i: None, lambda: 0
+"""
+
+FORMS = TENSORS + r"""
 off = {"f32": (0, 4, 8), "bf16": (0, 2, 8)}
 for dtype in ("bf16", "f32"):
     for m, k, n in ((4096, 4096, 1024), (8192, 1024, 1024), (4096, 2048, 8192), (1, 16384, 256), (300, 301, 302)):
@@ -219,3 +222,44 @@ def test_values_at_different_alignments_in_turn(shifts):
         assert ((out.double() - want).abs() <= bound + U * want.abs()).all()
         for got, w, e in zip(B.linear_grad(values[2], lhs, rhs), grads, bounds):
             assert ((got.double() - w).abs() <= e + UNIT["bf16"] * (w.abs() + e)).all()
+
+
+PROBABILITY = TENSORS + r"""
+import struct
+class Scalar:
+    # a number that a program changes in place, as a tensor of one element is
+    def __init__(self, v): self.v = v
+    def __mul__(self, x): return self.v * x
+    def __float__(self): return float(self.v)
+    def __ge__(self, x): return self.v >= x
+    def __le__(self, x): return self.v <= x
+
+drops = []
+real = B._run
+def keep(desc, run, need, given, like):
+    drops.append((B._LINEAR if run is B._lib.mrl_linear else B._LINEAR_GRAD).unpack(desc)[-3])
+    real(desc, run, need, given, like)
+B._run = keep
+lhs, rhs, g = row_major((8, 16), "f32"), row_major((16, 4), "f32"), row_major((8, 4), "f32")
+p = Scalar(0.25)
+for v in (0.25, 0.5, 0.0, 0.25):
+    p.v = v
+    B.linear(lhs, rhs, dropout=p)
+    B.linear_grad(g, lhs, rhs, dropout=p)
+assert drops == [16384, 16384, 32768, 32768, 0, 0, 16384, 16384], drops
+for v in (1.5, float("nan")):
+    for call in (lambda p: B.linear(lhs, rhs, dropout=p), lambda p: B.linear_grad(g, lhs, rhs, dropout=p)):
+        p.v = v
+        try:
+            call(p)
+        except B.MorelloError as e:
+            assert e.code == B.E_INVAL
+        else:
+            assert 0, v
+print("done")
+"""
+
+
+def test_a_probability_that_changes_in_place(tmp_path):
+    """A call takes the value that the probability has then, also where it is an object that had another one before."""
+    run_on_fake_hip(tmp_path, PROBABILITY)
