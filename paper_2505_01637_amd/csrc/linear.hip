@@ -750,12 +750,12 @@ __global__ __launch_bounds__(256) void grad_rows_kernel(const GradRows p, uint32
       const uint32_t row = (uint32_t)at, batch = row / p.M, m = row - batch * p.M;
       float v[8];
       load8(p.grad.data, p.grad.bf16, (int64_t)batch * p.grad.batch + (int64_t)m * p.grad.ld + n, valid, v);
-      if (p.drop.drop) drop8(p.drop, row, n, v);
       if (p.pre.data) {
         float z[8];
         load8(p.pre.data, p.pre.bf16, (int64_t)batch * p.pre.batch + (int64_t)m * p.pre.ld + n, valid, z);
         slope8(p.activation, z, v);
       }
+      if (p.drop.drop) drop8(p.drop, row, n, v);       // (last: a dropped element is 0 whatever its z was)
 #pragma unroll
       for (int e = 0; e < 8; e++) sum[e] += v[e];
       if (p.dz.data) store8(p.dz.data, p.dz.bf16, (int64_t)batch * p.dz.batch + (int64_t)m * p.dz.ld + n, 8, v);     // (zeros up to a multiple of 8)

@@ -263,3 +263,28 @@ print("done")
 def test_a_probability_that_changes_in_place(tmp_path):
     """A call takes the value that the probability has then, also where it is an object that had another one before."""
     run_on_fake_hip(tmp_path, PROBABILITY)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("activation", ["relu", "gelu", "silu"])
+def test_dropped_elements_of_a_gradient_are_zero_whatever_z_is(dtype, activation):
+    """One row of m x n, so that d_bias is dz itself: where an element is dropped dz is 0, where it is not NaN, infinite and
+    finite z count.  Two rows: a column's sum is that of the element that is kept."""
+    import torch
+    from paper_2505_01637_amd import binding as B
+    t = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    n = 256
+    kw = {"activation": activation, "dropout": 0.5, "seed": 6, "offset": 3}
+    bias, rhs = torch.zeros(n, device="cuda"), torch.zeros((8, n), device="cuda", dtype=t)
+    for m in (1, 2):
+        dropped = torch.from_numpy(scale_of((m, n), 0.5, 6, 3) == 0).cuda()
+        lhs, grad = torch.zeros((m, 8), device="cuda", dtype=t), torch.ones((m, n), device="cuda", dtype=t)
+        z = torch.full((m, n), float("nan"), device="cuda", dtype=t)
+        _, _, dz = B.linear_grad(grad, lhs, rhs, bias, z, **kw)
+        assert (dz[dropped.all(0)] == 0).all() and dz[~dropped.all(0)].isnan().all()
+        # NaN only where it is dropped: as if it were not there
+        clean = torch.full((m, n), 0.75, device="cuda", dtype=t)
+        _, _, want = B.linear_grad(grad, lhs, rhs, bias, clean, **kw)
+        d_lhs, d_rhs, dz = B.linear_grad(torch.where(dropped, float("inf"), grad), lhs + 1, rhs + 1, bias, torch.where(dropped, z, clean), **kw)
+        assert torch.equal(dz, want) and d_lhs.isfinite().all() and d_rhs.isfinite().all()
