@@ -512,7 +512,8 @@ int32_t mrl_linear(const mrl_linear_desc* desc, void* d_workspace, size_t worksp
 
 /* Gradients of a loss, given `grad`, its gradient by out:
  *   dz = D f'(z) grad;  d_lhs = dz rhs^T;  d_rhs = lhs^T dz;  d_bias = the sum of dz over batches and rows
- * (by the residual it is grad itself).  Each of the three is optional.  ReLU's slope at 0 is 0.
+ * (by the residual it is grad itself).  Each of the three is optional.  ReLU's slope at 0 is 0.  Where
+ * ReLU's z is not positive, or an element is dropped, dz is 0 even if grad is not finite; where z is NaN and is not dropped, so is dz.
  * Where d_rhs.batch is 0 and b is not 1 (batches that share rhs), d_rhs is k x n, the sum over the batches. */
 typedef struct {
   uint32_t b, m, k, n;

@@ -97,7 +97,8 @@ __device__ __forceinline__ void activate8(uint32_t act, float (&v)[8]) {
 }
 
 // v <- v f'(z).  The logistic value s times 1 - s falls off faster than any power of z grows, so where either is 0 the second
-// term of s + z u s (1 - s) is 0 too.
+// term of s + z u s (1 - s) is 0 too.  ReLU selects: where z <= 0 the result is 0 whatever v is (a product would keep NaN and infinities);
+// where z is NaN it is NaN, as f(z) is.
 __device__ __forceinline__ void slope8(uint32_t act, const float (&z)[8], float (&v)[8]) {
   if (act == kActGelu) {
 #pragma unroll
@@ -113,7 +114,7 @@ __device__ __forceinline__ void slope8(uint32_t act, const float (&z)[8], float 
     }
   } else if (act == kActRelu) {
 #pragma unroll
-    for (int e = 0; e < 8; e++) v[e] *= z[e] > 0.0f ? 1.0f : z[e] == z[e] ? 0.0f : z[e];
+    for (int e = 0; e < 8; e++) v[e] = z[e] > 0.0f ? v[e] : z[e] == z[e] ? 0.0f : z[e];
   }
 }
 

@@ -288,3 +288,32 @@ def test_dropped_elements_of_a_gradient_are_zero_whatever_z_is(dtype, activation
         _, _, want = B.linear_grad(grad, lhs, rhs, bias, clean, **kw)
         d_lhs, d_rhs, dz = B.linear_grad(torch.where(dropped, float("inf"), grad), lhs + 1, rhs + 1, bias, torch.where(dropped, z, clean), **kw)
         assert torch.equal(dz, want) and d_lhs.isfinite().all() and d_rhs.isfinite().all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("p", [0.0, 0.5])
+def test_relu_passes_nothing_on_where_z_is_not_positive(dtype, p):
+    """One row, so that d_bias is dz: 0 where z <= 0 whatever the gradient is, the gradient times D where z > 0, NaN where z is NaN (as
+    relu(z) is), 0 where it is dropped."""
+    import torch
+    from paper_2505_01637_amd import binding as B
+    t = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+    inf, nan = float("inf"), float("nan")
+    grads, zs = (1.5, -2.0, inf, -inf, nan), (1.0, inf, 2.0 ** -100, 0.0, -0.0, -3.0, -inf, -2.0 ** -100, nan)
+    pairs = [(g, z) for g in grads for z in zs] * 3
+    n = len(pairs)
+    grad, z = (torch.tensor([[x[i] for x in pairs]], device="cuda", dtype=t) for i in (0, 1))
+    lhs, rhs = torch.zeros((1, 8), device="cuda", dtype=t), torch.zeros((8, n), device="cuda", dtype=t)
+    d = scale_of((1, n), p, 11, 1)[0]
+    _, _, dz = B.linear_grad(grad, lhs, rhs, torch.zeros(n, device="cuda"), z, activation="relu", dropout=p, seed=11, offset=1)
+    want = [0.0 if k == 0 else nan if z != z else g * k if z > 0 else 0.0 for (g, z), k in zip(pairs, d)]
+    assert np.array_equal(f64(dz), np.array(want), equal_nan=True)
+    # and what the products make of it: an infinite gradient at z <= 0 reaches neither
+    grad, z = torch.ones((8, 16), device="cuda", dtype=t), torch.ones((8, 16), device="cuda", dtype=t)
+    grad[2, 3], z[2, 3] = inf, -1.0
+    d_lhs, d_rhs, d_bias = B.linear_grad(grad, torch.ones((8, 5), device="cuda", dtype=t), torch.ones((5, 16), device="cuda", dtype=t), torch.zeros(16, device="cuda"), z,
+                                         activation="relu")
+    rows, columns = torch.full((8,), 16.0, device="cuda"), torch.full((16,), 8.0, device="cuda")
+    rows[2], columns[3] = 15.0, 7.0
+    assert (d_lhs.float() == rows[:, None]).all() and (d_rhs.float() == columns).all() and torch.equal(d_bias, columns)
