@@ -772,8 +772,11 @@ def dropout(x, residual=None, *, dropout, seed=0, offset=0, out=None, stream=Non
             matrices += _ABSENT
             continue
         at = _rows(name, t, x.shape)
-        if x.dim() == 3 and x.shape[0] > 1 and at[4] != x.shape[1] * at[3]:
-            raise MorelloError(E_INVAL, "%s: its batches do not follow each other (strides %s)" % (name, t.stride()))
+        if x.dim() == 3 and x.shape[0] > 1:
+            if x.shape[1] <= 1:          # (a batch's only row has a stride that says nothing)
+                at = at[:3] + (at[4], at[4])
+            elif at[4] != x.shape[1] * at[3]:
+                raise MorelloError(E_INVAL, "%s: its batches do not follow each other (strides %s)" % (name, t.stride()))
         matrices += at
     rows = x.shape[0] * x.shape[1] if x.dim() == 3 else x.shape[0]
     desc = _DROPOUT.pack(rows, x.shape[-1], *matrices, drop_threshold(dropout), _word("seed", seed), _word("offset", offset))

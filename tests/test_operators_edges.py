@@ -158,6 +158,7 @@ class Tensor:
     def stride(self, i=None): return self.strides if i is None else self.strides[i]
     def get_device(self): return 0
     def is_contiguous(self): return True
+    def dim(self): return len(self.shape)
     def numel(self):
         n = 1
         for s in self.shape: n *= s
@@ -317,3 +318,54 @@ def test_relu_passes_nothing_on_where_z_is_not_positive(dtype, p):
     rows, columns = torch.full((8,), 16.0, device="cuda"), torch.full((16,), 8.0, device="cuda")
     rows[2], columns[3] = 15.0, 7.0
     assert (d_lhs.float() == rows[:, None]).all() and (d_rhs.float() == columns).all() and torch.equal(d_bias, columns)
+
+
+ONE_ROW = TENSORS + r"""
+calls = []
+class Library:                                     # what was asked of it, and the library's own answer
+    def __getattr__(self, name): return getattr(lib, name)
+    def mrl_dropout(self, desc, stream):
+        calls.append(B._DROPOUT.unpack(desc))
+        return lib.mrl_dropout(desc, stream)
+B._lib = Library()
+
+def swapped(a, b, c, ld=None):
+    # a x 1 x c as a transposed 1 x a x c shows it: the only row of a batch has a stride that nothing uses
+    return Tensor((a, 1, c), (ld or c, b, 1), "f32", P)
+
+for x, ld in ((swapped(3, 24, 8), 8), (swapped(3, 1, 8), 8), (swapped(3, 99, 8, 16), 16), (Tensor((1, 3, 8), (5, 8, 1), "f32", P), 8), (row_major((3, 4, 8), "f32"), 8)):
+    B.dropout(x, dropout=0.5, out=x)
+    rows = x.shape[0] * x.shape[1]
+    assert calls[-1][:2] == (rows, 8) and calls[-1][5] == calls[-1][15] == ld, calls[-1]
+    B.dropout(x, x, dropout=0.5)
+    B.dropout_grad(x, dropout=0.5)
+# and of batches without rows there is nothing to do
+for a, b in ((3, 0), (0, 3), (0, 0), (0, 1)):
+    B.dropout(row_major((a, b, 8), "f32"), dropout=0.5)
+    B.dropout(Tensor((a, b, 8), (8, 8, 1), "f32", P), dropout=0.5)
+# batches that do not follow each other are still refused
+for x in (Tensor((2, 3, 8), (32, 8, 1), "f32", P), Tensor((2, 2, 8), (8, 16, 1), "f32", P)):
+    try:
+        B.dropout(x, dropout=0.5)
+    except B.MorelloError as e:
+        assert e.code == B.E_INVAL
+    else:
+        assert 0
+print("done")
+"""
+
+
+def test_dropout_of_batches_of_one_row(tmp_path):
+    """The stride of a batch's only row says nothing: batches follow each other at their own stride."""
+    run_on_fake_hip(tmp_path, ONE_ROW)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_dropout_of_batches_of_one_row_on_data(dtype):
+    import torch
+    from paper_2505_01637_amd import binding as B
+    x = strided(np.random.default_rng(1).standard_normal((1, 5, 33)), dtype).transpose(0, 1)
+    assert x.is_contiguous() and x.shape == (5, 1, 33)
+    got = B.dropout(x, x, dropout=0.4, seed=3, offset=1)
+    assert torch.equal(got, B.dropout(x[:, 0], x[:, 0], dropout=0.4, seed=3, offset=1)[:, None])
