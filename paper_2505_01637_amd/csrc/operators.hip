@@ -37,8 +37,9 @@ int32_t check_matrix(const char* name, const mrl_matrix& x, uint64_t b, uint64_t
   CHECK((uintptr_t)x.data % (x.dtype == MRL_BF16 ? 2 : 4) == 0, "%s is not aligned to its elements", name);
   const uint64_t lines = x.layout ? columns : rows, width = x.layout ? rows : columns;
   CHECK(x.ld >= 0 && x.batch >= 0, "%s: negative stride", name);
-  // (the last element's offset: lines, widths and batches are below 2^31)
-  CHECK(x.ld < (int64_t)1 << 40 && x.batch < (int64_t)1 << 40, "%s: stride too large", name);
+  // the last element's offset, which products of 64 bits may not hold: the kernels' and those below do what it allows
+  CHECK(x.ld < (int64_t)1 << 40 && x.batch < (int64_t)1 << 40 && ((unsigned __int128)(lines - 1) * x.ld + (unsigned __int128)(b - 1) * x.batch) >> 56 == 0,
+        "%s: stride too large", name);
   if (written) {
     const bool rows_apart = lines == 1 || (uint64_t)x.ld >= width;
     const uint64_t one = (lines - 1) * (uint64_t)x.ld + width;                     // elements that a batch spans

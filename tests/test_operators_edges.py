@@ -369,3 +369,23 @@ def test_dropout_of_batches_of_one_row_on_data(dtype):
     assert x.is_contiguous() and x.shape == (5, 1, 33)
     got = B.dropout(x, x, dropout=0.4, seed=3, offset=1)
     assert torch.equal(got, B.dropout(x[:, 0], x[:, 0], dropout=0.4, seed=3, offset=1)[:, None])
+
+
+FAR = HOST + r"""
+# places beyond any address: two rows or batches that share one only when offsets are taken mod 2^64, and those that do not
+def out(b, m, ld, batch, n=6):
+    return B._LINEAR.pack(b, m, 8, n, P, 0, 0, 8, 0, P, 0, 0, n, 0, *NONE, *NONE, P, 0, 0, ld, batch, *NONE, 0, 0, 0, 0)
+for desc in (out(2, (1 << 25) + 1, 1 << 39, 1 << 39), out(2, (1 << 25) + 1, 1 << 39, 6), out(2, (1 << 26) + 1, 1 << 38, 1 << 38), out(1, 1 << 30, (1 << 40) - 1, 0),
+             out(1 << 30, 1, 6, (1 << 40) - 1)):
+    assert lib.mrl_linear(desc, None, 0, None) == B.E_INVAL, lib.mrl_last_error()
+    assert b"out" in lib.mrl_last_error(), lib.mrl_last_error()
+lhs = B._LINEAR.pack(1, 1 << 30, 8, 6, P, 0, 0, (1 << 40) - 1, 0, P, 0, 0, 6, 0, *NONE, *NONE, P, 0, 0, 6, 0, *NONE, 0, 0, 0, 0)
+assert lib.mrl_linear(lhs, None, 0, None) == B.E_INVAL and b"lhs" in lib.mrl_last_error(), lib.mrl_last_error()
+# large, but possible
+assert lib.mrl_linear(out(2, 1 << 12, 1 << 22, 1 << 35), None, 0, None) == 0, lib.mrl_last_error()
+print("done")
+"""
+
+
+def test_offsets_that_no_address_has(tmp_path):
+    run_on_fake_hip(tmp_path, FAR)
