@@ -389,3 +389,24 @@ print("done")
 
 def test_offsets_that_no_address_has(tmp_path):
     run_on_fake_hip(tmp_path, FAR)
+
+
+WORKSPACE = HOST + r"""
+import itertools
+size = C.c_size_t()
+for name, desc in (("mrl_linear", linear(1, 1 << 16, 64)), ("mrl_linear", linear(4096, 4096, 1024, at_rhs=8)), ("mrl_linear_grad", grad(100, 64, 64, act=1)),
+                   ("mrl_linear_grad", grad(4096, 1024, 1024, at=8)), ("mrl_linear_grad", grad(300, 64, 64, need_lhs=False, need_rhs=False, d_bias=True))):
+    assert getattr(lib, name + "_bytes")(desc, C.addressof(size)) == 0
+    assert size.value > 0, "a shape that needs a workspace"
+    call = getattr(lib, name)
+    took("_kernel")
+    for at, have, code in ((P, size.value - 1, B.E_NOMEM), (P, 0, B.E_NOMEM), (None, size.value, B.E_INVAL), (P + 8, size.value, B.E_INVAL)):
+        assert call(desc, at, have, None) == code, (name, at, have, lib.mrl_last_error())
+    assert took("_kernel") == {}, "a refused call launches nothing"
+    assert call(desc, P, size.value, None) == 0 and took("_kernel")
+print("done")
+"""
+
+
+def test_workspaces_that_are_too_small_or_not_there(tmp_path):
+    run_on_fake_hip(tmp_path, WORKSPACE)
