@@ -334,6 +334,8 @@ class Table:
         fused = spec[17] != 0                    # the bias's stride
         if fused == (bias is None):
             raise MorelloError(E_INVAL, "a FUSED Spec takes a bias, a Matmul none")
+        if fused and codes.get(bias.dtype) != spec[15]:
+            raise MorelloError(E_INVAL, "bias is %s, the Spec's is another type" % bias.dtype)
         dtype = next(d for d, c in codes.items() if c == spec[25])
         return linear(lhs, rhs, bias, None if fused else out, activation="relu" if fused else "none", dtype=dtype,
                       out=out, workspace=workspace)

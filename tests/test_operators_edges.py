@@ -410,3 +410,22 @@ print("done")
 
 def test_workspaces_that_are_too_small_or_not_there(tmp_path):
     run_on_fake_hip(tmp_path, WORKSPACE)
+
+
+@gpu
+def test_operator_of_a_spec_takes_the_types_of_the_spec():
+    """Table.apply refuses a bias of another type than the Spec's, as it does lhs and rhs, and an out of another type."""
+    import torch
+    from paper_2505_01637_amd import binding as B
+    from paper_2505_01637_amd import workloads as W
+    target, tabs = B.solve_config(W.config(5, max_size=16))
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    lhs, rhs, bias = (torch.randn(s, generator=gen, device="cuda") for s in ((8, 16), (16, 4), (4,)))
+    x = tabs["F"].coord_of_spec((1, 8, 16, 4), (3, 3, 3, 3, 3), layouts=(0, 0, 0, 0))
+    out = tabs["F"].apply(x, lhs, rhs, bias)
+    assert torch.equal(out, tabs["F"].apply(x, lhs[None], rhs, bias)[0])
+    for bad in (lambda: tabs["F"].apply(x, lhs, rhs, bias.bfloat16()), lambda: tabs["F"].apply(x, lhs, rhs, bias, out=out.bfloat16()),
+                lambda: tabs["F"].apply(x, lhs, rhs, bias.double()), lambda: tabs["F"].apply(x, lhs, rhs, bias[:3])):
+        with pytest.raises(B.MorelloError) as e:
+            bad()
+        assert e.value.code == B.E_INVAL
