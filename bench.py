@@ -24,8 +24,8 @@ HBM_PEAK_GBS = 8000.0          # MI355X published HBM3E peak
 
 def source_hash():
     """Hash of the solver's sources: a committed counter summary names the sources it was taken
-    with, so that a stale one is not passed off as this build's traffic.  (The operators that Specs
-    name are no part of a solve.)"""
+    with, so that a stale one is not passed off as this build's traffic.  (The operators on data
+    are no part of a solve.)"""
     import hashlib
     h = hashlib.sha256()
     d = os.path.join(ROOT, "paper_2505_01637_amd", "csrc")

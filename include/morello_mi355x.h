@@ -454,9 +454,10 @@ int32_t mrl_schedule(const mrl_table* tab, const mrl_coord* goal,
 int32_t mrl_copy_dense(const mrl_table* tab, uint64_t* cost_host, uint16_t* argmin_host);
 
 /* ---------------------------------------------------------------------------
- * The operators that Specs name, on data: a Matmul with bias, activation,
- * dropout and residual in its epilogue (the MATMUL and FUSED Specs), its
- * gradients, and dropout alone.
+ * Operators on data: the Matmul that MATMUL and FUSED Specs name (the latter with
+ * bias and ReLU in its epilogue; mrl_spec_linear describes it), and what
+ * training and serving a layer made of it needs besides, which no Spec names: GELU, SiLU,
+ * dropout and a residual in the epilogue, the gradients, dropout alone.
  *
  *   z   = lhs rhs + bias                       b x m x n, the sum over k
  *   out = residual + D f(z)

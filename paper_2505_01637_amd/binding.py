@@ -474,7 +474,7 @@ def solve_config(cfg, scratch_bytes=None):
     return target, solve_lattices(target, cfg["lattices"], scratch_bytes=scratch_bytes)
 
 
-# ---- the operators that Specs name, on torch tensors
+# ---- the operators on torch tensors: the Matmul that Specs name, and what a layer made of it needs besides
 
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 

@@ -382,7 +382,7 @@ struct Feed {
 // A wave of the 256 tile has 128 x 64 of it: 24 KB read from shared memory for 64 MFMA of a step, 192 KB and 64 KB written by all eight
 // waves in 2048 cycles of products.  8192-cube in bf16 805 us, 1360 TFLOP/s: 577 us without loads and reads of shared memory, 650 without the loads, 770
 // without the reads, 755 with every step's operands in L2; so what bounds it is the way of the operands to shared memory, then their
-// reads.  2048-cube in f32 (128 x 128, eight waves) 133 us, of which the products take 117 at the clock it runs at.
+// reads.  2048-cube in f32 (128 x 128, eight waves) 135 us, of which the products take 117 at the clock it runs at.
 template <class T, bool AKC, bool BKC, int TM, int TN, int WAVES_M, int WAVES_N, int STAGES>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void fast_kernel(const Product p, uint32_t steps, uint32_t per_split, uint32_t splits,
                                                                       uint32_t first, float* __restrict__ partial) {
@@ -878,7 +878,7 @@ Copy copy_b(const Product& p) { return copy_of(p.b, p.b_kc, p.ldb, p.batch_b, p.
 }  // namespace
 
 // How long a kernel takes, in us: a round of workgroups on the 256 compute units, one each or two at once, is `fixed` and a
-// step's time for each step along k.  Measured on products whose tiles are one whole round, 2048 and 8192 long along k:
+// step's time for each step along k.  What the rule takes, from products whose tiles are one whole round, 2048 and 8192 long along k:
 //                           step bf16 (one, two)   step f32 (one, two)
 //   256 x 256                    1.52     -          7.33     -
 //   256 x 128                    0.87     -          3.81     -
@@ -889,6 +889,13 @@ Copy copy_b(const Product& p) { return copy_of(p.b, p.b_kc, p.ldb, p.batch_b, p.
 //   few rows, any alignment      0.11    0.42        0.20    0.70
 //   128 x 128, any alignment     1.25    1.70        2.50    4.80
 //   64 x 64, any alignment       0.80    0.86        0.72    1.15
+//   64 x 64, narrow lines        2.0     3.0         2.0     3.0      (round numbers, see below)
+// The same products back to back in a graph, from odd elements on where any alignment is allowed, take 1.53, 0.93, 0.56 (two: 1.01), 0.28 (0.40), 0.13 (0.24),
+// 0.21 (0.40), 0.96 (1.33), 0.69 (0.66) and 2.1 (3.4) in bf16, 7.3, 3.8, 2.0 (3.8), 0.61 (1.05), 0.30 (0.58), 0.33 (0.64), 2.3 (4.2), 0.81 (1.26) and 1.1 (1.9) in f32.
+// Narrow lines (a line holds less than 16 bytes, so loads go element by element) were not measured when the rule was made, and f32 is priced too high: with the
+// measured times one narrow f32 product in seven would not be copied, or be split, and 40 such products took the same time on geometric mean, 0.7 to 1.5 of it
+// each.  `fixed` is set, not measured: with a launch and the results' stores a round takes 15, 9, 7, 5, 4, 4, 9, 2 and 2 beside its steps in bf16, 18, 14, 10, 6, 6, 8, 10, 5
+// and 10 in f32, so it holds 2 to 6 less, which all kernels have in common.
 // So a large tile does more per time (16 units of 64 x 64 in 1.52 against 1 in 0.25) and a small one leaves fewer compute units
 // without work.  Where the tiles are few, workgroups share a tile's sum and a second launch adds up: its time, and the partial sums
 // written and read at 4.5 TB/s (bf16: 1 x 16384 x 2048 17 us split and 31 whole, 4096 x 16384 x 1024 131 and 165).  Operands that are

@@ -1,4 +1,4 @@
-// Internal: the operators that Specs name, on data (include/morello_mi355x.h, mrl_linear and what follows): what the
+// Internal: the operators on data (include/morello_mi355x.h, mrl_linear and what follows): what the
 // kernels get, the random bits of a dropout, the activations, and loads and stores of eight neighbouring elements.
 #pragma once
 #include <stdint.h>

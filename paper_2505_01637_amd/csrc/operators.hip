@@ -1,4 +1,4 @@
-// C ABI of the operators that Specs name, on data (include/morello_mi355x.h): descriptor checks, workspace, and the
+// C ABI of the operators on data (include/morello_mi355x.h): descriptor checks, workspace, and the
 // products and passes that a call is made of.
 #include <hip/hip_runtime.h>
 

@@ -1,4 +1,4 @@
-"""Edges of the operators that Specs name, on data: what the library's host part launches there (on the CPU, on a runtime
+"""Edges of the operators on data: what the library's host part launches there (on the CPU, on a runtime
 that launches nothing but counts: fake_hip.c), and values against 64 bits on a GPU."""
 import numpy as np
 import pytest
