@@ -541,6 +541,75 @@ typedef struct {
 } mrl_dropout_desc;
 int32_t mrl_dropout(const mrl_dropout_desc* desc, void* hip_stream);
 
+/* Layer normalisation of rows, in front of a block of Matmuls:
+ *   mean = sum x / n,  var = sum (x - mean)^2 / n,  r = 1 / sqrt(var + eps)
+ *   out = (x - mean) r weight + bias
+ * over each of the b * m rows of n elements.  weight and bias are optional (1 and 0).  stats: 2 f32 a
+ * row without gaps, (mean, r) of the row, batch after batch: what the gradient needs; optional.  x, weight, bias and out
+ * may each be f32 or bf16.  out may be x itself. */
+typedef struct {
+  uint32_t b, m, n;              /* b * m, and each size, below 2^31                               */
+  float eps;                     /* finite, not negative                                           */
+  mrl_matrix x, out;             /* b x m x n, row-major                                           */
+  mrl_matrix weight, bias;       /* n neighbouring elements; optional                              */
+  void* stats;                   /* device, aligned to 4 bytes; optional                           */
+} mrl_layer_norm_desc;
+int32_t mrl_layer_norm(const mrl_layer_norm_desc* desc, void* hip_stream);
+
+/* Gradients of a loss, given `grad`, its gradient by out: with h = (x - mean) r and g = grad weight
+ *   d_x = residual + r (g - sum g / n - h sum(g h) / n)
+ *   d_weight = the sum of grad h, d_bias = the sum of grad, over batches and rows
+ * Each of the three is optional (its data NULL), and so is residual: the gradient that reaches x past
+ * the normalisation, as in a block with a residual.  d_x may be x, grad or residual itself.  n of 0: nothing is written. */
+typedef struct {
+  uint32_t b, m, n, reserved;
+  mrl_matrix grad, x, residual;  /* b x m x n, row-major                                           */
+  mrl_matrix weight;             /* as given to mrl_layer_norm                                     */
+  mrl_matrix d_x;                /* b x m x n, row-major                                           */
+  mrl_matrix d_weight, d_bias;   /* n neighbouring elements                                        */
+  const void* stats;             /* as mrl_layer_norm stored them                                  */
+} mrl_layer_norm_grad_desc;
+int32_t mrl_layer_norm_grad_bytes(const mrl_layer_norm_grad_desc* desc, size_t* bytes);
+int32_t mrl_layer_norm_grad(const mrl_layer_norm_grad_desc* desc, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Microscaled 4-bit floating point (MXFP4 of the OCP Microscaling Formats specification 1.0): a line of k values is kept in
+ * blocks of 32, each with a scale 2^e, e from -127 to 127, and 32 values of 0, 0.5, 1, 1.5, 2, 3, 4 and 6 and their negatives.
+ *   e = floor(log2(the block's largest magnitude)) - 2, at least -127 (also for a block of zeros)
+ *   value = the nearest one to x / 2^e, a tie to the one whose code is even, magnitudes beyond 6 to 6
+ * A block that holds an infinity or NaN stands for NaN, all of it: its scale is 255, its codes are 0.
+ *
+ * codes: b * lines lines of 64 bytes for each 128 values (k rounded up; 0 where there is none), two values a byte, the first
+ * in the low half; a code is the magnitude's number in the list above, plus 8 where it is negative.  Aligned to 16 bytes.
+ * scales: the byte e + 127 of every block, in the order in which the matrix instructions take them.  64
+ * lines (the last ones filled up with 0) by 128 values are 256 bytes: the scale of line 64 G + 32 i + 8 j + 4 k + l, block 4 s + g, is byte
+ *   ((((batch * groups + G) * steps + s) * 4 + g) * 16 + 4 j + l) * 4 + 2 i + k,   groups = ceil(lines / 64), steps = ceil(k / 128).
+ * Aligned to 4 bytes.  shared: every batch is the same matrix. */
+typedef struct { void *codes, *scales; uint32_t shared, reserved; } mrl_mx;
+
+/* x: b x lines x k, row-major, or column-major: neighbours of different lines are adjacent (a matrix k x lines that is
+ * row-major), f32 or bf16. */
+typedef struct {
+  uint32_t b, lines, k, reserved;        /* b * lines, and each size, below 2^31; k at most 2^24      */
+  mrl_matrix x;
+  mrl_mx blocks;
+} mrl_mx_desc;
+int32_t mrl_mx_quantize(const mrl_mx_desc* desc, void* hip_stream);        /* x -> blocks */
+int32_t mrl_mx_dequantize(const mrl_mx_desc* desc, void* hip_stream);      /* blocks -> x, row-major (exact in either type) */
+
+/* out = residual + f(lhs rhs + bias), as mrl_linear, of operands in blocks along k: rhs has n lines, lhs m; where lhs is given
+ * as a matrix it is quantised by the call as mrl_mx_quantize does.  Products within a block are exact, sums
+ * and the epilogue f32 (a sum whose parts leave f32's range is not defined). */
+typedef struct {
+  uint32_t b, m, k, n;           /* as for mrl_linear; k at most 2^24                               */
+  mrl_matrix lhs;                /* b x m x k, f32 or bf16, either layout; data NULL: lhs_blocks it is */
+  mrl_mx lhs_blocks, rhs;
+  mrl_matrix bias, residual;     /* optional                                                       */
+  mrl_matrix out;
+  uint32_t activation, reserved;
+} mrl_mx_linear_desc;
+int32_t mrl_mx_linear_bytes(const mrl_mx_linear_desc* desc, size_t* bytes);
+int32_t mrl_mx_linear(const mrl_mx_linear_desc* desc, void* d_workspace, size_t workspace_bytes, void* hip_stream);
+
 /* The operator of the Spec at x: sizes, types and layouts, strides of matrices without
  * gaps, bias and activation (data stays NULL; a FUSED Spec's bias is marked by its type
  * and a stride of 1).  For tables of MATMUL_ACCUM, MATMUL_PARALLEL, MATMUL_BOUNDED,

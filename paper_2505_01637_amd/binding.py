@@ -23,7 +23,8 @@ OK, E_INVAL, E_NOMEM, E_HIP, E_RANGE, E_BUFSZ, E_OVERFLOW = 0, -1, -2, -3, -4, -
 EXPORTS = ["mrl_target_create", "mrl_target_destroy", "mrl_geometry", "mrl_table_bytes", "mrl_solve", "mrl_solve_graph",
            "mrl_table_destroy", "mrl_query", "mrl_query_noalloc", "mrl_query_compressed", "mrl_rewrite_decode", "mrl_coord_of_spec",
            "mrl_emit_compressed", "mrl_schedule", "mrl_copy_dense", "mrl_linear_bytes", "mrl_linear", "mrl_linear_grad_bytes",
-           "mrl_linear_grad", "mrl_dropout", "mrl_spec_linear", "mrl_last_error"]
+           "mrl_linear_grad", "mrl_dropout", "mrl_layer_norm", "mrl_layer_norm_grad_bytes", "mrl_layer_norm_grad", "mrl_mx_quantize",
+           "mrl_mx_dequantize", "mrl_mx_linear_bytes", "mrl_mx_linear", "mrl_spec_linear", "mrl_last_error"]
 
 
 class MorelloError(RuntimeError):
@@ -112,10 +113,11 @@ def lib():
         _lib.mrl_target_destroy.restype = None
         _lib.mrl_table_destroy.restype = None
         # (the operators' calls are short: with these, plain integers and bytes go in without an object each)
-        for name in ("mrl_linear", "mrl_linear_grad"):
+        for name in ("mrl_linear", "mrl_linear_grad", "mrl_layer_norm_grad", "mrl_mx_linear"):
             getattr(_lib, name).argtypes = [C.c_char_p, C.c_void_p, C.c_size_t, C.c_void_p]
             getattr(_lib, name + "_bytes").argtypes = [C.c_char_p, C.c_void_p]
-        _lib.mrl_dropout.argtypes = [C.c_char_p, C.c_void_p]
+        for name in ("mrl_dropout", "mrl_layer_norm", "mrl_mx_quantize", "mrl_mx_dequantize"):
+            getattr(_lib, name).argtypes = [C.c_char_p, C.c_void_p]
     return _lib
 
 
@@ -482,15 +484,19 @@ ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 _LINEAR = struct.Struct("=4I" + "QIIqq" * 6 + "2I2Q")
 _LINEAR_GRAD = struct.Struct("=4I" + "QIIqq" * 7 + "2I2Q")
 _DROPOUT = struct.Struct("=2I" + "QIIqq" * 3 + "I4x2Q")
+_NORM = struct.Struct("=3If" + "QIIqq" * 4 + "Q")
+_NORM_GRAD = struct.Struct("=4I" + "QIIqq" * 7 + "Q")
+_MX = struct.Struct("=4I" + "QIIqq" + "QQII")
+_MX_LINEAR = struct.Struct("=4I" + "QIIqq" + "QQII" * 2 + "QIIqq" * 3 + "2I")
 _ABSENT = (0, 0, 0, 0, 0)
-_codes = _uint8 = None
+_codes = _uint8 = _float32 = None
 
 
 def _dtype_codes():
-    global _codes, _uint8
+    global _codes, _uint8, _float32
     if _codes is None:
         import torch
-        _codes, _uint8 = {torch.float32: 0, torch.bfloat16: 1}, torch.uint8
+        _codes, _uint8, _float32 = {torch.float32: 0, torch.bfloat16: 1}, torch.uint8, torch.float32
     return _codes
 
 
@@ -794,3 +800,240 @@ def dropout_grad(grad, *, dropout, seed=0, offset=0, out=None, stream=None):
 
 
 _dropout = dropout
+
+
+def _rows_count(name, t):
+    """(b, m, n) of a tensor of rows."""
+    sh = t.shape
+    if len(sh) == 2:
+        return 1, sh[0], sh[1]
+    if len(sh) == 3:
+        return tuple(sh)
+    raise MorelloError(E_INVAL, "%s has %d dimensions: two, or three with a batch" % (name, len(sh)))
+
+
+def _of(t):
+    return None if t is None else (t.shape, t.stride(), t.dtype)
+
+
+def _form_norm(key, x, weight, bias, dtype, out):
+    sizes = _rows_count("x", x)
+    if out is None:
+        out = x.new_empty(x.shape, dtype=x.dtype if dtype is None else dtype)
+    elif dtype is not None and out.dtype != dtype:
+        raise MorelloError(E_INVAL, "out is %s, not %s" % (out.dtype, dtype))
+    mats = [_rows("x", x, x.shape), _rows("out", out, x.shape)]
+    for name, v in (("weight", weight), ("bias", bias)):
+        mats.append(_ABSENT if v is None else _vector(name, v, sizes[2]))
+    return _keep_form(key, (sizes, *(m[1:] for m in mats), out.dtype))
+
+
+def layer_norm(x, weight=None, bias=None, *, eps=1e-5, stats=False, dtype=None, out=None, stream=None):
+    """(x - mean) r weight + bias over the last dimension, r = 1 / sqrt(variance + eps) (mrl_layer_norm); with stats=True
+    also (mean, r) of every row, float32 of x's leading dimensions by 2, which layer_norm_grad needs: (out, stats).
+
+    x: m x n or b x m x n, rows at any stride; weight, bias: n elements, 1 and 0 if None; each float32 or bfloat16.
+    dtype: out's type (x's if None); out: a tensor to write to, which may be x itself; stream: as for linear."""
+    on = _elsewhere((x, weight, bias, out), stream)
+    if on is not None:
+        with on:
+            return layer_norm(x, weight, bias, eps=eps, stats=stats, dtype=dtype, out=out)
+    key = ("norm", x.shape, x.stride(), x.dtype, _of(weight), _of(bias), _of(out), dtype)
+    sizes, mx, mo, mw, mb, dtype = _forms.get(key) or _form_norm(key, x, weight, bias, dtype, out)
+    if not 0.0 <= eps <= 3.4e38:
+        raise MorelloError(E_INVAL, "eps of %r is negative or not finite" % (eps,))
+    if out is None:
+        out = x.new_empty(x.shape, dtype=dtype)
+    kept = x.new_empty(x.shape[:-1] + (2,), dtype=_float32) if stats else None
+    desc = _NORM.pack(*sizes, eps, x.data_ptr(), *mx, out.data_ptr(), *mo, 0 if weight is None else weight.data_ptr(), *mw,
+                      0 if bias is None else bias.data_ptr(), *mb, kept.data_ptr() if stats else 0)
+    rc = lib().mrl_layer_norm(desc, _raw_stream(x.get_device()))
+    if rc:
+        _check(rc)
+    return (out, kept) if stats else out
+
+
+def _form_norm_grad(key, grad, x, stats, weight, bias, residual, need_x):
+    sizes = _rows_count("x", x)
+    if stats.shape != x.shape[:-1] + (2,) or stats.dtype != _float32 or not stats.is_contiguous():
+        raise MorelloError(E_INVAL, "stats of shape %s, %s: what layer_norm returns has shape %s, float32, without gaps" % (tuple(stats.shape), stats.dtype,
+                                                                                                            tuple(x.shape[:-1]) + (2,)))
+    mats = [_rows("grad", grad, x.shape), _rows("x", x, x.shape), _ABSENT if residual is None else _rows("residual", residual, x.shape),
+            _ABSENT if weight is None else _vector("weight", weight, sizes[2]), _rows("d_x", x.new_empty(x.shape), x.shape) if need_x else _ABSENT]
+    for name, v in (("weight", weight), ("bias", bias)):
+        mats.append(_ABSENT if v is None else _vector(name, v.new_empty(v.shape), sizes[2]))
+    desc = _NORM_GRAD.pack(*sizes, 0, *(v for m in mats for v in m), stats.data_ptr())
+    n = C.c_size_t()
+    _check(lib().mrl_layer_norm_grad_bytes(desc, C.addressof(n)))
+    return _keep_form(key, (sizes, *(m[1:] for m in mats), n.value))
+
+
+def layer_norm_grad(grad, x, stats, weight=None, bias=None, residual=None, *, need_x=True, workspace=None, stream=None):
+    """(d_x, d_weight, d_bias) of layer_norm(x, weight, bias), given `grad`, the gradient by its out, and the
+    `stats` that it returned (mrl_layer_norm_grad).  Each has its operand's type; None for d_x without need_x, and for a
+    weight or bias that is None.  residual: the gradient that reaches x past the normalisation, added to
+    d_x."""
+    on = _elsewhere((x, grad, stats, weight, bias, residual, workspace), stream)
+    if on is not None:
+        with on:
+            return layer_norm_grad(grad, x, stats, weight, bias, residual, need_x=need_x, workspace=workspace)
+    key = ("norm_grad", grad.shape, grad.stride(), grad.dtype, x.shape, x.stride(), x.dtype, _of(stats), _of(weight), _of(bias), _of(residual), need_x)
+    form = _forms.get(key)
+    if form is None:
+        form = _form_norm_grad(key, grad, x, stats, weight, bias, residual, need_x)
+    sizes, mg, mx, mr, mw, m_x, m_weight, m_bias, need = form
+    d_x = x.new_empty(x.shape) if need_x else None
+    d_weight = None if weight is None else weight.new_empty(weight.shape)
+    d_bias = None if bias is None else bias.new_empty(bias.shape)
+    desc = _NORM_GRAD.pack(*sizes, 0, grad.data_ptr(), *mg, x.data_ptr(), *mx, 0 if residual is None else residual.data_ptr(), *mr,
+                           0 if weight is None else weight.data_ptr(), *mw, d_x.data_ptr() if need_x else 0, *m_x,
+                           0 if weight is None else d_weight.data_ptr(), *m_weight, 0 if bias is None else d_bias.data_ptr(), *m_bias, stats.data_ptr())
+    _run(desc, _lib.mrl_layer_norm_grad, need, workspace, x)
+    return d_x, d_weight, d_bias
+
+
+# ---- microscaled 4-bit floating point
+
+class MX:
+    """A tensor in blocks of 32 values along k: 4 bits a value and a byte of scale a block (the header at mrl_mx has the format).
+
+    codes: uint8 of (batch,) lines x 64 ceil(k / 128); scales: uint8 of (batch,) ceil(lines / 64) x ceil(k / 128) x 4 x 16 x 4, both
+    without gaps.  dim: the dimension that the blocks run along, -1 (the lines are rows: the tensor is lines x k) or -2 (they are
+    columns: k x lines, as linear's rhs).  dtype: the type that the tensor had and is read back in."""
+    __slots__ = ("codes", "scales", "k", "dim", "dtype", "shape", "_key")
+
+    def __init__(self, codes, scales, k, *, dim=-1, dtype=None):
+        if dtype is None:
+            import torch
+            dtype = torch.bfloat16
+        # (worked out once for shapes: an MX may be made anew around the same tensors for every call)
+        key = ("mx", codes.shape, scales.shape, codes.stride(), scales.stride(), codes.dtype, scales.dtype, k, dim, dtype)
+        self.codes, self.scales, self.k, self.dim, self.dtype = codes, scales, k, dim, dtype
+        self.shape, self._key = _forms.get(key) or _form_mx(key, codes, scales, k, dim, dtype)
+
+    @property
+    def lines(self):
+        return self.codes.shape[-2]
+
+    def __repr__(self):
+        return "MX(shape=%s, dim=%d, dtype=%s)" % (tuple(self.shape), self.dim, self.dtype)
+
+
+def _form_mx(key, codes, scales, k, dim, dtype):
+    _dtype_codes()
+    if dim not in (-1, -2):
+        raise MorelloError(E_INVAL, "dim of %r: blocks run along the last dimension (-1) or the one before (-2)" % (dim,))
+    if dtype not in _codes:
+        raise MorelloError(E_INVAL, "%s: float32 and bfloat16 are what there is" % (dtype,))
+    if codes.dtype != _uint8 or scales.dtype != _uint8 or not codes.is_contiguous() or not scales.is_contiguous():
+        raise MorelloError(E_INVAL, "codes and scales are uint8 without gaps")
+    if len(codes.shape) not in (2, 3) or not 0 <= k < 1 << 31:
+        raise MorelloError(E_INVAL, "codes of shape %s: lines, or a batch of them" % (tuple(codes.shape),))
+    lead, lines, steps = tuple(codes.shape[:-2]), codes.shape[-2], -(-k // 128)
+    if codes.shape[-1] != 64 * steps or tuple(scales.shape) != lead + (-(-lines // 64), steps, 4, 16, 4):
+        raise MorelloError(E_INVAL, "codes of shape %s and scales of shape %s are not those of %d lines of %d values" % (
+            tuple(codes.shape), tuple(scales.shape), lines, k))
+    shape = codes.shape[:-2] + ((lines, k) if dim == -1 else (k, lines))
+    return _keep_form(key, (shape, (shape, dim, dtype)))
+
+
+def mx_quantize(x, *, dim=-1, out=None, stream=None):
+    """x in blocks of 32 values along `dim` (-1, or -2 as for linear's rhs): an MX (mrl_mx_quantize).  x: two dimensions, or three with a
+    batch; float32 or bfloat16, row- or column-major with any stride between lines.  out: an MX of this shape and dim to write to."""
+    on = _elsewhere((x,) if out is None else (x, out.codes, out.scales), stream)
+    if on is not None:
+        with on:
+            return mx_quantize(x, dim=dim, out=out)
+    key = ("mx_quantize", x.shape, x.stride(), x.dtype, dim)
+    form = _forms.get(key)
+    if form is None:
+        b, _, _ = _rows_count("x", x)
+        if dim not in (-1, -2):
+            raise MorelloError(E_INVAL, "dim of %r: blocks run along the last dimension (-1) or the one before (-2)" % (dim,))
+        # (lines along k: of x itself, or of its transpose)
+        lines = x if dim == -1 else x.transpose(-1, -2)
+        n, k = lines.shape[-2:]
+        steps = -(-k // 128)
+        form = _keep_form(key, ((b, n, k, 0), _matrix("x", lines)[1:], lines.shape[:-2] + (n, 64 * steps), lines.shape[:-2] + (-(-n // 64), steps, 4, 16, 4)))
+    sizes, m, codes, scales = form
+    if out is None:
+        out = MX(x.new_empty(codes, dtype=_uint8), x.new_empty(scales, dtype=_uint8), sizes[2], dim=dim, dtype=x.dtype)
+    elif out.shape != x.shape or out.dim != dim:
+        raise MorelloError(E_INVAL, "out is %r: x has shape %s, dim %d" % (out, tuple(x.shape), dim))
+    rc = lib().mrl_mx_quantize(_MX.pack(*sizes, x.data_ptr(), *m, out.codes.data_ptr(), out.scales.data_ptr(), 0, 0), _raw_stream(x.get_device()))
+    if rc:
+        _check(rc)
+    return out
+
+
+def mx_dequantize(q, *, dtype=None, stream=None):
+    """What an MX stands for, in q.dtype or `dtype`, both exact (mrl_mx_dequantize); with dim=-2 it comes column-major, as its lines are."""
+    on = _elsewhere((q.codes, q.scales), stream)
+    if on is not None:
+        with on:
+            return mx_dequantize(q, dtype=dtype)
+    dtype = q.dtype if dtype is None else dtype
+    key = ("mx_dequantize", q._key, dtype)
+    form = _forms.get(key)
+    if form is None:
+        lead, lines, k = q.codes.shape[:-2], q.lines, q.k
+        like = q.codes.new_empty(lead + (lines, k), dtype=dtype)
+        form = _keep_form(key, (_rows_count("x", like) + (0,), lead + (lines, k), _rows("x", like, like.shape)[1:]))
+    sizes, shape, m = form
+    out = q.codes.new_empty(shape, dtype=dtype)
+    rc = lib().mrl_mx_dequantize(_MX.pack(*sizes, out.data_ptr(), *m, q.codes.data_ptr(), q.scales.data_ptr(), 0, 0), _raw_stream(out.get_device()))
+    if rc:
+        _check(rc)
+    return out if q.dim == -1 else out.transpose(-1, -2)
+
+
+def _form_mx_linear(key, lhs, rhs, blocks, bias, residual, out, dtype, activation):
+    if rhs.dim != -2 or (blocks and lhs.dim != -1):
+        raise MorelloError(E_INVAL, "lhs is in blocks along its last dimension, rhs along the one before: %r, %r" % (lhs, rhs))
+    ls, rs = lhs.shape, rhs.shape
+    b, m, k = _rows_count("lhs", lhs)
+    if k != rs[-2] or (len(rs) == 3 and (len(ls) != 3 or ls[0] != rs[0])):
+        raise MorelloError(E_INVAL, "lhs of shape %s does not go with rhs of shape %s" % (tuple(ls), tuple(rs)))
+    n = rs[-1]
+    shape = ls[:-1] + (n,)
+    like = lhs.codes if blocks else lhs
+    if out is None:
+        out = like.new_empty(shape, dtype=lhs.dtype if dtype is None else dtype)
+    elif dtype is not None and out.dtype != dtype:
+        raise MorelloError(E_INVAL, "out is %s, not %s" % (out.dtype, dtype))
+    ml = _ABSENT if blocks else _matrix("lhs", lhs)
+    mats = [_ABSENT if bias is None else _vector("bias", bias, n), _ABSENT if residual is None else _rows("residual", residual, shape), _rows("out", out, shape)]
+    act = _activation(activation)
+    sizes, shared = (b, m, k, n), int(len(rs) == 2)
+    desc = _MX_LINEAR.pack(*sizes, *ml, *((like.data_ptr(), lhs.scales.data_ptr()) if blocks else (0, 0)), 0, 0, rhs.codes.data_ptr(), rhs.scales.data_ptr(), shared, 0,
+                           *(v for m in mats for v in m), act, 0)
+    need = C.c_size_t()
+    _check(lib().mrl_mx_linear_bytes(desc, C.addressof(need)))
+    return _keep_form(key, (shape, out.dtype, sizes, shared, ml[1:], *(m[1:] for m in mats), act, need.value))
+
+
+def mx_linear(lhs, rhs, bias=None, residual=None, *, activation="none", dtype=None, out=None, workspace=None, stream=None):
+    """out = residual + f(lhs rhs + bias) (mrl_mx_linear), as linear, of operands in blocks of 4-bit values.
+
+    rhs: an MX of k x n or b x k x n with dim=-2 (mx_quantize(weight, dim=-2)); lhs: an MX of m x k or b x m x k with dim=-1, or a tensor,
+    which the call quantises as mx_quantize does.  The other arguments are linear's; dtype: out's type (lhs's if None)."""
+    blocks = type(lhs) is MX
+    on = _elsewhere((lhs.codes if blocks else lhs, lhs.scales if blocks else None, rhs.codes, rhs.scales, bias, residual, out, workspace), stream)
+    if on is not None:
+        with on:
+            return mx_linear(lhs, rhs, bias, residual, activation=activation, dtype=dtype, out=out, workspace=workspace)
+    key = ("mx_linear", lhs._key if blocks else (lhs.shape, lhs.stride(), lhs.dtype), rhs._key, _of(bias), _of(residual), _of(out), dtype, activation)
+    form = _forms.get(key)
+    if form is None:
+        form = _form_mx_linear(key, lhs, rhs, blocks, bias, residual, out, dtype, activation)
+    shape, dtype, sizes, shared, ml, mb, ms, mo, act, need = form
+    if blocks:
+        like, first = lhs.codes, (0, *ml, lhs.codes.data_ptr(), lhs.scales.data_ptr())
+    else:
+        like, first = lhs, (lhs.data_ptr(), *ml, 0, 0)
+    if out is None:
+        out = like.new_empty(shape, dtype=dtype)
+    desc = _MX_LINEAR.pack(*sizes, *first, 0, 0, rhs.codes.data_ptr(), rhs.scales.data_ptr(), shared, 0, 0 if bias is None else bias.data_ptr(), *mb,
+                           0 if residual is None else residual.data_ptr(), *ms, out.data_ptr(), *mo, act, 0)
+    _run(desc, _lib.mrl_mx_linear, need, workspace, like)
+    return out

@@ -228,6 +228,53 @@ struct DropRows {
 };
 hipError_t launch_drop(const DropRows& d, hipStream_t st);
 
+// Layer normalisation of the rows of `batches` x M x N (N elements each), and what its gradient needs of them (mean, r) in `stats`, two f32 a row
+struct NormRows {
+  RowsOf x, out;
+  const void *weight, *bias;     // nullptr: 1, 0
+  uint32_t weight_bf16, bias_bf16;
+  float* stats;                  // nullptr: not wanted
+  uint32_t batches, M, N;
+  float eps;
+};
+hipError_t launch_norm(const NormRows& p, hipStream_t st);
+
+struct NormGrad {
+  RowsOf grad, x, residual, dx;  // dx.data nullptr: not wanted
+  const void* weight;
+  const float* stats;
+  void *dweight, *dbias;         // nullptr: not wanted
+  uint32_t weight_bf16, dweight_bf16, dbias_bf16;
+  uint32_t batches, M, N;
+};
+uint64_t norm_grad_bytes(const NormGrad& p);
+hipError_t launch_norm_grad(const NormGrad& p, float* partial, hipStream_t st);
+
+// `batches` matrices of `lines` lines of k values in blocks of 32 along k: 4 bits a value, a byte of scale a block (the header of the ABI has
+// the format).  Lines are whole steps of 128 values, 64 bytes; scales come for 64 lines and a step at a time.
+constexpr uint32_t mx_steps(uint32_t k) { return (k + 127) / 128; }
+constexpr uint64_t mx_code_bytes(uint32_t lines, uint32_t k) { return (uint64_t)lines * mx_steps(k) * 64; }
+constexpr uint64_t mx_scale_bytes(uint32_t lines, uint32_t k) { return ((uint64_t)lines + 63) / 64 * mx_steps(k) * 256; }
+
+// between x and its blocks, either way.  kc: x's neighbours along k are adjacent (RowsOf's rows are lines), else those along the lines (its rows are k).
+struct MxRows {
+  RowsOf x;
+  uint8_t *codes, *scales;
+  uint32_t kc, batches, lines, k;
+  uint32_t shared;               // blocks -> x: every batch is the same matrix
+};
+hipError_t launch_mx_quantize(const MxRows& p, hipStream_t st);
+hipError_t launch_mx_dequantize(const MxRows& p, hipStream_t st);
+
+// A product of operands in blocks.  p.a and p.b are codes, counted in units of four values (two bytes), K a multiple of 32 of them
+struct MxProduct {
+  Product p;
+  const uint8_t *scales_a, *scales_b;
+  int64_t scales_batch_a, scales_batch_b;
+};
+ProductPlan plan_mx(const MxProduct& p);
+hipError_t launch_mx(const MxProduct& p, const ProductPlan& plan, float* partial, hipStream_t st);       // without the sum over splits
+
 int32_t fail_with(int32_t code, const char* message);      // sets mrl_last_error, returns code
 
 }  // namespace mrl

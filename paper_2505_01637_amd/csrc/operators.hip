@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cstdarg>
 #include <cstdio>
 
@@ -236,6 +237,119 @@ int32_t plan_grad(const mrl_linear_grad_desc& d, GradPlan* out) {
   return MRL_OK;
 }
 
+int32_t check_stats(const void* stats, uint64_t rows, bool needed) {
+  CHECK(!needed || stats || !rows, "stats is NULL");
+  CHECK((uintptr_t)stats % 4 == 0, "stats is not aligned to its elements");
+  return MRL_OK;
+}
+
+int32_t norm_grad(const mrl_layer_norm_grad_desc& d, NormGrad* out) {
+  int32_t rc = check_common(d.b, d.m, 0, d.n, MRL_ACT_NONE, 0);
+  const uint64_t b = d.b;
+  const bool x = d.d_x.data || d.d_weight.data;
+  if (!rc) rc = check_matrix("grad", d.grad, x || d.d_bias.data ? b : 0, d.m, d.n, false, false);
+  if (!rc) rc = check_matrix("x", d.x, x ? b : 0, d.m, d.n, false, false);
+  if (!rc && d.residual.data) rc = check_matrix("residual", d.residual, b, d.m, d.n, false, false);
+  if (!rc) rc = check_vector("weight", d.weight, d.weight.data ? d.n : 0);
+  if (!rc && d.d_x.data) rc = check_matrix("d_x", d.d_x, b, d.m, d.n, true, false);
+  if (!rc && d.d_weight.data) rc = check_vector("d_weight", d.d_weight, d.n);
+  if (!rc && d.d_bias.data) rc = check_vector("d_bias", d.d_bias, d.n);
+  if (!rc) rc = check_stats(d.stats, b * d.m * d.n, x);
+  if (rc) return rc;
+  *out = NormGrad{rows_of(d.grad), rows_of(d.x), rows_of(d.residual), rows_of(d.d_x), d.weight.data, (const float*)d.stats, d.d_weight.data, d.d_bias.data,
+                  d.weight.dtype == MRL_BF16, d.d_weight.dtype == MRL_BF16, d.d_bias.dtype == MRL_BF16, d.b, d.m, d.n};
+  return MRL_OK;
+}
+
+constexpr uint32_t kMxMost = 1u << 24;       // k: offsets of a tile's lines are counted in 31 bits
+
+int32_t check_mx(const char* name, const mrl_mx& x, uint64_t b, uint32_t lines, uint32_t k) {
+  CHECK(k <= kMxMost, "%s: lines of %u values: 2^24 are the most", name, k);
+  if (!b || !lines || !k) return MRL_OK;
+  CHECK(x.codes && x.scales, "%s: codes or scales are NULL", name);
+  CHECK((uintptr_t)x.codes % 16 == 0 && (uintptr_t)x.scales % 4 == 0, "%s: codes are not aligned to 16 bytes, or scales not to 4", name);
+  return MRL_OK;
+}
+
+int32_t mx_rows(const mrl_mx_desc& d, bool back, MxRows* out) {
+  int32_t rc = check_common(d.b, d.lines, d.k, 0, MRL_ACT_NONE, 0);
+  if (!rc) rc = check_matrix("x", d.x, d.b, d.lines, d.k, back, !back);
+  if (!rc) rc = check_mx("blocks", d.blocks, d.b, d.lines, d.k);
+  if (rc) return rc;
+  CHECK(back || !d.blocks.shared || d.b <= 1, "blocks of several batches cannot be written to one matrix");
+  *out = MxRows{rows_of(d.x), (uint8_t*)d.blocks.codes, (uint8_t*)d.blocks.scales, d.x.layout == MRL_ROW_MAJOR, d.b, d.lines, d.k, d.blocks.shared != 0};
+  return MRL_OK;
+}
+
+// What a product of blocks is made of: lhs's own ones in the workspace (codes, then scales), then the partial sums.
+struct MxPlan {
+  bool quantizes;
+  MxRows lhs;
+  MxProduct by;
+  ProductPlan plan;
+  size_t codes_bytes, scales_bytes;
+  size_t bytes() const { return codes_bytes + scales_bytes + (size_t)plan.partial_bytes; }
+};
+
+int32_t plan_mx_linear(const mrl_mx_linear_desc& d, MxPlan* out) {
+  int32_t rc = check_common(d.b, d.m, d.k, d.n, d.activation, 0);
+  if (rc) return rc;
+  MxPlan g{};
+  const uint64_t b = d.b, reads = d.n ? b : 0;
+  g.quantizes = d.lhs.data && d.k;
+  CHECK(!d.lhs.data || !d.lhs_blocks.codes, "lhs is given twice");
+  if (d.lhs.data) rc = check_matrix("lhs", d.lhs, reads, d.m, d.k, false, true);
+  if (!rc) rc = check_mx("lhs", d.lhs_blocks, d.lhs.data ? 0 : reads, d.m, d.k);
+  if (!rc) rc = check_mx("rhs", d.rhs, d.m ? b : 0, d.n, d.k);
+  if (!rc && d.bias.data) rc = check_vector("bias", d.bias, d.n);
+  if (!rc && d.residual.data) rc = check_matrix("residual", d.residual, b, d.m, d.n, false, false);
+  if (!rc) rc = check_matrix("out", d.out, b, d.m, d.n, true, false);
+  if (rc) return rc;
+  Product& p = g.by.p;
+  p.bf16 = 1;
+  p.a_kc = p.b_kc = 1;
+  p.segs = 1;
+  p.batches = d.b;
+  p.M = d.m;
+  p.N = d.n;
+  p.K = mx_steps(d.k) * 32;
+  p.e.out = rows_of(d.out);
+  p.e.residual = rows_of(d.residual);
+  p.e.bias = d.bias.data;
+  p.e.bias_bf16 = d.bias.dtype == MRL_BF16;
+  p.e.activation = d.activation;
+  const auto follows = [&](const RowsOf& r) { return !r.data || (uint64_t)r.batch == (uint64_t)d.m * (uint64_t)r.ld; };
+  g.lhs = MxRows{rows_of(d.lhs), nullptr, nullptr, d.lhs.layout == MRL_ROW_MAJOR, d.b, d.m, d.k, 0};
+  // batches that share rhs and follow each other are rows of one product; a lhs in blocks is so where its batches are whole groups of lines
+  const bool one = d.lhs.data ? g.lhs.kc && follows(g.lhs.x) : d.m % 64 == 0 && !d.lhs_blocks.shared;
+  if (d.b > 1 && d.rhs.shared && one && follows(p.e.out) && follows(p.e.residual)) {
+    p.M = g.lhs.lines = d.b * d.m;
+    p.batches = g.lhs.batches = 1;
+  }
+  p.lda = p.ldb = p.wa = p.wb = p.K;
+  p.a = d.lhs_blocks.codes;
+  p.b = d.rhs.codes;
+  g.by.scales_a = (const uint8_t*)d.lhs_blocks.scales;
+  g.by.scales_b = (const uint8_t*)d.rhs.scales;
+  if (p.batches > 1) {
+    const bool sa = !d.lhs.data && d.lhs_blocks.shared, sb = d.rhs.shared;
+    p.batch_a = sa ? 0 : (int64_t)mx_code_bytes(p.M, d.k) / 2;
+    p.batch_b = sb ? 0 : (int64_t)mx_code_bytes(p.N, d.k) / 2;
+    g.by.scales_batch_a = sa ? 0 : (int64_t)mx_scale_bytes(p.M, d.k);
+    g.by.scales_batch_b = sb ? 0 : (int64_t)mx_scale_bytes(p.N, d.k);
+  }
+  g.plan = plan_mx(g.by);
+  if ((rc = check_product(p, g.plan))) return rc;
+  if (g.quantizes && p.M && p.N && p.batches) {
+    g.codes_bytes = align_up((size_t)(p.batches * mx_code_bytes(p.M, d.k)));
+    g.scales_bytes = align_up((size_t)(p.batches * mx_scale_bytes(p.M, d.k)));
+  } else {
+    g.quantizes = false;
+  }
+  *out = g;
+  return MRL_OK;
+}
+
 int32_t check_workspace(const void* d_workspace, size_t have, size_t need) {
   if (!need) return MRL_OK;
   if (have < need) return refuse(MRL_E_NOMEM, "workspace of %zu bytes, %zu are needed", have, need);
@@ -319,6 +433,84 @@ int32_t mrl_dropout(const mrl_dropout_desc* desc, void* hip_stream) {
   if (!rc) rc = check_matrix("out", d.out, 1, d.m, d.n, true, false);
   if (rc) return rc;
   return hip_status(launch_drop(DropRows{rows_of(d.x), rows_of(d.residual), rows_of(d.out), d.m, d.n, drop_of(d.drop, d.seed, d.offset)}, (hipStream_t)hip_stream));
+}
+
+int32_t mrl_layer_norm(const mrl_layer_norm_desc* desc, void* hip_stream) {
+  CHECK(desc, "NULL argument");
+  const mrl_layer_norm_desc& d = *desc;
+  int32_t rc = check_common(d.b, d.m, 0, d.n, MRL_ACT_NONE, 0);
+  CHECK(d.eps >= 0.0f && d.eps <= FLT_MAX, "eps is negative or not finite");
+  if (!rc) rc = check_matrix("x", d.x, d.b, d.m, d.n, false, false);
+  if (!rc) rc = check_matrix("out", d.out, d.b, d.m, d.n, true, false);
+  if (!rc) rc = check_vector("weight", d.weight, d.weight.data ? d.n : 0);
+  if (!rc) rc = check_vector("bias", d.bias, d.bias.data ? d.n : 0);
+  if (!rc) rc = check_stats(d.stats, 0, false);
+  if (rc) return rc;
+  return hip_status(launch_norm(NormRows{rows_of(d.x), rows_of(d.out), d.weight.data, d.bias.data, d.weight.dtype == MRL_BF16, d.bias.dtype == MRL_BF16,
+                                         (float*)d.stats, d.b, d.m, d.n, d.eps}, (hipStream_t)hip_stream));
+}
+
+int32_t mrl_layer_norm_grad_bytes(const mrl_layer_norm_grad_desc* desc, size_t* bytes) {
+  CHECK(desc && bytes, "NULL argument");
+  NormGrad g;
+  const int32_t rc = norm_grad(*desc, &g);
+  if (rc) return rc;
+  *bytes = norm_grad_bytes(g);
+  return MRL_OK;
+}
+
+int32_t mrl_layer_norm_grad(const mrl_layer_norm_grad_desc* desc, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+  CHECK(desc, "NULL argument");
+  NormGrad g;
+  int32_t rc = norm_grad(*desc, &g);
+  if (rc) return rc;
+  if ((rc = check_workspace(d_workspace, workspace_bytes, norm_grad_bytes(g)))) return rc;
+  return hip_status(launch_norm_grad(g, (float*)d_workspace, (hipStream_t)hip_stream));
+}
+
+int32_t mrl_mx_quantize(const mrl_mx_desc* desc, void* hip_stream) {
+  CHECK(desc, "NULL argument");
+  MxRows p;
+  const int32_t rc = mx_rows(*desc, false, &p);
+  return rc ? rc : hip_status(launch_mx_quantize(p, (hipStream_t)hip_stream));
+}
+
+int32_t mrl_mx_dequantize(const mrl_mx_desc* desc, void* hip_stream) {
+  CHECK(desc, "NULL argument");
+  MxRows p;
+  const int32_t rc = mx_rows(*desc, true, &p);
+  return rc ? rc : hip_status(launch_mx_dequantize(p, (hipStream_t)hip_stream));
+}
+
+int32_t mrl_mx_linear_bytes(const mrl_mx_linear_desc* desc, size_t* bytes) {
+  CHECK(desc && bytes, "NULL argument");
+  MxPlan g;
+  const int32_t rc = plan_mx_linear(*desc, &g);
+  if (rc) return rc;
+  *bytes = g.bytes();
+  return MRL_OK;
+}
+
+int32_t mrl_mx_linear(const mrl_mx_linear_desc* desc, void* d_workspace, size_t workspace_bytes, void* hip_stream) {
+  CHECK(desc, "NULL argument");
+  MxPlan g;
+  int32_t rc = plan_mx_linear(*desc, &g);
+  if (rc) return rc;
+  if ((rc = check_workspace(d_workspace, workspace_bytes, g.bytes()))) return rc;
+  const hipStream_t st = (hipStream_t)hip_stream;
+  hipError_t e = hipSuccess;
+  if (g.quantizes) {
+    g.by.p.a = g.lhs.codes = (uint8_t*)d_workspace;
+    g.by.scales_a = g.lhs.scales = (uint8_t*)d_workspace + g.codes_bytes;
+    e = launch_mx_quantize(g.lhs, st);
+  }
+  float* const partial = (float*)((char*)d_workspace + g.codes_bytes + g.scales_bytes);
+  if (e == hipSuccess) e = launch_mx(g.by, g.plan, partial, st);
+  const Product* const products[2] = {&g.by.p, nullptr};
+  const ProductPlan* const plans[2] = {&g.plan, nullptr};
+  const float* const partials[2] = {partial, nullptr};
+  if (e == hipSuccess && g.plan.splits > 1) e = launch_rest(products, plans, partials, nullptr, nullptr, st);
+  return hip_status(e);
 }
 
 }  // extern "C"

@@ -204,7 +204,8 @@ __device__ __forceinline__ void put8(const Product& p, const Place& at, uint32_t
 // through shared memory that is the wave's own, PASS blocks of 16 rows at a time, so that a row's results are stored side by side (lines of
 // 128 bytes and more) and the epilogue is a short loop: unrolled over the registers it is as long as the instruction cache.  The 16-byte chunks of a
 // row lie at their number xor the row's, against bank conflicts.
-template <class T, int PASS, int BM, int BN>
+// MIXED: A's rows are in B's order.
+template <class T, int PASS, int BM, int BN, bool MIXED = false>
 __device__ __forceinline__ void write_out(const Product& p, const Place& at, uint32_t splits, uint32_t m0, uint32_t n0, uint32_t lane,
                                           const f32x4 (&acc)[BM][BN], char* mine, float* __restrict__ partial) {
   constexpr uint32_t CHUNKS = BN * 4, GROUPS = BN * 2, ROWS = 64 / GROUPS;      // chunks and groups of 8 columns of a row; rows at a time
@@ -227,7 +228,7 @@ __device__ __forceinline__ void write_out(const Product& p, const Place& at, uin
     if (n < p.N) {
 #pragma unroll 2
       for (uint32_t r = lane / GROUPS; r < 16 * PASS; r += ROWS) {
-        const uint32_t m = m0 + row_of<T, false>(h + (r >> 4), r & 15);
+        const uint32_t m = m0 + row_of<T, MIXED>(h + (r >> 4), r & 15);
         if (m >= p.M) continue;
         float v[8];
 #pragma unroll

@@ -1,0 +1,328 @@
+"""Layer normalisation and its gradients (binding.layer_norm, layer_norm_grad) against 64 bits.
+
+Tolerances.  u = 2^-24.  A row's sums are taken by lanes that add at most n / 64 + 8 elements each, whose sums are added in at
+most 24 steps more, so a sum of n values is within c u times the sum of their magnitudes, c = n / 64 + 32.  With d = x - about (one
+rounding; about is the mean but for c u mean|x|), the rest that puts the mean right is within c u mean|d|, the variance within (c + 8) u of itself
+(all its terms are positive), r within half of that and three roundings.  So h is within (c / 2 + 10) u |h| + (c + 4) u r mean|d|, plus
+what second-order terms of the shift leave, c^2 u^2 r mean|x|; weight and bias add two roundings.
+Gradient: h and g are two roundings from what the given stats make them; S g and S g h within (c + 6) u of the sums of
+magnitudes; dx adds five roundings of its terms; a sum over m rows is within (m + 8) u of the sum of magnitudes.
+What is stored is rounded once more.
+"""
+import numpy as np
+import pytest
+
+from paper_2505_01637_amd import binding as B
+from test_operators import U, UNIT, _torch, check, f64, strided
+
+gpu = pytest.mark.gpu
+EPS = 1e-5
+
+
+def norm_of(x, w, b, eps=EPS):
+    """(out, mean, r, bound of out) in 64 bits; the bound without the rounding of what is stored."""
+    n = x.shape[-1]
+    c = n / 64 + 32
+    mean = x.mean(-1, keepdims=True)
+    d = x - mean
+    r = 1 / np.sqrt((d * d).mean(-1, keepdims=True) + eps)
+    h = d * r
+    w = np.ones(n) if w is None else w
+    off = (c / 2 + 10) * U * np.abs(h) + (c + 4) * U * r * np.abs(d).mean(-1, keepdims=True) + (c * U) ** 2 * r * np.abs(x).mean(-1, keepdims=True)
+    out = h * w
+    bound = off * np.abs(w) + 2 * U * np.abs(out)
+    if b is not None:
+        out = out + b
+        bound = bound + U * np.abs(out)
+    return out, mean[..., 0], r[..., 0], bound
+
+
+def vector(rng, n, dtype, scale, shift):
+    if dtype is None:
+        return None
+    torch, types = _torch()
+    return torch.from_numpy(rng.standard_normal(n) * scale + shift).to(types[dtype]).cuda()
+
+
+def case_norm(shape, dtype="f32", weight="f32", bias="f32", out=None, gap=0, start=0, offset=0.5, seed=3):
+    torch, types = _torch()
+    rng = np.random.default_rng(seed)
+    n = shape[-1]
+    x = strided(rng.standard_normal(shape) * np.exp(0.5 * rng.standard_normal(n)) + offset, dtype, gap=gap, start=start)
+    w, b = vector(rng, n, weight, 0.2, 1.0), vector(rng, n, bias, 0.1, 0.0)
+    got, stats = B.layer_norm(x, w, b, eps=EPS, stats=True, dtype=types[out or dtype])
+    want, mean, r, bound = norm_of(f64(x), None if w is None else f64(w), None if b is None else f64(b))
+    check(got, want, bound, out or dtype, "out")
+    X, c = f64(x), n / 64 + 32
+    check(stats[..., 0], mean, (c * U * np.abs(X - mean[..., None]).mean(-1) + (c * U) ** 2 * np.abs(X).mean(-1)), "f32", "mean")
+    check(stats[..., 1], r, (c / 2 + 8) * U * r, "f32", "r")
+    assert torch.equal(B.layer_norm(x, w, b, eps=EPS, dtype=types[out or dtype]), got)
+    return x, w, b, got, stats
+
+
+def case_grad(shape, dtype="f32", weight="f32", bias="f32", residual=True, grad=None, need_x=True, gap=0, start=0, seed=4):
+    torch, types = _torch()
+    rng = np.random.default_rng(seed)
+    n, m = shape[-1], int(np.prod(shape[:-1]))
+    x = strided(rng.standard_normal(shape) + 0.3, dtype, gap=gap, start=start)
+    g = strided(rng.standard_normal(shape), grad or dtype, gap=gap, start=start)
+    w, b = vector(rng, n, weight, 0.2, 1.0), vector(rng, n, bias, 0.1, 0.0)
+    res = strided(rng.standard_normal(shape), dtype, gap=gap) if residual else None
+    _, stats = B.layer_norm(x, w, b, eps=EPS, stats=True)
+    dx, dw, db = B.layer_norm_grad(g, x, stats, w, b, res, need_x=need_x)
+    X, G, S = f64(x), f64(g), f64(stats)
+    h = (X - S[..., :1]) * S[..., 1:]
+    r = S[..., 1:]
+    gw = G if w is None else G * f64(w)
+    mean = lambda v: v.mean(-1, keepdims=True)      # noqa: E731
+    a, c = mean(gw), mean(gw * h)
+    want = r * (gw - a - h * c)
+    k = n / 64 + 38
+    bound = r * (5 * U * (np.abs(gw) + np.abs(a) + np.abs(h * c)) + k * U * (mean(np.abs(gw)) + np.abs(h) * mean(np.abs(gw * h)))) + U * np.abs(want)
+    if residual:
+        want = want + f64(res)
+        bound = bound + U * np.abs(want)
+    if need_x:
+        check(dx, want, bound, dtype, "dx")
+    else:
+        assert dx is None
+    rows = tuple(range(len(shape) - 1))
+    if w is None:
+        assert dw is None
+    else:
+        check(dw, (G * h).sum(rows), (m + 8) * U * np.abs(G * h).sum(rows), weight, "dw")
+    if b is None:
+        assert db is None
+    else:
+        check(db, G.sum(rows), (m + 8) * U * np.abs(G).sum(rows), bias, "db")
+    return g, x, stats, w, b, res, (dx, dw, db)
+
+
+SHAPES = [(1, 1), (3, 1), (1, 2), (5, 7), (2, 8), (4, 9), (3, 63), (7, 64), (2, 511), (6, 512), (5, 513), (3, 1000), (4, 2048), (2, 2049), (3, 4096), (3, 4097),
+          (2, 8192), (2, 8200), (1, 16384), (2, 16385), (1, 32768), (2, 32769), (1, 70001), (300, 40), (1030, 24), (2, 3, 65), (3, 1, 130), (1, 4, 16)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_norm_shapes(shape, dtype):
+    case_norm(shape, dtype)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,weight,bias,out", [("f32", None, None, "bf16"), ("bf16", "bf16", None, "f32"), ("bf16", None, "bf16", "bf16"), ("f32", "bf16", "f32", "f32"),
+                                                   ("bf16", "f32", "bf16", "bf16")])
+@pytest.mark.parametrize("n", [5, 96, 1001, 5000, 40000])
+def test_norm_types(dtype, weight, bias, out, n):
+    case_norm((9, n), dtype, weight, bias, out)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("gap,start", [(8, 0), (1, 0), (3, 1), (0, 3)])
+@pytest.mark.parametrize("shape", [(5, 24), (3, 7, 100), (4, 1000), (2, 5003)], ids=str)
+def test_norm_strides(shape, gap, start, dtype):
+    case_norm(shape, dtype, gap=gap, start=start)
+    case_grad(shape, dtype, gap=gap, start=start)
+
+
+@gpu
+def test_norm_far_from_zero():
+    """A mean 30,000 times the deviation: sums of x alone would leave h off by 0.01."""
+    for n in (64, 2048, 10000, 40000):
+        case_norm((3, n), "f32", offset=30000.0)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_grad_shapes(shape, dtype):
+    case_grad(shape, dtype)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,weight,bias,grad,residual,need_x", [("f32", None, None, "f32", False, True), ("bf16", "f32", "f32", "f32", True, True), ("f32", "bf16", None, "bf16", False, True),
+                                                                    ("bf16", None, "bf16", "bf16", True, True), ("bf16", "bf16", "bf16", "bf16", False, False), ("f32", None, "f32", "f32", False, False),
+                                                                    ("f32", "f32", None, "f32", False, False)])
+@pytest.mark.parametrize("shape", [(4, 5), (70, 96), (40, 1001), (33, 5000), (3, 40000)], ids=str)
+def test_grad_types(shape, dtype, weight, bias, grad, residual, need_x):
+    case_grad(shape, dtype, weight, bias, residual, grad, need_x)
+
+
+@gpu
+@pytest.mark.parametrize("shape", [(5000, 64), (2500, 520), (20000, 8)], ids=str)
+def test_grad_many_rows(shape):
+    case_grad(shape, "bf16", "f32", "f32")
+
+
+@gpu
+def test_grad_against_differences():
+    """f32, steps of 2^-6: central differences of S (out target) in 64 bits are off by step^2 times the third derivative, below 1e-3 here."""
+    torch, _ = _torch()
+    rng = np.random.default_rng(8)
+    x, w, b, t = rng.standard_normal((3, 20)), rng.standard_normal(20) + 1, rng.standard_normal(20), rng.standard_normal((3, 20))
+    cu = lambda v: torch.from_numpy(v).float().cuda()       # noqa: E731
+    _, stats = B.layer_norm(cu(x), cu(w), cu(b), stats=True)
+    got = B.layer_norm_grad(cu(t), cu(x), stats, cu(w), cu(b))
+    loss = lambda x, w, b: (norm_of(x, w, b)[0] * t).sum()      # noqa: E731
+    for i, d in enumerate(got):
+        args = [x, w, b]
+        for at in np.ndindex(args[i].shape):
+            e = np.zeros_like(args[i])
+            e[at] = 2.0 ** -6
+            up, down = list(args), list(args)
+            up[i], down[i] = args[i] + e, args[i] - e
+            assert abs((loss(*up) - loss(*down)) * 32 - d[at].item()) < 1e-2 * (1 + abs(d[at].item())), (i, at)
+
+
+@gpu
+@pytest.mark.parametrize("n", [40, 3000, 40000])
+def test_norm_values_that_are_not_finite(n):
+    """A row with an infinity or NaN is NaN, its statistics too but for the mean; the others are what they were."""
+    torch, _ = _torch()
+    x = torch.randn((5, n), device="cuda")
+    clean, clean_stats = B.layer_norm(x, stats=True)
+    x[1, 3], x[3, n - 1] = float("inf"), float("nan")
+    out, stats = B.layer_norm(x, stats=True)
+    for i in range(5):
+        if i in (1, 3):
+            assert out[i].isnan().all() and stats[i, 1].isnan() and not stats[i, 0].isfinite()
+        else:
+            assert torch.equal(out[i], clean[i]) and torch.equal(stats[i], clean_stats[i])
+    grad = torch.randn((5, n), device="cuda")
+    dx, _, _ = B.layer_norm_grad(grad, x, stats)
+    assert dx[[1, 3]].isnan().all() and torch.equal(dx[[0, 2, 4]], B.layer_norm_grad(grad, x.nan_to_num(posinf=0), clean_stats)[0][[0, 2, 4]])
+    # a row of equal elements: 0 / sqrt(eps)
+    same = torch.full((2, n), 3.25, device="cuda")
+    out, stats = B.layer_norm(same, eps=1e-4, stats=True)
+    assert (out == 0).all() and (stats[:, 0] == 3.25).all() and ((stats[:, 1] - 100).abs() < 1e-4).all()
+
+
+@gpu
+def test_norm_in_place_and_the_same_bits():
+    torch, _ = _torch()
+    for shape in ((7, 100), (40, 2048), (9, 6000), (2, 50000), (3000, 64)):
+        x, grad, w = torch.randn(shape, device="cuda").bfloat16(), torch.randn(shape, device="cuda").bfloat16(), torch.randn(shape[-1], device="cuda")
+        want, stats = B.layer_norm(x, w, stats=True)
+        grads = B.layer_norm_grad(grad, x, stats, w, w, grad)
+        for _ in range(4):
+            assert torch.equal(B.layer_norm(x, w), want)
+            again = B.layer_norm_grad(grad, x, stats, w, w, grad)
+            assert all(torch.equal(a, b) for a, b in zip(grads, again))
+        y = x.clone()
+        assert B.layer_norm(y, w, out=y) is y and torch.equal(y, want)
+        # d_x where x, grad or the residual was: through the library, which the binding gives new memory
+        for which in range(3):
+            ops = [grad.clone(), x.clone(), grad.clone()]
+            m = [(t.data_ptr(), 1, 0, shape[1], 0) for t in ops]
+            d = B._NORM_GRAD.pack(1, *shape, 0, *(v for q in m for v in q), w.data_ptr(), 0, 0, 1, 0, *m[which], *B._ABSENT, *B._ABSENT, stats.data_ptr())
+            assert B.lib().mrl_layer_norm_grad(d, None, 0, torch.cuda.current_stream().cuda_stream) == 0
+            assert torch.equal(ops[which], grads[0]), which
+
+
+@gpu
+def test_norm_streams_graphs_and_workspaces():
+    torch, _ = _torch()
+    m, n = 700, 520
+    x, grad, w, b = (torch.randn(s, device="cuda") for s in ((m, n), (m, n), (n,), (n,)))
+    want, stats = B.layer_norm(x, w, b, stats=True)
+    grads = B.layer_norm_grad(grad, x, stats, w, b, grad)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got, _ = B.layer_norm(x, w, b, stats=True, stream=side)
+    got_grads = B.layer_norm_grad(grad, x, stats, w, b, grad, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(got, want) and all(torch.equal(p, q) for p, q in zip(got_grads, grads))
+    # two graphs that share a workspace the caller keeps, replayed in turn with other inputs
+    work = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+    inputs = [[t.clone() for t in (x, grad)] for _ in range(2)]
+    graphs, results = [], []
+    for xi, gi in inputs:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out, s = B.layer_norm(xi, w, b, stats=True)
+            results.append((out, *B.layer_norm_grad(gi, xi, s, w, b, gi, workspace=work)))
+        graphs.append(graph)
+    for turn in range(4):
+        for (xi, gi), graph, res in zip(inputs, graphs, results):
+            xi.copy_(torch.randn_like(xi))
+            gi.copy_(torch.randn_like(gi))
+            graph.replay()
+            torch.cuda.synchronize()
+            out, s = B.layer_norm(xi, w, b, stats=True)
+            for p, q in zip(res, (out, *B.layer_norm_grad(gi, xi, s, w, b, gi))):
+                assert torch.equal(p, q), turn
+
+
+@gpu
+def test_norm_beyond_32_bits():
+    """5 GB of rows: offsets past 2^32 bytes and 2^31 elements."""
+    torch, _ = _torch()
+    m, n = 1200000, 2048
+    x = torch.empty((m, n), device="cuda", dtype=torch.bfloat16).normal_()
+    out, stats = B.layer_norm(x, stats=True)
+    dx, _, _ = B.layer_norm_grad(out, x, stats)
+    for at in (0, 1048576 - 5, m - 10):
+        want, mean, r, bound = norm_of(f64(x[at:at + 10]), None, None)
+        check(out[at:at + 10], want, bound, "bf16", at)
+        X, G, S = f64(x[at:at + 10]), f64(out[at:at + 10]), f64(stats[at:at + 10])
+        h = (X - S[:, :1]) * S[:, 1:]
+        mag = np.abs(G).mean(-1, keepdims=True) + np.abs(h) * np.abs(G * h).mean(-1, keepdims=True)
+        check(dx[at:at + 10], S[:, 1:] * (G - G.mean(-1, keepdims=True) - h * (G * h).mean(-1, keepdims=True)), S[:, 1:] * 80 * U * (mag + np.abs(G)), "bf16", at)
+
+
+@gpu
+@pytest.mark.parametrize("shape", [(0, 16), (4, 0), (0, 3, 8), (2, 0, 8)], ids=str)
+def test_norm_sizes_of_zero(shape):
+    torch, _ = _torch()
+    x, w = torch.empty(shape, device="cuda"), torch.ones(shape[-1], device="cuda")
+    out, stats = B.layer_norm(x, w, w, stats=True)
+    assert out.shape == shape and stats.shape == shape[:-1] + (2,)
+    dx, dw, db = B.layer_norm_grad(x, x, stats, w, w)
+    assert dx.shape == shape and (dw == 0).all() and (db == 0).all()
+
+
+@gpu
+def test_norm_refusals():
+    torch, _ = _torch()
+    x, w = torch.randn((4, 16), device="cuda"), torch.ones(16, device="cuda")
+    _, stats = B.layer_norm(x, stats=True)
+
+    def refused(f):
+        with pytest.raises(B.MorelloError) as e:
+            f()
+        assert e.value.code == B.E_INVAL
+
+    for f in (lambda: B.layer_norm(x[0]), lambda: B.layer_norm(x.half()), lambda: B.layer_norm(x, w[:15]), lambda: B.layer_norm(x, w.cpu()), lambda: B.layer_norm(x, bias=w.half()),
+              lambda: B.layer_norm(x, eps=-1.0), lambda: B.layer_norm(x, eps=float("nan")), lambda: B.layer_norm(x, eps=float("inf")), lambda: B.layer_norm(x.t()),
+              lambda: B.layer_norm(x, out=x[:2]), lambda: B.layer_norm(x, out=x, dtype=torch.bfloat16), lambda: B.layer_norm(x, out=x[:1].expand(4, 16)),
+              lambda: B.layer_norm_grad(x, x, stats[:3]), lambda: B.layer_norm_grad(x, x, stats.double()), lambda: B.layer_norm_grad(x[:3], x, stats),
+              lambda: B.layer_norm_grad(x, x, stats, w[:3]), lambda: B.layer_norm_grad(x, x, stats.t().contiguous().t()), lambda: B.layer_norm_grad(x, x, stats, residual=x[:3])):
+        refused(f)
+
+
+def test_norm_refusals_without_a_gpu():
+    """The library's checks are host code: nothing is launched (the addresses are of nothing)."""
+    P, lib = 1 << 20, B.lib()
+    mat = lambda d=P, t=0, l=0, ld=16, batch=64: (d, t, l, ld, batch)        # noqa: E731
+
+    def norm(b=1, m=4, n=16, eps=1e-5, x=mat(), out=mat(), w=B._ABSENT, bias=B._ABSENT, stats=0):
+        return lib.mrl_layer_norm(B._NORM.pack(b, m, n, eps, *x, *out, *w, *bias, stats), None)
+
+    def grad(b=1, m=4, n=16, g=mat(), x=mat(), res=B._ABSENT, w=B._ABSENT, dx=mat(), dw=B._ABSENT, db=B._ABSENT, stats=P, run=True):
+        import ctypes as C
+        d, size = B._NORM_GRAD.pack(b, m, n, 0, *g, *x, *res, *w, *dx, *dw, *db, stats), C.c_size_t()
+        rc = lib.mrl_layer_norm_grad_bytes(d, C.addressof(size))
+        return rc or (lib.mrl_layer_norm_grad(d, None, 0, None) if run else size.value)
+
+    for rc in (norm(eps=-1.0), norm(eps=float("nan")), norm(x=mat(0)), norm(out=mat(0)), norm(x=mat(t=2)), norm(x=mat(l=1)), norm(out=mat(ld=15)), norm(x=mat(P + 2)), norm(stats=P + 2),
+               norm(w=mat(P + 1)), norm(b=1 << 31), norm(b=1 << 16, m=1 << 16), norm(x=mat(ld=-1)), norm(x=mat(ld=1 << 41)), norm(b=2, out=mat(batch=8)),
+               grad(stats=0), grad(x=mat(0)), grad(g=mat(0)), grad(dx=mat(ld=3)), grad(w=mat(P + 2)), grad(dw=mat(P + 2)), grad(res=mat(t=7)), grad(stats=P + 1)):
+        assert rc == B.E_INVAL
+    # gradients of many rows sum over blocks of them in a workspace, which is asked for
+    big = dict(m=1 << 16, g=mat(), x=mat(), dw=(P, 0, 0, 1, 0), db=(P, 0, 0, 1, 0))
+    need = grad(run=False, **big)
+    assert need >= 0 and (need == 0 or grad(**big) == B.E_NOMEM)
+    with pytest.raises(B.MorelloError):
+        import torch
+        B.layer_norm(torch.ones(2, 4))
