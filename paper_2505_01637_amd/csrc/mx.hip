@@ -91,40 +91,264 @@ __device__ __forceinline__ f32x4 multiply(const i32x4& a, const i32x4& b, uint32
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(y, x, acc, 4, 4, OB, (int)sb, OA, (int)sa);       // (4: both operands are 4-bit floating point)
 }
 
-// A tile of 64 x 64, a quarter a wave, operands straight from memory.
-__global__ __launch_bounds__(256) void mx_kernel(const MxProduct x, uint32_t first) {
+// The same with places that are known once loops are unrolled.
+__device__ __forceinline__ f32x4 multiply(const bf16x8& a, const bf16x8& b, uint32_t sa, uint32_t sb, int oa, int ob, const f32x4& acc) {
+  const i32x4 x = __builtin_bit_cast(i32x4, a), y = __builtin_bit_cast(i32x4, b);
+  switch (oa * 4 + ob) {
+    case 0: return multiply<0, 0>(x, y, sa, sb, acc);
+    case 1: return multiply<0, 1>(x, y, sa, sb, acc);
+    case 2: return multiply<0, 2>(x, y, sa, sb, acc);
+    case 3: return multiply<0, 3>(x, y, sa, sb, acc);
+    case 4: return multiply<1, 0>(x, y, sa, sb, acc);
+    case 5: return multiply<1, 1>(x, y, sa, sb, acc);
+    case 6: return multiply<1, 2>(x, y, sa, sb, acc);
+    case 7: return multiply<1, 3>(x, y, sa, sb, acc);
+    case 8: return multiply<2, 0>(x, y, sa, sb, acc);
+    case 9: return multiply<2, 1>(x, y, sa, sb, acc);
+    case 10: return multiply<2, 2>(x, y, sa, sb, acc);
+    case 11: return multiply<2, 3>(x, y, sa, sb, acc);
+    case 12: return multiply<3, 0>(x, y, sa, sb, acc);
+    case 13: return multiply<3, 1>(x, y, sa, sb, acc);
+    case 14: return multiply<3, 2>(x, y, sa, sb, acc);
+    default: return multiply<3, 3>(x, y, sa, sb, acc);
+  }
+}
+
+// 256 bytes from memory to shared memory, four a lane.
+__device__ __forceinline__ void load4_to_lds(uint32_t lds, uint32_t offset, u32x4 buffer) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(buffer) : "memory");
+}
+
+// A step is 256 values, 128 bytes of codes a line, so tiles lie in shared memory and get there as those of two-byte operands do; a half step is one
+// instruction's 128 values.  Both operands' lines are in the order that the products of linear.hip have for B, which is the one that scales are stored in.
+constexpr uint32_t kUnits = 64;            // of four values, in a step
+
+// The scales of a tile of `groups` groups of 64 lines: 256 bytes for a group and half step.
+struct Scales {
+  u32x4 buffer;
+  uint32_t pitch;                          // bytes from a group to the next
+  __device__ __forceinline__ void init(const uint8_t* scales, uint32_t line, uint32_t lines, uint32_t halves, uint32_t groups) {
+    pitch = halves * 256;
+    const uint64_t base = (uint64_t)(scales + (uint64_t)(line / 64) * pitch);
+    buffer = u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)base), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(base >> 32) & 0xFFFFu),
+                   (uint32_t)__builtin_amdgcn_readfirstlane(min(groups, (lines + 63) / 64 - line / 64) * pitch), 0x27000u};
+  }
+  // (a half step that is not there has scales of 0, as its codes are: the byte that happens to follow could be a NaN's)
+  __device__ __forceinline__ void load(uint32_t group, uint32_t half, uint32_t lds, uint32_t lane) const {
+    load4_to_lds(lds, half * 256 < pitch ? group * pitch + half * 256 + lane * 4 : kOutside, buffer);
+  }
+};
+
+// A wave's scales of W of a tile's lines from `first` on, for a half step: four blocks a word.
+template <int W>
+__device__ __forceinline__ void read_scales(lds_ptr slots, uint32_t first, uint32_t kk, uint32_t lane, uint32_t (&s)[(W + 63) / 64]) {
+#pragma unroll
+  for (uint32_t i = 0; i < (W + 63) / 64; i++) s[i] = *(const __attribute__((address_space(3))) uint32_t*)(slots + ((first / 64 + i) * 2 + kk) * 256 + lane * 4);
+  if (W < 64) s[0] >>= first % 64 / 16 * 8;
+}
+
+// One tile of TM x TN, WAVES_M x WAVES_N waves, STAGES steps in shared memory: the loop of linear.hip's fast_kernel.
+template <int TM, int TN, int WAVES_M, int WAVES_N, int STAGES>
+__global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void mx_tile_kernel(const MxProduct x, uint32_t steps, uint32_t per_split, uint32_t splits, uint32_t first,
+                                                                         float* __restrict__ partial) {
+  constexpr int WAVES = WAVES_M * WAVES_N, THREADS = 64 * WAVES, WM = TM / WAVES_M, WN = TN / WAVES_N, BM = WM / 16, BN = WN / 16;
+  constexpr int PASS = BM > 4 ? BM / 2 : BM;
+  constexpr int GA = TM / 64, GB = TN / 64, SLOTS = 2 * (GA + GB), EACH = (SLOTS + WAVES - 1) / WAVES;       // 256 bytes of scales; and how many a wave loads
+  constexpr uint32_t CODES = (TM + TN) * kStep, STAGE = CODES + EACH * WAVES * 256, OUT = 16 * PASS * WN * 4;
+  __shared__ __attribute__((aligned(1024))) char lds[STAGES * STAGE];
+  static_assert(WAVES * OUT <= sizeof lds, "the results go where the stages were");
   const Product& p = x.p;
-  __shared__ __attribute__((aligned(16))) char lds[4][32 * 32 * 4];
-  const Place at = place(first, (p.M + 63) / 64, (p.N + 63) / 64, 1);
-  const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane & 15, g = lane >> 4;
-  const uint32_t m0 = at.tm * 64 + wave / 2 * 32, n0 = at.tn * 64 + wave % 2 * 32, steps = p.K / 32;
-  const uint8_t* const sa = x.scales_a + (int64_t)at.batch * x.scales_batch_a + (uint64_t)at.tm * steps * 256 + lane * 4;
-  const uint8_t* const sb = x.scales_b + (int64_t)at.batch * x.scales_batch_b + (uint64_t)at.tn * steps * 256 + lane * 4;
-  const char *a[2], *b[2];
-#pragma unroll
-  for (int i = 0; i < 2; i++) {
-    a[i] = (const char*)p.a + ((int64_t)at.batch * p.batch_a + (int64_t)min(m0 + row_of<bf16, true>(i, q), p.M - 1) * p.lda) * 2 + g * 16;
-    b[i] = (const char*)p.b + ((int64_t)at.batch * p.batch_b + (int64_t)min(n0 + row_of<bf16, true>(i, q), p.N - 1) * p.ldb) * 2 + g * 16;
-  }
-  f32x4 acc[2][2];
-#pragma unroll
-  for (int i = 0; i < 2; i++)
-#pragma unroll
-    for (int j = 0; j < 2; j++) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  for (uint32_t s = 0; s < steps; s++) {
-    const uint32_t ka = *(const uint32_t*)(sa + (uint64_t)s * 256) >> wave / 2 * 16, kb = *(const uint32_t*)(sb + (uint64_t)s * 256) >> wave % 2 * 16;
-    i32x4 va[2], vb[2];
-#pragma unroll
-    for (int i = 0; i < 2; i++) {
-      va[i] = *(const i32x4*)(a[i] + (uint64_t)s * 64);
-      vb[i] = *(const i32x4*)(b[i] + (uint64_t)s * 64);
+
+  const Place at = place(first, (p.M + TM - 1) / TM, (p.N + TN - 1) / TN, splits);
+  const uint32_t m0 = at.tm * TM, n0 = at.tn * TN;
+  const uint32_t t = threadIdx.x, lane = t & 63, q = lane & 15, g = lane >> 4;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const uint32_t wm = wave / WAVES_N * WM, wn = wave % WAVES_N * WN;
+
+  Feed<bf16, true, true, TM, THREADS> fa;
+  Feed<bf16, true, true, TN, THREADS> fb;
+  fa.init(p.lda, t);
+  fb.init(p.ldb, t);
+  Scales sa, sb;
+  sa.init(x.scales_a + (int64_t)at.batch * x.scales_batch_a, m0, p.M, p.K / 32, GA);
+  sb.init(x.scales_b + (int64_t)at.batch * x.scales_batch_b, n0, p.N, p.K / 32, GB);
+  constexpr int NA = decltype(fa)::N, NB = decltype(fb)::N, LOADS = NA + NB + EACH;
+
+  const uint32_t from = at.split * per_split, end = min(from + per_split, steps), n = end > from ? end - from : 0;
+  // the next step to load: where it starts in either operand, the bytes that are left behind that
+  uint32_t step = from;
+  const char* ca = (const char*)p.a + ((int64_t)at.batch * p.batch_a + (int64_t)m0 * p.lda + (int64_t)from * kUnits) * 2;
+  const char* cb = (const char*)p.b + ((int64_t)at.batch * p.batch_b + (int64_t)n0 * p.ldb + (int64_t)from * kUnits) * 2;
+  int64_t left_a = ((int64_t)(p.M - m0) * p.lda - (int64_t)from * kUnits) * 2, left_b = ((int64_t)(p.N - n0) * p.ldb - (int64_t)from * kUnits) * 2;
+  // (behind the last step the buffers have no bytes: zeros are written that nothing uses, and every step has the same loads under way)
+  u32x4 buf_a, buf_b;
+  uint32_t to, ks, half;
+  const auto aim = [&](uint32_t stage) {          // at the next step, to be put into `stage`
+    const bool more = step < end;
+    to = (uint32_t)(uintptr_t)(lds_ptr)lds + stage * STAGE;
+    ks = p.K - step * kUnits;
+    half = more ? step * 2 : 0x7FFFFFu;
+    buf_a = fa.buffer(ca, more ? left_a : 0);
+    buf_b = fb.buffer(cb, more ? left_b : 0);
+    if (!more) return;
+    step++;
+    ca += kStep;
+    cb += kStep;
+    left_a -= kStep;
+    left_b -= kStep;
+  };
+  const auto load = [&](int i) {
+    if (i < NA) fa.load(i, buf_a, ks, to + wave * 1024, t);
+    else if (i < NA + NB) fb.load(i - NA, buf_b, ks, to + TM * kStep + wave * 1024, t);
+    else {
+      const uint32_t slot = wave * EACH + (i - NA - NB), lds_at = to + CODES + slot * 256;
+      if (slot < 2 * GA) sa.load(slot >> 1, half + (slot & 1), lds_at, lane);
+      else sb.load(slot < SLOTS ? (slot - 2 * GA) >> 1 : 0, slot < SLOTS ? half + (slot & 1) : 0x7FFFFFu, lds_at, lane);
     }
-    acc[0][0] = multiply<0, 0>(va[0], vb[0], ka, kb, acc[0][0]);
-    acc[0][1] = multiply<0, 1>(va[0], vb[1], ka, kb, acc[0][1]);
-    acc[1][0] = multiply<1, 0>(va[1], vb[0], ka, kb, acc[1][0]);
-    acc[1][1] = multiply<1, 1>(va[1], vb[1], ka, kb, acc[1][1]);
+  };
+  f32x4 acc[BM][BN];
+#pragma unroll
+  for (int i = 0; i < BM; i++)
+#pragma unroll
+    for (int j = 0; j < BN; j++) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+  constexpr int NM = BM > 4 ? BM / 2 : BM, PHASES = 2 * BM / NM;
+  constexpr bool SPREAD = BM > 4;
+  static_assert(!SPREAD || LOADS <= PHASES * NM, "one load at most beside a part of the products");
+  bf16x8 oa[2][NM], ob[2][BN];
+  uint32_t ka[2][(WM + 63) / 64], kb[2][(WN + 63) / 64];
+  const auto read_a = [&](lds_ptr stage, int m, int kk, bf16x8 (&o)[NM]) { read_blocks<bf16, true, true, TM>(stage, wm, m, kk, q, g, o); };
+  const auto read_b = [&](lds_ptr stage, int kk) {        // and the scales of the half step
+    read_blocks<bf16, true, true, TN>(stage + TM * kStep, wn, 0, kk, q, g, ob[kk]);
+    read_scales<WM>(stage + CODES, wm, kk, lane, ka[kk]);
+    read_scales<WN>(stage + CODES + 2 * GA * 256, wn, kk, lane, kb[kk]);
+  };
+  if (n) {
+#pragma unroll
+    for (int s = 0; s < STAGES; s++) {
+      aim(s);
+#pragma unroll
+      for (int i = 0; i < LOADS; i++) load(i);
+    }
+    arrive<(STAGES - 1) * LOADS>();
+    read_a((lds_ptr)lds, 0, 0, oa[0]);
+    read_b((lds_ptr)lds, 0);
+    uint32_t cur = 0;
+    for (uint32_t s = 0; s < n; s++) {
+      const uint32_t next = cur + 1 == STAGES ? 0 : cur + 1;
+#pragma unroll
+      for (int ph = 0; ph < PHASES; ph++) {
+        const int then = (ph + 1) % PHASES, kk = then / (PHASES / 2), m = then % (PHASES / 2) * NM;
+        if (ph == PHASES - 1) {
+          arrive<(STAGES - 2) * LOADS>();
+          aim(cur);
+#pragma unroll
+          for (int i = 0; i < (SPREAD ? 0 : LOADS); i++) load(i);
+        }
+        const lds_ptr stage = (lds_ptr)lds + (ph == PHASES - 1 ? next : cur) * STAGE;
+        read_a(stage, m, kk, oa[then & 1]);
+        if (m == 0) read_b(stage, kk);
+#pragma unroll
+        for (int part = 0; part < NM; part++) {
+          const int i = ph % (PHASES / 2) * NM + part, k = ph / (PHASES / 2);
+#pragma unroll
+          for (int j = 0; j < BN; j++) acc[i][j] = multiply(oa[ph & 1][part], ob[k][j], ka[k][i / 4], kb[k][j / 4], i % 4, j % 4, acc[i][j]);
+          // (in the first step, before its barrier, the last stage's loads again: the same bytes to the same place)
+          if (SPREAD && then * NM + part < LOADS) {
+            load(then * NM + part);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      cur = next;
+    }
+    arrive<0>();                  // nothing is under way to shared memory when it is given up
   }
-  write_out<bf16, 2, 2, 2, true>(p, at, 1, m0, n0, lane, acc, lds[wave], nullptr);
+  write_out<bf16, PASS, BM, BN, true>(p, at, splits, m0 + wm, n0 + wn, lane, acc, lds + wave * OUT, partial);
+}
+
+// Few rows: the loop of linear.hip's rows_kernel, the sum split among the waves of a workgroup, each with a ring of its own.  A tile of 16 rows, in their own
+// order (so their scales are bytes here and there of the group's), and 64 columns.
+template <int WAVES, int STAGES>
+__global__ __launch_bounds__(64 * WAVES) void mx_rows_kernel(const MxProduct x, uint32_t steps, uint32_t per_split, uint32_t splits, uint32_t first, float* __restrict__ partial) {
+  constexpr int TM = 16, TN = 64, BN = TN / 16;
+  constexpr uint32_t CODES = (TM + TN) * kStep, STAGE = CODES + 4 * 256;
+  __shared__ __attribute__((aligned(1024))) char lds[WAVES][STAGES * STAGE];
+  const Product& p = x.p;
+
+  const Place at = place(first, (p.M + TM - 1) / TM, (p.N + TN - 1) / TN, splits);
+  const uint32_t m0 = at.tm * TM, n0 = at.tn * TN;
+  const uint32_t t = threadIdx.x, lane = t & 63, q = lane & 15, g = lane >> 4;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(t >> 6);
+
+  float bias[8];
+  bias8(p.e, n0 + t % 8 * 8, n0 + t % 8 * 8 < p.N ? p.N - (n0 + t % 8 * 8) : 0, bias);
+  Feed<bf16, true, false, TM, 64> fa;
+  Feed<bf16, true, true, TN, 64> fb;
+  fa.init(p.lda, lane);
+  fb.init(p.ldb, lane);
+  Scales sa, sb;
+  sa.init(x.scales_a + (int64_t)at.batch * x.scales_batch_a, m0, p.M, p.K / 32, 1);
+  sb.init(x.scales_b + (int64_t)at.batch * x.scales_batch_b, n0, p.N, p.K / 32, 1);
+  constexpr int LOADS = decltype(fa)::N + decltype(fb)::N + 4;
+
+  const uint32_t end = min(at.split * per_split + per_split, steps);
+  uint32_t step = at.split * per_split + wave;    // the next one to load
+  const uint32_t n = end > step ? (end - step + WAVES - 1) / WAVES : 0;
+  const char* const ca = (const char*)p.a + ((int64_t)at.batch * p.batch_a + (int64_t)m0 * p.lda) * 2;
+  const char* const cb = (const char*)p.b + ((int64_t)at.batch * p.batch_b + (int64_t)n0 * p.ldb) * 2;
+  const int64_t size_a = (int64_t)(p.M - m0) * p.lda * 2, size_b = (int64_t)(p.N - n0) * p.ldb * 2;
+  char* const ring = lds[wave];
+  const auto load = [&](uint32_t stage) {
+    const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr)ring + stage * STAGE);
+    const bool more = step < end;
+    const uint32_t s = more ? step : 0, half = more ? step * 2 : 0x7FFFFFu;
+    const u32x4 buf_a = fa.buffer(ca + (int64_t)s * kStep, more ? size_a - (int64_t)s * kStep : 0);
+    const u32x4 buf_b = fb.buffer(cb + (int64_t)s * kStep, more ? size_b - (int64_t)s * kStep : 0);
+#pragma unroll
+    for (int i = 0; i < fb.N; i++) fb.load(i, buf_b, p.K - s * kUnits, to + TM * kStep, lane);
+#pragma unroll
+    for (uint32_t kk = 0; kk < 2; kk++) sb.load(0, half + kk, to + CODES + (2 + kk) * 256, lane);
+#pragma unroll
+    for (int i = 0; i < fa.N; i++) fa.load(i, buf_a, p.K - s * kUnits, to, lane);
+#pragma unroll
+    for (uint32_t kk = 0; kk < 2; kk++) sa.load(0, half + kk, to + CODES + kk * 256, lane);
+    step += WAVES;
+  };
+
+  f32x4 acc[1][BN];
+#pragma unroll
+  for (int j = 0; j < BN; j++) acc[0][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  const uint32_t mine = scale_at(m0 % 64 + q, g);
+
+  if (n) {
+#pragma unroll
+    for (int s = 0; s < STAGES; s++) load(s);
+    uint32_t cur = 0;
+    for (uint32_t s = 0; s < n; s++) {
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 1) * LOADS) : "memory");
+      const lds_ptr tile = (lds_ptr)ring + cur * STAGE;
+      bf16x8 oa[2][1], ob[2][BN];
+      uint32_t ka[2], kb[2][1];
+#pragma unroll
+      for (uint32_t kk = 0; kk < 2; kk++) {
+        read_blocks<bf16, true, false, TM>(tile, 0, 0, kk, q, g, oa[kk]);
+        read_blocks<bf16, true, true, TN>(tile + TM * kStep, 0, 0, kk, q, g, ob[kk]);
+        ka[kk] = *(const __attribute__((address_space(3))) uint8_t*)(tile + CODES + kk * 256 + mine);
+        read_scales<TN>(tile + CODES + 512, 0, kk, lane, kb[kk]);
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // read before the place is loaded again
+      load(cur);
+#pragma unroll
+      for (int kk = 0; kk < 2; kk++)
+#pragma unroll
+        for (int j = 0; j < BN; j++) acc[0][j] = multiply(oa[kk][0], ob[kk][j], ka[kk], kb[kk][0], 0, j, acc[0][j]);
+      cur = cur + 1 == STAGES ? 0 : cur + 1;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  }
+  add_waves<bf16, WAVES>(p, at, splits, m0, n0, t, bias, acc, &lds[0][0], sizeof lds[0], partial);
 }
 
 }  // namespace
@@ -138,15 +362,53 @@ hipError_t launch_mx_dequantize(const MxRows& p, hipStream_t st) {
   return in_launches((items + 255) / 256, [&](uint64_t first, uint32_t n) { mx_dequantize_kernel<<<n, 256, 0, st>>>(p, first); });
 }
 
+// How long a kernel takes, in us, as linear.hip's rule has it: a round of workgroups on the 256 compute units, one each or two at once, is `fixed`
+// and a step's time for each step along k.
+struct Kernel { uint32_t id, tm, tn; float fixed, one, two; };
+constexpr Kernel kKernels[] = {
+    {kFast256, 256, 256, 11, 1.52f, 0}, {kFast256x128, 256, 128, 6, 0.87f, 0}, {kFast128, 128, 128, 4, 0.50f, 0.93f}, {kFast64, 64, 64, 2, 0.25f, 0.37f}, {kRows, 16, 64, 3, 0.12f, 0.24f},
+};
+constexpr float kLaunch1 = 6, kBytes = 4.5e6f;                     // a further launch, us; bytes a us
+
 ProductPlan plan_mx(const MxProduct& x) {
+  const Product& p = x.p;
   ProductPlan plan{};
-  plan.splits = 1;
-  plan.blocks = (uint64_t)x.p.batches * ((x.p.M + 63) / 64) * ((x.p.N + 63) / 64);
+  plan.steps = (p.K + kUnits - 1) / kUnits;
+  const float out = (float)p.batches * p.M * p.N * 4;
+  float best = 0;
+  for (const Kernel& k : kKernels) {
+    const uint64_t tiles = (uint64_t)((p.M + k.tm - 1) / k.tm) * ((p.N + k.tn - 1) / k.tn) * p.batches;
+    for (uint32_t splits = 1; splits <= 64; splits = splits == 1 ? 2 : splits & splits - 1 ? splits / 3 * 4 : splits / 2 * 3) {
+      const uint32_t per = (plan.steps + splits - 1) / splits;
+      if (splits > 1 && (per < 4 || tiles * splits > 1024)) break;
+      const float one = k.fixed + per * k.one, two = k.two ? k.fixed + per * k.two : 2 * one;
+      const uint64_t blocks = tiles * splits, rounds = blocks / 512, rest = blocks % 512;
+      float t = rounds * two + (rest > 256 ? two : rest ? one : 0);
+      if (splits > 1) t += kLaunch1 + (splits + 1) * out / kBytes;
+      if (best && t >= best) continue;
+      best = t;
+      plan.kernel = k.id == kFast128 && blocks <= 256 ? kFast128Alone : k.id;
+      plan.per_split = per;
+      plan.splits = per ? (plan.steps + per - 1) / per : 1;
+      plan.blocks = tiles * plan.splits;
+    }
+  }
+  plan.partial_bytes = plan.splits > 1 ? (uint64_t)plan.splits * p.batches * p.M * ((p.N + 7) / 8 * 8) * 4 : 0;
   return plan;
 }
 
-hipError_t launch_mx(const MxProduct& x, const ProductPlan& plan, float*, hipStream_t st) {
-  return in_launches(plan.blocks, [&](uint64_t first, uint32_t n) { mx_kernel<<<n, 256, 0, st>>>(x, (uint32_t)first); });
+hipError_t launch_mx(const MxProduct& x, const ProductPlan& plan, float* partial, hipStream_t st) {
+  return in_launches(plan.blocks, [&](uint64_t first, uint32_t n) {
+    const auto go = [&](auto kernel, uint32_t threads) { kernel<<<n, threads, 0, st>>>(x, plan.steps, plan.per_split, plan.splits, (uint32_t)first, partial); };
+    switch (plan.kernel) {
+      case kFast256: return go(mx_tile_kernel<256, 256, 2, 4, 2>, 512);
+      case kFast256x128: return go(mx_tile_kernel<256, 128, 4, 2, 3>, 512);
+      case kFast128: return go(mx_tile_kernel<128, 128, 2, 4, 2>, 512);
+      case kFast128Alone: return go(mx_tile_kernel<128, 128, 2, 4, 4>, 512);
+      case kFast64: return go(mx_tile_kernel<64, 64, 2, 2, 4>, 256);
+      default: return go(mx_rows_kernel<4, 3>, 256);
+    }
+  });
 }
 
 }  // namespace mrl
