@@ -30,58 +30,139 @@ __device__ __forceinline__ uint32_t scale_at(uint32_t line, uint32_t g) {
   return ((g * 16 + (line >> 3 & 3) * 4 + (line & 3)) << 2) + (line >> 5) * 2 + (line >> 2 & 1);
 }
 
-// A block a thread: 64 lines by a step of 128 values a workgroup.
+// What a workgroup quantises or reads back: 64 lines by a step of 128 values.  Lanes take eight neighbouring values of a line, sixteen lanes a line.
+struct Tile64 {
+  uint32_t s, group, batch;                // step, group of lines, batch
+  uint64_t scales;                         // where the tile's 256 bytes of scales lie
+  __device__ __forceinline__ Tile64(const MxRows& p, uint64_t id, bool shared) {
+    const uint32_t steps = mx_steps(p.k), groups = (p.lines + 63) / 64;
+    const uint64_t outer = id / steps;
+    s = (uint32_t)(id - outer * steps);
+    batch = (uint32_t)(outer / groups);
+    group = (uint32_t)(outer - (uint64_t)batch * groups);
+    scales = (((uint64_t)(shared ? 0 : batch) * groups + group) * steps + s) * 256;
+  }
+};
+// The codes of a line's step.
+__device__ __forceinline__ uint8_t* codes_of(const MxRows& p, uint32_t batch, uint32_t line, uint32_t s) {
+  const uint32_t steps = mx_steps(p.k);
+  return p.codes + (((uint64_t)batch * p.lines + line) * steps + s) * 64;
+}
+
+// The largest of four lanes'.
+__device__ __forceinline__ uint32_t max4(uint32_t x) {
+  x = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xF, 0xF, true));        // lanes 1, 0, 3, 2
+  return max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xF, 0xF, true));     // lanes 2, 3, 0, 1
+}
+
+// Lines whose neighbours along k are adjacent: four lanes share a block.
+template <class T>
 __global__ __launch_bounds__(256) void mx_quantize_kernel(const MxRows p, uint64_t first) {
-  const uint32_t steps = mx_steps(p.k), groups = (p.lines + 63) / 64;
-  const uint64_t id = first + blockIdx.x;
-  const uint32_t s = (uint32_t)(id % steps), group = (uint32_t)(id / steps % groups), batch = (uint32_t)(id / steps / groups);
-  const uint32_t l = threadIdx.x & 63, g = threadIdx.x >> 6, line = group * 64 + l, k0 = s * 128 + g * 32;
-  float v[32];
+  __shared__ __attribute__((aligned(4))) uint8_t scales[256];
+  const Tile64 at(p, first + blockIdx.x, false);
+  const uint32_t c = threadIdx.x & 15, l0 = threadIdx.x >> 4, k = at.s * 128 + c * 8, valid = k < p.k ? p.k - k : 0;
+  const T* const x = (const T*)p.x.data + (int64_t)at.batch * p.x.batch + k;
+  float v[4][8];
+#pragma unroll
+  for (uint32_t i = 0; i < 4; i++) {
+    const uint32_t line = at.group * 64 + i * 16 + l0;
+    load8(x + (int64_t)line * p.x.ld, line < p.lines ? valid : 0, v[i]);
+  }
+#pragma unroll
+  for (uint32_t i = 0; i < 4; i++) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int e = 0; e < 8; e++) most = max(most, __float_as_uint(v[i][e]) & 0x7FFFFFFFu);
+    most = max4(most);
+    const bool finite = most < 0x7F800000u;
+    const uint32_t scale = finite ? scale_of(most) : 255, l = i * 16 + l0, line = at.group * 64 + l;
+    if ((c & 3) == 0) scales[scale_at(l, c >> 2)] = (uint8_t)scale;
+    const uint32_t codes = finite ? codes8(v[i], power_of(scale)) : 0;
+    if (line < p.lines) *(uint32_t*)(codes_of(p, at.batch, line, at.s) + c * 4) = codes;
+  }
+  __syncthreads();
+  if (threadIdx.x < 64) *(uint32_t*)(p.scales + at.scales + threadIdx.x * 4) = *(const uint32_t*)(scales + threadIdx.x * 4);
+}
+
+// Lines that are adjacent (a matrix k x lines that is row-major): the tile comes row by row, 16 bytes a lane, and goes through shared memory, from
+// which a thread takes a block; so do the codes, so that a line's 64 bytes are stored side by side.
+template <class T>
+__global__ __launch_bounds__(256) void mx_quantize_across_kernel(const MxRows p, uint64_t first) {
+  constexpr uint32_t E = 16 / sizeof(T), PER = 64 / E, ROWS = 256 / PER;     // elements of a load, loads of a row of 64 lines, rows at a time
+  __shared__ __attribute__((aligned(16))) T tile[128][64];
+  __shared__ __attribute__((aligned(16))) u32x4 codes[64][5];                // (a place more a line, against bank conflicts)
+  __shared__ __attribute__((aligned(4))) uint8_t scales[256];
+  const Tile64 at(p, first + blockIdx.x, false);
+  const uint32_t k0 = at.s * 128, line0 = at.group * 64, c = threadIdx.x % PER * E, r0 = threadIdx.x / PER;
+  const T* const x = (const T*)p.x.data + (int64_t)at.batch * p.x.batch + line0 + c;
+  const uint32_t there = line0 + c < p.lines ? p.lines - line0 - c : 0;
+  u32x4 v[128 / ROWS];
+#pragma unroll
+  for (uint32_t i = 0; i < 128 / ROWS; i++) {
+    const uint32_t k = k0 + i * ROWS + r0;
+    const T* const from = x + (int64_t)k * p.x.ld;
+    const uint32_t valid = k < p.k ? there : 0;
+    if (valid >= E) {
+      __builtin_memcpy(&v[i], from, 16);
+    } else {
+      T t[E];
+#pragma unroll
+      for (uint32_t e = 0; e < E; e++) t[e] = e < valid ? from[e] : (T)0.0f;
+      __builtin_memcpy(&v[i], t, 16);
+    }
+  }
+#pragma unroll
+  for (uint32_t i = 0; i < 128 / ROWS; i++) *(u32x4*)&tile[i * ROWS + r0][c] = v[i];
+  __syncthreads();
+  const uint32_t l = threadIdx.x & 63, g = threadIdx.x >> 6;
+  float w[4][8];
   uint32_t most = 0;
 #pragma unroll
-  for (int e = 0; e < 32; e++) {
-    const uint32_t k = k0 + e;
-    v[e] = 0.0f;
-    if (line < p.lines && k < p.k) {
-      const int64_t at = (int64_t)batch * p.x.batch + (p.kc ? (int64_t)line * p.x.ld + k : (int64_t)k * p.x.ld + line);
-      v[e] = p.x.bf16 ? (float)((const bf16*)p.x.data)[at] : ((const float*)p.x.data)[at];
-    }
-    most = max(most, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+  for (int i = 0; i < 32; i++) {
+    w[i / 8][i % 8] = (float)tile[g * 32 + i][l];
+    most = max(most, __float_as_uint(w[i / 8][i % 8]) & 0x7FFFFFFFu);
   }
   const bool finite = most < 0x7F800000u;
   const uint32_t scale = finite ? scale_of(most) : 255;
-  p.scales[(((uint64_t)batch * groups + group) * steps + s) * 256 + scale_at(l, g)] = (uint8_t)scale;
-  if (line >= p.lines) return;
-  u32x4 c = {0, 0, 0, 0};
+  scales[scale_at(l, g)] = (uint8_t)scale;
+  u32x4 q = {0, 0, 0, 0};
   if (finite) {
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-      const float x[8] = {v[8 * i], v[8 * i + 1], v[8 * i + 2], v[8 * i + 3], v[8 * i + 4], v[8 * i + 5], v[8 * i + 6], v[8 * i + 7]};
-      c[i] = codes8(x, power_of(scale));
-    }
+    for (int i = 0; i < 4; i++) q[i] = codes8(w[i], power_of(scale));
   }
-  *(u32x4*)(p.codes + (((uint64_t)batch * p.lines + line) * steps + s) * 64 + g * 16) = c;
+  codes[l][g] = q;
+  __syncthreads();
+  const uint32_t line = threadIdx.x >> 2, part = threadIdx.x & 3;
+  if (line0 + line < p.lines) *(u32x4*)(codes_of(p, at.batch, line0 + line, at.s) + part * 16) = codes[line][part];
+  if (threadIdx.x < 64) *(uint32_t*)(p.scales + at.scales + threadIdx.x * 4) = *(const uint32_t*)(scales + threadIdx.x * 4);
 }
 
-// Eight values a thread.
+// Blocks to values, in the order of mx_quantize_kernel.
+template <class T>
 __global__ __launch_bounds__(256) void mx_dequantize_kernel(const MxRows p, uint64_t first) {
-  const uint32_t per = (p.k + 7) / 8, steps = mx_steps(p.k), groups = (p.lines + 63) / 64;
-  const uint64_t id = (first + blockIdx.x) * 256 + threadIdx.x, row = id / per;
-  if (row >= (uint64_t)p.batches * p.lines) return;
-  const uint32_t at = (uint32_t)(id - row * per), batch = (uint32_t)(row / p.lines), line = (uint32_t)(row - (uint64_t)batch * p.lines);
-  const uint32_t from = p.shared ? 0 : batch, s = at / 16, g = at / 4 % 4;
-  const uint32_t c = *(const uint32_t*)(p.codes + (((uint64_t)from * p.lines + line) * steps) * 64 + at * 4);
-  const uint32_t scale = p.scales[(((uint64_t)from * groups + line / 64) * steps + s) * 256 + scale_at(line & 63, g)];
-  const float power = scale == 255 ? __uint_as_float(0x7FC00000u) : power_of(scale);
-  float v[8];
+  const Tile64 at(p, first + blockIdx.x, p.shared);
+  const uint32_t c = threadIdx.x & 15, l0 = threadIdx.x >> 4, k = at.s * 128 + c * 8;
+  if (k >= p.k) return;
+  uint32_t codes[4], scale[4];
 #pragma unroll
-  for (int e = 0; e < 8; e++) {
-    const uint32_t code = c >> 4 * e & 15, m = code & 7;
-    // magnitudes below 1 are 0 and 0.5; the others have an exponent of two bits above one of mantissa
-    const float a = m < 2 ? 0.5f * (float)m : __uint_as_float((126 + (m >> 1)) << 23 | (m & 1) << 22);
-    v[e] = (code & 8 ? -a : a) * power;
+  for (uint32_t i = 0; i < 4; i++) {
+    const uint32_t line = min(at.group * 64 + i * 16 + l0, p.lines - 1);
+    codes[i] = *(const uint32_t*)(codes_of(p, p.shared ? 0 : at.batch, line, at.s) + c * 4);
+    scale[i] = p.scales[at.scales + scale_at(line & 63, c >> 2)];
   }
-  store8(p.x.data, p.x.bf16, (int64_t)batch * p.x.batch + (int64_t)line * p.x.ld + at * 8, p.k - at * 8, v);
+  T* const x = (T*)p.x.data + (int64_t)at.batch * p.x.batch + k;
+#pragma unroll
+  for (uint32_t i = 0; i < 4; i++) {
+    const uint32_t line = at.group * 64 + i * 16 + l0;
+    if (line >= p.lines) break;
+    const float power = power_of(scale[i]);
+    const f32x2 t[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[i], power, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[i], power, 1),
+                        __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[i], power, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[i], power, 3)};
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; e++) v[e] = scale[i] == 255 ? __uint_as_float(0x7FC00000u) : t[e / 2][e % 2];
+    store8(x + (int64_t)line * p.x.ld, p.k - k, v);
+  }
 }
 
 // acc += a's block of 16 lines times b's over 128 values; sa and sb hold four blocks' scales, byte by byte.
@@ -354,12 +435,19 @@ __global__ __launch_bounds__(64 * WAVES) void mx_rows_kernel(const MxProduct x, 
 }  // namespace
 
 hipError_t launch_mx_quantize(const MxRows& p, hipStream_t st) {
-  return in_launches((uint64_t)p.batches * ((p.lines + 63ull) / 64) * mx_steps(p.k), [&](uint64_t first, uint32_t n) { mx_quantize_kernel<<<n, 256, 0, st>>>(p, first); });
+  return in_launches((uint64_t)p.batches * ((p.lines + 63ull) / 64) * mx_steps(p.k), [&](uint64_t first, uint32_t n) {
+    if (p.kc && p.x.bf16) mx_quantize_kernel<bf16><<<n, 256, 0, st>>>(p, first);
+    else if (p.kc) mx_quantize_kernel<float><<<n, 256, 0, st>>>(p, first);
+    else if (p.x.bf16) mx_quantize_across_kernel<bf16><<<n, 256, 0, st>>>(p, first);
+    else mx_quantize_across_kernel<float><<<n, 256, 0, st>>>(p, first);
+  });
 }
 
 hipError_t launch_mx_dequantize(const MxRows& p, hipStream_t st) {
-  const uint64_t items = (uint64_t)p.batches * p.lines * ((p.k + 7ull) / 8);
-  return in_launches((items + 255) / 256, [&](uint64_t first, uint32_t n) { mx_dequantize_kernel<<<n, 256, 0, st>>>(p, first); });
+  return in_launches((uint64_t)p.batches * ((p.lines + 63ull) / 64) * mx_steps(p.k), [&](uint64_t first, uint32_t n) {
+    if (p.x.bf16) mx_dequantize_kernel<bf16><<<n, 256, 0, st>>>(p, first);
+    else mx_dequantize_kernel<float><<<n, 256, 0, st>>>(p, first);
+  });
 }
 
 // How long a kernel takes, in us, as linear.hip's rule has it: a round of workgroups on the 256 compute units, one each or two at once, is `fixed`
