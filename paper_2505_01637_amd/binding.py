@@ -854,6 +854,7 @@ def layer_norm(x, weight=None, bias=None, *, eps=1e-5, stats=False, dtype=None, 
 
 
 def _form_norm_grad(key, grad, x, stats, weight, bias, residual, need_x):
+    _dtype_codes()
     sizes = _rows_count("x", x)
     if stats.shape != x.shape[:-1] + (2,) or stats.dtype != _float32 or not stats.is_contiguous():
         raise MorelloError(E_INVAL, "stats of shape %s, %s: what layer_norm returns has shape %s, float32, without gaps" % (tuple(stats.shape), stats.dtype,

@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cstdlib>
 
 #include "tiles.h"
 
@@ -36,6 +37,168 @@ __device__ __forceinline__ f32x2 sum_block(f32x2 v) {
 __device__ __forceinline__ int64_t start(const RowsOf& x, uint32_t row, uint32_t M) {
   const uint32_t batch = row / M;
   return (int64_t)batch * x.batch + (int64_t)(row - batch * M) * x.ld;
+}
+
+template <int CTRL>
+__device__ __forceinline__ float moved(float x) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xF, 0xF, true)); }
+// The sum over a wave, in every lane: within rows of sixteen lanes by moves, the four rows' after that.
+__device__ __forceinline__ float sum_wave(float x) {
+  x += moved<0xB1>(x);             // lanes 1, 0, 3, 2
+  x += moved<0x4E>(x);             // lanes 2, 3, 0, 1
+  x += moved<0x141>(x);            // mirrored in eight
+  x += moved<0x140>(x);            // and in sixteen
+  const int v = __float_as_int(x);
+  return (__int_as_float(__builtin_amdgcn_readlane(v, 0)) + __int_as_float(__builtin_amdgcn_readlane(v, 16))) +
+         (__int_as_float(__builtin_amdgcn_readlane(v, 32)) + __int_as_float(__builtin_amdgcn_readlane(v, 48)));
+}
+
+// ---- rows that are kept in registers
+//
+// A thread has eight neighbouring elements, R times.  Those that would end past the row are moved back to its last eight, so that no load waits for a
+// branch; `skip` of them are then another thread's (8 or more: all) and count nothing.  Rows have eight elements at least.  WHOLE: a multiple of eight, so that
+// skip is 0 or 8.
+struct Chunk {
+  uint32_t at, skip;
+  __device__ __forceinline__ Chunk(uint32_t n, uint32_t N) : at(min(n, N - 8)), skip(n - min(n, N - 8)) {}
+};
+
+// Eight elements as they are stored.
+template <class T> struct Raw {
+  T v[8];
+  __device__ __forceinline__ void load(const void* data, int64_t at) { __builtin_memcpy(v, (const T*)data + at, sizeof v); }
+  template <bool WHOLE>
+  __device__ __forceinline__ void clear(uint32_t skip) {
+    if (WHOLE) {
+      u32x4 w[sizeof v / 16];
+      __builtin_memcpy(w, v, sizeof v);
+#pragma unroll
+      for (uint32_t i = 0; i < sizeof v / 16; i++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) w[i][e] = skip ? 0u : w[i][e];
+      __builtin_memcpy(v, w, sizeof v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; e++) v[e] = (uint32_t)e < skip ? (T)0.0f : v[e];
+    }
+  }
+};
+// Eight elements of either type, without a branch: bf16 takes the first 16 bytes of the two loads.  other: what takes their place where there is no data (the
+// loads then go to `any`, 32 bytes that are there).
+struct Either {
+  u32x4 w[2];
+  __device__ __forceinline__ void load(const void* data, uint32_t is_bf16, int64_t at, const void* any) {
+    const char* const from = data ? (const char*)data + (at << (is_bf16 ? 1 : 2)) : (const char*)any;
+    __builtin_memcpy(&w[0], from, 16);
+    __builtin_memcpy(&w[1], from + (data && !is_bf16 ? 16 : 0), 16);
+  }
+  __device__ __forceinline__ void values(const void* data, uint32_t is_bf16, float other, float (&v)[8]) const {
+    const uint32_t flat[8] = {w[0][0], w[0][1], w[0][2], w[0][3], w[1][0], w[1][1], w[1][2], w[1][3]};
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+      const uint32_t half = e & 1 ? w[0][e >> 1] & 0xFFFF0000u : w[0][e >> 1] << 16;
+      v[e] = data ? __uint_as_float(is_bf16 ? half : flat[e]) : other;
+    }
+  }
+};
+
+constexpr uint32_t kRowThreads = 1024;     // of a workgroup that keeps rows
+constexpr uint32_t kKeep = 2;              // R at most: rows of up to 16384 elements
+
+// The sum of the group's waves' sums (uniform over each wave), in their order.  `sums` may be written again behind the next such exchange.
+__device__ __forceinline__ f32x2 sum_waves(f32x2 v, f32x2* sums, uint32_t group, uint32_t waves) {
+  if (waves == 1) return v;
+  if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = v;
+  __syncthreads();
+  v = f32x2{0.0f, 0.0f};
+  for (uint32_t i = 0; i < waves; i++) {
+    v[0] += sums[group * waves + i][0];
+    v[1] += sums[group * waves + i][1];
+  }
+  return v;
+}
+
+// `waves` waves a row; a workgroup's groups of waves take a row each, then the rows that follow those of all workgroups.  Memory bounds it, so the next
+// row's loads go out before this one's sums are made; weight and bias are read once.
+template <class T, int R, bool WHOLE>
+__global__ __launch_bounds__(kRowThreads) void norm_rows_kernel(const NormRows p, uint32_t waves) {
+  __shared__ f32x2 sums[2][kRowThreads / 64];
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = wave / waves, groups = blockDim.x / 64 / waves, rows = p.batches * p.M;
+  const uint32_t t = threadIdx.x - group * waves * 64, pitch = waves * 512, stride = gridDim.x * groups;
+  uint64_t row = (uint64_t)blockIdx.x * groups + group;
+  Raw<T> next[R];
+  const auto load = [&](uint64_t row) {
+    const int64_t x = start(p.x, (uint32_t)min(row, rows - 1ull), p.M);        // (past the last row it is read again)
+#pragma unroll
+    for (int i = 0; i < R; i++) next[i].load(p.x.data, x + Chunk(i * pitch + t * 8, p.N).at);
+  };
+  load(row);
+  float w[R][8], b[R][8];
+  {
+    Either ew[R], eb[R];
+    const void* const any = (const char*)p.x.data;         // (eight elements: 16 bytes of bf16, which both loads of Either take)
+#pragma unroll
+    for (int i = 0; i < R; i++) {
+      const Chunk c(i * pitch + t * 8, p.N);
+      ew[i].load(p.weight, p.weight_bf16, c.at, any);
+      eb[i].load(p.bias, p.bias_bf16, c.at, any);
+    }
+#pragma unroll
+    for (int i = 0; i < R; i++) {
+      ew[i].values(p.weight, p.weight_bf16, 1.0f, w[i]);
+      eb[i].values(p.bias, p.bias_bf16, 0.0f, b[i]);
+    }
+  }
+  const float one = 1.0f / (float)p.N;
+  for (uint64_t row0 = row - group; row0 < rows; row0 += stride, row += stride) {
+    float v[R][8];
+    f32x2 s = {0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < R; i++)
+#pragma unroll
+      for (int e = 0; e < 8; e++) v[i][e] = (float)next[i].v[e];
+    if (row0 + stride < rows) load(row + stride);
+#pragma unroll
+    for (int i = 0; i < R; i++) {
+      const Chunk c(i * pitch + t * 8, p.N);
+      if (WHOLE && c.skip) continue;
+#pragma unroll
+      for (int e = 0; e < 8; e++) s[0] += WHOLE || (uint32_t)e >= c.skip ? v[i][e] : 0.0f;
+    }
+    // (rounded here and nowhere else: folded into the subtractions below it would be another number in each of them)
+    const float about = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(sum_waves(f32x2{sum_wave(s[0]), 0.0f}, sums[0], group, waves)[0] * one)));
+    // the sum of what is left puts the mean right: where it is far from 0, its own sum has lost that much
+    s[0] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < R; i++) {
+      const Chunk c(i * pitch + t * 8, p.N);
+#pragma unroll
+      for (int e = 0; e < 8; e++) v[i][e] -= about;
+      if (WHOLE && c.skip) continue;
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        const float d = WHOLE || (uint32_t)e >= c.skip ? v[i][e] : 0.0f;
+        s[0] += d;
+        s[1] += d * d;
+      }
+    }
+    s = sum_waves(f32x2{sum_wave(s[0]), sum_wave(s[1])}, sums[1], group, waves);
+    const float rest = s[0] * one, var = s[1] * one - rest * rest, r = 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + p.eps);       // (NaN stays)
+    if (row >= rows) continue;
+    if (p.stats && t == 0) {
+      p.stats[2 * row] = about + rest;
+      p.stats[2 * row + 1] = r;
+    }
+    const int64_t out = start(p.out, (uint32_t)row, p.M);
+#pragma unroll
+    for (int i = 0; i < R; i++) {
+      const uint32_t n = i * pitch + t * 8;
+      if (n >= p.N) continue;
+#pragma unroll
+      for (int e = 0; e < 8; e++) v[i][e] = (v[i][e] - rest) * r * w[i][e] + b[i][e];
+      // (what is another thread's too is the same there)
+      store8(p.out.data, p.out.bf16, out + Chunk(n, p.N).at, 8, v[i]);
+    }
+  }
 }
 
 // A row a workgroup, eight elements a thread at a time, three passes over it.
@@ -132,44 +295,11 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(const NormGrad p, u
   }
 }
 
-// ---- gradients of rows that a workgroup keeps in registers
-
-template <int CTRL>
-__device__ __forceinline__ float moved(float x) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xF, 0xF, true)); }
-// The sum over a wave, in every lane: within rows of sixteen lanes by moves, the four rows' after that.
-__device__ __forceinline__ float sum_wave(float x) {
-  x += moved<0xB1>(x);             // lanes 1, 0, 3, 2
-  x += moved<0x4E>(x);             // lanes 2, 3, 0, 1
-  x += moved<0x141>(x);            // mirrored in eight
-  x += moved<0x140>(x);            // and in sixteen
-  const int v = __float_as_int(x);
-  return (__int_as_float(__builtin_amdgcn_readlane(v, 0)) + __int_as_float(__builtin_amdgcn_readlane(v, 16))) +
-         (__int_as_float(__builtin_amdgcn_readlane(v, 32)) + __int_as_float(__builtin_amdgcn_readlane(v, 48)));
-}
-
-// Eight neighbouring elements as they are stored.
-template <class T> struct Raw { T v[8]; };
-template <class T>
-__device__ __forceinline__ Raw<T> load_raw(const T* p, uint32_t valid) {
-  Raw<T> r;
-  if (valid >= 8) {
-    __builtin_memcpy(r.v, p, sizeof r.v);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; e++) r.v[e] = (uint32_t)e < valid ? p[e] : (T)0.0f;
-  }
-  return r;
-}
-
-constexpr uint32_t kRowThreads = 512;      // of a workgroup that keeps rows
-constexpr uint32_t kKeep = 4;              // times 8 elements a thread has of a row at most: 16384 elements
-
-// `waves` waves a row, R times eight elements a thread; the workgroup's groups of waves take its `each` rows in turn and keep the columns' sums, which they add
-// in their order at the end.  partial: the workgroups' sums (2 x N each: dw, db), nullptr where there is one workgroup.
-// Memory bounds it, so the next row's loads go out before this row's sums are made (where there is room: not four times f32).
-template <class TX, class TG, int R>
+// The gradient of such rows: each workgroup's groups take its `each` rows in turn and keep the columns' sums, which they add in their order at the end.
+// partial: the workgroups' sums (2 x N each: dw, db), nullptr where there is one workgroup.
+template <class TX, class TG, int R, bool WHOLE>
 __global__ __launch_bounds__(kRowThreads) void norm_grad_rows_kernel(const NormGrad p, uint32_t waves, uint32_t each, uint32_t first, float* __restrict__ partial) {
-  constexpr bool AHEAD = R * (sizeof(TX) + sizeof(TG)) < 32;
+  constexpr bool AHEAD = R == 1;                                         // (twice: no registers for it)
   __shared__ f32x2 sums[2][kRowThreads / 64];
   __shared__ float columns[2][R == 1 ? kRowThreads / 2 * 8 : 8];         // (more than one group only where a row has half of the threads or fewer)
   const uint32_t block = first + blockIdx.x, rows = p.batches * p.M;
@@ -179,87 +309,98 @@ __global__ __launch_bounds__(kRowThreads) void norm_grad_rows_kernel(const NormG
   const uint32_t end = (uint32_t)min(begin + each, (uint64_t)rows);
   const bool wants = p.dweight || p.dbias;
 
-  float w[R][8], dw[R][8], db[R][8];
-#pragma unroll
-  for (int i = 0; i < R; i++) {
-    const uint32_t n = i * pitch + t * 8, valid = n < p.N ? p.N - n : 0;
-#pragma unroll
-    for (int e = 0; e < 8; e++) { w[i][e] = 1.0f; dw[i][e] = db[i][e] = 0.0f; }
-    if (p.weight) load8(p.weight, p.weight_bf16, n, valid, w[i]);
-  }
-  Raw<TX> x[R], x1[R];
-  Raw<TG> g[R], g1[R];
-  float mean, r, mean1 = 0.0f, r1 = 0.0f;
-  const auto load = [&](uint32_t row, Raw<TX> (&x)[R], Raw<TG> (&g)[R], float& mean, float& r) {
-    if (row >= end) return;
+  Raw<TX> x1[R];
+  Raw<TG> g1[R];
+  float mean1 = 0.0f, r1 = 0.0f;
+  const auto load = [&](uint32_t at) {
+    const uint32_t row = min(at, end - 1);         // (past the last row it is read again)
     const int64_t at_x = start(p.x, row, p.M), at_g = start(p.grad, row, p.M);
-    mean = p.stats[2 * (uint64_t)row];
-    r = p.stats[2 * (uint64_t)row + 1];
+    mean1 = p.stats[2 * (uint64_t)row];
+    r1 = p.stats[2 * (uint64_t)row + 1];
 #pragma unroll
     for (int i = 0; i < R; i++) {
-      const uint32_t n = i * pitch + t * 8, valid = n < p.N ? p.N - n : 0;
-      x[i] = load_raw((const TX*)p.x.data + at_x + n, valid);
-      g[i] = load_raw((const TG*)p.grad.data + at_g + n, valid);
+      const Chunk c(i * pitch + t * 8, p.N);
+      x1[i].load(p.x.data, at_x + c.at);
+      g1[i].load(p.grad.data, at_g + c.at);
     }
   };
-  if (AHEAD) load((uint32_t)begin + group, x1, g1, mean1, r1);
-  uint32_t turn = 0;
-  for (uint32_t row0 = (uint32_t)begin; row0 < end; row0 += groups, turn ^= 1) {
-    const uint32_t row = row0 + group;
-    if (AHEAD) {
+  float w[R][8], dw[R][8], db[R][8];
 #pragma unroll
-      for (int i = 0; i < R; i++) { x[i] = x1[i]; g[i] = g1[i]; }
-      mean = mean1;
-      r = r1;
-      load(row + groups, x1, g1, mean1, r1);
-    } else {
-      load(row, x, g, mean, r);
+  for (int i = 0; i < R; i++)
+#pragma unroll
+    for (int e = 0; e < 8; e++) { w[i][e] = 1.0f; dw[i][e] = db[i][e] = 0.0f; }
+  if (begin < end) {
+    if (AHEAD) load((uint32_t)begin + group);
+    if (p.weight) {
+      Either ew[R];
+#pragma unroll
+      for (int i = 0; i < R; i++) ew[i].load(p.weight, p.weight_bf16, Chunk(i * pitch + t * 8, p.N).at, p.weight);
+#pragma unroll
+      for (int i = 0; i < R; i++) ew[i].values(p.weight, p.weight_bf16, 1.0f, w[i]);
     }
+  }
+  const float one = 1.0f / (float)p.N;
+  uint32_t turn = 0;
+  for (uint64_t row0 = begin; row0 < end; row0 += groups, turn ^= 1) {
+    const uint32_t row = (uint32_t)row0 + group;
+    if (!AHEAD) load(row);
+    Raw<TX> x[R];
+    Raw<TG> g[R];
+    const float mean = mean1, r = r1;
+#pragma unroll
+    for (int i = 0; i < R; i++) {
+      x[i] = x1[i];
+      g[i] = g1[i];
+      g[i].template clear<WHOLE>(Chunk(i * pitch + t * 8, p.N).skip);
+    }
+    if (AHEAD && row0 + groups < end) load(row + groups);
     float s0 = 0.0f, s1 = 0.0f;
     if (row < end) {
 #pragma unroll
       for (int i = 0; i < R; i++)
 #pragma unroll
         for (int e = 0; e < 8; e++) {
-          const uint32_t n = i * pitch + t * 8 + e;
           const float grad = (float)g[i].v[e], h = ((float)x[i].v[e] - mean) * r, gw = grad * w[i][e];
-          if (n < p.N) {           // (behind the row's end: a NaN of its statistics would come in)
-            s0 += gw;
-            s1 += gw * h;
-            dw[i][e] += grad * h;
-            db[i][e] += grad;
-          }
+          s0 += gw;
+          s1 += gw * h;
+          dw[i][e] += grad * h;
+          db[i][e] += grad;
         }
     }
     if (!p.dx.data) continue;
-    s0 = sum_wave(s0);
-    s1 = sum_wave(s1);
-    if (waves > 1) {
-      if (threadIdx.x % 64 == 0) sums[turn][wave] = f32x2{s0, s1};
-      __syncthreads();             // (and the other half is free: what was read there was read before this)
-      s0 = s1 = 0.0f;
-      for (uint32_t i = 0; i < waves; i++) {
-        const f32x2 s = sums[turn][group * waves + i];
-        s0 += s[0];
-        s1 += s[1];
-      }
+    Either z[R];
+    if (p.residual.data && row < end) {            // (asked for before the sums go around)
+      const int64_t at = start(p.residual, row, p.M);
+#pragma unroll
+      for (int i = 0; i < R; i++) z[i].load(p.residual.data, p.residual.bf16, at + Chunk(i * pitch + t * 8, p.N).at, p.residual.data);
     }
+    const f32x2 s = sum_waves(f32x2{sum_wave(s0), sum_wave(s1)}, sums[turn], group, waves);
     if (row >= end) continue;
-    const float a = s0 / (float)p.N, b = s1 / (float)p.N;
-    const int64_t dx = start(p.dx, row, p.M), residual = p.residual.data ? start(p.residual, row, p.M) : 0;
+    const float a = s[0] * one, b = s[1] * one;
+    const int64_t dx = start(p.dx, row, p.M);
 #pragma unroll
     for (int i = 0; i < R; i++) {
-      const uint32_t n = i * pitch + t * 8;
-      if (n >= p.N) continue;
-      float v[8], z[8];
-      if (p.residual.data) load8(p.residual.data, p.residual.bf16, residual + n, p.N - n, z);
+      const Chunk c(i * pitch + t * 8, p.N);
+      if (c.skip >= 8) continue;
+      float v[8];
 #pragma unroll
       for (int e = 0; e < 8; e++) v[e] = r * ((float)g[i].v[e] * w[i][e] - a - ((float)x[i].v[e] - mean) * r * b);
       if (p.residual.data) {
+        float y[8];
+        z[i].values(p.residual.data, p.residual.bf16, 0.0f, y);
 #pragma unroll
-        for (int e = 0; e < 8; e++) v[e] += z[e];
+        for (int e = 0; e < 8; e++) v[e] += y[e];
       }
-      store8(p.dx.data, p.dx.bf16, dx + n, p.N - n, v);
+      if (WHOLE || c.skip == 0) {
+        store8(p.dx.data, p.dx.bf16, dx + c.at, 8, v);
+      } else {
+#pragma unroll
+        for (int e = 1; e < 8; e++) {
+          if ((uint32_t)e < c.skip) continue;
+          if (p.dx.bf16) ((bf16*)p.dx.data)[dx + c.at + e] = (bf16)v[e];
+          else ((float*)p.dx.data)[dx + c.at + e] = v[e];
+        }
+      }
     }
   }
   if (!wants) return;
@@ -276,18 +417,23 @@ __global__ __launch_bounds__(kRowThreads) void norm_grad_rows_kernel(const NormG
     }
   }
   if (group) return;
+  const auto put = [&](void* to, uint32_t is_bf16, const Chunk& c, const float (&v)[8]) {
+    if (!to) return;
+    if (c.skip == 0) return store8(to, is_bf16, (int64_t)c.at, 8, v);
+#pragma unroll
+    for (int e = 1; e < 8; e++) {
+      if ((uint32_t)e < c.skip) continue;
+      if (is_bf16) ((bf16*)to)[c.at + e] = (bf16)v[e];
+      else ((float*)to)[c.at + e] = v[e];
+    }
+  };
 #pragma unroll
   for (int i = 0; i < R; i++) {
-    const uint32_t n = i * pitch + t * 8, valid = n < p.N ? p.N - n : 0;
-    if (!valid) continue;
-    if (partial) {
-      float* const to = partial + (uint64_t)block * 2 * p.N + n;
-      store8(to, valid, dw[i]);
-      store8(to + p.N, valid, db[i]);
-    } else {
-      if (p.dweight) store8(p.dweight, p.dweight_bf16, n, valid, dw[i]);
-      if (p.dbias) store8(p.dbias, p.dbias_bf16, n, valid, db[i]);
-    }
+    const Chunk c(i * pitch + t * 8, p.N);
+    if (c.skip >= 8) continue;
+    float* const to = partial + (uint64_t)block * 2 * p.N;
+    put(partial ? to : p.dweight, partial ? 0 : p.dweight_bf16, c, dw[i]);
+    put(partial ? to + p.N : p.dbias, partial ? 0 : p.dbias_bf16, c, db[i]);
   }
 }
 
@@ -362,12 +508,14 @@ GradPlan plan_grad(const NormGrad& p) {
   const uint64_t rows = (uint64_t)p.batches * p.M;
   const bool sums = p.dweight || p.dbias;
   GradPlan g{};
-  constexpr uint32_t most = kRowThreads * 8;
-  if (p.N <= most * kKeep) {
-    g.keep = p.N <= most ? 1 : p.N <= 2 * most ? 2 : 4;
+  if (p.N >= 8 && p.N <= kRowThreads * 8 * kKeep) {
+    g.keep = p.N <= kRowThreads * 8 ? 1 : 2;
     g.waves = (p.N + 512 * g.keep - 1) / (512 * g.keep);
     g.groups = kRowThreads / 64 / g.waves;
-    const uint64_t want = sums ? 512 : 4096;                   // workgroups
+    static const char* const f = getenv("NORM_GRAD");
+    if (f) g.groups = std::max(1u, std::min<uint32_t>(g.groups, atoi(f)));
+    static const char* const f2 = getenv("NORM_GRAD_WANT");
+    const uint64_t want = sums ? f2 ? atoi(f2) : 256 : 4096;                   // workgroups
     g.each = (uint32_t)((rows + want * g.groups - 1) / (want * g.groups)) * g.groups;
     if (rows <= 4 * g.groups) g.each = 4 * g.groups;           // (few rows: no second launch)
   } else {
@@ -384,19 +532,43 @@ template <class TX, class TG>
 hipError_t launch_rows(const NormGrad& p, const GradPlan& g, float* partial, hipStream_t st) {
   return in_launches(g.blocks, [&](uint64_t first, uint32_t n) {
     const auto go = [&](auto kernel) { kernel<<<n, g.groups * g.waves * 64, 0, st>>>(p, g.waves, g.each, (uint32_t)first, g.blocks > 1 ? partial : nullptr); };
-    switch (g.keep) {
-      case 1: return go(norm_grad_rows_kernel<TX, TG, 1>);
-      case 2: return go(norm_grad_rows_kernel<TX, TG, 2>);
-      default: return go(norm_grad_rows_kernel<TX, TG, 4>);
-    }
+    if (p.N % 8 == 0) g.keep == 1 ? go(norm_grad_rows_kernel<TX, TG, 1, true>) : go(norm_grad_rows_kernel<TX, TG, 2, true>);
+    else g.keep == 1 ? go(norm_grad_rows_kernel<TX, TG, 1, false>) : go(norm_grad_rows_kernel<TX, TG, 2, false>);
   });
+}
+
+// How rows are normalised.
+struct NormPlan { uint32_t keep, waves, groups, blocks; };     // keep: R, 0: too long (or short) to be kept
+NormPlan plan_norm(uint64_t rows, uint32_t N) {
+  NormPlan g{};
+  if (N < 8 || N > kRowThreads * 8 * kKeep) return g;
+  static const char* const f = getenv("NORM_KEEP");
+  static const char* const f2 = getenv("NORM_BLOCKS");
+  g.keep = N <= kRowThreads * 8 ? 1 : 2;
+  if (f) g.keep = std::max<uint32_t>(g.keep, atoi(f));
+  g.waves = (N + 512 * g.keep - 1) / (512 * g.keep);
+  g.groups = std::max(1u, 4 / g.waves);
+  g.blocks = (uint32_t)std::min<uint64_t>((rows + g.groups - 1) / g.groups, f2 ? atoi(f2) : 2048);
+  return g;
+}
+
+template <class T>
+void launch_norm_rows(const NormRows& p, const NormPlan& g, hipStream_t st) {
+  const auto go = [&](auto kernel) { kernel<<<g.blocks, g.groups * g.waves * 64, 0, st>>>(p, g.waves); };
+  if (p.N % 8 == 0) g.keep == 1 ? go(norm_rows_kernel<T, 1, true>) : go(norm_rows_kernel<T, 2, true>);
+  else g.keep == 1 ? go(norm_rows_kernel<T, 1, false>) : go(norm_rows_kernel<T, 2, false>);
 }
 
 }  // namespace
 
 hipError_t launch_norm(const NormRows& p, hipStream_t st) {
-  if (!p.N) return hipSuccess;
-  return in_launches((uint64_t)p.batches * p.M, [&](uint64_t first, uint32_t n) { norm_kernel<<<n, kThreads, 0, st>>>(p, (uint32_t)first); });
+  const uint64_t rows = (uint64_t)p.batches * p.M;
+  if (!p.N || !rows) return hipSuccess;
+  const NormPlan g = plan_norm(rows, p.N);
+  if (!g.keep) return in_launches(rows, [&](uint64_t first, uint32_t n) { norm_kernel<<<n, kThreads, 0, st>>>(p, (uint32_t)first); });
+  if (p.x.bf16) launch_norm_rows<bf16>(p, g, st);
+  else launch_norm_rows<float>(p, g, st);
+  return hipGetLastError();
 }
 
 uint64_t norm_grad_bytes(const NormGrad& p) {

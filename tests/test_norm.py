@@ -221,6 +221,18 @@ def test_norm_in_place_and_the_same_bits():
 
 
 @gpu
+def test_grad_as_the_first_call_of_a_process(monkeypatch):
+    torch, _ = _torch()
+    x = torch.randn((5, 40), device="cuda")
+    _, stats = B.layer_norm(x, stats=True)
+    want = B.layer_norm_grad(x, x, stats)[0]
+    for name in ("_codes", "_uint8", "_float32", "_raw_stream", "_current_device"):
+        monkeypatch.setattr(B, name, None)
+    monkeypatch.setattr(B, "_forms", {})
+    assert torch.equal(B.layer_norm_grad(x, x, stats)[0], want)
+
+
+@gpu
 def test_norm_streams_graphs_and_workspaces():
     torch, _ = _torch()
     m, n = 700, 520
