@@ -55,18 +55,46 @@ __device__ __forceinline__ uint32_t max4(uint32_t x) {
   return max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xF, 0xF, true));     // lanes 2, 3, 0, 1
 }
 
+// Eight neighbouring values of a line of K, K at least 8, without a branch that a load would wait for: a chunk that ends past the line is read from the line's
+// last eight and moved down, zeros behind it.
+template <class T> struct Eight {
+  T t[8];
+  __device__ __forceinline__ void load(const T* line, uint32_t k, uint32_t K) { __builtin_memcpy(t, line + min(k, K - 8), sizeof t); }
+  __device__ __forceinline__ void values(uint32_t k, uint32_t K, float (&v)[8]) const {
+    const uint32_t past = k + 8 > K ? k + 8 - K : 0;
+#pragma unroll
+    for (int e = 0; e < 8; e++) v[e] = (float)t[e];
+    if (K % 8) {
+#pragma unroll
+      for (int by = 1; by < 8; by *= 2)
+#pragma unroll
+        for (int e = 0; e < 8; e++) v[e] = past & by ? (e + by < 8 ? v[e + by] : 0.0f) : v[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 8; e++) v[e] = past >= 8 ? 0.0f : v[e];
+  }
+};
+
 // Lines whose neighbours along k are adjacent: four lanes share a block.
 template <class T>
 __global__ __launch_bounds__(256) void mx_quantize_kernel(const MxRows p, uint64_t first) {
   __shared__ __attribute__((aligned(4))) uint8_t scales[256];
   const Tile64 at(p, first + blockIdx.x, false);
-  const uint32_t c = threadIdx.x & 15, l0 = threadIdx.x >> 4, k = at.s * 128 + c * 8, valid = k < p.k ? p.k - k : 0;
-  const T* const x = (const T*)p.x.data + (int64_t)at.batch * p.x.batch + k;
+  const uint32_t c = threadIdx.x & 15, l0 = threadIdx.x >> 4, k = at.s * 128 + c * 8;
+  const T* const x = (const T*)p.x.data + (int64_t)at.batch * p.x.batch;
   float v[4][8];
+  if (p.k >= 8) {
+    Eight<T> t[4];
 #pragma unroll
-  for (uint32_t i = 0; i < 4; i++) {
-    const uint32_t line = at.group * 64 + i * 16 + l0;
-    load8(x + (int64_t)line * p.x.ld, line < p.lines ? valid : 0, v[i]);
+    for (uint32_t i = 0; i < 4; i++) t[i].load(x + (int64_t)min(at.group * 64 + i * 16 + l0, p.lines - 1) * p.x.ld, k, p.k);
+#pragma unroll
+    for (uint32_t i = 0; i < 4; i++) t[i].values(at.group * 64 + i * 16 + l0 < p.lines ? k : p.k, p.k, v[i]);
+  } else {
+#pragma unroll
+    for (uint32_t i = 0; i < 4; i++) {
+      const uint32_t line = at.group * 64 + i * 16 + l0;
+      load8(x + (int64_t)line * p.x.ld + k, line < p.lines && k < p.k ? p.k - k : 0, v[i]);
+    }
   }
 #pragma unroll
   for (uint32_t i = 0; i < 4; i++) {
@@ -151,6 +179,7 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(const MxRows p, uint
     scale[i] = p.scales[at.scales + scale_at(line & 63, c >> 2)];
   }
   T* const x = (T*)p.x.data + (int64_t)at.batch * p.x.batch + k;
+  const bool past = (uint64_t)p.batches * p.lines * p.k * sizeof(T) >= kPast;
 #pragma unroll
   for (uint32_t i = 0; i < 4; i++) {
     const uint32_t line = at.group * 64 + i * 16 + l0;
@@ -161,7 +190,8 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(const MxRows p, uint
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; e++) v[e] = scale[i] == 255 ? __uint_as_float(0x7FC00000u) : t[e / 2][e % 2];
-    store8(x + (int64_t)line * p.x.ld, p.k - k, v);
+    if (past && p.k - k >= 8) store8_past(x + (int64_t)line * p.x.ld, v);
+    else store8(x + (int64_t)line * p.x.ld, p.k - k, v);
   }
 }
 
@@ -226,6 +256,66 @@ __device__ __forceinline__ void read_scales(lds_ptr slots, uint32_t first, uint3
 #pragma unroll
   for (uint32_t i = 0; i < (W + 63) / 64; i++) s[i] = *(const __attribute__((address_space(3))) uint32_t*)(slots + ((first / 64 + i) * 2 + kk) * 256 + lane * 4);
   if (W < 64) s[0] >>= first % 64 / 16 * 8;
+}
+
+// A wave's results through shared memory of its own, PASS blocks of 16 rows at a time, as write_out of tiles.h has them go, but in their order: then what
+// is left to a row's eight columns is its place one row of lanes on.  (Its address worked out anew for each, and the checks of what there is to add, make that
+// twice as long: 62 us of 198 for 8192 x 2048 x 16384 without an activation.)
+template <int PASS, int BM, int BN>
+__device__ __forceinline__ void store_results(const Product& p, const Place& at, uint32_t splits, uint32_t m0, uint32_t n0, uint32_t lane, const f32x4 (&acc)[BM][BN],
+                                              char* mine, float* __restrict__ partial) {
+  constexpr uint32_t CHUNKS = BN * 4, GROUPS = BN * 2, ROWS = 64 / GROUPS;      // chunks and groups of 8 columns of a row; rows at a time
+  const Epilogue& e = p.e;
+  const uint32_t q = lane & 15, g = lane >> 4;
+  const uint32_t c = lane % GROUPS, n = n0 + c * 8, l = lane / GROUPS;
+  float bias[8];
+  bias8(e, n, n < p.N ? p.N - n : 0, bias);
+  const uint32_t pitch = (p.N + 7) & ~7u;
+  const RowsOf out = splits > 1 ? RowsOf{partial + (uint64_t)at.split * p.batches * p.M * pitch, pitch, (int64_t)p.M * pitch, 0} : e.out;
+  const bool ends = splits == 1, residual = ends && e.residual.data, past = ends && ((uint64_t)p.batches * p.M * p.N << (out.bf16 ? 1 : 2)) >= kPast;
+  const uint32_t valid = splits > 1 ? 8 : n < p.N ? p.N - n : 0, out_shift = out.bf16 ? 1 : 2, res_shift = e.residual.bf16 ? 1 : 2;
+  char* to = (char*)out.data + (((int64_t)at.batch * out.batch + (int64_t)(m0 + l) * out.ld + n) << out_shift);
+  const char* from = (const char*)e.residual.data + (((int64_t)at.batch * e.residual.batch + (int64_t)(m0 + l) * e.residual.ld + n) << res_shift);
+  const int64_t to_step = ROWS * out.ld << out_shift, from_step = ROWS * e.residual.ld << res_shift;
+#pragma unroll
+  for (int h = 0; h < BM; h += PASS) {
+#pragma unroll
+    for (int i = 0; i < PASS; i++) {
+      const uint32_t r = row_of<bf16, true>(i, q);
+#pragma unroll
+      for (int j = 0; j < BN; j++) *(f32x4*)(mine + (r * CHUNKS + ((j / 2 * 8 + 2 * g + j % 2) ^ (r & (CHUNKS - 1)))) * 16) = acc[h + i][j];
+    }
+    asm volatile("" ::: "memory");         // (a wave's accesses to shared memory are done in their order)
+    if (n < p.N) {
+#pragma unroll 4
+      for (uint32_t r = l; r < 16 * PASS; r += ROWS) {
+        if (m0 + h * 16 + r >= p.M) break;
+        float v[8];
+#pragma unroll
+        for (int x = 0; x < 2; x++) {
+          const f32x4 t = *(const f32x4*)(mine + (r * CHUNKS + ((2 * c + x) ^ (r & (CHUNKS - 1)))) * 16);
+#pragma unroll
+          for (int k = 0; k < 4; k++) v[4 * x + k] = t[k];
+        }
+        if (ends) {
+#pragma unroll
+          for (int k = 0; k < 8; k++) v[k] += bias[k];
+          activate8(e.activation, v);
+        }
+        if (residual) {
+          float y[8];
+          load8(from, e.residual.bf16, 0, valid, y);
+#pragma unroll
+          for (int k = 0; k < 8; k++) v[k] += y[k];
+          from += from_step;
+        }
+        if (past && valid >= 8) store8_past(to, out.bf16, 0, v);
+        else store8(to, out.bf16, 0, valid, v);
+        to += to_step;
+      }
+    }
+    asm volatile("" ::: "memory");
+  }
 }
 
 // One tile of TM x TN, WAVES_M x WAVES_N waves, STAGES steps in shared memory: the loop of linear.hip's fast_kernel.
@@ -346,16 +436,55 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void mx_tile_kernel(cons
     }
     arrive<0>();                  // nothing is under way to shared memory when it is given up
   }
-  write_out<bf16, PASS, BM, BN, true>(p, at, splits, m0 + wm, n0 + wn, lane, acc, lds + wave * OUT, partial);
+  store_results<PASS>(p, at, splits, m0 + wm, n0 + wn, lane, acc, lds + wave * OUT, partial);
+}
+
+// lhs of a product of few rows that the workgroup puts into blocks itself, in shared memory: `rows` lines of `per` steps, then a byte of scale for each half step,
+// quarter of it and line.
+constexpr uint32_t kOwnLhs = 48 * 1024;
+__host__ __device__ constexpr uint32_t own_pitch(uint32_t per) { return per * kStep + 64; }       // (64 more, against bank conflicts)
+__host__ __device__ constexpr uint64_t own_bytes(uint32_t rows, uint32_t per) { return (uint64_t)rows * own_pitch(per) + (uint64_t)per * 2 * 64; }
+
+// Eight values a thread, four threads a block, BATCH times before the first is used.
+template <class T>
+__device__ __forceinline__ void own_blocks(const MxRows& x, uint32_t batch, uint32_t m0, uint32_t rows, uint32_t step0, uint32_t per, char* codes, uint8_t* scales) {
+  constexpr uint32_t BATCH = 4;
+  const uint32_t line = per * 32, items = rows * line, k0 = step0 * 256;         // chunks of eight of a line
+  const T* const from = (const T*)x.x.data + (int64_t)batch * x.x.batch + (int64_t)m0 * x.x.ld;
+  for (uint32_t first = threadIdx.x; first < items; first += BATCH * blockDim.x) {
+    Eight<T> t[BATCH];
+#pragma unroll
+    for (uint32_t b = 0; b < BATCH; b++) {
+      const uint32_t i = min(first + b * blockDim.x, items - 1), r = i / line;
+      t[b].load(from + (int64_t)r * x.x.ld, k0 + (i - r * line) * 8, x.k);
+    }
+#pragma unroll
+    for (uint32_t b = 0; b < BATCH; b++) {
+      const uint32_t i = first + b * blockDim.x, r = i / line, c = i - r * line;
+      if (i >= items) continue;    // (four lanes of a block at once)
+      float v[8];
+      t[b].values(k0 + c * 8, x.k, v);
+      uint32_t most = 0;
+#pragma unroll
+      for (int e = 0; e < 8; e++) most = max(most, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+      most = max4(most);
+      const bool finite = most < 0x7F800000u;
+      const uint32_t scale = finite ? scale_of(most) : 255;
+      *(uint32_t*)(codes + r * own_pitch(per) + c * 4) = finite ? codes8(v, power_of(scale)) : 0;
+      if (c % 4 == 0) scales[c / 4 * 16 + r] = (uint8_t)scale;
+    }
+  }
 }
 
 // Few rows: the loop of linear.hip's rows_kernel, the sum split among the waves of a workgroup, each with a ring of its own.  A tile of 16 rows, in their own
-// order (so their scales are bytes here and there of the group's), and 64 columns.
-template <int WAVES, int STAGES>
+// order (so their scales are bytes here and there of the group's), and 64 columns.  OWN: lhs is a matrix of T, which the workgroup puts into blocks while its first
+// steps of rhs are under way (1 x 2048 x 16384 5.1 us and 4.0 for a launch of its own before it; one launch 6.4).
+template <int WAVES, int STAGES, class T, bool OWN>
 __global__ __launch_bounds__(64 * WAVES) void mx_rows_kernel(const MxProduct x, uint32_t steps, uint32_t per_split, uint32_t splits, uint32_t first, float* __restrict__ partial) {
   constexpr int TM = 16, TN = 64, BN = TN / 16;
-  constexpr uint32_t CODES = (TM + TN) * kStep, STAGE = CODES + 4 * 256;
+  constexpr uint32_t A = OWN ? 0 : TM * kStep, CODES = A + TN * kStep, SA = OWN ? 0 : 512, STAGE = CODES + SA + 512;
   __shared__ __attribute__((aligned(1024))) char lds[WAVES][STAGES * STAGE];
+  __shared__ __attribute__((aligned(16))) char own[OWN ? kOwnLhs : 16];
   const Product& p = x.p;
 
   const Place at = place(first, (p.M + TM - 1) / TM, (p.N + TN - 1) / TN, splits);
@@ -367,15 +496,17 @@ __global__ __launch_bounds__(64 * WAVES) void mx_rows_kernel(const MxProduct x, 
   bias8(p.e, n0 + t % 8 * 8, n0 + t % 8 * 8 < p.N ? p.N - (n0 + t % 8 * 8) : 0, bias);
   Feed<bf16, true, false, TM, 64> fa;
   Feed<bf16, true, true, TN, 64> fb;
-  fa.init(p.lda, lane);
   fb.init(p.ldb, lane);
   Scales sa, sb;
-  sa.init(x.scales_a + (int64_t)at.batch * x.scales_batch_a, m0, p.M, p.K / 32, 1);
+  if (!OWN) {
+    fa.init(p.lda, lane);
+    sa.init(x.scales_a + (int64_t)at.batch * x.scales_batch_a, m0, p.M, p.K / 32, 1);
+  }
   sb.init(x.scales_b + (int64_t)at.batch * x.scales_batch_b, n0, p.N, p.K / 32, 1);
-  constexpr int LOADS = decltype(fa)::N + decltype(fb)::N + 4;
+  constexpr int LOADS = decltype(fb)::N + 2 + (OWN ? 0 : decltype(fa)::N + 2);
 
-  const uint32_t end = min(at.split * per_split + per_split, steps);
-  uint32_t step = at.split * per_split + wave;    // the next one to load
+  const uint32_t begin = at.split * per_split, end = min(begin + per_split, steps);
+  uint32_t step = begin + wave;                   // the next one to load
   const uint32_t n = end > step ? (end - step + WAVES - 1) / WAVES : 0;
   const char* const ca = (const char*)p.a + ((int64_t)at.batch * p.batch_a + (int64_t)m0 * p.lda) * 2;
   const char* const cb = (const char*)p.b + ((int64_t)at.batch * p.batch_b + (int64_t)n0 * p.ldb) * 2;
@@ -385,39 +516,52 @@ __global__ __launch_bounds__(64 * WAVES) void mx_rows_kernel(const MxProduct x, 
     const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr)ring + stage * STAGE);
     const bool more = step < end;
     const uint32_t s = more ? step : 0, half = more ? step * 2 : 0x7FFFFFu;
-    const u32x4 buf_a = fa.buffer(ca + (int64_t)s * kStep, more ? size_a - (int64_t)s * kStep : 0);
     const u32x4 buf_b = fb.buffer(cb + (int64_t)s * kStep, more ? size_b - (int64_t)s * kStep : 0);
 #pragma unroll
-    for (int i = 0; i < fb.N; i++) fb.load(i, buf_b, p.K - s * kUnits, to + TM * kStep, lane);
+    for (int i = 0; i < fb.N; i++) fb.load(i, buf_b, p.K - s * kUnits, to + A, lane);
 #pragma unroll
-    for (uint32_t kk = 0; kk < 2; kk++) sb.load(0, half + kk, to + CODES + (2 + kk) * 256, lane);
+    for (uint32_t kk = 0; kk < 2; kk++) sb.load(0, half + kk, to + CODES + SA + kk * 256, lane);
+    if (!OWN) {
+      const u32x4 buf_a = fa.buffer(ca + (int64_t)s * kStep, more ? size_a - (int64_t)s * kStep : 0);
 #pragma unroll
-    for (int i = 0; i < fa.N; i++) fa.load(i, buf_a, p.K - s * kUnits, to, lane);
+      for (int i = 0; i < fa.N; i++) fa.load(i, buf_a, p.K - s * kUnits, to, lane);
 #pragma unroll
-    for (uint32_t kk = 0; kk < 2; kk++) sa.load(0, half + kk, to + CODES + kk * 256, lane);
+      for (uint32_t kk = 0; kk < 2; kk++) sa.load(0, half + kk, to + CODES + kk * 256, lane);
+    }
     step += WAVES;
   };
 
   f32x4 acc[1][BN];
 #pragma unroll
   for (int j = 0; j < BN; j++) acc[0][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  const uint32_t mine = scale_at(m0 % 64 + q, g);
+  const uint32_t rows = min(p.M - m0, (uint32_t)TM), per = end > begin ? end - begin : 0;
+  const uint32_t mine = OWN ? g * 16 + min(q, rows - 1) : scale_at(m0 % 64 + q, g);        // where the lane's scales of a half step lie
+  uint8_t* const own_scales = (uint8_t*)own + rows * own_pitch(per);
 
   if (n) {
 #pragma unroll
     for (int s = 0; s < STAGES; s++) load(s);
-    uint32_t cur = 0;
-    for (uint32_t s = 0; s < n; s++) {
+  }
+  if (OWN && per) own_blocks<T>(x.lhs, at.batch, m0, rows, begin, per, own, own_scales);
+  if (OWN) __syncthreads();
+  if (n) {
+    uint32_t cur = 0, at_own = wave;              // the step of the workgroup's
+    for (uint32_t s = 0; s < n; s++, at_own += WAVES) {
       asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 1) * LOADS) : "memory");
       const lds_ptr tile = (lds_ptr)ring + cur * STAGE;
       bf16x8 oa[2][1], ob[2][BN];
       uint32_t ka[2], kb[2][1];
 #pragma unroll
       for (uint32_t kk = 0; kk < 2; kk++) {
-        read_blocks<bf16, true, false, TM>(tile, 0, 0, kk, q, g, oa[kk]);
-        read_blocks<bf16, true, true, TN>(tile + TM * kStep, 0, 0, kk, q, g, ob[kk]);
-        ka[kk] = *(const __attribute__((address_space(3))) uint8_t*)(tile + CODES + kk * 256 + mine);
-        read_scales<TN>(tile + CODES + 512, 0, kk, lane, kb[kk]);
+        if (OWN) {
+          oa[kk][0] = *(const bf16x8*)(own + min(q, rows - 1) * own_pitch(per) + at_own * kStep + kk * 64 + g * 16);
+          ka[kk] = own_scales[(at_own * 2 + kk) * 64 + mine];
+        } else {
+          read_blocks<bf16, true, false, TM>(tile, 0, 0, kk, q, g, oa[kk]);
+          ka[kk] = *(const __attribute__((address_space(3))) uint8_t*)(tile + CODES + kk * 256 + mine);
+        }
+        read_blocks<bf16, true, true, TN>(tile + A, 0, 0, kk, q, g, ob[kk]);
+        read_scales<TN>(tile + CODES + SA, 0, kk, lane, kb[kk]);
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // read before the place is loaded again
       load(cur);
@@ -454,7 +598,8 @@ hipError_t launch_mx_dequantize(const MxRows& p, hipStream_t st) {
 // and a step's time for each step along k.
 struct Kernel { uint32_t id, tm, tn; float fixed, one, two; };
 constexpr Kernel kKernels[] = {
-    {kFast256, 256, 256, 11, 1.52f, 0}, {kFast256x128, 256, 128, 6, 0.87f, 0}, {kFast128, 128, 128, 4, 0.50f, 0.93f}, {kFast64, 64, 64, 2, 0.25f, 0.37f}, {kRows, 16, 64, 3, 0.12f, 0.24f},
+    {kFast256, 256, 256, 15, 1.88f, 0},       {kFast256x128, 256, 128, 11, 1.155f, 0}, {kFast128, 128, 128, 8, 0.764f, 1.11f},
+    {kFast64, 64, 64, 4.5f, 0.413f, 0.545f},  {kRows, 16, 64, 3, 0.33f, 0.5f},
 };
 constexpr float kLaunch1 = 6, kBytes = 4.5e6f;                     // a further launch, us; bytes a us
 
@@ -485,16 +630,22 @@ ProductPlan plan_mx(const MxProduct& x) {
   return plan;
 }
 
+bool mx_takes_rows(const MxProduct& x, const ProductPlan& plan, const MxRows& lhs) {
+  return plan.kernel == kRows && lhs.kc && lhs.k >= 8 && own_bytes(std::min(x.p.M, 16u), plan.per_split) <= kOwnLhs;
+}
+
 hipError_t launch_mx(const MxProduct& x, const ProductPlan& plan, float* partial, hipStream_t st) {
   return in_launches(plan.blocks, [&](uint64_t first, uint32_t n) {
     const auto go = [&](auto kernel, uint32_t threads) { kernel<<<n, threads, 0, st>>>(x, plan.steps, plan.per_split, plan.splits, (uint32_t)first, partial); };
     switch (plan.kernel) {
       case kFast256: return go(mx_tile_kernel<256, 256, 2, 4, 2>, 512);
       case kFast256x128: return go(mx_tile_kernel<256, 128, 4, 2, 3>, 512);
-      case kFast128: return go(mx_tile_kernel<128, 128, 2, 4, 2>, 512);
+      case kFast128: return go(mx_tile_kernel<128, 128, 2, 2, 2>, 256);
       case kFast128Alone: return go(mx_tile_kernel<128, 128, 2, 4, 4>, 512);
       case kFast64: return go(mx_tile_kernel<64, 64, 2, 2, 4>, 256);
-      default: return go(mx_rows_kernel<4, 3>, 256);
+      default:
+        if (!x.lhs.x.data) return go(mx_rows_kernel<4, 3, bf16, false>, 256);
+        return x.lhs.x.bf16 ? go(mx_rows_kernel<4, 3, bf16, true>, 256) : go(mx_rows_kernel<4, 3, float, true>, 256);
     }
   });
 }

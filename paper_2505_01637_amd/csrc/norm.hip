@@ -5,7 +5,6 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <cstdlib>
 
 #include "tiles.h"
 
@@ -149,6 +148,7 @@ __global__ __launch_bounds__(kRowThreads) void norm_rows_kernel(const NormRows p
     }
   }
   const float one = 1.0f / (float)p.N;
+  const bool past = p.out.bf16 && (uint64_t)rows * p.N * 2 >= kPast;           // (f32, 32 bytes a lane, is not faster so)
   for (uint64_t row0 = row - group; row0 < rows; row0 += stride, row += stride) {
     float v[R][8];
     f32x2 s = {0.0f, 0.0f};
@@ -196,7 +196,8 @@ __global__ __launch_bounds__(kRowThreads) void norm_rows_kernel(const NormRows p
 #pragma unroll
       for (int e = 0; e < 8; e++) v[i][e] = (v[i][e] - rest) * r * w[i][e] + b[i][e];
       // (what is another thread's too is the same there)
-      store8(p.out.data, p.out.bf16, out + Chunk(n, p.N).at, 8, v[i]);
+      if (past) store8_past((bf16*)p.out.data + out + Chunk(n, p.N).at, v[i]);
+      else store8(p.out.data, p.out.bf16, out + Chunk(n, p.N).at, 8, v[i]);
     }
   }
 }
@@ -340,6 +341,7 @@ __global__ __launch_bounds__(kRowThreads) void norm_grad_rows_kernel(const NormG
     }
   }
   const float one = 1.0f / (float)p.N;
+  const bool past = p.dx.bf16 && (uint64_t)rows * p.N * 2 >= kPast;
   uint32_t turn = 0;
   for (uint64_t row0 = begin; row0 < end; row0 += groups, turn ^= 1) {
     const uint32_t row = (uint32_t)row0 + group;
@@ -392,7 +394,8 @@ __global__ __launch_bounds__(kRowThreads) void norm_grad_rows_kernel(const NormG
         for (int e = 0; e < 8; e++) v[e] += y[e];
       }
       if (WHOLE || c.skip == 0) {
-        store8(p.dx.data, p.dx.bf16, dx + c.at, 8, v);
+        if (past) store8_past((bf16*)p.dx.data + dx + c.at, v);
+        else store8(p.dx.data, p.dx.bf16, dx + c.at, 8, v);
       } else {
 #pragma unroll
         for (int e = 1; e < 8; e++) {
@@ -512,10 +515,7 @@ GradPlan plan_grad(const NormGrad& p) {
     g.keep = p.N <= kRowThreads * 8 ? 1 : 2;
     g.waves = (p.N + 512 * g.keep - 1) / (512 * g.keep);
     g.groups = kRowThreads / 64 / g.waves;
-    static const char* const f = getenv("NORM_GRAD");
-    if (f) g.groups = std::max(1u, std::min<uint32_t>(g.groups, atoi(f)));
-    static const char* const f2 = getenv("NORM_GRAD_WANT");
-    const uint64_t want = sums ? f2 ? atoi(f2) : 256 : 4096;                   // workgroups
+    const uint64_t want = sums ? 256 : 4096;                   // workgroups
     g.each = (uint32_t)((rows + want * g.groups - 1) / (want * g.groups)) * g.groups;
     if (rows <= 4 * g.groups) g.each = 4 * g.groups;           // (few rows: no second launch)
   } else {
@@ -542,13 +542,10 @@ struct NormPlan { uint32_t keep, waves, groups, blocks; };     // keep: R, 0: to
 NormPlan plan_norm(uint64_t rows, uint32_t N) {
   NormPlan g{};
   if (N < 8 || N > kRowThreads * 8 * kKeep) return g;
-  static const char* const f = getenv("NORM_KEEP");
-  static const char* const f2 = getenv("NORM_BLOCKS");
-  g.keep = N <= kRowThreads * 8 ? 1 : 2;
-  if (f) g.keep = std::max<uint32_t>(g.keep, atoi(f));
+  g.keep = N <= 512 ? 1 : 2;
   g.waves = (N + 512 * g.keep - 1) / (512 * g.keep);
   g.groups = std::max(1u, 4 / g.waves);
-  g.blocks = (uint32_t)std::min<uint64_t>((rows + g.groups - 1) / g.groups, f2 ? atoi(f2) : 2048);
+  g.blocks = (uint32_t)std::min<uint64_t>((rows + g.groups - 1) / g.groups, 2048);
   return g;
 }
 

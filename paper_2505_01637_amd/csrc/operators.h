@@ -269,10 +269,12 @@ hipError_t launch_mx_dequantize(const MxRows& p, hipStream_t st);
 // A product of operands in blocks.  p.a and p.b are codes, counted in units of four values (two bytes), K a multiple of 32 of them
 struct MxProduct {
   Product p;
+  MxRows lhs;                    // where x.data is given: a's values, which the kernel puts into blocks itself (mx_takes_rows)
   const uint8_t *scales_a, *scales_b;
   int64_t scales_batch_a, scales_batch_b;
 };
 ProductPlan plan_mx(const MxProduct& p);
+bool mx_takes_rows(const MxProduct& p, const ProductPlan& plan, const MxRows& lhs);
 hipError_t launch_mx(const MxProduct& p, const ProductPlan& plan, float* partial, hipStream_t st);       // without the sum over splits
 
 int32_t fail_with(int32_t code, const char* message);      // sets mrl_last_error, returns code

@@ -340,7 +340,10 @@ int32_t plan_mx_linear(const mrl_mx_linear_desc& d, MxPlan* out) {
   }
   g.plan = plan_mx(g.by);
   if ((rc = check_product(p, g.plan))) return rc;
-  if (g.quantizes && p.M && p.N && p.batches) {
+  if (g.quantizes && mx_takes_rows(g.by, g.plan, g.lhs)) {
+    g.by.lhs = g.lhs;
+    g.quantizes = false;
+  } else if (g.quantizes && p.M && p.N && p.batches) {
     g.codes_bytes = align_up((size_t)(p.batches * mx_code_bytes(p.M, d.k)));
     g.scales_bytes = align_up((size_t)(p.batches * mx_scale_bytes(p.M, d.k)));
   } else {

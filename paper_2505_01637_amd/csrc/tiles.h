@@ -22,6 +22,25 @@ hipError_t in_launches(uint64_t blocks, F&& f) {
   return hipSuccess;
 }
 
+// Eight neighbouring elements past the caches: what is too large to stay there only pushes out what is read again, and is written back when the tiles of all
+// compute units end together (8192 x 2048 x 16384 in 4 bits, 268 MB of results: 259 us, and 220 so).
+template <class T>
+__device__ __forceinline__ void store8_past(T* p, const float (&v)[8]) {
+  typedef uint32_t words __attribute__((ext_vector_type(4), aligned(2)));
+  T t[8];
+#pragma unroll
+  for (int e = 0; e < 8; e++) t[e] = (T)v[e];
+  words w[sizeof t / 16];
+  __builtin_memcpy(w, t, sizeof t);
+#pragma unroll
+  for (uint32_t i = 0; i < sizeof t / 16; i++) __builtin_nontemporal_store(w[i], (words*)p + i);
+}
+__device__ __forceinline__ void store8_past(void* data, uint32_t is_bf16, int64_t at, const float (&v)[8]) {
+  if (is_bf16) store8_past((bf16*)data + at, v);
+  else store8_past((float*)data + at, v);
+}
+constexpr uint64_t kPast = 32 << 20;       // bytes from which it is done: the dies' caches together
+
 // ---- tiles in shared memory
 //
 // A step holds 128 bytes along k of every row (column) of the tile, as chunks of 16 bytes.  KC: the operand's neighbours along k
@@ -204,8 +223,7 @@ __device__ __forceinline__ void put8(const Product& p, const Place& at, uint32_t
 // through shared memory that is the wave's own, PASS blocks of 16 rows at a time, so that a row's results are stored side by side (lines of
 // 128 bytes and more) and the epilogue is a short loop: unrolled over the registers it is as long as the instruction cache.  The 16-byte chunks of a
 // row lie at their number xor the row's, against bank conflicts.
-// MIXED: A's rows are in B's order.
-template <class T, int PASS, int BM, int BN, bool MIXED = false>
+template <class T, int PASS, int BM, int BN>
 __device__ __forceinline__ void write_out(const Product& p, const Place& at, uint32_t splits, uint32_t m0, uint32_t n0, uint32_t lane,
                                           const f32x4 (&acc)[BM][BN], char* mine, float* __restrict__ partial) {
   constexpr uint32_t CHUNKS = BN * 4, GROUPS = BN * 2, ROWS = 64 / GROUPS;      // chunks and groups of 8 columns of a row; rows at a time
@@ -228,7 +246,7 @@ __device__ __forceinline__ void write_out(const Product& p, const Place& at, uin
     if (n < p.N) {
 #pragma unroll 2
       for (uint32_t r = lane / GROUPS; r < 16 * PASS; r += ROWS) {
-        const uint32_t m = m0 + row_of<T, MIXED>(h + (r >> 4), r & 15);
+        const uint32_t m = m0 + row_of<T, false>(h + (r >> 4), r & 15);
         if (m >= p.M) continue;
         float v[8];
 #pragma unroll
