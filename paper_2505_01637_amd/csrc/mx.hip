@@ -238,16 +238,26 @@ constexpr uint32_t kUnits = 64;            // of four values, in a step
 struct Scales {
   u32x4 buffer;
   uint32_t pitch;                          // bytes from a group to the next
-  __device__ __forceinline__ void init(const uint8_t* scales, uint32_t line, uint32_t lines, uint32_t halves, uint32_t groups) {
-    pitch = halves * 256;
+  __device__ __forceinline__ Scales(const uint8_t* scales, uint32_t line, uint32_t lines, uint32_t halves, uint32_t groups) : pitch(halves * 256) {
     const uint64_t base = (uint64_t)(scales + (uint64_t)(line / 64) * pitch);
     buffer = u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)base), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(base >> 32) & 0xFFFFu),
                    (uint32_t)__builtin_amdgcn_readfirstlane(min(groups, (lines + 63) / 64 - line / 64) * pitch), 0x27000u};
   }
-  // (a half step that is not there has scales of 0, as its codes are: the byte that happens to follow could be a NaN's)
-  __device__ __forceinline__ void load(uint32_t group, uint32_t half, uint32_t lds, uint32_t lane) const {
-    load4_to_lds(lds, half * 256 < pitch ? group * pitch + half * 256 + lane * 4 : kOutside, buffer);
+};
+constexpr uint32_t kNoHalf = 0x400000;     // beyond any half step
+// The 256 bytes of a group and every other half step from `odd` on, as a wave loads them.  A half step that is not there has scales of 0, as its codes are: the byte
+// that happens to follow could be a NaN's.  (Worked out without a branch: with one the loop's products were moved behind its barrier, a step of 256 x 256 x 256
+// took 1.88 us.)
+struct Slot {
+  u32x4 buffer;
+  uint32_t offset, odd, halves;
+  __device__ __forceinline__ void init(const Scales& s, uint32_t group, uint32_t half, uint32_t lane) {
+    buffer = s.buffer;
+    odd = half;
+    halves = s.pitch / 256;
+    offset = group * s.pitch + lane * 4;
   }
+  __device__ __forceinline__ void load(uint32_t half, uint32_t lds) const { load4_to_lds(lds, half + odd < halves ? offset + (half + odd) * 256 : kOutside, buffer); }
 };
 
 // A wave's scales of W of a tile's lines from `first` on, for a half step: four blocks a word.
@@ -340,9 +350,13 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void mx_tile_kernel(cons
   Feed<bf16, true, true, TN, THREADS> fb;
   fa.init(p.lda, t);
   fb.init(p.ldb, t);
-  Scales sa, sb;
-  sa.init(x.scales_a + (int64_t)at.batch * x.scales_batch_a, m0, p.M, p.K / 32, GA);
-  sb.init(x.scales_b + (int64_t)at.batch * x.scales_batch_b, n0, p.N, p.K / 32, GB);
+  const Scales sa(x.scales_a + (int64_t)at.batch * x.scales_batch_a, m0, p.M, p.K / 32, GA), sb(x.scales_b + (int64_t)at.batch * x.scales_batch_b, n0, p.N, p.K / 32, GB);
+  Slot slots[EACH];                // first A's groups, two half steps each, then B's
+#pragma unroll
+  for (int i = 0; i < EACH; i++) {
+    const uint32_t slot = wave * EACH + i, group = slot / 2;
+    slots[i].init(group < GA ? sa : sb, group < GA ? group : group - GA, slot < SLOTS ? slot & 1 : kNoHalf, lane);
+  }
   constexpr int NA = decltype(fa)::N, NB = decltype(fb)::N, LOADS = NA + NB + EACH;
 
   const uint32_t from = at.split * per_split, end = min(from + per_split, steps), n = end > from ? end - from : 0;
@@ -358,24 +372,20 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void mx_tile_kernel(cons
     const bool more = step < end;
     to = (uint32_t)(uintptr_t)(lds_ptr)lds + stage * STAGE;
     ks = p.K - step * kUnits;
-    half = more ? step * 2 : 0x7FFFFFu;
+    half = more ? step * 2 : kNoHalf;
     buf_a = fa.buffer(ca, more ? left_a : 0);
     buf_b = fb.buffer(cb, more ? left_b : 0);
-    if (!more) return;
-    step++;
-    ca += kStep;
-    cb += kStep;
-    left_a -= kStep;
-    left_b -= kStep;
+    const uint32_t on = more ? kStep : 0;
+    step += more;
+    ca += on;
+    cb += on;
+    left_a -= on;
+    left_b -= on;
   };
   const auto load = [&](int i) {
     if (i < NA) fa.load(i, buf_a, ks, to + wave * 1024, t);
     else if (i < NA + NB) fb.load(i - NA, buf_b, ks, to + TM * kStep + wave * 1024, t);
-    else {
-      const uint32_t slot = wave * EACH + (i - NA - NB), lds_at = to + CODES + slot * 256;
-      if (slot < 2 * GA) sa.load(slot >> 1, half + (slot & 1), lds_at, lane);
-      else sb.load(slot < SLOTS ? (slot - 2 * GA) >> 1 : 0, slot < SLOTS ? half + (slot & 1) : 0x7FFFFFu, lds_at, lane);
-    }
+    else slots[i - NA - NB].load(half, to + CODES + (wave * EACH + (i - NA - NB)) * 256);
   };
   f32x4 acc[BM][BN];
 #pragma unroll
@@ -497,12 +507,13 @@ __global__ __launch_bounds__(64 * WAVES) void mx_rows_kernel(const MxProduct x, 
   Feed<bf16, true, false, TM, 64> fa;
   Feed<bf16, true, true, TN, 64> fb;
   fb.init(p.ldb, lane);
-  Scales sa, sb;
-  if (!OWN) {
-    fa.init(p.lda, lane);
-    sa.init(x.scales_a + (int64_t)at.batch * x.scales_batch_a, m0, p.M, p.K / 32, 1);
+  Slot sa[2], sb[2];
+  if (!OWN) fa.init(p.lda, lane);
+#pragma unroll
+  for (uint32_t kk = 0; kk < 2; kk++) {
+    if (!OWN) sa[kk].init(Scales(x.scales_a + (int64_t)at.batch * x.scales_batch_a, m0, p.M, p.K / 32, 1), 0, kk, lane);
+    sb[kk].init(Scales(x.scales_b + (int64_t)at.batch * x.scales_batch_b, n0, p.N, p.K / 32, 1), 0, kk, lane);
   }
-  sb.init(x.scales_b + (int64_t)at.batch * x.scales_batch_b, n0, p.N, p.K / 32, 1);
   constexpr int LOADS = decltype(fb)::N + 2 + (OWN ? 0 : decltype(fa)::N + 2);
 
   const uint32_t begin = at.split * per_split, end = min(begin + per_split, steps);
@@ -515,18 +526,18 @@ __global__ __launch_bounds__(64 * WAVES) void mx_rows_kernel(const MxProduct x, 
   const auto load = [&](uint32_t stage) {
     const uint32_t to = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_ptr)ring + stage * STAGE);
     const bool more = step < end;
-    const uint32_t s = more ? step : 0, half = more ? step * 2 : 0x7FFFFFu;
+    const uint32_t s = more ? step : 0, half = more ? step * 2 : kNoHalf;
     const u32x4 buf_b = fb.buffer(cb + (int64_t)s * kStep, more ? size_b - (int64_t)s * kStep : 0);
 #pragma unroll
     for (int i = 0; i < fb.N; i++) fb.load(i, buf_b, p.K - s * kUnits, to + A, lane);
 #pragma unroll
-    for (uint32_t kk = 0; kk < 2; kk++) sb.load(0, half + kk, to + CODES + SA + kk * 256, lane);
+    for (uint32_t kk = 0; kk < 2; kk++) sb[kk].load(half, to + CODES + SA + kk * 256);
     if (!OWN) {
       const u32x4 buf_a = fa.buffer(ca + (int64_t)s * kStep, more ? size_a - (int64_t)s * kStep : 0);
 #pragma unroll
       for (int i = 0; i < fa.N; i++) fa.load(i, buf_a, p.K - s * kUnits, to, lane);
 #pragma unroll
-      for (uint32_t kk = 0; kk < 2; kk++) sa.load(0, half + kk, to + CODES + kk * 256, lane);
+      for (uint32_t kk = 0; kk < 2; kk++) sa[kk].load(half, to + CODES + kk * 256);
     }
     step += WAVES;
   };
