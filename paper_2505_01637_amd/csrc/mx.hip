@@ -394,8 +394,8 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void mx_tile_kernel(cons
     for (int j = 0; j < BN; j++) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
   constexpr int NM = BM > 4 ? BM / 2 : BM, PHASES = 2 * BM / NM;
-  constexpr bool SPREAD = BM > 4;
-  static_assert(!SPREAD || LOADS <= PHASES * NM, "one load at most beside a part of the products");
+  // (4096 x 16384 x 2048 by tiles of 256 x 128 83 us with a step's loads all at once, 77 spread)
+  constexpr bool SPREAD = LOADS <= PHASES * NM;      // one beside a part of the products
   bf16x8 oa[2][NM], ob[2][BN];
   uint32_t ka[2][(WM + 63) / 64], kb[2][(WN + 63) / 64];
   const auto read_a = [&](lds_ptr stage, int m, int kk, bf16x8 (&o)[NM]) { read_blocks<bf16, true, true, TM>(stage, wm, m, kk, q, g, o); };
@@ -609,8 +609,8 @@ hipError_t launch_mx_dequantize(const MxRows& p, hipStream_t st) {
 // and a step's time for each step along k.
 struct Kernel { uint32_t id, tm, tn; float fixed, one, two; };
 constexpr Kernel kKernels[] = {
-    {kFast256, 256, 256, 15, 1.88f, 0},       {kFast256x128, 256, 128, 11, 1.155f, 0}, {kFast128, 128, 128, 8, 0.764f, 1.11f},
-    {kFast64, 64, 64, 4.5f, 0.413f, 0.545f},  {kRows, 16, 64, 3, 0.33f, 0.5f},
+    {kFast256, 256, 256, 12, 1.70f, 0},       {kFast256x128, 256, 128, 10.5f, 1.045f, 0}, {kFast128, 128, 128, 8, 0.666f, 1.083f},
+    {kFast64, 64, 64, 4.5f, 0.388f, 0.545f},  {kRows, 16, 64, 3, 0.33f, 0.45f},
 };
 constexpr float kLaunch1 = 6, kBytes = 4.5e6f;                     // a further launch, us; bytes a us
 
