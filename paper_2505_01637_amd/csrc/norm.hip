@@ -302,7 +302,7 @@ template <class TX, class TG, int R, bool WHOLE>
 __global__ __launch_bounds__(kRowThreads) void norm_grad_rows_kernel(const NormGrad p, uint32_t waves, uint32_t each, uint32_t first, float* __restrict__ partial) {
   constexpr bool AHEAD = R == 1;                                         // (twice: no registers for it)
   __shared__ f32x2 sums[2][kRowThreads / 64];
-  __shared__ float columns[2][R == 1 ? kRowThreads / 2 * 8 : 8];         // (more than one group only where a row has half of the threads or fewer)
+  __shared__ float columns[R == 1 ? 2 * kRowThreads * 8 : 8];            // (rows of two chunks a thread take all waves)
   const uint32_t block = first + blockIdx.x, rows = p.batches * p.M;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = wave / waves, groups = blockDim.x / 64 / waves;
   const uint32_t t = threadIdx.x - group * waves * 64, pitch = waves * 512;
@@ -407,19 +407,26 @@ __global__ __launch_bounds__(kRowThreads) void norm_grad_rows_kernel(const NormG
     }
   }
   if (!wants) return;
-  for (uint32_t k = 1; k < groups; k++) {          // the other groups' sums to the first, one after the other
-    __syncthreads();
-    if (group == k) {
+  float* const mine = partial + (uint64_t)block * 2 * p.N;
+  if (R == 1 && groups > 1) {      // a column a thread, the groups' sums in their order
+    float* const at = columns + group * pitch + t * 8;
 #pragma unroll
-      for (int e = 0; e < 8; e++) { columns[0][t * 8 + e] = dw[0][e]; columns[1][t * 8 + e] = db[0][e]; }
-    }
+    for (int e = 0; e < 8; e++) { at[e] = dw[0][e]; at[kRowThreads * 8 + e] = db[0][e]; }
     __syncthreads();
-    if (group == 0) {
-#pragma unroll
-      for (int e = 0; e < 8; e++) { dw[0][e] += columns[0][t * 8 + e]; db[0][e] += columns[1][t * 8 + e]; }
+    for (uint32_t i = threadIdx.x; i < 2 * pitch; i += blockDim.x) {
+      const uint32_t which = i >= pitch, n = i - which * pitch;
+      const Chunk c(n & ~7u, p.N);
+      if ((n & 7) < c.skip) continue;
+      float s = 0.0f;
+      for (uint32_t k = 0; k < groups; k++) s += columns[which * kRowThreads * 8 + k * pitch + n];
+      const uint32_t column = c.at + (n & 7), is_bf16 = which ? p.dbias_bf16 : p.dweight_bf16;
+      void* const to = which ? p.dbias : p.dweight;
+      if (partial) mine[which * p.N + column] = s;
+      else if (to && is_bf16) ((bf16*)to)[column] = (bf16)s;
+      else if (to) ((float*)to)[column] = s;
     }
+    return;
   }
-  if (group) return;
   const auto put = [&](void* to, uint32_t is_bf16, const Chunk& c, const float (&v)[8]) {
     if (!to) return;
     if (c.skip == 0) return store8(to, is_bf16, (int64_t)c.at, 8, v);
@@ -434,9 +441,8 @@ __global__ __launch_bounds__(kRowThreads) void norm_grad_rows_kernel(const NormG
   for (int i = 0; i < R; i++) {
     const Chunk c(i * pitch + t * 8, p.N);
     if (c.skip >= 8) continue;
-    float* const to = partial + (uint64_t)block * 2 * p.N;
-    put(partial ? to : p.dweight, partial ? 0 : p.dweight_bf16, c, dw[i]);
-    put(partial ? to + p.N : p.dbias, partial ? 0 : p.dbias_bf16, c, db[i]);
+    put(partial ? mine : p.dweight, partial ? 0 : p.dweight_bf16, c, dw[i]);
+    put(partial ? mine + p.N : p.dbias, partial ? 0 : p.dbias_bf16, c, db[i]);
   }
 }
 
