@@ -33,20 +33,23 @@ __device__ __forceinline__ f32x2 sum_block(f32x2 v) {
   return v;
 }
 
-__device__ __forceinline__ int64_t start(const RowsOf& x, uint32_t row, uint32_t M) {
-  const uint32_t batch = row / M;
+__device__ __forceinline__ int64_t start(const RowsOf& x, uint32_t row, uint32_t M, uint32_t batches) {
+  const uint32_t batch = batches == 1 ? 0 : row / M;
   return (int64_t)batch * x.batch + (int64_t)(row - batch * M) * x.ld;
 }
 
 template <int CTRL>
 __device__ __forceinline__ float moved(float x) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xF, 0xF, true)); }
-// The sum over a wave, in every lane: within rows of sixteen lanes by moves, the four rows' after that.
-__device__ __forceinline__ float sum_wave(float x) {
+// The sum over sixteen neighbouring lanes, in each of them.
+__device__ __forceinline__ float sum16(float x) {
   x += moved<0xB1>(x);             // lanes 1, 0, 3, 2
   x += moved<0x4E>(x);             // lanes 2, 3, 0, 1
   x += moved<0x141>(x);            // mirrored in eight
-  x += moved<0x140>(x);            // and in sixteen
-  const int v = __float_as_int(x);
+  return x + moved<0x140>(x);      // and in sixteen
+}
+// The sum over a wave, in every lane: the four sixteens' one after the other.
+__device__ __forceinline__ float sum_wave(float x) {
+  const int v = __float_as_int(sum16(x));
   return (__int_as_float(__builtin_amdgcn_readlane(v, 0)) + __int_as_float(__builtin_amdgcn_readlane(v, 16))) +
          (__int_as_float(__builtin_amdgcn_readlane(v, 32)) + __int_as_float(__builtin_amdgcn_readlane(v, 48)));
 }
@@ -102,9 +105,25 @@ struct Either {
 
 constexpr uint32_t kRowThreads = 1024;     // of a workgroup that keeps rows
 constexpr uint32_t kKeep = 2;              // R at most: rows of up to 16384 elements
+constexpr uint32_t kNarrow = 128;          // elements of a row that sixteen lanes have
 
-// The sum of the group's waves' sums (uniform over each wave), in their order.  `sums` may be written again behind the next such exchange.
-__device__ __forceinline__ f32x2 sum_waves(f32x2 v, f32x2* sums, uint32_t group, uint32_t waves) {
+// Which threads a row has: LANES of them, 16 for rows of up to 128 elements, or 64 for `waves` waves.
+template <int LANES>
+struct Team {
+  uint32_t waves, size, group, groups, t;          // threads of a row; the thread's row of the workgroup's; its place in it
+  __device__ __forceinline__ Team(uint32_t waves) : waves(waves) {
+    size = LANES == 64 ? waves * 64 : LANES;
+    group = LANES == 64 ? (uint32_t)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / waves : threadIdx.x / LANES;
+    groups = blockDim.x / size;
+    t = threadIdx.x - group * size;
+  }
+  // The sums over the row's threads, in each of them, added in one order.  `sums` may be written again behind the next such exchange.
+  __device__ __forceinline__ f32x2 sum(f32x2 v, f32x2* sums) const;
+};
+template <int LANES>
+__device__ __forceinline__ f32x2 Team<LANES>::sum(f32x2 v, f32x2* sums) const {
+  if (LANES == 16) return f32x2{sum16(v[0]), sum16(v[1])};
+  v = f32x2{sum_wave(v[0]), sum_wave(v[1])};
   if (waves == 1) return v;
   if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = v;
   __syncthreads();
@@ -118,15 +137,15 @@ __device__ __forceinline__ f32x2 sum_waves(f32x2 v, f32x2* sums, uint32_t group,
 
 // `waves` waves a row; a workgroup's groups of waves take a row each, then the rows that follow those of all workgroups.  Memory bounds it, so the next
 // row's loads go out before this one's sums are made; weight and bias are read once.
-template <class T, int R, bool WHOLE>
+template <class T, int R, int LANES, bool WHOLE>
 __global__ __launch_bounds__(kRowThreads) void norm_rows_kernel(const NormRows p, uint32_t waves) {
   __shared__ f32x2 sums[2][kRowThreads / 64];
-  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = wave / waves, groups = blockDim.x / 64 / waves, rows = p.batches * p.M;
-  const uint32_t t = threadIdx.x - group * waves * 64, pitch = waves * 512, stride = gridDim.x * groups;
-  uint64_t row = (uint64_t)blockIdx.x * groups + group;
+  const Team<LANES> team(waves);
+  const uint32_t rows = p.batches * p.M, t = team.t, pitch = team.size * 8, stride = gridDim.x * team.groups;
+  uint64_t row = (uint64_t)blockIdx.x * team.groups + team.group;
   Raw<T> next[R];
   const auto load = [&](uint64_t row) {
-    const int64_t x = start(p.x, (uint32_t)min(row, rows - 1ull), p.M);        // (past the last row it is read again)
+    const int64_t x = start(p.x, (uint32_t)min(row, rows - 1ull), p.M, p.batches);        // (past the last row it is read again)
 #pragma unroll
     for (int i = 0; i < R; i++) next[i].load(p.x.data, x + Chunk(i * pitch + t * 8, p.N).at);
   };
@@ -149,7 +168,7 @@ __global__ __launch_bounds__(kRowThreads) void norm_rows_kernel(const NormRows p
   }
   const float one = 1.0f / (float)p.N;
   const bool past = p.out.bf16 && (uint64_t)rows * p.N * 2 >= kPast;           // (f32, 32 bytes a lane, is not faster so)
-  for (uint64_t row0 = row - group; row0 < rows; row0 += stride, row += stride) {
+  for (uint64_t row0 = row - team.group; row0 < rows; row0 += stride, row += stride) {
     float v[R][8];
     f32x2 s = {0.0f, 0.0f};
 #pragma unroll
@@ -164,8 +183,8 @@ __global__ __launch_bounds__(kRowThreads) void norm_rows_kernel(const NormRows p
 #pragma unroll
       for (int e = 0; e < 8; e++) s[0] += WHOLE || (uint32_t)e >= c.skip ? v[i][e] : 0.0f;
     }
-    // (rounded here and nowhere else: folded into the subtractions below it would be another number in each of them)
-    const float about = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(sum_waves(f32x2{sum_wave(s[0]), 0.0f}, sums[0], group, waves)[0] * one)));
+    float about = team.sum(f32x2{s[0], 0.0f}, sums[0])[0] * one;
+    asm volatile("" : "+v"(about));        // (rounded here and nowhere else: folded into the subtractions below it would be another number in each of them)
     // the sum of what is left puts the mean right: where it is far from 0, its own sum has lost that much
     s[0] = 0.0f;
 #pragma unroll
@@ -181,14 +200,14 @@ __global__ __launch_bounds__(kRowThreads) void norm_rows_kernel(const NormRows p
         s[1] += d * d;
       }
     }
-    s = sum_waves(f32x2{sum_wave(s[0]), sum_wave(s[1])}, sums[1], group, waves);
+    s = team.sum(s, sums[1]);
     const float rest = s[0] * one, var = s[1] * one - rest * rest, r = 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + p.eps);       // (NaN stays)
     if (row >= rows) continue;
     if (p.stats && t == 0) {
       p.stats[2 * row] = about + rest;
       p.stats[2 * row + 1] = r;
     }
-    const int64_t out = start(p.out, (uint32_t)row, p.M);
+    const int64_t out = start(p.out, (uint32_t)row, p.M, p.batches);
 #pragma unroll
     for (int i = 0; i < R; i++) {
       const uint32_t n = i * pitch + t * 8;
@@ -205,7 +224,7 @@ __global__ __launch_bounds__(kRowThreads) void norm_rows_kernel(const NormRows p
 // A row a workgroup, eight elements a thread at a time, three passes over it.
 __global__ __launch_bounds__(kThreads) void norm_kernel(const NormRows p, uint32_t first) {
   const uint32_t row = first + blockIdx.x;
-  const int64_t x = start(p.x, row, p.M), out = start(p.out, row, p.M);
+  const int64_t x = start(p.x, row, p.M, p.batches), out = start(p.out, row, p.M, p.batches);
   const float N = (float)p.N;
   float v[8];
   f32x2 s = {0.0f, 0.0f};
@@ -256,7 +275,7 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(const NormRows p, uint32
 // dx, a row a workgroup: two passes over it.
 __global__ __launch_bounds__(kThreads) void norm_grad_kernel(const NormGrad p, uint32_t first) {
   const uint32_t row = first + blockIdx.x;
-  const int64_t x = start(p.x, row, p.M), grad = start(p.grad, row, p.M), dx = start(p.dx, row, p.M);
+  const int64_t x = start(p.x, row, p.M, p.batches), grad = start(p.grad, row, p.M, p.batches), dx = start(p.dx, row, p.M, p.batches);
   const float mean = p.stats[2 * (uint64_t)row], r = p.stats[2 * (uint64_t)row + 1];
   float v[8], g[8], w[8];
   const auto load = [&](uint64_t n) {              // h and g
@@ -288,7 +307,7 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(const NormGrad p, u
 #pragma unroll
     for (int e = 0; e < 8; e++) v[e] = r * (g[e] - a - v[e] * b);
     if (p.residual.data) {
-      load8(p.residual.data, p.residual.bf16, start(p.residual, row, p.M) + n, p.N - n, g);
+      load8(p.residual.data, p.residual.bf16, start(p.residual, row, p.M, p.batches) + n, p.N - n, g);
 #pragma unroll
       for (int e = 0; e < 8; e++) v[e] += g[e];
     }
@@ -298,14 +317,14 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(const NormGrad p, u
 
 // The gradient of such rows: each workgroup's groups take its `each` rows in turn and keep the columns' sums, which they add in their order at the end.
 // partial: the workgroups' sums (2 x N each: dw, db), nullptr where there is one workgroup.
-template <class TX, class TG, int R, bool WHOLE>
+template <class TX, class TG, int R, int LANES, bool WHOLE>
 __global__ __launch_bounds__(kRowThreads) void norm_grad_rows_kernel(const NormGrad p, uint32_t waves, uint32_t each, uint32_t first, float* __restrict__ partial) {
   constexpr bool AHEAD = R == 1;                                         // (twice: no registers for it)
   __shared__ f32x2 sums[2][kRowThreads / 64];
   __shared__ float columns[R == 1 ? 2 * kRowThreads * 8 : 8];            // (rows of two chunks a thread take all waves)
   const uint32_t block = first + blockIdx.x, rows = p.batches * p.M;
-  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = wave / waves, groups = blockDim.x / 64 / waves;
-  const uint32_t t = threadIdx.x - group * waves * 64, pitch = waves * 512;
+  const Team<LANES> team(waves);
+  const uint32_t group = team.group, groups = team.groups, t = team.t, pitch = team.size * 8;
   const uint64_t begin = (uint64_t)block * each;
   const uint32_t end = (uint32_t)min(begin + each, (uint64_t)rows);
   const bool wants = p.dweight || p.dbias;
@@ -315,7 +334,7 @@ __global__ __launch_bounds__(kRowThreads) void norm_grad_rows_kernel(const NormG
   float mean1 = 0.0f, r1 = 0.0f;
   const auto load = [&](uint32_t at) {
     const uint32_t row = min(at, end - 1);         // (past the last row it is read again)
-    const int64_t at_x = start(p.x, row, p.M), at_g = start(p.grad, row, p.M);
+    const int64_t at_x = start(p.x, row, p.M, p.batches), at_g = start(p.grad, row, p.M, p.batches);
     mean1 = p.stats[2 * (uint64_t)row];
     r1 = p.stats[2 * (uint64_t)row + 1];
 #pragma unroll
@@ -372,14 +391,14 @@ __global__ __launch_bounds__(kRowThreads) void norm_grad_rows_kernel(const NormG
     if (!p.dx.data) continue;
     Either z[R];
     if (p.residual.data && row < end) {            // (asked for before the sums go around)
-      const int64_t at = start(p.residual, row, p.M);
+      const int64_t at = start(p.residual, row, p.M, p.batches);
 #pragma unroll
       for (int i = 0; i < R; i++) z[i].load(p.residual.data, p.residual.bf16, at + Chunk(i * pitch + t * 8, p.N).at, p.residual.data);
     }
-    const f32x2 s = sum_waves(f32x2{sum_wave(s0), sum_wave(s1)}, sums[turn], group, waves);
+    const f32x2 s = team.sum(f32x2{s0, s1}, sums[turn]);
     if (row >= end) continue;
     const float a = s[0] * one, b = s[1] * one;
-    const int64_t dx = start(p.dx, row, p.M);
+    const int64_t dx = start(p.dx, row, p.M, p.batches);
 #pragma unroll
     for (int i = 0; i < R; i++) {
       const Chunk c(i * pitch + t * 8, p.N);
@@ -458,11 +477,11 @@ __global__ __launch_bounds__(256) void norm_columns_kernel(const NormGrad p, uin
       if (at >= rows) break;
       const uint32_t row = (uint32_t)at;
       float x[8], g[8];
-      load8(p.grad.data, p.grad.bf16, start(p.grad, row, p.M) + n, p.N - n, g);
+      load8(p.grad.data, p.grad.bf16, start(p.grad, row, p.M, p.batches) + n, p.N - n, g);
 #pragma unroll
       for (int e = 0; e < 8; e++) db[e] += g[e];
       if (!p.dweight) continue;
-      load8(p.x.data, p.x.bf16, start(p.x, row, p.M) + n, p.N - n, x);
+      load8(p.x.data, p.x.bf16, start(p.x, row, p.M, p.batches) + n, p.N - n, x);
       const float mean = p.stats[2 * at], r = p.stats[2 * at + 1];
 #pragma unroll
       for (int e = 0; e < 8; e++) dw[e] += g[e] * ((x[e] - mean) * r);
@@ -520,7 +539,7 @@ GradPlan plan_grad(const NormGrad& p) {
   if (p.N >= 8 && p.N <= kRowThreads * 8 * kKeep) {
     g.keep = p.N <= kRowThreads * 8 ? 1 : 2;
     g.waves = (p.N + 512 * g.keep - 1) / (512 * g.keep);
-    g.groups = kRowThreads / 64 / g.waves;
+    g.groups = kRowThreads / (p.N <= kNarrow ? 16 : 64 * g.waves);
     const uint64_t want = sums ? 256 : 4096;                   // workgroups
     g.each = (uint32_t)((rows + want * g.groups - 1) / (want * g.groups)) * g.groups;
     if (rows <= 4 * g.groups) g.each = 4 * g.groups;           // (few rows: no second launch)
@@ -537,9 +556,11 @@ GradPlan plan_grad(const NormGrad& p) {
 template <class TX, class TG>
 hipError_t launch_rows(const NormGrad& p, const GradPlan& g, float* partial, hipStream_t st) {
   return in_launches(g.blocks, [&](uint64_t first, uint32_t n) {
-    const auto go = [&](auto kernel) { kernel<<<n, g.groups * g.waves * 64, 0, st>>>(p, g.waves, g.each, (uint32_t)first, g.blocks > 1 ? partial : nullptr); };
-    if (p.N % 8 == 0) g.keep == 1 ? go(norm_grad_rows_kernel<TX, TG, 1, true>) : go(norm_grad_rows_kernel<TX, TG, 2, true>);
-    else g.keep == 1 ? go(norm_grad_rows_kernel<TX, TG, 1, false>) : go(norm_grad_rows_kernel<TX, TG, 2, false>);
+    const auto go = [&](auto kernel) { kernel<<<n, g.groups * (p.N <= kNarrow ? 16 : 64 * g.waves), 0, st>>>(p, g.waves, g.each, (uint32_t)first, g.blocks > 1 ? partial : nullptr); };
+    const bool whole = p.N % 8 == 0;
+    if (p.N <= kNarrow) whole ? go(norm_grad_rows_kernel<TX, TG, 1, 16, true>) : go(norm_grad_rows_kernel<TX, TG, 1, 16, false>);
+    else if (g.keep == 1) whole ? go(norm_grad_rows_kernel<TX, TG, 1, 64, true>) : go(norm_grad_rows_kernel<TX, TG, 1, 64, false>);
+    else whole ? go(norm_grad_rows_kernel<TX, TG, 2, 64, true>) : go(norm_grad_rows_kernel<TX, TG, 2, 64, false>);
   });
 }
 
@@ -550,16 +571,18 @@ NormPlan plan_norm(uint64_t rows, uint32_t N) {
   if (N < 8 || N > kRowThreads * 8 * kKeep) return g;
   g.keep = N <= 512 ? 1 : 2;
   g.waves = (N + 512 * g.keep - 1) / (512 * g.keep);
-  g.groups = std::max(1u, 4 / g.waves);
+  g.groups = N <= kNarrow ? 16 : std::max(1u, 4 / g.waves);
   g.blocks = (uint32_t)std::min<uint64_t>((rows + g.groups - 1) / g.groups, 2048);
   return g;
 }
 
 template <class T>
 void launch_norm_rows(const NormRows& p, const NormPlan& g, hipStream_t st) {
-  const auto go = [&](auto kernel) { kernel<<<g.blocks, g.groups * g.waves * 64, 0, st>>>(p, g.waves); };
-  if (p.N % 8 == 0) g.keep == 1 ? go(norm_rows_kernel<T, 1, true>) : go(norm_rows_kernel<T, 2, true>);
-  else g.keep == 1 ? go(norm_rows_kernel<T, 1, false>) : go(norm_rows_kernel<T, 2, false>);
+  const auto go = [&](auto kernel) { kernel<<<g.blocks, g.groups * (p.N <= kNarrow ? 16 : 64 * g.waves), 0, st>>>(p, g.waves); };
+  const bool whole = p.N % 8 == 0;
+  if (p.N <= kNarrow) whole ? go(norm_rows_kernel<T, 1, 16, true>) : go(norm_rows_kernel<T, 1, 16, false>);
+  else if (g.keep == 1) whole ? go(norm_rows_kernel<T, 1, 64, true>) : go(norm_rows_kernel<T, 1, 64, false>);
+  else whole ? go(norm_rows_kernel<T, 2, 64, true>) : go(norm_rows_kernel<T, 2, 64, false>);
 }
 
 }  // namespace
