@@ -572,7 +572,8 @@ NormPlan plan_norm(uint64_t rows, uint32_t N) {
   g.keep = N <= 512 ? 1 : 2;
   g.waves = (N + 512 * g.keep - 1) / (512 * g.keep);
   g.groups = N <= kNarrow ? 16 : std::max(1u, 4 / g.waves);
-  g.blocks = (uint32_t)std::min<uint64_t>((rows + g.groups - 1) / g.groups, 2048);
+  const uint32_t waves = N <= kNarrow ? 4 : g.groups * g.waves;
+  g.blocks = (uint32_t)std::min<uint64_t>((rows + g.groups - 1) / g.groups, 8192 / waves);        // (as many waves as the card has room for)
   return g;
 }
 
