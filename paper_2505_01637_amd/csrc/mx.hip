@@ -469,7 +469,7 @@ constexpr uint32_t kOwnLhs = 48 * 1024;
 __host__ __device__ constexpr uint32_t own_pitch(uint32_t per) { return per * kStep + 64; }       // (64 more, against bank conflicts)
 __host__ __device__ constexpr uint64_t own_bytes(uint32_t rows, uint32_t per) { return (uint64_t)rows * own_pitch(per) + (uint64_t)per * 2 * 64; }
 
-// Eight values a thread, four threads a block, BATCH times before the first is used.
+// Eight values a thread, four threads a block, BATCH times before the first is used.  (x.k is at least 8.)
 template <class T>
 __device__ __forceinline__ void own_blocks(const MxRows& x, uint32_t batch, uint32_t m0, uint32_t rows, uint32_t step0, uint32_t per, char* codes, uint8_t* scales) {
   constexpr uint32_t BATCH = 4;
@@ -620,29 +620,38 @@ hipError_t launch_mx_dequantize(const MxRows& p, hipStream_t st) {
 }
 
 // How long a kernel takes, in us, as linear.hip's rule has it: a round of workgroups on the 256 compute units, one each or two at once, is `fixed`
-// and a step's time for each step along k.
+// and a step's time for each step along k.  Measured on products whose tiles are one whole round (or two at once), 2048 and 16384 long along k, replayed in a graph.
 struct Kernel { uint32_t id, tm, tn; float fixed, one, two; };
 constexpr Kernel kKernels[] = {
     {kFast256, 256, 256, 12, 1.70f, 0},       {kFast256x128, 256, 128, 10.5f, 1.045f, 0}, {kFast128, 128, 128, 8, 0.666f, 1.083f},
-    {kFast64, 64, 64, 4.5f, 0.388f, 0.545f},  {kRows, 16, 64, 3, 0.33f, 0.45f},
+    {kFast64, 64, 64, 4.4f, 0.388f, 0.545f},  {kRows, 16, 64, 2.5f, 0, 0},
 };
-constexpr float kLaunch1 = 6, kBytes = 4.5e6f;                     // a further launch, us; bytes a us
+constexpr float kLaunch1 = 3, kQuantize = 2, kBytes = 4.5e6f;      // a further launch, one for lhs's blocks, us; bytes a us
+// Few rows: one workgroup at once, whose step takes 0.15 us until the columns' tiles and splits are so many that memory's 6.5 TB/s bound it (0.33 us for 256); lhs's blocks
+// take it 0.8 us for each 1024 chunks of eight values.  (1 x 16384 x 2048 alone, in 4 and 8 splits 12.0, 8.7 and 8.3 us; 16 x 4096 x 4096 alone, in 2 and 4 14.5, 12.1 and 9.6.)
+float rows_time(uint64_t blocks, uint64_t columns, uint32_t per, uint32_t rows, bool own) {
+  const float step = std::max(0.15f, 0.0013f * std::min<uint64_t>(columns, 256));
+  return 1 + (float)((blocks + 255) / 256) * (2.5f + per * step + (own ? 0.8f * ((rows * per * 32 + 1023) / 1024) : 0));
+}
+bool fits_own(const MxRows& lhs, uint32_t rows, uint32_t per) { return lhs.kc && lhs.k >= 8 && own_bytes(std::min(rows, 16u), per) <= kOwnLhs; }
 
-ProductPlan plan_mx(const MxProduct& x) {
+ProductPlan plan_mx(const MxProduct& x, const MxRows* lhs) {
   const Product& p = x.p;
   ProductPlan plan{};
   plan.steps = (p.K + kUnits - 1) / kUnits;
   const float out = (float)p.batches * p.M * p.N * 4;
   float best = 0;
   for (const Kernel& k : kKernels) {
-    const uint64_t tiles = (uint64_t)((p.M + k.tm - 1) / k.tm) * ((p.N + k.tn - 1) / k.tn) * p.batches;
+    const uint64_t columns = (uint64_t)((p.N + k.tn - 1) / k.tn) * p.batches, tiles = (uint64_t)((p.M + k.tm - 1) / k.tm) * columns;
     for (uint32_t splits = 1; splits <= 64; splits = splits == 1 ? 2 : splits & splits - 1 ? splits / 3 * 4 : splits / 2 * 3) {
       const uint32_t per = (plan.steps + splits - 1) / splits;
       if (splits > 1 && (per < 4 || tiles * splits > 1024)) break;
-      const float one = k.fixed + per * k.one, two = k.two ? k.fixed + per * k.two : 2 * one;
       const uint64_t blocks = tiles * splits, rounds = blocks / 512, rest = blocks % 512;
-      float t = rounds * two + (rest > 256 ? two : rest ? one : 0);
+      const bool own = lhs && k.id == kRows && fits_own(*lhs, p.M, per);
+      const float one = k.fixed + per * k.one, two = k.two ? k.fixed + per * k.two : 2 * one;
+      float t = k.id == kRows ? rows_time(blocks, columns * splits, per, std::min(p.M, 16u), own) : rounds * two + (rest > 256 ? two : rest ? one : 0);
       if (splits > 1) t += kLaunch1 + (splits + 1) * out / kBytes;
+      if (lhs && !own) t += kQuantize;
       if (best && t >= best) continue;
       best = t;
       plan.kernel = k.id == kFast128 && blocks <= 256 ? kFast128Alone : k.id;
@@ -655,9 +664,7 @@ ProductPlan plan_mx(const MxProduct& x) {
   return plan;
 }
 
-bool mx_takes_rows(const MxProduct& x, const ProductPlan& plan, const MxRows& lhs) {
-  return plan.kernel == kRows && lhs.kc && lhs.k >= 8 && own_bytes(std::min(x.p.M, 16u), plan.per_split) <= kOwnLhs;
-}
+bool mx_takes_rows(const MxProduct& x, const ProductPlan& plan, const MxRows& lhs) { return plan.kernel == kRows && fits_own(lhs, x.p.M, plan.per_split); }
 
 hipError_t launch_mx(const MxProduct& x, const ProductPlan& plan, float* partial, hipStream_t st) {
   return in_launches(plan.blocks, [&](uint64_t first, uint32_t n) {

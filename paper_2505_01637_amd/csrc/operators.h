@@ -273,7 +273,7 @@ struct MxProduct {
   const uint8_t *scales_a, *scales_b;
   int64_t scales_batch_a, scales_batch_b;
 };
-ProductPlan plan_mx(const MxProduct& p);
+ProductPlan plan_mx(const MxProduct& p, const MxRows* lhs);       // lhs: a's values, where it is not in blocks yet
 bool mx_takes_rows(const MxProduct& p, const ProductPlan& plan, const MxRows& lhs);
 hipError_t launch_mx(const MxProduct& p, const ProductPlan& plan, float* partial, hipStream_t st);       // without the sum over splits
 
