@@ -557,10 +557,12 @@ template <class TX, class TG>
 hipError_t launch_rows(const NormGrad& p, const GradPlan& g, float* partial, hipStream_t st) {
   return in_launches(g.blocks, [&](uint64_t first, uint32_t n) {
     const auto go = [&](auto kernel) { kernel<<<n, g.groups * (p.N <= kNarrow ? 16 : 64 * g.waves), 0, st>>>(p, g.waves, g.each, (uint32_t)first, g.blocks > 1 ? partial : nullptr); };
-    const bool whole = p.N % 8 == 0;
-    if (p.N <= kNarrow) whole ? go(norm_grad_rows_kernel<TX, TG, 1, 16, true>) : go(norm_grad_rows_kernel<TX, TG, 1, 16, false>);
-    else if (g.keep == 1) whole ? go(norm_grad_rows_kernel<TX, TG, 1, 64, true>) : go(norm_grad_rows_kernel<TX, TG, 1, 64, false>);
-    else whole ? go(norm_grad_rows_kernel<TX, TG, 2, 64, true>) : go(norm_grad_rows_kernel<TX, TG, 2, 64, false>);
+    // (rows of two types, and narrow ones, are taken to end anywhere)
+    constexpr bool MAY = sizeof(TX) == sizeof(TG);
+    const bool whole = MAY && p.N % 8 == 0;
+    if (p.N <= kNarrow) go(norm_grad_rows_kernel<TX, TG, 1, 16, false>);
+    else if (g.keep == 1) whole ? go(norm_grad_rows_kernel<TX, TG, 1, 64, MAY>) : go(norm_grad_rows_kernel<TX, TG, 1, 64, false>);
+    else whole ? go(norm_grad_rows_kernel<TX, TG, 2, 64, MAY>) : go(norm_grad_rows_kernel<TX, TG, 2, 64, false>);
   });
 }
 
@@ -581,7 +583,7 @@ template <class T>
 void launch_norm_rows(const NormRows& p, const NormPlan& g, hipStream_t st) {
   const auto go = [&](auto kernel) { kernel<<<g.blocks, g.groups * (p.N <= kNarrow ? 16 : 64 * g.waves), 0, st>>>(p, g.waves); };
   const bool whole = p.N % 8 == 0;
-  if (p.N <= kNarrow) whole ? go(norm_rows_kernel<T, 1, 16, true>) : go(norm_rows_kernel<T, 1, 16, false>);
+  if (p.N <= kNarrow) go(norm_rows_kernel<T, 1, 16, false>);
   else if (g.keep == 1) whole ? go(norm_rows_kernel<T, 1, 64, true>) : go(norm_rows_kernel<T, 1, 64, false>);
   else whole ? go(norm_rows_kernel<T, 2, 64, true>) : go(norm_rows_kernel<T, 2, 64, false>);
 }

@@ -385,9 +385,10 @@ def test_refusals_of_the_library():
                rows(lib.mrl_mx_quantize, k=1 << 25), rows(lib.mrl_mx_quantize, lines=1 << 31), rows(lib.mrl_mx_dequantize, x=mat(l=1)), rows(lib.mrl_mx_dequantize, x=mat(ld=255)),
                rows(lib.mrl_mx_dequantize, x=mat(t=2)), rows(lib.mrl_mx_dequantize, b=2, x=mat(batch=256))):
         assert rc == B.E_INVAL, lib.mrl_last_error()
-    # the workspace holds lhs in blocks: at least 4 lines of 128 bytes
-    assert linear(m=400) == B.E_NOMEM and linear(m=400, work=P, have=100) == B.E_NOMEM
-    assert linear(m=400, work=P + 16, have=1 << 30) == B.E_INVAL
+    # the workspace holds lhs in blocks where its neighbours along k are not adjacent: 4 lines of 128 bytes at least
+    across = mat(l=1, ld=512)
+    assert linear(lhs=across) == B.E_NOMEM and linear(lhs=across, work=P, have=100) == B.E_NOMEM
+    assert linear(lhs=across, work=P + 16, have=1 << 30) == B.E_INVAL
     with pytest.raises(B.MorelloError):
         import torch
         B.mx_quantize(torch.ones(2, 4))
