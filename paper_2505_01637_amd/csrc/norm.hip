@@ -319,7 +319,7 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(const NormGrad p, u
 // partial: the workgroups' sums (2 x N each: dw, db), nullptr where there is one workgroup.
 template <class TX, class TG, int R, int LANES, bool WHOLE>
 __global__ __launch_bounds__(kRowThreads) void norm_grad_rows_kernel(const NormGrad p, uint32_t waves, uint32_t each, uint32_t first, float* __restrict__ partial) {
-  constexpr bool AHEAD = R == 1;                                         // (twice: no registers for it)
+  constexpr bool AHEAD = R == 1 || (WHOLE && sizeof(TX) + sizeof(TG) == 4);      // (else there are no registers for it)
   __shared__ f32x2 sums[2][kRowThreads / 64];
   __shared__ float columns[R == 1 ? 2 * kRowThreads * 8 : 8];            // (rows of two chunks a thread take all waves)
   const uint32_t block = first + blockIdx.x, rows = p.batches * p.M;
