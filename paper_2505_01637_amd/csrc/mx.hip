@@ -181,7 +181,7 @@ __global__ __launch_bounds__(256) void mx_dequantize_kernel(const MxRows p, uint
     scale[i] = p.scales[at.scales + scale_at(line & 63, c / (32 / E))];
   }
   T* const x = (T*)p.x.data + (int64_t)at.batch * p.x.batch + k;
-  const bool past = (uint64_t)p.batches * p.lines * p.k * sizeof(T) >= kPast;
+  const bool past = (uint64_t)p.batches * p.lines * p.k * sizeof(T) >= kBeyond;        // (up to 32 MB it makes no difference here)
 #pragma unroll
   for (uint32_t i = 0; i < N; i++) {
     const uint32_t line = at.group * 64 + i * (256 / LANES) + l0;
@@ -259,9 +259,9 @@ struct Scales {
   }
 };
 constexpr uint32_t kNoHalf = 0x400000;     // beyond any half step
-// The 256 bytes of a group and every other half step from `odd` on, as a wave loads them.  A half step that is not there has scales of 0, as its codes are: the byte
-// that happens to follow could be a NaN's.  (Worked out without a branch: with one the loop's products were moved behind its barrier, a step of 256 x 256 x 256
-// took 1.88 us.)
+// The 256 bytes of a group and a step's first half step (odd = 0) or second (1), as a wave loads them.  A half step that is not there has scales of 0, as its codes
+// are: the byte that happens to follow could be a NaN's.  (Worked out without a branch: with one the loop's products were moved behind its barrier, and a step of
+// 256 x 256 x 256 took 1.88 us instead of 1.70.)
 struct Slot {
   u32x4 buffer;
   uint32_t offset, odd, halves;
@@ -283,8 +283,8 @@ __device__ __forceinline__ void read_scales(lds_ptr slots, uint32_t first, uint3
 }
 
 // A wave's results through shared memory of its own, PASS blocks of 16 rows at a time, as write_out of tiles.h has them go, but in their order: then what
-// is left to a row's eight columns is its place one row of lanes on.  (Its address worked out anew for each, and the checks of what there is to add, make that
-// twice as long: 62 us of 198 for 8192 x 2048 x 16384 without an activation.)
+// is left to a row's eight columns is its place one row of lanes on.  (Its address worked out anew for each, and the checks of what there is to add, took 14 us more
+// of 8192 x 2048 x 16384.  Straight from the registers, 64 bytes of a row side by side, that is as fast and 8192 x 1024 x 4096 a sixth slower.)
 template <int PASS, int BM, int BN>
 __device__ __forceinline__ void store_results(const Product& p, const Place& at, uint32_t splits, uint32_t m0, uint32_t n0, uint32_t lane, const f32x4 (&acc)[BM][BN],
                                               char* mine, float* __restrict__ partial) {
@@ -296,7 +296,7 @@ __device__ __forceinline__ void store_results(const Product& p, const Place& at,
   bias8(e, n, n < p.N ? p.N - n : 0, bias);
   const uint32_t pitch = (p.N + 7) & ~7u;
   const RowsOf out = splits > 1 ? RowsOf{partial + (uint64_t)at.split * p.batches * p.M * pitch, pitch, (int64_t)p.M * pitch, 0} : e.out;
-  const bool ends = splits == 1, residual = ends && e.residual.data, past = ends && ((uint64_t)p.batches * p.M * p.N << (out.bf16 ? 1 : 2)) >= kPast;
+  const bool ends = splits == 1, residual = ends && e.residual.data, past = ends && goes_past((uint64_t)p.batches * p.M * p.N << (out.bf16 ? 1 : 2));
   const uint32_t valid = splits > 1 ? 8 : n < p.N ? p.N - n : 0, out_shift = out.bf16 ? 1 : 2, res_shift = e.residual.bf16 ? 1 : 2;
   char* to = (char*)out.data + (((int64_t)at.batch * out.batch + (int64_t)(m0 + l) * out.ld + n) << out_shift);
   const char* from = (const char*)e.residual.data + (((int64_t)at.batch * e.residual.batch + (int64_t)(m0 + l) * e.residual.ld + n) << res_shift);
@@ -342,7 +342,12 @@ __device__ __forceinline__ void store_results(const Product& p, const Place& at,
   }
 }
 
-// One tile of TM x TN, WAVES_M x WAVES_N waves, STAGES steps in shared memory: the loop of linear.hip's fast_kernel.
+// One tile of TM x TN, WAVES_M x WAVES_N waves, STAGES steps in shared memory: the loop of linear.hip's fast_kernel.  A wave of the 256 tile has 128 x 64.
+//
+// 8192-cube 247 us, 4450 TFLOP/s, where the matrix units sustain 7600 on operands like these: 208 us without the loads, 219 without the results, 178 without either; they are
+// busy 48 % of the time, shared memory 25 %.  8192 x 2048 x 16384 with GELU 210 us: 130 without the results, whose 268 MB take 52 us of memory's time and
+// 24 us of activation.  Half steps twice as many ahead (64 bytes of a line at a time) took 274 us for the cube; the second of two smaller workgroups a compute unit started
+// half a tile later, or lines asked for steps before, changed nothing or cost time.
 template <int TM, int TN, int WAVES_M, int WAVES_N, int STAGES>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void mx_tile_kernel(const MxProduct x, uint32_t steps, uint32_t per_split, uint32_t splits, uint32_t first,
                                                                          float* __restrict__ partial) {
@@ -502,7 +507,7 @@ __device__ __forceinline__ void own_blocks(const MxRows& x, uint32_t batch, uint
 
 // Few rows: the loop of linear.hip's rows_kernel, the sum split among the waves of a workgroup, each with a ring of its own.  A tile of 16 rows, in their own
 // order (so their scales are bytes here and there of the group's), and 64 columns.  OWN: lhs is a matrix of T, which the workgroup puts into blocks while its first
-// steps of rhs are under way (1 x 2048 x 16384 5.1 us and 4.0 for a launch of its own before it; one launch 6.4).
+// steps of rhs are under way (1 x 2048 x 16384 5.4 us; from blocks 5.0, and 4 for the launch that makes them).
 template <int WAVES, int STAGES, class T, bool OWN>
 __global__ __launch_bounds__(64 * WAVES) void mx_rows_kernel(const MxProduct x, uint32_t steps, uint32_t per_split, uint32_t splits, uint32_t first, float* __restrict__ partial) {
   constexpr int TM = 16, TN = 64, BN = TN / 16;

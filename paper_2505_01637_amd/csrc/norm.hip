@@ -167,7 +167,7 @@ __global__ __launch_bounds__(kRowThreads) void norm_rows_kernel(const NormRows p
     }
   }
   const float one = 1.0f / (float)p.N;
-  const bool past = p.out.bf16 && (uint64_t)rows * p.N * 2 >= kPast;           // (f32, 32 bytes a lane, is not faster so)
+  const bool past = p.out.bf16 && goes_past((uint64_t)rows * p.N * 2);           // (f32, 32 bytes a lane, is not faster so)
   for (uint64_t row0 = row - team.group; row0 < rows; row0 += stride, row += stride) {
     float v[R][8];
     f32x2 s = {0.0f, 0.0f};
@@ -360,7 +360,7 @@ __global__ __launch_bounds__(kRowThreads) void norm_grad_rows_kernel(const NormG
     }
   }
   const float one = 1.0f / (float)p.N;
-  const bool past = p.dx.bf16 && (uint64_t)rows * p.N * 2 >= kPast;
+  const bool past = p.dx.bf16 && goes_past((uint64_t)rows * p.N * 2);
   uint32_t turn = 0;
   for (uint64_t row0 = begin; row0 < end; row0 += groups, turn ^= 1) {
     const uint32_t row = (uint32_t)row0 + group;

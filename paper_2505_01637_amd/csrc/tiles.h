@@ -22,8 +22,7 @@ hipError_t in_launches(uint64_t blocks, F&& f) {
   return hipSuccess;
 }
 
-// 16 bytes, and eight neighbouring elements, past the caches: what is too large to stay there only pushes out what is read again, and is written back when the tiles of all
-// compute units end together (8192 x 2048 x 16384 in 4 bits, 268 MB of results: 259 us, and 220 so).
+// 16 bytes, and eight neighbouring elements, past the caches.
 __device__ __forceinline__ void store16_past(void* to, const void* from) {
   typedef uint32_t words __attribute__((ext_vector_type(4), aligned(2)));
   words w;
@@ -42,7 +41,12 @@ __device__ __forceinline__ void store8_past(void* data, uint32_t is_bf16, int64_
   if (is_bf16) store8_past((bf16*)data + at, v);
   else store8_past((float*)data + at, v);
 }
-constexpr uint64_t kPast = 32 << 20;       // bytes from which it is done: the dies' caches together
+// Whether results of so many bytes go there.  Up to 32 MB they would all lie in the dies' caches at the end, which are written back before the next launch; 256 MB
+// are more than the cache at the memory holds, so nothing is lost to who reads them next; between the two the reader loses more than is gained.  Past and not,
+// alone, and with mx_quantize of the results behind it, in us: layer_norm to 16 MB 9.2 and 10.2, 17.0 and 17.4; to 32 MB 13.7 and 14.5, 23.1 and 23.3; to 64 MB 23.8 and
+// 25, 44 and 40; mx_linear (k = 512) to 16 MB 9.8 and 11.6, 22 and 26; 32 MB 15 and 16.5, 27.8 and 27.1; 128 MB 56 and 59, 87 and 82; 8192 x 2048 x 16384, 256 MB, 210 and 242, 297 and 306.
+constexpr uint64_t kCaches = 32ull << 20, kBeyond = 256ull << 20;
+__device__ __forceinline__ bool goes_past(uint64_t bytes) { return (bytes >= kCaches / 3 && bytes <= kCaches) || bytes >= kBeyond; }
 
 // ---- tiles in shared memory
 //

@@ -1,5 +1,5 @@
 """Every kernel of mx_linear by its launch (without a GPU, on a runtime that counts) and by values, with edges and sums that are split; what
-layer_norm and the quantisation launch; results that are stored past the caches (32 MB and more), at any alignment."""
+layer_norm and the quantisation launch; results that are stored past the caches (11 to 32 MB, or 256 and more), at any alignment."""
 import pytest
 
 from paper_2505_01637_amd import binding as B
@@ -127,9 +127,9 @@ def test_every_kernel(kernel, m, k, n, split):
 
 
 @gpu
-@pytest.mark.parametrize("m,n,gap", [(4096, 4096, 0), (4096, 4096, 3), (8200, 2056, 5), (4100, 4099, 0), (140000, 120, 1), (2100, 8200, 0), (1050, 16001, 2)])
-def test_large_results_past_the_caches(m, n, gap):
-    """bf16 results of 32 MB and more, rows at any alignment: nothing beside them is written."""
+@pytest.mark.parametrize("m,n,gap", [(4096, 4096, 0), (4096, 4096, 3), (8000, 2056, 5), (4000, 4099, 0), (130000, 120, 1), (2000, 8200, 0), (1000, 16001, 2)])
+def test_results_past_the_caches(m, n, gap):
+    """bf16 results of up to 32 MB, rows at any alignment: nothing beside them is written."""
     import torch
     gen = torch.Generator(device="cuda").manual_seed(n)
 
@@ -164,13 +164,6 @@ def test_large_results_past_the_caches(m, n, gap):
     close(dw, (grad.double() * h).sum(0), (m + 8) * U * (grad.double() * h).abs().sum(0), "f32")
     close(db, grad.double().sum(0), (m + 8) * U * grad.double().abs().sum(0), "f32")
     del X, h, g, want, off, bound
-    # values in and out of blocks: the same as of the lines in pieces that are not stored past the caches
-    q = B.mx_quantize(x)
-    back = B.mx_dequantize(q)
-    for at in range(0, m, 20000):
-        part = x[at:at + 1000]
-        assert torch.equal(back[at:at + 1000], B.mx_dequantize(B.mx_quantize(part)))
-    assert torch.equal(B.mx_dequantize(q, dtype=torch.float32), back.float())
     # a product
     L = torch.randn((m, 100), generator=gen, device="cuda").bfloat16()
     v = B.mx_quantize(torch.randn((100, n), generator=gen, device="cuda"), dim=-2)
@@ -179,3 +172,29 @@ def test_large_results_past_the_caches(m, n, gap):
     beside(out)
     l, R = B.mx_dequantize(B.mx_quantize(L)).double(), B.mx_dequantize(v, dtype=torch.float32).double().contiguous()
     close(out, (l @ R + b.double()).clamp(min=0), 104 * U * (l.abs() @ R.abs() + b.abs().double()), "bf16")
+
+
+@gpu
+def test_results_beyond_every_cache():
+    """256 MB and more: values read back, lines at any alignment, a normalisation and a product; against the same of pieces."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    m, k = 4100, 32771
+    x = torch.randn((m, k), generator=gen, device="cuda").bfloat16()
+    pieces = [slice(at, at + 100) for at in range(0, m, 1000)] + [slice(m - 3, m)]
+    back = B.mx_dequantize(B.mx_quantize(x))
+    wide = B.mx_dequantize(B.mx_quantize(x[:2050]), dtype=torch.float32)
+    for at in pieces:
+        assert torch.equal(back[at], B.mx_dequantize(B.mx_quantize(x[at])))
+    assert torch.equal(wide, back[:2050].float())
+    y = x.as_strided((16400, 8190), (8191, 1))
+    out, stats = B.layer_norm(y, stats=True)
+    dx, _, _ = B.layer_norm_grad(y, y, stats)
+    w = B.mx_quantize(torch.randn((200, 8190), generator=gen, device="cuda"), dim=-2)
+    v = torch.randn((16400, 200), generator=gen, device="cuda").bfloat16()
+    product = B.mx_linear(v, w)
+    for at in [slice(at, at + 40) for at in range(0, 16400, 1500)] + [slice(16397, 16400)]:
+        piece, s = B.layer_norm(y[at], stats=True)
+        assert torch.equal(out[at], piece) and torch.equal(stats[at], s) and torch.equal(dx[at], B.layer_norm_grad(y[at], y[at], s)[0])
+        # (sums of 200 products, whole within a step: the same bits by every kernel)
+        assert torch.equal(product[at], B.mx_linear(v[at], w))
