@@ -30,7 +30,7 @@ def source_hash():
     h = hashlib.sha256()
     d = os.path.join(ROOT, "paper_2505_01637_amd", "csrc")
     for name in sorted(os.listdir(d)):
-        if name.endswith((".hip", ".h")) and name not in ("operators.h", "operators.hip", "linear.hip"):
+        if name.endswith((".hip", ".h")) and name not in ("operators.h", "operators.hip", "linear.hip", "norm.hip", "mx.hip", "tiles.h"):
             with open(os.path.join(d, name), "rb") as f:
                 h.update(name.encode() + b"\0" + f.read())
     return h.hexdigest()[:16]

@@ -5,6 +5,7 @@
 The program is what the framework's table says about the block's first half as a Spec (Matmul, bias add, ReLU) of the
 paper's machine; Table.apply computes the same Spec on data.  Training and decoding run on binding.linear and
 binding.linear_grad alone: no mask of either dropout is stored, the gradient draws it again from seed and step.
+Normed is the block behind a layer normalisation, Served that with its weights in 4-bit blocks.
 
     python examples/feed_forward.py
 """
@@ -57,6 +58,42 @@ class FeedForward:
         return B.linear(h, self.w2, self.b2, x)
 
 
+class Normed:
+    """x + the block's branch of layer_norm(x); scale and shift of the normalisation in f32."""
+
+    def __init__(self, block, device="cuda"):
+        width = block.w1.shape[0]
+        self.block, self.scale, self.shift = block, torch.ones(width, device=device), torch.zeros(width, device=device)
+
+    def forward(self, x):
+        y, stats = B.layer_norm(x, self.scale, self.shift, stats=True)
+        b = self.block
+        h, z = B.linear(y, b.w1, b.b1, activation="gelu", pre=True)
+        return B.linear(h, b.w2, b.b2, x), (x, stats, y, h, z)
+
+    def backward(self, grad, saved):
+        """(gradient by x, gradients by scale, shift and the block's four parameters)."""
+        x, stats, y, h, z = saved
+        b = self.block
+        d_h, d_w2, d_b2 = B.linear_grad(grad, h, b.w2, b.b2)
+        d_y, d_w1, d_b1 = B.linear_grad(d_h, y, b.w1, b.b1, z, activation="gelu")
+        d_x, d_scale, d_shift = B.layer_norm_grad(d_y, x, stats, self.scale, self.shift, grad)
+        return d_x, [d_scale, d_shift, d_w1, d_b1, d_w2, d_b2]
+
+
+class Served:
+    """Normed for decoding, its two weight matrices in microscaled 4-bit floating point: a quarter of what bf16 reads."""
+
+    def __init__(self, normed):
+        self.normed = normed
+        self.w1, self.w2 = (B.mx_quantize(w, dim=-2) for w in (normed.block.w1, normed.block.w2))
+
+    def token(self, x):
+        n = self.normed
+        h = B.mx_linear(B.layer_norm(x, n.scale, n.shift), self.w1, n.block.b1, activation="gelu")
+        return B.mx_linear(h, self.w2, n.block.b2, x)
+
+
 def program(width, hidden, rows):
     """The program of relu(x w1 + b1), rows x width by width x hidden in f32, and the Spec computed on data."""
     cfg = W.config(5, max_size=max(width, hidden, rows))
@@ -93,3 +130,6 @@ if __name__ == "__main__":
     print("loss %.4f -> %.4f in %d steps" % (losses[0], losses[-1], len(losses)))
     x = torch.randn(1, 256, device="cuda").bfloat16()
     print("one token:", tuple(model.token(x).shape))
+    normed = Normed(model)
+    served, whole = Served(normed).token(x).float(), normed.forward(x)[0].float()
+    print("behind a normalisation, weights in 4 bits: %.2g of its norm from bf16" % ((served - whole).norm() / whole.norm()).item())

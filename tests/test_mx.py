@@ -392,3 +392,35 @@ def test_refusals_of_the_library():
     with pytest.raises(B.MorelloError):
         import torch
         B.mx_quantize(torch.ones(2, 4))
+
+
+@gpu
+def test_feed_forward_example_normed_and_served():
+    """The example's block behind a normalisation: its gradients are autograd's of the formula in 64 bits, and what is served is the formula on
+    the values that its weights' blocks stand for."""
+    import os
+    import sys
+    torch, _ = _torch()
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import feed_forward as F
+    model = F.Normed(F.FeedForward(64, 96, 0.0, seed=3))
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    x, g = (torch.randn(40, 64, generator=gen, device="cuda").bfloat16() for _ in range(2))
+    model.scale += 0.1 * torch.randn(64, generator=gen, device="cuda")
+    out, saved = model.forward(x)
+    d_x, grads = model.backward(g, saved)
+    b = model.block
+    ps = [p.double().requires_grad_() for p in (x, model.scale, model.shift, b.w1, b.b1, b.w2, b.b2)]
+    y = torch.nn.functional.layer_norm(ps[0], (64,)) * ps[1] + ps[2]
+    want = ps[0] + torch.nn.functional.gelu(y @ ps[3] + ps[4], approximate="tanh") @ ps[5] + ps[6]
+    want.backward(g.double())
+    # chained bf16 roundings (y, z, h, out, d_h, dz, d_y, the gradients): twelve units of 2^-8, of the norm, as they are independent
+    for got, p in zip([d_x] + grads, ps):
+        assert got.shape == p.shape and (got.double() - p.grad).norm() <= 12 * 2.0 ** -8 * p.grad.norm()
+    assert (out.double() - want).norm() <= 4 * 2.0 ** -8 * want.norm()
+    served = F.Served(model)
+    for m in (1, 40):
+        y = B.layer_norm(x[:m], model.scale, model.shift)
+        h = B.mx_linear(y, served.w1, b.b1, activation="gelu")
+        o = B.mx_dequantize(B.mx_quantize(h)).double() @ B.mx_dequantize(served.w2).double() + b.b2.double() + x[:m].double()
+        assert (served.token(x[:m]).double() - o).norm() <= 2.0 ** -8 * o.norm()
