@@ -955,10 +955,14 @@ def mx_quantize(x, *, dim=-1, out=None, stream=None):
         lines = x if dim == -1 else x.transpose(-1, -2)
         n, k = lines.shape[-2:]
         steps = -(-k // 128)
-        form = _keep_form(key, ((b, n, k, 0), _matrix("x", lines)[1:], lines.shape[:-2] + (n, 64 * steps), lines.shape[:-2] + (-(-n // 64), steps, 4, 16, 4)))
-    sizes, m, codes, scales = form
+        codes, scales = lines.shape[:-2] + (n, 64 * steps), lines.shape[:-2] + (-(-n // 64), steps, 4, 16, 4)
+        form = ((b, n, k, 0), _matrix("x", lines)[1:], codes, scales, MX(x.new_empty(codes, dtype=_uint8), x.new_empty(scales, dtype=_uint8), k, dim=dim, dtype=x.dtype)._key)
+        _keep_form(key, form)
+    sizes, m, codes, scales, kept = form
     if out is None:
-        out = MX(x.new_empty(codes, dtype=_uint8), x.new_empty(scales, dtype=_uint8), sizes[2], dim=dim, dtype=x.dtype)
+        out = MX.__new__(MX)       # (its checks are the form's)
+        out.codes, out.scales, out.k, out.dim, out.dtype = x.new_empty(codes, dtype=_uint8), x.new_empty(scales, dtype=_uint8), sizes[2], dim, x.dtype
+        out.shape, out._key = x.shape, kept
     elif out.shape != x.shape or out.dim != dim:
         raise MorelloError(E_INVAL, "out is %r: x has shape %s, dim %d" % (out, tuple(x.shape), dim))
     rc = lib().mrl_mx_quantize(_MX.pack(*sizes, x.data_ptr(), *m, out.codes.data_ptr(), out.scales.data_ptr(), 0, 0), _raw_stream(x.get_device()))
@@ -1010,7 +1014,7 @@ def _form_mx_linear(key, lhs, rhs, blocks, bias, residual, out, dtype, activatio
                            *(v for m in mats for v in m), act, 0)
     need = C.c_size_t()
     _check(lib().mrl_mx_linear_bytes(desc, C.addressof(need)))
-    return _keep_form(key, (shape, out.dtype, sizes, shared, ml[1:], *(m[1:] for m in mats), act, need.value))
+    return _keep_form(key, (shape, None if out.dtype == like.dtype else out.dtype, sizes, shared, ml[1:], *(m[1:] for m in mats), act, need.value))
 
 
 def mx_linear(lhs, rhs, bias=None, residual=None, *, activation="none", dtype=None, out=None, workspace=None, stream=None):
@@ -1033,7 +1037,7 @@ def mx_linear(lhs, rhs, bias=None, residual=None, *, activation="none", dtype=No
     else:
         like, first = lhs, (lhs.data_ptr(), *ml, 0, 0)
     if out is None:
-        out = like.new_empty(shape, dtype=dtype)
+        out = like.new_empty(shape) if dtype is None else like.new_empty(shape, dtype=dtype)
     desc = _MX_LINEAR.pack(*sizes, *first, 0, 0, rhs.codes.data_ptr(), rhs.scales.data_ptr(), shared, 0, 0 if bias is None else bias.data_ptr(), *mb,
                            0 if residual is None else residual.data_ptr(), *ms, out.data_ptr(), *mo, act, 0)
     _run(desc, _lib.mrl_mx_linear, need, workspace, like)
