@@ -325,6 +325,45 @@ def test_block_of_the_operators():
 
 
 @gpu
+def test_blocks_that_batches_share():
+    """The library's `shared`, which the binding sets for rhs alone: every batch of lhs the same blocks, of rhs too, and read back."""
+    torch, _ = _torch()
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    b, m, k, n = 3, 70, 200, 50
+    x, w = torch.randn((m, k), generator=gen, device="cuda").bfloat16(), torch.randn((b, k, n), generator=gen, device="cuda")
+    q, many = B.mx_quantize(x), B.mx_quantize(w, dim=-2)
+    one = B.mx_quantize(w[0], dim=-2)
+    stream = torch.cuda.current_stream().cuda_stream
+    for rhs, shared in ((many, 0), (one, 1)):
+        out = torch.full((b, m, n), 7.0, device="cuda")
+        d = B._MX_LINEAR.pack(b, m, k, n, *B._ABSENT, q.codes.data_ptr(), q.scales.data_ptr(), 1, 0, rhs.codes.data_ptr(), rhs.scales.data_ptr(), shared, 0,
+                              *B._ABSENT, *B._ABSENT, out.data_ptr(), 0, 0, n, m * n, 0, 0)
+        size = C.c_size_t()
+        assert B.lib().mrl_mx_linear_bytes(d, C.addressof(size)) == 0
+        work = torch.empty(size.value, dtype=torch.uint8, device="cuda")
+        assert B.lib().mrl_mx_linear(d, work.data_ptr() if size.value else None, size.value, stream) == 0
+        want = B.mx_linear(x.expand(b, m, k), many if shared == 0 else one, dtype=torch.float32)
+        assert torch.equal(out, want)
+    out = torch.full((b, m, k), 7.0, device="cuda")
+    assert B.lib().mrl_mx_dequantize(B._MX.pack(b, m, k, 0, out.data_ptr(), 0, 0, k, m * k, q.codes.data_ptr(), q.scales.data_ptr(), 1, 0), stream) == 0
+    assert torch.equal(out, B.mx_dequantize(q, dtype=torch.float32).expand(b, m, k))
+
+
+@gpu
+def test_operands_that_repeat():
+    """Rows and batches that are the same memory again (strides of 0) are read as they are."""
+    torch, _ = _torch()
+    gen = torch.Generator(device="cuda").manual_seed(10)
+    row, rhs = torch.randn((1, 300), generator=gen, device="cuda").bfloat16(), torch.randn((300, 90), generator=gen, device="cuda")
+    w = B.mx_quantize(rhs, dim=-2)
+    want = B.mx_linear(row, w)
+    for m in (2, 40, 200):
+        assert torch.equal(B.mx_linear(row.expand(m, 300), w), want.expand(m, 90))
+        assert torch.equal(B.mx_linear(row.expand(2, m, 300), w), want.expand(2, m, 90))
+        assert torch.equal(B.mx_quantize(row.expand(m, 300)).codes, B.mx_quantize(row.expand(m, 300).contiguous()).codes)
+
+
+@gpu
 def test_beyond_32_bits():
     """Codes and values past 4 GB: 70,000 x 131,072 values."""
     torch, _ = _torch()
@@ -389,9 +428,13 @@ def test_refusals_of_the_library():
     across = mat(l=1, ld=512)
     assert linear(lhs=across) == B.E_NOMEM and linear(lhs=across, work=P, have=100) == B.E_NOMEM
     assert linear(lhs=across, work=P + 16, have=1 << 30) == B.E_INVAL
-    with pytest.raises(B.MorelloError):
-        import torch
-        B.mx_quantize(torch.ones(2, 4))
+    import torch
+    blocks = B.MX(torch.zeros((4, 64), dtype=torch.uint8), torch.zeros((1, 1, 4, 16, 4), dtype=torch.uint8), 100, dim=-2)
+    assert blocks.shape == (100, 4) and blocks.lines == 4
+    for f in (lambda: B.mx_quantize(torch.ones(2, 4)), lambda: B.mx_dequantize(blocks), lambda: B.mx_linear(torch.ones(2, 100), blocks)):
+        with pytest.raises(B.MorelloError) as e:
+            f()
+        assert "there is no CPU path" in str(e.value)
 
 
 @gpu

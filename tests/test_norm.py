@@ -221,6 +221,26 @@ def test_norm_in_place_and_the_same_bits():
 
 
 @gpu
+def test_norm_operands_that_repeat():
+    """Rows that are the same memory again (a stride of 0), of x and of its gradient: as if they were there."""
+    torch, _ = _torch()
+    for m, n in ((5, 100), (300, 40), (40, 2050), (3, 20000)):
+        x, g = torch.randn((1, n), device="cuda").expand(m, n), torch.randn((1, n), device="cuda").expand(m, n)
+        w = torch.randn(n, device="cuda")
+        out, stats = B.layer_norm(x, w, stats=True)
+        whole, s = B.layer_norm(x.contiguous(), w, stats=True)
+        assert torch.equal(out, whole) and torch.equal(stats, s)
+        for p, q in zip(B.layer_norm_grad(g, x, stats, w, w, g), B.layer_norm_grad(g.contiguous(), x.contiguous(), stats, w, w, g.contiguous())):
+            assert p.shape == q.shape and p.is_contiguous() and torch.equal(p, q)
+    # batches in another order than their memory's
+    x = torch.randn((6, 4, 100), device="cuda").transpose(0, 1)
+    out, stats = B.layer_norm(x, stats=True)
+    assert out.shape == x.shape and torch.equal(out, B.layer_norm(x.contiguous()))
+    dx, _, _ = B.layer_norm_grad(x, x, stats)
+    assert torch.equal(dx, B.layer_norm_grad(x.contiguous(), x.contiguous(), stats)[0])
+
+
+@gpu
 def test_grad_as_the_first_call_of_a_process(monkeypatch):
     torch, _ = _torch()
     x = torch.randn((5, 40), device="cuda")
