@@ -560,7 +560,7 @@ int32_t mrl_layer_norm(const mrl_layer_norm_desc* desc, void* hip_stream);
 /* Gradients of a loss, given `grad`, its gradient by out: with h = (x - mean) r and g = grad weight
  *   d_x = residual + r (g - sum g / n - h sum(g h) / n)
  *   d_weight = the sum of grad h, d_bias = the sum of grad, over batches and rows
- * Each of the three is optional (its data NULL), and so is residual: the gradient that reaches x past
+ * Each of the three is optional (its data NULL; grad, x and stats are needed for any of them), and so is residual: the gradient that reaches x past
  * the normalisation, as in a block with a residual.  d_x may be x, grad or residual itself.  n of 0: nothing is written. */
 typedef struct {
   uint32_t b, m, n, reserved;

@@ -136,7 +136,8 @@ __device__ __forceinline__ f32x2 Team<LANES>::sum(f32x2 v, f32x2* sums) const {
 }
 
 // `waves` waves a row; a workgroup's groups of waves take a row each, then the rows that follow those of all workgroups.  Memory bounds it, so the next
-// row's loads go out before this one's sums are made; weight and bias are read once.
+// row's loads go out before this one's sums are made; weight and bias are read once.  8192 x 2048 in bf16 12.9 us, 5.2 TB/s (21.8 by workgroups of a row each whose loads wait
+// for branches); f32 22.4 us, 6.0 TB/s.
 template <class T, int R, int LANES, bool WHOLE>
 __global__ __launch_bounds__(kRowThreads) void norm_rows_kernel(const NormRows p, uint32_t waves) {
   __shared__ f32x2 sums[2][kRowThreads / 64];
@@ -316,7 +317,8 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(const NormGrad p, u
 }
 
 // The gradient of such rows: each workgroup's groups take its `each` rows in turn and keep the columns' sums, which they add in their order at the end.
-// partial: the workgroups' sums (2 x N each: dw, db), nullptr where there is one workgroup.
+// partial: the workgroups' sums (2 x N each: dw, db), nullptr where there is one workgroup.  8192 x 2048 in bf16 with a residual 28 us, and 3.9 for norm_sums_kernel, of 26
+// that memory takes for what has to be read and written.
 template <class TX, class TG, int R, int LANES, bool WHOLE>
 __global__ __launch_bounds__(kRowThreads) void norm_grad_rows_kernel(const NormGrad p, uint32_t waves, uint32_t each, uint32_t first, float* __restrict__ partial) {
   constexpr bool AHEAD = R == 1 || (WHOLE && sizeof(TX) + sizeof(TG) == 4);      // (else there are no registers for it)
@@ -527,7 +529,8 @@ __global__ __launch_bounds__(1024) void norm_sums_kernel(const NormGrad p, uint3
   else ((float*)to)[n] = s;
 }
 
-// How a gradient is launched, by its sizes alone (and whether column sums are wanted).
+// How a gradient is launched, by its sizes alone (and whether column sums are wanted).  A workgroup a compute unit where they are: more of them write and read more sums, and
+// take longer from the start (8192 x 2048 in bf16 256 workgroups 34 us, 512 36, 1024 42; 4096 x 16384 99, 108, 141).
 struct GradPlan {
   uint32_t keep, waves, groups;            // R and the waves of a row (0: too long to be kept), rows at a time of a workgroup
   uint32_t each, blocks;                   // rows of a workgroup (of a block of rows), how many of them
@@ -566,7 +569,7 @@ hipError_t launch_rows(const NormGrad& p, const GradPlan& g, float* partial, hip
   });
 }
 
-// How rows are normalised.
+// How rows are normalised: two chunks a thread where a wave would have more than one (8192 x 2048 in bf16 16.2 us with one, 14.2 with two; 32768 x 512 13.8 and 16).
 struct NormPlan { uint32_t keep, waves, groups, blocks; };     // keep: R, 0: too long (or short) to be kept
 NormPlan plan_norm(uint64_t rows, uint32_t N) {
   NormPlan g{};

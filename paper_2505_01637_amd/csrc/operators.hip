@@ -246,15 +246,15 @@ int32_t check_stats(const void* stats, uint64_t rows, bool needed) {
 int32_t norm_grad(const mrl_layer_norm_grad_desc& d, NormGrad* out) {
   int32_t rc = check_common(d.b, d.m, 0, d.n, MRL_ACT_NONE, 0);
   const uint64_t b = d.b;
-  const bool x = d.d_x.data || d.d_weight.data;
-  if (!rc) rc = check_matrix("grad", d.grad, x || d.d_bias.data ? b : 0, d.m, d.n, false, false);
-  if (!rc) rc = check_matrix("x", d.x, x ? b : 0, d.m, d.n, false, false);
+  const bool any = d.d_x.data || d.d_weight.data || d.d_bias.data;        // (x and stats are read for the sum of grad too, by the pass that makes all three)
+  if (!rc) rc = check_matrix("grad", d.grad, any ? b : 0, d.m, d.n, false, false);
+  if (!rc) rc = check_matrix("x", d.x, any ? b : 0, d.m, d.n, false, false);
   if (!rc && d.residual.data) rc = check_matrix("residual", d.residual, b, d.m, d.n, false, false);
   if (!rc) rc = check_vector("weight", d.weight, d.weight.data ? d.n : 0);
   if (!rc && d.d_x.data) rc = check_matrix("d_x", d.d_x, b, d.m, d.n, true, false);
   if (!rc && d.d_weight.data) rc = check_vector("d_weight", d.d_weight, d.n);
   if (!rc && d.d_bias.data) rc = check_vector("d_bias", d.d_bias, d.n);
-  if (!rc) rc = check_stats(d.stats, b * d.m * d.n, x);
+  if (!rc) rc = check_stats(d.stats, b * d.m * d.n, any);
   if (rc) return rc;
   *out = NormGrad{rows_of(d.grad), rows_of(d.x), rows_of(d.residual), rows_of(d.d_x), d.weight.data, (const float*)d.stats, d.d_weight.data, d.d_bias.data,
                   d.weight.dtype == MRL_BF16, d.d_weight.dtype == MRL_BF16, d.d_bias.dtype == MRL_BF16, d.b, d.m, d.n};

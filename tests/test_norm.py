@@ -351,6 +351,12 @@ def test_norm_refusals_without_a_gpu():
                norm(w=mat(P + 1)), norm(b=1 << 31), norm(b=1 << 16, m=1 << 16), norm(x=mat(ld=-1)), norm(x=mat(ld=1 << 41)), norm(b=2, out=mat(batch=8)),
                grad(stats=0), grad(x=mat(0)), grad(g=mat(0)), grad(dx=mat(ld=3)), grad(w=mat(P + 2)), grad(dw=mat(P + 2)), grad(res=mat(t=7)), grad(stats=P + 1)):
         assert rc == B.E_INVAL
+    # d_bias alone is made by the pass that makes all three: it has to have what that reads
+    alone = dict(dx=B._ABSENT, db=(P, 0, 0, 1, 0))
+    for n in (16, 5, 20000):
+        t = mat(ld=n, batch=4 * n)
+        for rc in (grad(n=n, g=t, x=mat(0, ld=n), **alone), grad(n=n, g=t, x=t, stats=0, **alone), grad(n=n, g=mat(0, ld=n), x=t, **alone)):
+            assert rc == B.E_INVAL
     # gradients of many rows sum over blocks of them in a workspace, which is asked for
     big = dict(m=1 << 16, g=mat(), x=mat(), dw=(P, 0, 0, 1, 0), db=(P, 0, 0, 1, 0))
     need = grad(run=False, **big)
