@@ -289,6 +289,7 @@ template <int PASS, int BM, int BN>
 __device__ __forceinline__ void store_results(const Product& p, const Place& at, uint32_t splits, uint32_t m0, uint32_t n0, uint32_t lane, const f32x4 (&acc)[BM][BN],
                                               char* mine, float* __restrict__ partial) {
   constexpr uint32_t CHUNKS = BN * 4, GROUPS = BN * 2, ROWS = 64 / GROUPS;      // chunks and groups of 8 columns of a row; rows at a time
+  constexpr uint32_t UNITS = 16 * PASS / ROWS < 4 ? 16 * PASS / ROWS : 4;       // times that, before the first is stored: a branch for all of them
   const Epilogue& e = p.e;
   const uint32_t q = lane & 15, g = lane >> 4;
   const uint32_t c = lane % GROUPS, n = n0 + c * 8, l = lane / GROUPS;
@@ -311,31 +312,46 @@ __device__ __forceinline__ void store_results(const Product& p, const Place& at,
     }
     asm volatile("" ::: "memory");         // (a wave's accesses to shared memory are done in their order)
     if (n < p.N) {
-#pragma unroll 4
-      for (uint32_t r = l; r < 16 * PASS; r += ROWS) {
-        if (m0 + h * 16 + r >= p.M) break;
-        float v[8];
+#pragma unroll 1
+      for (uint32_t r = l; r < 16 * PASS; r += UNITS * ROWS) {
+        const uint32_t m = m0 + h * 16 + r;
+        float v[UNITS][8];
 #pragma unroll
-        for (int x = 0; x < 2; x++) {
-          const f32x4 t = *(const f32x4*)(mine + (r * CHUNKS + ((2 * c + x) ^ (r & (CHUNKS - 1)))) * 16);
+        for (uint32_t u = 0; u < UNITS; u++)
 #pragma unroll
-          for (int k = 0; k < 4; k++) v[4 * x + k] = t[k];
-        }
+          for (int x = 0; x < 2; x++) {
+            const uint32_t line = r + u * ROWS;
+            const f32x4 t = *(const f32x4*)(mine + (line * CHUNKS + ((2 * c + x) ^ (line & (CHUNKS - 1)))) * 16);
+#pragma unroll
+            for (int k = 0; k < 4; k++) v[u][4 * x + k] = t[k];
+          }
         if (ends) {
 #pragma unroll
-          for (int k = 0; k < 8; k++) v[k] += bias[k];
-          activate8(e.activation, v);
-        }
-        if (residual) {
-          float y[8];
-          load8(from, e.residual.bf16, 0, valid, y);
+          for (uint32_t u = 0; u < UNITS; u++)
 #pragma unroll
-          for (int k = 0; k < 8; k++) v[k] += y[k];
-          from += from_step;
+            for (int k = 0; k < 8; k++) v[u][k] += bias[k];
+          const auto activate = [&](uint32_t act) {
+#pragma unroll
+            for (uint32_t u = 0; u < UNITS; u++) activate8(act, v[u]);
+          };
+          if (e.activation == kActRelu) activate(kActRelu);
+          else if (e.activation == kActGelu) activate(kActGelu);
+          else if (e.activation == kActSilu) activate(kActSilu);
         }
-        if (past && valid >= 8) store8_past(to, out.bf16, 0, v);
-        else store8(to, out.bf16, 0, valid, v);
-        to += to_step;
+#pragma unroll
+        for (uint32_t u = 0; u < UNITS; u++) {
+          if (m + u * ROWS >= p.M) break;
+          if (residual) {
+            float y[8];
+            load8(from + u * from_step, e.residual.bf16, 0, valid, y);
+#pragma unroll
+            for (int k = 0; k < 8; k++) v[u][k] += y[k];
+          }
+          if (past && valid >= 8) store8_past(to + u * to_step, out.bf16, 0, v[u]);
+          else store8(to + u * to_step, out.bf16, 0, valid, v[u]);
+        }
+        from += UNITS * from_step;
+        to += UNITS * to_step;
       }
     }
     asm volatile("" ::: "memory");
@@ -345,8 +361,8 @@ __device__ __forceinline__ void store_results(const Product& p, const Place& at,
 // One tile of TM x TN, WAVES_M x WAVES_N waves, STAGES steps in shared memory: the loop of linear.hip's fast_kernel.  A wave of the 256 tile has 128 x 64.
 //
 // 8192-cube 247 us, 4450 TFLOP/s, where the matrix units sustain 7600 on operands like these: 208 us without the loads, 219 without the results, 178 without either; they are
-// busy 48 % of the time, shared memory 25 %.  8192 x 2048 x 16384 with GELU 210 us: 130 without the results, whose 268 MB take 52 us of memory's time and
-// 24 us of activation.  Half steps twice as many ahead (64 bytes of a line at a time) took 274 us for the cube; the second of two smaller workgroups a compute unit started
+// busy 48 % of the time, shared memory 25 %.  8192 x 2048 x 16384 with GELU 208 us: 130 without the results, whose 268 MB take 52 us of memory's time and
+// whose activation takes 36 (172 without it: an exponential and a reciprocal are a quarter of the rate).  Half steps twice as many ahead (64 bytes of a line at a time) took 274 us for the cube; the second of two smaller workgroups a compute unit started
 // half a tile later, or lines asked for steps before, changed nothing or cost time.
 template <int TM, int TN, int WAVES_M, int WAVES_N, int STAGES>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void mx_tile_kernel(const MxProduct x, uint32_t steps, uint32_t per_split, uint32_t splits, uint32_t first,
