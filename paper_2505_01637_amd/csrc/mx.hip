@@ -361,9 +361,10 @@ __device__ __forceinline__ void store_results(const Product& p, const Place& at,
 // One tile of TM x TN, WAVES_M x WAVES_N waves, STAGES steps in shared memory: the loop of linear.hip's fast_kernel.  A wave of the 256 tile has 128 x 64.
 //
 // 8192-cube 247 us, 4450 TFLOP/s, where the matrix units sustain 7600 on operands like these: 208 us without the loads, 219 without the results, 178 without either; they are
-// busy 48 % of the time, shared memory 25 %.  8192 x 2048 x 16384 with GELU 208 us: 130 without the results, whose 268 MB take 52 us of memory's time and
-// whose activation takes 36 (172 without it: an exponential and a reciprocal are a quarter of the rate).  Half steps twice as many ahead (64 bytes of a line at a time) took 274 us for the cube; the second of two smaller workgroups a compute unit started
-// half a tile later, or lines asked for steps before, changed nothing or cost time.
+// busy 48 % of the time, shared memory 25 %.  8192 x 2048 x 16384 with GELU 208 us: 130 without the results, whose 268 MB take 52 us of memory's time and whose
+// activation takes 36 (172 without it: an exponential and a reciprocal are a quarter of the rate).  Half steps twice as many ahead (64 bytes of a line at a time) took
+// 274 us for the cube; the second of two smaller workgroups a compute unit started half a tile later, or lines asked for steps before, changed nothing or cost
+// time.
 template <int TM, int TN, int WAVES_M, int WAVES_N, int STAGES>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void mx_tile_kernel(const MxProduct x, uint32_t steps, uint32_t per_split, uint32_t splits, uint32_t first,
                                                                          float* __restrict__ partial) {

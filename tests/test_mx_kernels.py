@@ -27,7 +27,7 @@ from paper_2505_01637_amd import binding as B
 lib = B.lib()
 NONE, P = (0, 0, 0, 0, 0), 1 << 20                # (addresses that nothing reads)
 NAMES = ("mx_tile_kernelILi256ELi256E", "mx_tile_kernelILi256ELi128E", "mx_tile_kernelILi128ELi128ELi2ELi2E", "mx_tile_kernelILi128ELi128ELi2ELi4E", "mx_tile_kernelILi64E",
-         "mx_rows_kernel", "mx_quantize_across", "mx_quantize_kernel", "mx_dequantize", "rest_kernel", "norm_grad_rows", "norm_columns", "norm_sums", "norm_grad_kernel", "norm_rows",
+         "mx_rows_kernel", "mx_quantize_across", "mx_quantize_kernel", "mx_dequantize", "rest_kernel", "norm_grad_rows", "norm_columns", "norm_sums", "norm_grad_kernel", "norm_grad_few", "norm_few", "norm_rows",
          "norm_kernel")
 
 def took():
@@ -82,8 +82,9 @@ assert q(lib.mrl_mx_dequantize, (P, 0, 0, 300, 0)) == 0 and took() == {"mx_dequa
 # rows in registers from 8 to 16384 elements
 for m, n in ((1, 8), (5, 128), (8192, 2048), (3, 16384)):
     assert norm(m, n) == {"norm_rows": 1}, (m, n)
-for m, n in ((1, 1), (100, 7), (2, 16385)):
-    assert norm(m, n) == {"norm_kernel": 1}, (m, n)
+for m, n in ((1, 1), (100, 7)):
+    assert norm(m, n) == {"norm_few": 1}, (m, n)
+assert norm(2, 16385) == {"norm_kernel": 1}
 assert norm(0, 8) == {} and norm(8, 0) == {}
 for m, n in ((1, 2048), (8, 1000), (64, 128), (4, 16384)):
     assert grad(m, n) == ({"norm_grad_rows": 1}, 0), "the sums of few rows need no second launch"
@@ -91,7 +92,7 @@ got, size = grad(8192, 2048)
 assert got == {"norm_grad_rows": 1, "norm_sums": 1} and size == 256 * 2 * 2048 * 4
 assert grad(8192, 2048, sums=False) == ({"norm_grad_rows": 1}, 0) and grad(8192, 2048, x=False)[0] == {"norm_grad_rows": 1, "norm_sums": 1}
 assert grad(100, 20000) == ({"norm_grad_kernel": 1, "norm_columns": 1, "norm_sums": 1}, 2 * 2 * 20000 * 4)
-assert grad(64, 5)[0] == {"norm_grad_kernel": 1, "norm_columns": 1}
+assert grad(64, 5)[0] == {"norm_grad_few": 1, "norm_columns": 1}
 assert grad(100, 64, x=False, sums=False) == ({}, 0) and grad(5, 0) == ({}, 0)
 assert grad(0, 64) == ({"norm_grad_rows": 1}, 0), "the sums over no rows are zeros"
 print("done")

@@ -99,7 +99,7 @@ def case_grad(shape, dtype="f32", weight="f32", bias="f32", residual=True, grad=
 
 
 SHAPES = [(1, 1), (3, 1), (1, 2), (5, 7), (2, 8), (4, 9), (3, 63), (7, 64), (2, 511), (6, 512), (5, 513), (3, 1000), (4, 2048), (2, 2049), (3, 4096), (3, 4097),
-          (2, 8192), (2, 8200), (1, 16384), (2, 16385), (1, 32768), (2, 32769), (1, 70001), (300, 40), (1030, 24), (2, 3, 65), (3, 1, 130), (1, 4, 16)]
+          (2, 8192), (2, 8200), (1, 16384), (2, 16385), (1, 32768), (2, 32769), (1, 70001), (300, 40), (1030, 24), (1000, 7), (700, 3), (2, 130, 5), (2, 3, 65), (3, 1, 130), (1, 4, 16)]
 
 
 @gpu
