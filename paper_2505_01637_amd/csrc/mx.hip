@@ -251,8 +251,7 @@ constexpr uint32_t kUnits = 64;            // of four values, in a step
 // The scales of a tile of `groups` groups of 64 lines: 256 bytes for a group and half step.
 struct Scales {
   u32x4 buffer;
-  uint32_t pitch;                          // bytes from a group to the next
-  __device__ __forceinline__ Scales(const uint8_t* scales, uint32_t line, uint32_t lines, uint32_t halves, uint32_t groups) : pitch(halves * 256) {
+  __device__ __forceinline__ Scales(const uint8_t* scales, uint32_t line, uint32_t lines, uint32_t pitch, uint32_t groups) {
     const uint64_t base = (uint64_t)(scales + (uint64_t)(line / 64) * pitch);
     buffer = u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)base), (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(base >> 32) & 0xFFFFu),
                    (uint32_t)__builtin_amdgcn_readfirstlane(min(groups, (lines + 63) / 64 - line / 64) * pitch), 0x27000u};
@@ -263,15 +262,13 @@ constexpr uint32_t kNoHalf = 0x400000;     // beyond any half step
 // are: the byte that happens to follow could be a NaN's.  (Worked out without a branch: with one the loop's products were moved behind its barrier, and a step of
 // 256 x 256 x 256 took 1.88 us instead of 1.70.)
 struct Slot {
-  u32x4 buffer;
   uint32_t offset, odd, halves;
-  __device__ __forceinline__ void init(const Scales& s, uint32_t group, uint32_t half, uint32_t lane) {
-    buffer = s.buffer;
+  __device__ __forceinline__ void init(uint32_t pitch, uint32_t group, uint32_t half, uint32_t lane) {
     odd = half;
-    halves = s.pitch / 256;
-    offset = group * s.pitch + lane * 4;
+    halves = pitch / 256;
+    offset = group * pitch + lane * 4;
   }
-  __device__ __forceinline__ void load(uint32_t half, uint32_t lds) const { load4_to_lds(lds, half + odd < halves ? offset + (half + odd) * 256 : kOutside, buffer); }
+  __device__ __forceinline__ void load(uint32_t half, uint32_t lds, u32x4 buffer) const { load4_to_lds(lds, half + odd < halves ? offset + (half + odd) * 256 : kOutside, buffer); }
 };
 
 // A wave's scales of W of a tile's lines from `first` on, for a half step: four blocks a word.
@@ -282,102 +279,160 @@ __device__ __forceinline__ void read_scales(lds_ptr slots, uint32_t first, uint3
   if (W < 64) s[0] >>= first % 64 / 16 * 8;
 }
 
-// A wave's results through shared memory of its own, PASS blocks of 16 rows at a time, as write_out of tiles.h has them go, but in their order: then what
-// is left to a row's eight columns is its place one row of lanes on.  (Its address worked out anew for each, and the checks of what there is to add, took 14 us more
-// of 8192 x 2048 x 16384.  Straight from the registers, 64 bytes of a row side by side, that is as fast and 8192 x 1024 x 4096 a sixth slower.)
-template <int PASS, int BM, int BN>
+// A wave's results.  A lane has row row_of(i, q) and, of the pair of blocks 2 j, 2 j + 1, the eight columns from 32 j + 8 g on; they are finished in its registers
+// and go 16 rows of 128 bytes at a time through shared memory that is the wave's own (16-byte chunks, at their number xor the row's, against bank conflicts), so
+// that neighbouring lanes store neighbouring bytes.  As sums, before the epilogue (write_out of tiles.h), 4096 x 16384 x 2048 with a residual took 85 us instead of 75, 8192 x 2048 x 16384 177
+// instead of 171; with halves changed between lanes eight apart instead, whole lines but in another order of lanes, rows that start at odd elements take an eighth longer.
+constexpr uint32_t kOut = 16 * 128;
+template <int BM, int BN>
 __device__ __forceinline__ void store_results(const Product& p, const Place& at, uint32_t splits, uint32_t m0, uint32_t n0, uint32_t lane, const f32x4 (&acc)[BM][BN],
                                               char* mine, float* __restrict__ partial) {
-  constexpr uint32_t CHUNKS = BN * 4, GROUPS = BN * 2, ROWS = 64 / GROUPS;      // chunks and groups of 8 columns of a row; rows at a time
-  constexpr uint32_t UNITS = 16 * PASS / ROWS < 4 ? 16 * PASS / ROWS : 4;       // times that, before the first is stored: a branch for all of them
+  constexpr int PAIRS = BN / 2;
   const Epilogue& e = p.e;
-  const uint32_t q = lane & 15, g = lane >> 4;
-  const uint32_t c = lane % GROUPS, n = n0 + c * 8, l = lane / GROUPS;
-  float bias[8];
-  bias8(e, n, n < p.N ? p.N - n : 0, bias);
+  const uint32_t q = lane & 15, g = lane >> 4, n = n0 + 8 * g;
   const uint32_t pitch = (p.N + 7) & ~7u;
   const RowsOf out = splits > 1 ? RowsOf{partial + (uint64_t)at.split * p.batches * p.M * pitch, pitch, (int64_t)p.M * pitch, 0} : e.out;
   const bool ends = splits == 1, residual = ends && e.residual.data, past = ends && goes_past((uint64_t)p.batches * p.M * p.N << (out.bf16 ? 1 : 2));
-  const uint32_t valid = splits > 1 ? 8 : n < p.N ? p.N - n : 0, out_shift = out.bf16 ? 1 : 2, res_shift = e.residual.bf16 ? 1 : 2;
-  char* to = (char*)out.data + (((int64_t)at.batch * out.batch + (int64_t)(m0 + l) * out.ld + n) << out_shift);
-  const char* from = (const char*)e.residual.data + (((int64_t)at.batch * e.residual.batch + (int64_t)(m0 + l) * e.residual.ld + n) << res_shift);
-  const int64_t to_step = ROWS * out.ld << out_shift, from_step = ROWS * e.residual.ld << res_shift;
+  const uint32_t activation = ends ? e.activation : 0, out_shift = out.bf16 ? 1 : 2, width = ends ? p.N : pitch;
+  const auto valid = [&](uint32_t column) { return column < width ? width - column : 0; };
+  float bias[PAIRS][8];
 #pragma unroll
-  for (int h = 0; h < BM; h += PASS) {
+  for (int j = 0; j < PAIRS; j++) {
+    if (ends) bias8(e, n + 32 * j, valid(n + 32 * j), bias[j]);
+    else
 #pragma unroll
-    for (int i = 0; i < PASS; i++) {
-      const uint32_t r = row_of<bf16, true>(i, q);
+      for (int k = 0; k < 8; k++) bias[j][k] = 0.0f;
+  }
+  const char* from = (const char*)e.residual.data + (((int64_t)at.batch * e.residual.batch + (int64_t)m0 * e.residual.ld + n) << (e.residual.bf16 ? 1 : 2));
+  char* to = (char*)out.data + (((int64_t)at.batch * out.batch + (int64_t)m0 * out.ld + n0) << out_shift);
+  const auto store = [&](uint32_t row, uint32_t column, const uint32_t (&w)[4]) {       // 16 bytes
+    const uint32_t left = valid(n0 + column) << out_shift;
+    if (m0 + row >= p.M) return;
+    char* here = to + (((int64_t)row * out.ld + column) << out_shift);
+    if (left >= 16) {
+      if (past) store16_past(here, w);
+      else __builtin_memcpy(here, w, 16);
+    } else {
 #pragma unroll
-      for (int j = 0; j < BN; j++) *(f32x4*)(mine + (r * CHUNKS + ((j / 2 * 8 + 2 * g + j % 2) ^ (r & (CHUNKS - 1)))) * 16) = acc[h + i][j];
-    }
-    asm volatile("" ::: "memory");         // (a wave's accesses to shared memory are done in their order)
-    if (n < p.N) {
-#pragma unroll 1
-      for (uint32_t r = l; r < 16 * PASS; r += UNITS * ROWS) {
-        const uint32_t m = m0 + h * 16 + r;
-        float v[UNITS][8];
-#pragma unroll
-        for (uint32_t u = 0; u < UNITS; u++)
-#pragma unroll
-          for (int x = 0; x < 2; x++) {
-            const uint32_t line = r + u * ROWS;
-            const f32x4 t = *(const f32x4*)(mine + (line * CHUNKS + ((2 * c + x) ^ (line & (CHUNKS - 1)))) * 16);
-#pragma unroll
-            for (int k = 0; k < 4; k++) v[u][4 * x + k] = t[k];
-          }
-        if (ends) {
-#pragma unroll
-          for (uint32_t u = 0; u < UNITS; u++)
-#pragma unroll
-            for (int k = 0; k < 8; k++) v[u][k] += bias[k];
-          const auto activate = [&](uint32_t act) {
-#pragma unroll
-            for (uint32_t u = 0; u < UNITS; u++) activate8(act, v[u]);
-          };
-          if (e.activation == kActRelu) activate(kActRelu);
-          else if (e.activation == kActGelu) activate(kActGelu);
-          else if (e.activation == kActSilu) activate(kActSilu);
-        }
-#pragma unroll
-        for (uint32_t u = 0; u < UNITS; u++) {
-          if (m + u * ROWS >= p.M) break;
-          if (residual) {
-            float y[8];
-            load8(from + u * from_step, e.residual.bf16, 0, valid, y);
-#pragma unroll
-            for (int k = 0; k < 8; k++) v[u][k] += y[k];
-          }
-          if (past && valid >= 8) store8_past(to + u * to_step, out.bf16, 0, v[u]);
-          else store8(to + u * to_step, out.bf16, 0, valid, v[u]);
-        }
-        from += UNITS * from_step;
-        to += UNITS * to_step;
+      for (uint32_t k = 0; k < 4; k++) {
+        if (4 * k + 4 <= left) __builtin_memcpy(here + 4 * k, &w[k], 4);
+        else if (4 * k + 2 <= left) __builtin_memcpy(here + 4 * k, &w[k], 2);
       }
     }
-    asm volatile("" ::: "memory");
+  };
+#pragma unroll
+  for (int i = 0; i < BM; i++) {
+    const uint32_t row = row_of<bf16, true>(i, q);
+    float v[PAIRS][8];
+#pragma unroll
+    for (int j = 0; j < PAIRS; j++)
+#pragma unroll
+      for (int k = 0; k < 8; k++) v[j][k] = acc[i][2 * j + k / 4][k % 4] + bias[j][k];
+    const auto activate = [&](uint32_t act) {
+#pragma unroll
+      for (int j = 0; j < PAIRS; j++) activate8(act, v[j]);
+    };
+    if (activation == kActRelu) activate(kActRelu);
+    else if (activation == kActGelu) activate(kActGelu);
+    else if (activation == kActSilu) activate(kActSilu);
+    if (residual && m0 + row < p.M) {
+      float y[PAIRS][8];
+#pragma unroll
+      for (int j = 0; j < PAIRS; j++) load8(from, e.residual.bf16, (int64_t)row * e.residual.ld + 32 * j, valid(n + 32 * j), y[j]);
+#pragma unroll
+      for (int j = 0; j < PAIRS; j++)
+#pragma unroll
+        for (int k = 0; k < 8; k++) v[j][k] += y[j][k];
+    }
+    // 16 rows of eight chunks of 16 bytes (four, where the wave has no more columns), and of those what a lane stores
+    const auto put = [&](uint32_t chunk, const uint32_t (&w)[4]) { __builtin_memcpy(mine + (q * 8 + (chunk ^ (q & 7))) * 16, w, 16); };
+    const auto go = [&](uint32_t column, uint32_t chunks) {
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (uint32_t h = 0; h < 2; h++) {
+        if (h * 64 >= 16 * chunks) break;
+        const uint32_t r = (lane + h * 64) / chunks, c = lane % chunks;
+        uint32_t w[4];
+        __builtin_memcpy(w, mine + (r * 8 + (c ^ (r & 7))) * 16, 16);
+        store(row_of<bf16, true>(i, r), column + c * (out.bf16 ? 8 : 4), w);
+      }
+      asm volatile("" ::: "memory");
+    };
+    if (out.bf16) {
+#pragma unroll
+      for (int j = 0; j < PAIRS; j++) {
+        bf16 t[8];
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 8; k++) t[k] = (bf16)v[j][k];
+        __builtin_memcpy(w, t, 16);
+        put(j % 2 * 4 + g, w);
+        if (j % 2 || PAIRS == 1) go(32 * (j & ~1), PAIRS == 1 ? 4 : 8);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < PAIRS; j++) {
+        uint32_t w[2][4];
+        __builtin_memcpy(w, v[j], 32);
+        put(2 * g, w[0]);
+        put(2 * g + 1, w[1]);
+        go(32 * j, 8);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);     // (or the next rows' values are worked out first, and kept)
   }
 }
 
-// One tile of TM x TN, WAVES_M x WAVES_N waves, STAGES steps in shared memory: the loop of linear.hip's fast_kernel.  A wave of the 256 tile has 128 x 64.
+// The arguments lie in memory.  All their lines are asked for at once here: as the compiler has it, a few at a time where they are used, several trips there follow each
+// other (8192 x 2048 x 16384 197 us instead of 195, 4096^3 0.7 us more).
+__device__ __forceinline__ void ask_for(const MxProduct& x) {
+  constexpr int LINES = (sizeof(MxProduct) + 63) / 64;
+  uint32_t w[6];
+  static_assert(LINES == 6, "a word of each line");
+#pragma unroll
+  for (int i = 0; i < LINES; i++) __builtin_memcpy(&w[i], (const char*)&x + i * 64, 4);
+  asm volatile("" ::"s"(w[0]), "s"(w[1]), "s"(w[2]), "s"(w[3]), "s"(w[4]), "s"(w[5]));
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// What store_results needs of a product in the arguments' memory.
+typedef const __attribute__((address_space(4))) Product& product_ref;
+__device__ __forceinline__ Product results_of(product_ref p) {
+  const auto rows = [](const __attribute__((address_space(4))) RowsOf& r) { return RowsOf{r.data, r.ld, r.batch, r.bf16}; };
+  Product by{};
+  by.batches = p.batches;
+  by.M = p.M;
+  by.N = p.N;
+  by.e.out = rows(p.e.out);
+  by.e.residual = rows(p.e.residual);
+  by.e.bias = p.e.bias;
+  by.e.bias_bf16 = p.e.bias_bf16;
+  by.e.activation = p.e.activation;
+  return by;
+}
+
+// Tiles of TM x TN, WAVES_M x WAVES_N waves, STAGES steps in shared memory: the loop of linear.hip's fast_kernel.  A wave of the 256 tile has 128 x 64.  Where there are
+// more tiles than run at once, a workgroup has several (two stages: only then every wait of the loop is for all loads under way, results among them): the last steps of a
+// tile load the first ones of the next, and its results leave meanwhile.
 //
-// 8192-cube 247 us, 4450 TFLOP/s, where the matrix units sustain 7600 on operands like these: 208 us without the loads, 219 without the results, 178 without either; they are
-// busy 48 % of the time, shared memory 25 %.  8192 x 2048 x 16384 with GELU 208 us: 130 without the results, whose 268 MB take 52 us of memory's time and whose
-// activation takes 36 (172 without it: an exponential and a reciprocal are a quarter of the rate).  Half steps twice as many ahead (64 bytes of a line at a time) took
-// 274 us for the cube; the second of two smaller workgroups a compute unit started half a tile later, or lines asked for steps before, changed nothing or cost
-// time.
+// 8192-cube 257 us, 4280 TFLOP/s, where the matrix units sustain 7600 on operands like these: they are busy 48 % of the time, shared memory 25 %.  8192 x 2048 x 16384 with GELU
+// 195 us (206 with a workgroup a tile): 109 of products, the results' 268 MB are 52 us of memory's time, the activation takes 32 (163 without it: an exponential and a reciprocal
+// are a quarter of the rate).  Half steps twice as many ahead (64 bytes of a line at a time) took 274 us for the cube where this took 247; the second of two smaller workgroups a
+// compute unit started half a tile later, or lines asked for steps before, changed nothing or cost time.
 template <int TM, int TN, int WAVES_M, int WAVES_N, int STAGES>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void mx_tile_kernel(const MxProduct x, uint32_t steps, uint32_t per_split, uint32_t splits, uint32_t first,
-                                                                         float* __restrict__ partial) {
+                                                                         uint32_t tiles) {
   constexpr int WAVES = WAVES_M * WAVES_N, THREADS = 64 * WAVES, WM = TM / WAVES_M, WN = TN / WAVES_N, BM = WM / 16, BN = WN / 16;
-  constexpr int PASS = BM > 4 ? BM / 2 : BM;
   constexpr int GA = TM / 64, GB = TN / 64, SLOTS = 2 * (GA + GB), EACH = (SLOTS + WAVES - 1) / WAVES;       // 256 bytes of scales; and how many a wave loads
-  constexpr uint32_t CODES = (TM + TN) * kStep, STAGE = CODES + EACH * WAVES * 256, OUT = 16 * PASS * WN * 4;
-  __shared__ __attribute__((aligned(1024))) char lds[STAGES * STAGE];
-  static_assert(WAVES * OUT <= sizeof lds, "the results go where the stages were");
+  constexpr uint32_t CODES = (TM + TN) * kStep, STAGE = CODES + EACH * WAVES * 256;
+  constexpr bool MORE = STAGES == 2;       // a workgroup may have several tiles
+  __shared__ __attribute__((aligned(1024))) char lds[STAGES * STAGE + (MORE ? WAVES * kOut : 0)];
   const Product& p = x.p;
 
-  const Place at = place(first, (p.M + TM - 1) / TM, (p.N + TN - 1) / TN, splits);
-  const uint32_t m0 = at.tm * TM, n0 = at.tn * TN;
+  ask_for(x);
+  const uint32_t tiles_m = (p.M + TM - 1) / TM, tiles_n = (p.N + TN - 1) / TN;
+  Stretch mine(first, tiles);
+  Place at = place_of(mine.id, tiles_m, tiles_n, splits);
   const uint32_t t = threadIdx.x, lane = t & 63, q = lane & 15, g = lane >> 4;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const uint32_t wm = wave / WAVES_N * WM, wn = wave % WAVES_N * WN;
@@ -386,31 +441,45 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void mx_tile_kernel(cons
   Feed<bf16, true, true, TN, THREADS> fb;
   fa.init(p.lda, t);
   fb.init(p.ldb, t);
-  const Scales sa(x.scales_a + (int64_t)at.batch * x.scales_batch_a, m0, p.M, p.K / 32, GA), sb(x.scales_b + (int64_t)at.batch * x.scales_batch_b, n0, p.N, p.K / 32, GB);
+  const uint32_t from = at.split * per_split, end = min(from + per_split, steps), n = end > from ? end - from : 0;
+  const uint32_t pitch = p.K / 32 * 256;   // bytes of scales from 64 lines to the next
   Slot slots[EACH];                // first A's groups, two half steps each, then B's
+  static_assert(2 * GA % EACH == 0, "a wave has slots of one operand");
 #pragma unroll
   for (int i = 0; i < EACH; i++) {
     const uint32_t slot = wave * EACH + i, group = slot / 2;
-    slots[i].init(group < GA ? sa : sb, group < GA ? group : group - GA, slot < SLOTS ? slot & 1 : kNoHalf, lane);
+    slots[i].init(pitch, group < GA ? group : group - GA, slot < SLOTS ? slot & 1 : kNoHalf, lane);
   }
+  // the step to load next and the one that its tile ends before, where that starts in either operand, the bytes that are left behind that, the scales
+  uint32_t step, till;
+  const char *ca, *cb;
+  int64_t left_a, left_b;
+  u32x4 scales;
+  const auto begin = [&](const Place& at) {
+    const uint32_t m0 = at.tm * TM, n0 = at.tn * TN;
+    step = from;
+    till = end;
+    ca = (const char*)p.a + ((int64_t)at.batch * p.batch_a + (int64_t)m0 * p.lda + (int64_t)from * kUnits) * 2;
+    cb = (const char*)p.b + ((int64_t)at.batch * p.batch_b + (int64_t)n0 * p.ldb + (int64_t)from * kUnits) * 2;
+    left_a = ((int64_t)(p.M - m0) * p.lda - (int64_t)from * kUnits) * 2;
+    left_b = ((int64_t)(p.N - n0) * p.ldb - (int64_t)from * kUnits) * 2;
+    const bool of_a = wave * EACH < 2 * GA;
+    scales = Scales((of_a ? x.scales_a : x.scales_b) + (int64_t)at.batch * (of_a ? x.scales_batch_a : x.scales_batch_b), of_a ? m0 : n0, of_a ? p.M : p.N, pitch, of_a ? GA : GB).buffer;
+  };
+  begin(at);
   constexpr int NA = decltype(fa)::N, NB = decltype(fb)::N, LOADS = NA + NB + EACH;
 
-  const uint32_t from = at.split * per_split, end = min(from + per_split, steps), n = end > from ? end - from : 0;
-  // the next step to load: where it starts in either operand, the bytes that are left behind that
-  uint32_t step = from;
-  const char* ca = (const char*)p.a + ((int64_t)at.batch * p.batch_a + (int64_t)m0 * p.lda + (int64_t)from * kUnits) * 2;
-  const char* cb = (const char*)p.b + ((int64_t)at.batch * p.batch_b + (int64_t)n0 * p.ldb + (int64_t)from * kUnits) * 2;
-  int64_t left_a = ((int64_t)(p.M - m0) * p.lda - (int64_t)from * kUnits) * 2, left_b = ((int64_t)(p.N - n0) * p.ldb - (int64_t)from * kUnits) * 2;
   // (behind the last step the buffers have no bytes: zeros are written that nothing uses, and every step has the same loads under way)
-  u32x4 buf_a, buf_b;
+  u32x4 buf_a, buf_b, buf_s;
   uint32_t to, ks, half;
   const auto aim = [&](uint32_t stage) {          // at the next step, to be put into `stage`
-    const bool more = step < end;
+    const bool more = step < till;
     to = (uint32_t)(uintptr_t)(lds_ptr)lds + stage * STAGE;
     ks = p.K - step * kUnits;
     half = more ? step * 2 : kNoHalf;
     buf_a = fa.buffer(ca, more ? left_a : 0);
     buf_b = fb.buffer(cb, more ? left_b : 0);
+    buf_s = scales;                // (the last loads of a step may go out when the next tile has begun)
     const uint32_t on = more ? kStep : 0;
     step += more;
     ca += on;
@@ -421,14 +490,8 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void mx_tile_kernel(cons
   const auto load = [&](int i) {
     if (i < NA) fa.load(i, buf_a, ks, to + wave * 1024, t);
     else if (i < NA + NB) fb.load(i - NA, buf_b, ks, to + TM * kStep + wave * 1024, t);
-    else slots[i - NA - NB].load(half, to + CODES + (wave * EACH + (i - NA - NB)) * 256);
+    else slots[i - NA - NB].load(half, to + CODES + (wave * EACH + (i - NA - NB)) * 256, buf_s);
   };
-  f32x4 acc[BM][BN];
-#pragma unroll
-  for (int i = 0; i < BM; i++)
-#pragma unroll
-    for (int j = 0; j < BN; j++) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-
   constexpr int NM = BM > 4 ? BM / 2 : BM, PHASES = 2 * BM / NM;
   // (4096 x 16384 x 2048 by tiles of 256 x 128 83 us with a step's loads all at once, 77 spread)
   constexpr bool SPREAD = LOADS <= PHASES * NM;      // one beside a part of the products
@@ -448,41 +511,71 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void mx_tile_kernel(cons
       for (int i = 0; i < LOADS; i++) load(i);
     }
     arrive<(STAGES - 1) * LOADS>();
-    read_a((lds_ptr)lds, 0, 0, oa[0]);
-    read_b((lds_ptr)lds, 0);
-    uint32_t cur = 0;
-    for (uint32_t s = 0; s < n; s++) {
-      const uint32_t next = cur + 1 == STAGES ? 0 : cur + 1;
-#pragma unroll
-      for (int ph = 0; ph < PHASES; ph++) {
-        const int then = (ph + 1) % PHASES, kk = then / (PHASES / 2), m = then % (PHASES / 2) * NM;
-        if (ph == PHASES - 1) {
-          arrive<(STAGES - 2) * LOADS>();
-          aim(cur);
-#pragma unroll
-          for (int i = 0; i < (SPREAD ? 0 : LOADS); i++) load(i);
-        }
-        const lds_ptr stage = (lds_ptr)lds + (ph == PHASES - 1 ? next : cur) * STAGE;
-        read_a(stage, m, kk, oa[then & 1]);
-        if (m == 0) read_b(stage, kk);
-#pragma unroll
-        for (int part = 0; part < NM; part++) {
-          const int i = ph % (PHASES / 2) * NM + part, k = ph / (PHASES / 2);
-#pragma unroll
-          for (int j = 0; j < BN; j++) acc[i][j] = multiply(oa[ph & 1][part], ob[k][j], ka[k][i / 4], kb[k][j / 4], i % 4, j % 4, acc[i][j]);
-          // (in the first step, before its barrier, the last stage's loads again: the same bytes to the same place)
-          if (SPREAD && then * NM + part < LOADS) {
-            load(then * NM + part);
-            __builtin_amdgcn_sched_barrier(0);
-          }
-        }
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      cur = next;
-    }
-    arrive<0>();                  // nothing is under way to shared memory when it is given up
   }
-  store_results<PASS>(p, at, splits, m0 + wm, n0 + wn, lane, acc, lds + wave * OUT, partial);
+  uint32_t cur = 0;
+  for (;;) {
+    const bool more = MORE && mine.id + mine.every < mine.end;
+    f32x4 acc[BM][BN];
+#pragma unroll
+    for (int i = 0; i < BM; i++)
+#pragma unroll
+      for (int j = 0; j < BN; j++) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (n) {
+      read_a((lds_ptr)lds + cur * STAGE, 0, 0, oa[0]);
+      read_b((lds_ptr)lds + cur * STAGE, 0);
+    }
+    // (the last steps load the next tile's first ones.  Which tile that is is found between two runs of one loop: selected inside it, 8192^3 took 309 us instead of 257)
+    const uint32_t early = n - min(n, (uint32_t)STAGES);
+    Place behind = at;
+#pragma unroll 1
+    for (uint32_t last = 0; last < (MORE ? 2 : 1); last++) {
+      for (uint32_t s = MORE ? last ? n - early : early : n; s; s--) {
+        const uint32_t next = cur + 1 == STAGES ? 0 : cur + 1;
+#pragma unroll
+        for (int ph = 0; ph < PHASES; ph++) {
+          const int then = (ph + 1) % PHASES, kk = then / (PHASES / 2), m = then % (PHASES / 2) * NM;
+          if (ph == PHASES - 1) {
+            arrive<(STAGES - 2) * LOADS>();
+            aim(cur);
+#pragma unroll
+            for (int i = 0; i < (SPREAD ? 0 : LOADS); i++) load(i);
+          }
+          const lds_ptr stage = (lds_ptr)lds + (ph == PHASES - 1 ? next : cur) * STAGE;
+          read_a(stage, m, kk, oa[then & 1]);
+          if (m == 0) read_b(stage, kk);
+          if (WM >= 64 && WN >= 64) __builtin_amdgcn_sched_barrier(0);      // (the scales of fewer lines are shifted, which would be waited for here)
+#pragma unroll
+          for (int part = 0; part < NM; part++) {
+            const int i = ph % (PHASES / 2) * NM + part, k = ph / (PHASES / 2);
+#pragma unroll
+            for (int j = 0; j < BN; j++) acc[i][j] = multiply(oa[ph & 1][part], ob[k][j], ka[k][i / 4], kb[k][j / 4], i % 4, j % 4, acc[i][j]);
+            // (in the first step, before its barrier, the last stage's loads again: the same bytes to the same place)
+            if (SPREAD && then * NM + part < LOADS) {
+              load(then * NM + part);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        cur = next;
+      }
+      if (MORE && !last) {
+        mine.id += mine.every;
+        till = from;
+        if (more) begin(behind = place_of(mine.id, tiles_m, tiles_n, splits));
+      }
+    }
+    if (!MORE && n) arrive<0>();    // nothing is under way to shared memory where the results go
+    // the arguments and the lane are asked for anew: what is worked out of them for the results would be kept in registers beside the products, and a scalar load that
+    // could still be under way makes every wait for a read of shared memory one for all of them
+    auto again = (const __attribute__((address_space(4))) MxProduct*)__builtin_amdgcn_kernarg_segment_ptr();
+    uint32_t own = lane;
+    asm volatile("" : "+s"(again), "+v"(own));
+    store_results(results_of(again->p), at, splits, at.tm * TM + wm, at.tn * TN + wn, own, acc, lds + (MORE ? STAGES * STAGE : 0) + wave * kOut, again->partial);
+    if (!more) break;
+    at = behind;
+  }
+  if (MORE) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // nor when it is given up
 }
 
 // lhs of a product of few rows that the workgroup puts into blocks itself, in shared memory: `rows` lines of `per` steps, then a byte of scale for each half step,
@@ -543,12 +636,14 @@ __global__ __launch_bounds__(64 * WAVES) void mx_rows_kernel(const MxProduct x, 
   Feed<bf16, true, false, TM, 64> fa;
   Feed<bf16, true, true, TN, 64> fb;
   fb.init(p.ldb, lane);
+  const uint32_t pitch = p.K / 32 * 256;
+  const Scales scales_a(x.scales_a + (int64_t)at.batch * x.scales_batch_a, m0, p.M, pitch, 1), scales_b(x.scales_b + (int64_t)at.batch * x.scales_batch_b, n0, p.N, pitch, 1);
   Slot sa[2], sb[2];
   if (!OWN) fa.init(p.lda, lane);
 #pragma unroll
   for (uint32_t kk = 0; kk < 2; kk++) {
-    if (!OWN) sa[kk].init(Scales(x.scales_a + (int64_t)at.batch * x.scales_batch_a, m0, p.M, p.K / 32, 1), 0, kk, lane);
-    sb[kk].init(Scales(x.scales_b + (int64_t)at.batch * x.scales_batch_b, n0, p.N, p.K / 32, 1), 0, kk, lane);
+    if (!OWN) sa[kk].init(pitch, 0, kk, lane);
+    sb[kk].init(pitch, 0, kk, lane);
   }
   constexpr int LOADS = decltype(fb)::N + 2 + (OWN ? 0 : decltype(fa)::N + 2);
 
@@ -567,13 +662,13 @@ __global__ __launch_bounds__(64 * WAVES) void mx_rows_kernel(const MxProduct x, 
 #pragma unroll
     for (int i = 0; i < fb.N; i++) fb.load(i, buf_b, p.K - s * kUnits, to + A, lane);
 #pragma unroll
-    for (uint32_t kk = 0; kk < 2; kk++) sb[kk].load(half, to + CODES + SA + kk * 256);
+    for (uint32_t kk = 0; kk < 2; kk++) sb[kk].load(half, to + CODES + SA + kk * 256, scales_b.buffer);
     if (!OWN) {
       const u32x4 buf_a = fa.buffer(ca + (int64_t)s * kStep, more ? size_a - (int64_t)s * kStep : 0);
 #pragma unroll
       for (int i = 0; i < fa.N; i++) fa.load(i, buf_a, p.K - s * kUnits, to, lane);
 #pragma unroll
-      for (uint32_t kk = 0; kk < 2; kk++) sa[kk].load(half, to + CODES + kk * 256);
+      for (uint32_t kk = 0; kk < 2; kk++) sa[kk].load(half, to + CODES + kk * 256, scales_a.buffer);
     }
     step += WAVES;
   };
@@ -689,19 +784,27 @@ ProductPlan plan_mx(const MxProduct& x, const MxRows* lhs) {
 bool mx_takes_rows(const MxProduct& x, const ProductPlan& plan, const MxRows& lhs) { return plan.kernel == kRows && fits_own(lhs, x.p.M, plan.per_split); }
 
 hipError_t launch_mx(const MxProduct& x, const ProductPlan& plan, float* partial, hipStream_t st) {
-  return in_launches(plan.blocks, [&](uint64_t first, uint32_t n) {
-    const auto go = [&](auto kernel, uint32_t threads) { kernel<<<n, threads, 0, st>>>(x, plan.steps, plan.per_split, plan.splits, (uint32_t)first, partial); };
-    switch (plan.kernel) {
-      case kFast256: return go(mx_tile_kernel<256, 256, 2, 4, 2>, 512);
-      case kFast256x128: return go(mx_tile_kernel<256, 128, 4, 2, 3>, 512);
-      case kFast128: return go(mx_tile_kernel<128, 128, 2, 2, 2>, 256);
-      case kFast128Alone: return go(mx_tile_kernel<128, 128, 2, 4, 4>, 512);
-      case kFast64: return go(mx_tile_kernel<64, 64, 2, 2, 4>, 256);
-      default:
-        if (!x.lhs.x.data) return go(mx_rows_kernel<4, 3, bf16, false>, 256);
-        return x.lhs.x.bf16 ? go(mx_rows_kernel<4, 3, bf16, true>, 256) : go(mx_rows_kernel<4, 3, float, true>, 256);
-    }
-  });
+  MxProduct by = x;
+  by.partial = partial;
+  const auto tiles = [&](auto kernel, uint32_t threads, uint32_t at_once) {
+    const auto go = [&](uint64_t first, uint32_t n, uint32_t tiles) { kernel<<<n, threads, 0, st>>>(by, plan.steps, plan.per_split, plan.splits, (uint32_t)first, tiles); };
+    if (!at_once || plan.splits > 1 || plan.steps < 2 || plan.blocks <= at_once) return in_launches(plan.blocks, [&](uint64_t first, uint32_t n) { go(first, n, n); });
+    go(0, at_once, (uint32_t)plan.blocks);
+    return hipGetLastError();
+  };
+  const auto rows = [&](auto kernel) {
+    return in_launches(plan.blocks, [&](uint64_t first, uint32_t n) { kernel<<<n, 256, 0, st>>>(x, plan.steps, plan.per_split, plan.splits, (uint32_t)first, partial); });
+  };
+  switch (plan.kernel) {
+    case kFast256: return tiles(mx_tile_kernel<256, 256, 2, 4, 2>, 512, 256);
+    case kFast256x128: return tiles(mx_tile_kernel<256, 128, 4, 2, 3>, 512, 0);
+    case kFast128: return tiles(mx_tile_kernel<128, 128, 2, 2, 2>, 256, 512);
+    case kFast128Alone: return tiles(mx_tile_kernel<128, 128, 2, 4, 4>, 512, 0);
+    case kFast64: return tiles(mx_tile_kernel<64, 64, 2, 2, 4>, 256, 0);
+    default:
+      if (!x.lhs.x.data) return rows(mx_rows_kernel<4, 3, bf16, false>);
+      return x.lhs.x.bf16 ? rows(mx_rows_kernel<4, 3, bf16, true>) : rows(mx_rows_kernel<4, 3, float, true>);
+  }
 }
 
 }  // namespace mrl

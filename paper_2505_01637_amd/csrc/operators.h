@@ -272,6 +272,7 @@ struct MxProduct {
   MxRows lhs;                    // where x.data is given: a's values, which the kernel puts into blocks itself (mx_takes_rows)
   const uint8_t *scales_a, *scales_b;
   int64_t scales_batch_a, scales_batch_b;
+  float* partial;                // (set by launch_mx)
 };
 ProductPlan plan_mx(const MxProduct& p, const MxRows* lhs);       // lhs: a's values, where it is not in blocks yet
 bool mx_takes_rows(const MxProduct& p, const ProductPlan& plan, const MxRows& lhs);

@@ -194,9 +194,7 @@ struct Place { uint32_t tm, tn, split, batch; };
 // Workgroups go to the eight dies in turn, each with an L2 of its own: a die gets a stretch of consecutive tiles, and
 // consecutive tiles are kGroup rows of tiles high, so that the tiles that are worked on at once share rows and columns there.
 constexpr uint32_t kDies = 8, kGroup = 8;
-__device__ __forceinline__ Place place(uint32_t first, uint32_t tiles_m, uint32_t tiles_n, uint32_t splits) {
-  const uint32_t i = blockIdx.x, die = i % kDies, each = gridDim.x / kDies, rest = gridDim.x % kDies;
-  uint32_t id = first + die * each + min(die, rest) + i / kDies;
+__device__ __forceinline__ Place place_of(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, uint32_t splits) {
   const uint32_t tiles = tiles_m * tiles_n, outer = id / tiles;
   id -= outer * tiles;
   Place at;
@@ -207,6 +205,20 @@ __device__ __forceinline__ Place place(uint32_t first, uint32_t tiles_m, uint32_
   at.tm = top + id % high;
   at.tn = id / high;
   return at;
+}
+// A workgroup's stretch of `tiles`: those of its die from `id` to before `end`, of which it takes every `every`-th.
+struct Stretch {
+  uint32_t id, end, every;
+  __device__ __forceinline__ Stretch(uint32_t first, uint32_t tiles) {
+    const uint32_t die = blockIdx.x % kDies, each = tiles / kDies, rest = tiles % kDies;
+    id = first + die * each + min(die, rest);
+    end = id + each + (die < rest);
+    id += blockIdx.x / kDies;
+    every = gridDim.x / kDies + (die < gridDim.x % kDies);       // the workgroups of the die
+  }
+};
+__device__ __forceinline__ Place place(uint32_t first, uint32_t tiles_m, uint32_t tiles_n, uint32_t splits) {
+  return place_of(Stretch(first, gridDim.x).id, tiles_m, tiles_n, splits);
 }
 
 // Four neighbouring columns of a pair of blocks' results, the first (x = 0) or last of the eight that a lane has.

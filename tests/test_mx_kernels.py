@@ -66,6 +66,9 @@ for kernel, m, k, n, split in KERNELS_HERE:
     assert (size > 0) == split, (m, k, n, size)
     got, _ = linear(m, k, n, columns=True)
     assert got.get("mx_quantize_across") == 1, (m, k, n, got)
+for i, (b, m, k, n) in enumerate(SEVERAL_HERE):
+    got, size = linear(m, k, n, blocks=True, b=b)
+    assert got == {"mx_tile_kernelILi256ELi256E" if i < 4 else "mx_tile_kernelILi128ELi128ELi2ELi2E": 1} and size == 0, (b, m, k, n, got)
 # a token: one launch, no workspace, from either type
 for dtype in (0, 1):
     assert linear(1, 2048, 16384, dtype) == ({"mx_rows_kernel": 1}, 0)
@@ -100,12 +103,16 @@ print("done")
 
 
 def test_what_is_launched(tmp_path):
-    run_on_fake_hip(tmp_path, BODY.replace("KERNELS_HERE", repr(KERNELS)))
+    run_on_fake_hip(tmp_path, BODY.replace("KERNELS_HERE", repr(KERNELS)).replace("SEVERAL_HERE", repr(SEVERAL)))
 
 
 def close(got, want, bound, dtype):
     """All on the GPU, in 64 bits: |got - want| <= bound, and a rounding of what is stored."""
     assert ((got.double() - want).abs() <= bound + UNIT[dtype] * (want.abs() + bound) + 1e-37).all()
+
+
+# More tiles than run at once, of 256 x 256 and of 128 x 128; sums of two steps, of a step's part more, and of more.
+SEVERAL = [(1, 8000, 512, 4090), (1, 8192, 520, 4096), (2, 4000, 1030, 4001), (1, 32700, 300, 1000), (1, 4224, 512, 4224), (1, 4190, 700, 4221), (3, 2400, 512, 2408)]
 
 
 @gpu
@@ -125,6 +132,29 @@ def test_every_kernel(kernel, m, k, n, split):
     close(out, z + bias.double() + res.double(), (k + 4) * U * (S + bias.abs().double()) + 2 * U * res.abs().double(), "bf16")
     out = B.mx_linear(x.t().contiguous().t(), w, bias, activation="relu", dtype=torch.float32)
     close(out, (z + bias.double()).clamp(min=0), (k + 4) * U * (S + bias.abs().double()), "f32")
+
+
+@gpu
+@pytest.mark.parametrize("b,m,k,n", SEVERAL)
+def test_several_tiles_a_workgroup(b, m, k, n):
+    """More tiles than run at once: the lines' and blocks' scales differ widely, so that a tile with another's operands or scales is seen."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(m + k)
+
+    def spread(*shape):
+        return torch.randn(shape, generator=gen, device="cuda") * torch.exp2(torch.randint(-9, 10, (*shape[:-1], 1), generator=gen, device="cuda").float())
+
+    x = (spread(b, m, k) * torch.exp2(torch.randint(-3, 4, (b, m, (k + 31) // 32), generator=gen, device="cuda").float()).repeat_interleave(32, -1)[..., :k]).bfloat16()
+    q, w = B.mx_quantize(x), B.mx_quantize(spread(b, n, k).transpose(1, 2) * k ** -0.5, dim=-2)
+    bias, res = torch.randn(n, generator=gen, device="cuda"), torch.randn((b, m, n), generator=gen, device="cuda")
+    many = torch.full((b, m + 1, n), 7.0, device="cuda", dtype=torch.bfloat16)
+    out, full = B.mx_linear(q, w, bias, res, out=many[:, :m]), B.mx_linear(x, w, dtype=torch.float32)
+    assert (many[:, m] == 7.0).all()
+    L, R = B.mx_dequantize(q, dtype=torch.float32).double(), B.mx_dequantize(w, dtype=torch.float32).double()
+    for i in range(b):
+        z, S = L[i] @ R[i].contiguous(), L[i].abs() @ R[i].abs().contiguous()
+        close(full[i], z, (k + 2) * U * S, "f32")
+        close(out[i], z + bias.double() + res[i].double(), (k + 4) * U * (S + bias.abs().double()) + 2 * U * res[i].abs().double(), "bf16")
 
 
 @gpu
