@@ -258,8 +258,8 @@ struct Scales {
   }
 };
 constexpr uint32_t kNoHalf = 0x400000;     // beyond any half step
-// The 256 bytes of a group and a step's first half step (odd = 0) or second (1), as a wave loads them.  A half step that is not there has scales of 0, as its codes
-// are: the byte that happens to follow could be a NaN's.  (Worked out without a branch: with one the loop's products were moved behind its barrier, and a step of
+// The 256 bytes of a group and a step's first half step (odd = 0) or second (1), as a wave loads them.  A half step that is not there has scales of 0
+// (2^-127): the byte that happens to follow could be a NaN's.  (Worked out without a branch: with one the loop's products were moved behind its barrier, and a step of
 // 256 x 256 x 256 took 1.88 us instead of 1.70.)
 struct Slot {
   uint32_t offset, odd, halves;
@@ -415,8 +415,8 @@ __device__ __forceinline__ Product results_of(product_ref p) {
 // more tiles than run at once, a workgroup has several (two stages: only then every wait of the loop is for all loads under way, results among them): the last steps of a
 // tile load the first ones of the next, and its results leave meanwhile.
 //
-// 8192-cube 257 us, 4280 TFLOP/s, where the matrix units sustain 7600 on operands like these: they are busy 48 % of the time, shared memory 25 %.  8192 x 2048 x 16384 with GELU
-// 195 us (206 with a workgroup a tile): 109 of products, the results' 268 MB are 52 us of memory's time, the activation takes 32 (163 without it: an exponential and a reciprocal
+// 8192-cube 252 us, 4360 TFLOP/s, where the matrix units sustain 7600 on operands like these: they are busy 48 % of the time, shared memory 25 %.  8192 x 2048 x 16384 with GELU
+// 191 us (206 with a workgroup a tile): 109 of products, the results' 268 MB are 52 us of memory's time, the activation takes 31 (160 without it: an exponential and a reciprocal
 // are a quarter of the rate).  Half steps twice as many ahead (64 bytes of a line at a time) took 274 us for the cube where this took 247; the second of two smaller workgroups a
 // compute unit started half a tile later, or lines asked for steps before, changed nothing or cost time.
 template <int TM, int TN, int WAVES_M, int WAVES_N, int STAGES>
@@ -471,11 +471,10 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void mx_tile_kernel(cons
 
   // (behind the last step the buffers have no bytes: zeros are written that nothing uses, and every step has the same loads under way)
   u32x4 buf_a, buf_b, buf_s;
-  uint32_t to, ks, half;
+  uint32_t to, half;
   const auto aim = [&](uint32_t stage) {          // at the next step, to be put into `stage`
     const bool more = step < till;
     to = (uint32_t)(uintptr_t)(lds_ptr)lds + stage * STAGE;
-    ks = p.K - step * kUnits;
     half = more ? step * 2 : kNoHalf;
     buf_a = fa.buffer(ca, more ? left_a : 0);
     buf_b = fb.buffer(cb, more ? left_b : 0);
@@ -488,8 +487,10 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void mx_tile_kernel(cons
     left_b -= on;
   };
   const auto load = [&](int i) {
-    if (i < NA) fa.load(i, buf_a, ks, to + wave * 1024, t);
-    else if (i < NA + NB) fb.load(i - NA, buf_b, ks, to + TM * kStep + wave * 1024, t);
+    // (Of a last half step that is not there the next line's codes come.  They are finite and their scales 2^-127 each, so that their products are less than half of any
+    // sum's last bit, which is 2^-149 at least.  Left out by a comparison and two selections a load, 8192^3 took 254 us instead of 252, 4096 x 16384 x 2048 71.6 instead of 69.5.)
+    if (i < NA) load_to_lds(to + wave * 1024 + i * THREADS * 16, fa.offset[i], buf_a);
+    else if (i < NA + NB) load_to_lds(to + TM * kStep + wave * 1024 + (i - NA) * THREADS * 16, fb.offset[i - NA], buf_b);
     else slots[i - NA - NB].load(half, to + CODES + (wave * EACH + (i - NA - NB)) * 256, buf_s);
   };
   constexpr int NM = BM > 4 ? BM / 2 : BM, PHASES = 2 * BM / NM;

@@ -158,6 +158,25 @@ def test_several_tiles_a_workgroup(b, m, k, n):
 
 
 @gpu
+@pytest.mark.parametrize("m,k,n", [(8000, 640, 4090), (4000, 640, 4090), (2000, 900, 2040), (600, 128, 600), (300, 1000, 300), (9, 385, 70)])
+def test_a_line_depends_on_no_other(m, k, n):
+    """An odd number of half steps: what follows a line in memory is the next line, here with values that would be seen."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(k)
+    x, w = torch.randn((m, k), generator=gen, device="cuda"), torch.randn((n, k), generator=gen, device="cuda")
+    x[::7] *= 1e-22                                # (products down to the smallest that there are)
+    w[::5] *= 1e-22
+    want = B.mx_linear(B.mx_quantize(x), B.mx_quantize(w.t(), dim=-2), dtype=torch.float32)
+    x2, w2 = x.clone(), w.clone()
+    x2[1::2] = torch.randn((m // 2, k), generator=gen, device="cuda") * 1e30
+    x2[3::4, 0] = float("nan")
+    w2[1::2] = torch.randn((n // 2, k), generator=gen, device="cuda") * 1e30
+    w2[3::4, 0] = float("inf")
+    got = B.mx_linear(B.mx_quantize(x2), B.mx_quantize(w2.t(), dim=-2), dtype=torch.float32)
+    assert torch.equal(got[::2, ::2], want[::2, ::2]) and torch.isnan(got[3::4]).all() and torch.isnan(got[:, 3::4]).all()
+
+
+@gpu
 @pytest.mark.parametrize("m,n,gap", [(4096, 4096, 0), (4096, 4096, 3), (8000, 2056, 5), (4000, 4099, 0), (130000, 120, 1), (2000, 8200, 0), (1000, 16001, 2)])
 def test_results_past_the_caches(m, n, gap):
     """bf16 results of up to 32 MB, rows at any alignment: nothing beside them is written."""
