@@ -415,7 +415,7 @@ __device__ __forceinline__ Product results_of(product_ref p) {
 // more tiles than run at once, a workgroup has several (two stages: only then every wait of the loop is for all loads under way, results among them): the last steps of a
 // tile load the first ones of the next, and its results leave meanwhile.
 //
-// 8192-cube 252 us, 4360 TFLOP/s, where the matrix units sustain 7600 on operands like these: they are busy 48 % of the time, shared memory 25 %.  8192 x 2048 x 16384 with GELU
+// 8192-cube 252 us, 4360 TFLOP/s, where the matrix units sustain 7600 on operands like these: they are busy 54 % of its cycles, at 1.9 GHz, shared memory 25 %.  8192 x 2048 x 16384 with GELU
 // 191 us (206 with a workgroup a tile): 109 of products, the results' 268 MB are 52 us of memory's time, the activation takes 31 (160 without it: an exponential and a reciprocal
 // are a quarter of the rate).  Half steps twice as many ahead (64 bytes of a line at a time) took 274 us for the cube where this took 247; the second of two smaller workgroups a
 // compute unit started half a tile later, or lines asked for steps before, changed nothing or cost time.
@@ -545,6 +545,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void mx_tile_kernel(cons
           read_a(stage, m, kk, oa[then & 1]);
           if (m == 0) read_b(stage, kk);
           if (WM >= 64 && WN >= 64) __builtin_amdgcn_sched_barrier(0);      // (the scales of fewer lines are shifted, which would be waited for here)
+          __builtin_amdgcn_s_setprio(1);        // (a wave with products goes first; without, 8192^3 takes 1 % longer)
 #pragma unroll
           for (int part = 0; part < NM; part++) {
             const int i = ph % (PHASES / 2) * NM + part, k = ph / (PHASES / 2);
@@ -556,6 +557,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void mx_tile_kernel(cons
               __builtin_amdgcn_sched_barrier(0);
             }
           }
+          __builtin_amdgcn_s_setprio(0);
           __builtin_amdgcn_sched_barrier(0);
         }
         cur = next;
