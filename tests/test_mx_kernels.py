@@ -150,6 +150,8 @@ def test_several_tiles_a_workgroup(b, m, k, n):
     many = torch.full((b, m + 1, n), 7.0, device="cuda", dtype=torch.bfloat16)
     out, full = B.mx_linear(q, w, bias, res, out=many[:, :m]), B.mx_linear(x, w, dtype=torch.float32)
     assert (many[:, m] == 7.0).all()
+    same = res.clone()
+    assert B.mx_linear(q, w, bias, same, out=same) is same and torch.equal(same, B.mx_linear(q, w, bias, res, dtype=torch.float32))
     L, R = B.mx_dequantize(q, dtype=torch.float32).double(), B.mx_dequantize(w, dtype=torch.float32).double()
     for i in range(b):
         z, S = L[i] @ R[i].contiguous(), L[i].abs() @ R[i].abs().contiguous()
