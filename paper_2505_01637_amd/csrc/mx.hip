@@ -582,10 +582,13 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void mx_tile_kernel(cons
 }
 
 // lhs of a product of few rows that the workgroup puts into blocks itself, in shared memory: `rows` lines of `per` steps, then a byte of scale for each half step,
-// quarter of it and line.
-constexpr uint32_t kOwnLhs = 48 * 1024;
+// quarter of it and line.  It has kOwnChunks chunks of eight values at most: more take longer than a launch that puts lhs into blocks once for all (us, here and there: of 1024 chunks
+// 6.1 and 7.6, 2048 7.2 and 7.6, 4096 9.5 and 7.7 for 4, 8 and 16 x 2048 x 16384; 9.8 and 11.9, 11.0 and 11.8, 13.4 and 11.8 for 1, 2 and 4 x 8192 x 8192).
+constexpr uint32_t kOwnChunks = 2048;
 __host__ __device__ constexpr uint32_t own_pitch(uint32_t per) { return per * kStep + 64; }       // (64 more, against bank conflicts)
-__host__ __device__ constexpr uint64_t own_bytes(uint32_t rows, uint32_t per) { return (uint64_t)rows * own_pitch(per) + (uint64_t)per * 2 * 64; }
+__host__ __device__ constexpr uint32_t own_bytes(uint32_t rows, uint32_t per) { return rows * own_pitch(per) + per * 2 * 64; }
+constexpr uint32_t kOwnLhs = own_bytes(1, kOwnChunks / 32);       // (the most that rows * per * 32 chunks take, of one to sixteen rows)
+static_assert(own_bytes(16, kOwnChunks / 512) <= kOwnLhs, "of more rows it is less");
 
 // Eight values a thread, four threads a block, BATCH times before the first is used.  (x.k is at least 8.)
 template <class T>
@@ -753,7 +756,7 @@ float rows_time(uint64_t blocks, uint64_t columns, uint32_t per, uint32_t rows, 
   const float step = std::max(0.15f, 0.0013f * std::min<uint64_t>(columns, 256));
   return 1 + (float)((blocks + 255) / 256) * (2.5f + per * step + (own ? 0.8f * ((rows * per * 32 + 1023) / 1024) : 0));
 }
-bool fits_own(const MxRows& lhs, uint32_t rows, uint32_t per) { return lhs.kc && lhs.k >= 8 && own_bytes(std::min(rows, 16u), per) <= kOwnLhs; }
+bool fits_own(const MxRows& lhs, uint32_t rows, uint32_t per) { return lhs.kc && lhs.k >= 8 && (uint64_t)std::min(rows, 16u) * per * 32 <= kOwnChunks; }
 
 ProductPlan plan_mx(const MxProduct& x, const MxRows* lhs) {
   const Product& p = x.p;
