@@ -306,7 +306,7 @@ __device__ __forceinline__ void store_results(const Product& p, const Place& at,
   const char* from = (const char*)e.residual.data + (((int64_t)at.batch * e.residual.batch + (int64_t)m0 * e.residual.ld + n) << (e.residual.bf16 ? 1 : 2));
   char* to = (char*)out.data + (((int64_t)at.batch * out.batch + (int64_t)m0 * out.ld + n0) << out_shift);
   const auto store = [&](uint32_t row, uint32_t column, const uint32_t (&w)[4]) {       // 16 bytes
-    const uint32_t left = valid(n0 + column) << out_shift;
+    const uint32_t left = bytes_there(valid(n0 + column), out_shift);
     if (m0 + row >= p.M) return;
     char* here = to + (((int64_t)row * out.ld + column) << out_shift);
     if (left >= 16) {

@@ -29,6 +29,10 @@ __device__ __forceinline__ void store16_past(void* to, const void* from) {
   __builtin_memcpy(&w, from, 16);
   __builtin_nontemporal_store(w, (words*)to);
 }
+// Bytes that are there of 16, given the elements of 2^shift bytes that are left of the row: up to 2^31 of them, whose bytes 32 bits do not hold.
+constexpr __host__ __device__ uint32_t bytes_there(uint32_t left, uint32_t shift) { return (left < 16u >> shift ? left : 16u >> shift) << shift; }
+static_assert(bytes_there(1u << 30, 2) == 16 && bytes_there((1u << 30) + 3, 2) == 16 && bytes_there(0x7FFFFFFF, 1) == 16 && bytes_there(3, 2) == 12 && bytes_there(7, 1) == 14 &&
+              bytes_there(0, 1) == 0, "");
 template <class T>
 __device__ __forceinline__ void store8_past(T* p, const float (&v)[8]) {
   T t[8];
