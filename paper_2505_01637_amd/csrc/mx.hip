@@ -756,9 +756,11 @@ float rows_time(uint64_t blocks, uint64_t columns, uint32_t per, uint32_t rows, 
   const float step = std::max(0.15f, 0.0013f * std::min<uint64_t>(columns, 256));
   return 1 + (float)((blocks + 255) / 256) * (2.5f + per * step + (own ? 0.8f * ((rows * per * 32 + 1023) / 1024) : 0));
 }
-bool fits_own(const MxRows& lhs, uint32_t rows, uint32_t per) { return lhs.kc && lhs.k >= 8 && (uint64_t)std::min(rows, 16u) * per * 32 <= kOwnChunks; }
+bool fits_own(uint32_t rows, uint32_t per) { return (uint64_t)std::min(rows, 16u) * per * 32 <= kOwnChunks; }
 
-ProductPlan plan_mx(const MxProduct& x, const MxRows* lhs) {
+// By the sizes alone: the kernel and the splits are the order of the sums, which is to be the same for a lhs in blocks as for one that the call puts into them.  So both
+// are priced as a row-major matrix is.  (One size in eighty would be split otherwise from blocks: 3 x 5250 x 768 takes 7.1 us so and would take 6.3, 2 x 16129 x 4087 12.2 and 13.8.)
+ProductPlan plan_mx(const MxProduct& x) {
   const Product& p = x.p;
   ProductPlan plan{};
   plan.steps = (p.K + kUnits - 1) / kUnits;
@@ -770,11 +772,11 @@ ProductPlan plan_mx(const MxProduct& x, const MxRows* lhs) {
       const uint32_t per = (plan.steps + splits - 1) / splits;
       if (splits > 1 && (per < 4 || tiles * splits > 1024)) break;
       const uint64_t blocks = tiles * splits, rounds = blocks / 512, rest = blocks % 512;
-      const bool own = lhs && k.id == kRows && fits_own(*lhs, p.M, per);
+      const bool own = k.id == kRows && fits_own(p.M, per);
       const float one = k.fixed + per * k.one, two = k.two ? k.fixed + per * k.two : 2 * one;
       float t = k.id == kRows ? rows_time(blocks, columns * splits, per, std::min(p.M, 16u), own) : rounds * two + (rest > 256 ? two : rest ? one : 0);
       if (splits > 1) t += kLaunch1 + (splits + 1) * out / kBytes;
-      if (lhs && !own) t += kQuantize;
+      if (!own) t += kQuantize;
       if (best && t >= best) continue;
       best = t;
       plan.kernel = k.id == kFast128 && blocks <= 256 ? kFast128Alone : k.id;
@@ -787,7 +789,7 @@ ProductPlan plan_mx(const MxProduct& x, const MxRows* lhs) {
   return plan;
 }
 
-bool mx_takes_rows(const MxProduct& x, const ProductPlan& plan, const MxRows& lhs) { return plan.kernel == kRows && fits_own(lhs, x.p.M, plan.per_split); }
+bool mx_takes_rows(const MxProduct& x, const ProductPlan& plan, const MxRows& lhs) { return plan.kernel == kRows && lhs.kc && lhs.k >= 8 && fits_own(x.p.M, plan.per_split); }
 
 hipError_t launch_mx(const MxProduct& x, const ProductPlan& plan, float* partial, hipStream_t st) {
   MxProduct by = x;

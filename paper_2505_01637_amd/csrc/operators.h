@@ -274,7 +274,7 @@ struct MxProduct {
   int64_t scales_batch_a, scales_batch_b;
   float* partial;                // (set by launch_mx)
 };
-ProductPlan plan_mx(const MxProduct& p, const MxRows* lhs);       // lhs: a's values, where it is not in blocks yet
+ProductPlan plan_mx(const MxProduct& p);
 bool mx_takes_rows(const MxProduct& p, const ProductPlan& plan, const MxRows& lhs);
 hipError_t launch_mx(const MxProduct& p, const ProductPlan& plan, float* partial, hipStream_t st);       // without the sum over splits
 

@@ -338,7 +338,7 @@ int32_t plan_mx_linear(const mrl_mx_linear_desc& d, MxPlan* out) {
     g.by.scales_batch_a = sa ? 0 : (int64_t)mx_scale_bytes(p.M, d.k);
     g.by.scales_batch_b = sb ? 0 : (int64_t)mx_scale_bytes(p.N, d.k);
   }
-  g.plan = plan_mx(g.by, g.quantizes ? &g.lhs : nullptr);
+  g.plan = plan_mx(g.by);
   if ((rc = check_product(p, g.plan))) return rc;
   if (g.quantizes && mx_takes_rows(g.by, g.plan, g.lhs)) {
     g.by.lhs = g.lhs;

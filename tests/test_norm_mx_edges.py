@@ -3,6 +3,7 @@ and sums whose order is the same however lhs is given."""
 import pytest
 
 from paper_2505_01637_amd import binding as B
+from test_host_part import run_on_fake_hip
 from test_operators import U
 
 gpu = pytest.mark.gpu
@@ -32,3 +33,66 @@ def test_rows_of_four_gigabytes(n):
     assert ((tail - want[:, :tail.shape[1]]).abs() <= 2 * bound[:, :tail.shape[1]]).all()
     del out, codes, scales, near, tail
     torch.cuda.empty_cache()
+
+
+# (m, k, n) at which a lhs in blocks and one that the call puts into them would be split differently if what the latter costs counted
+APART = [(2, 6152, 1876), (8, 4709, 395), (7, 5403, 192), (5, 14490, 2167), (3, 5690, 3186), (2, 5078, 39), (6, 4800, 669), (6, 10624, 1081), (2, 16129, 4087), (17, 5413, 16)]
+
+HEAD = r"""
+import ctypes as C, math, random, sys
+sys.path.insert(0, sys.argv[2])
+sys.modules["torch"] = None                       # (its own runtime would be loaded first)
+hip = C.CDLL(sys.argv[1], mode=C.RTLD_GLOBAL)
+hip.fake_blocks_of.restype = C.c_uint64
+from paper_2505_01637_amd import binding as B
+lib = B.lib()
+NONE, P = (0, 0, 0, 0, 0), 1 << 20                # (addresses that nothing reads)
+"""
+
+ORDER = HEAD + r"""
+def plan(how, b, m, k, n, shared):
+    # the products' kernel, its workgroups, and the bytes of partial sums
+    lhs = {"blocks": NONE, "columns": (P, 1, 1, m, m * k), "bf16": (P, 1, 0, k, m * k), "f32 and a gap": (P, 0, 0, k + 1, m * (k + 1))}[how]
+    d = B._MX_LINEAR.pack(b, m, k, n, *lhs, *((P, P) if how == "blocks" else (0, 0)), 0, 0, P, P, shared, 0, *NONE, *NONE, P, 1, 0, n, m * n, 0, 0)
+    size = C.c_size_t()
+    assert lib.mrl_mx_linear_bytes(d, C.addressof(size)) == 0, lib.mrl_last_error()
+    hip.fake_blocks_of(b"mx_")
+    hip.fake_launches_of(b"mx_quantize")
+    assert lib.mrl_mx_linear(d, P, size.value, None) == 0, lib.mrl_last_error()
+    up = lambda x: (x + 255) // 256 * 256
+    steps = -(-k // 128)
+    mine = (up(b * m * steps * 64) + up((-(-b * m // 64) if shared else b * -(-m // 64)) * steps * 256)) if hip.fake_launches_of(b"mx_quantize") else 0
+    names = [t for t in ("mx_tile_kernelILi256ELi256E", "mx_tile_kernelILi256ELi128E", "mx_tile_kernelILi128ELi128ELi2ELi2E", "mx_tile_kernelILi128ELi128ELi2ELi4E", "mx_tile_kernelILi64E", "mx_rows_kernel")
+             if hip.fake_launches_of(t.encode())]
+    return names, hip.fake_blocks_of(b"mx_tile") + hip.fake_blocks_of(b"mx_rows"), size.value - mine
+
+r = random.Random(5)
+size = lambda lo, hi: int(math.exp(r.uniform(math.log(lo), math.log(hi))))
+cases = [(1, *c, 0) for c in APART] + [(2, *c, 0) for c in APART]
+for i in range(3000):
+    cases.append((1, size(1, 64 if i % 2 else 8192), size(1, 20000), size(1, 20000), 0))
+for i in range(300):                              # batches with a rhs each, and rows of whole groups of 64 that share one
+    cases.append((r.randint(2, 9), size(1, 300), size(1, 20000), size(1, 5000), 0))
+    cases.append((r.randint(2, 9), 64 * r.randint(1, 5), size(1, 20000), size(1, 5000), 1))
+for case in cases:
+    plans = [plan(how, *case) for how in (("blocks", "bf16", "f32 and a gap") if case[0] > 1 and case[4] else ("blocks", "bf16", "f32 and a gap", "columns"))]
+    assert len(plans[0][0]) == 1 and all(p == plans[0] for p in plans), (case, plans)
+print("done")
+"""
+
+
+def test_sums_have_one_order_however_lhs_is_given(tmp_path):
+    """A lhs in blocks, of either type with its rows' elements adjacent, and with its columns': the same kernel, workgroups and splits."""
+    run_on_fake_hip(tmp_path, ORDER.replace("APART", repr(APART)))
+
+
+@gpu
+@pytest.mark.parametrize("m,k,n", APART)
+def test_the_same_bits_however_lhs_is_given(m, k, n):
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(m + k)
+    x = torch.randn((m, k), generator=gen, device="cuda").bfloat16()
+    w = B.mx_quantize(torch.randn((k, n), generator=gen, device="cuda"), dim=-2)
+    want = B.mx_linear(x, w, dtype=torch.float32)
+    for lhs in (x.float(), x.t().contiguous().t(), B.mx_quantize(x)):
+        assert torch.equal(B.mx_linear(lhs, w, dtype=torch.float32), want)
