@@ -12,6 +12,7 @@ namespace mrl {
 namespace {
 
 constexpr uint32_t kThreads = 1024;        // of a workgroup that goes over a row in passes
+constexpr uint32_t kLaunchRows = kLaunch / (kThreads / 512);       // such workgroups of a launch
 
 // The sums of two values over the workgroup, in every thread.  Their order is that of the threads.
 __device__ __forceinline__ f32x2 sum_block(f32x2 v) {
@@ -705,7 +706,7 @@ hipError_t launch_norm(const NormRows& p, hipStream_t st) {
   if (!p.N || !rows) return hipSuccess;
   const NormPlan g = plan_norm(rows, p.N);
   if (p.N < 8) return in_launches((rows + 255) / 256, [&](uint64_t first, uint32_t n) { norm_few_kernel<<<n, 256, 0, st>>>(p, (uint32_t)first); });
-  if (!g.keep) return in_launches(rows, [&](uint64_t first, uint32_t n) { norm_kernel<<<n, kThreads, 0, st>>>(p, (uint32_t)first); });
+  if (!g.keep) return in_launches(rows, [&](uint64_t first, uint32_t n) { norm_kernel<<<n, kThreads, 0, st>>>(p, (uint32_t)first); }, kLaunchRows);
   if (p.x.bf16) launch_norm_rows<bf16>(p, g, st);
   else launch_norm_rows<float>(p, g, st);
   return hipGetLastError();
@@ -734,7 +735,7 @@ hipError_t launch_norm_grad(const NormGrad& p, float* partial, hipStream_t st) {
     if (e == hipSuccess && p.dx.data && p.N < 8)
       e = in_launches((rows + 255) / 256, [&](uint64_t first, uint32_t n) { norm_grad_few_kernel<<<n, 256, 0, st>>>(p, (uint32_t)first); });
     else if (e == hipSuccess && p.dx.data)
-      e = in_launches(rows, [&](uint64_t first, uint32_t n) { norm_grad_kernel<<<n, kThreads, 0, st>>>(p, (uint32_t)first); });
+      e = in_launches(rows, [&](uint64_t first, uint32_t n) { norm_grad_kernel<<<n, kThreads, 0, st>>>(p, (uint32_t)first); }, kLaunchRows);
   }
   if (e == hipSuccess && sums && g.blocks > 1) {
     norm_sums_kernel<<<(uint32_t)((2ull * p.N + 31) / 32), 1024, 0, st>>>(p, g.blocks, partial);

@@ -9,13 +9,13 @@ namespace mrl {
 namespace {
 
 constexpr int kStep = 128;                 // bytes of a step along k: 64 bf16 or 32 f32
-constexpr uint32_t kLaunch = 1u << 22;     // workgroups of a launch
+constexpr uint32_t kLaunch = 1u << 22;     // workgroups of a launch, of up to 512 threads: it has fewer than 2^32
 
-// Work of `blocks` workgroups in launches of at most kLaunch: f(first, count)
+// Work of `blocks` workgroups in launches of at most `most`: f(first, count)
 template <class F>
-hipError_t in_launches(uint64_t blocks, F&& f) {
-  for (uint64_t at = 0; at < blocks; at += kLaunch) {
-    f(at, (uint32_t)std::min<uint64_t>(kLaunch, blocks - at));
+hipError_t in_launches(uint64_t blocks, F&& f, uint32_t most = kLaunch) {
+  for (uint64_t at = 0; at < blocks; at += most) {
+    f(at, (uint32_t)std::min<uint64_t>(most, blocks - at));
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

@@ -96,3 +96,26 @@ def test_the_same_bits_however_lhs_is_given(m, k, n):
     want = B.mx_linear(x, w, dtype=torch.float32)
     for lhs in (x.float(), x.t().contiguous().t(), B.mx_quantize(x)):
         assert torch.equal(B.mx_linear(lhs, w, dtype=torch.float32), want)
+
+
+MANY = HEAD + r"""
+x = lambda m, n: (P, 1, 0, n, m * n)
+same = lambda n: (P, 1, 0, 0, 0)                  # every row the same memory
+for m, n in (((1 << 22) - 1, 16385), (1 << 22, 16385), (5000000, 16385), ((1 << 23) + 3, 20000), (5000000, 64), (1 << 30, 3)):
+    for t in (x(m, n), same(n)):
+        hip.fake_blocks_of(b"norm_")
+        assert lib.mrl_layer_norm(B._NORM.pack(1, m, n, 1e-5, *t, *x(m, n), *NONE, *NONE, P), None) == 0, (m, n, lib.mrl_last_error())
+        assert n < 8192 or hip.fake_blocks_of(b"norm_") == m, "a workgroup for each long row"
+        for sums in (0, 1):
+            v = (P, 0, 0, 1, 0) if sums else NONE
+            d = B._NORM_GRAD.pack(1, m, n, 0, *t, *t, *NONE, *NONE, *x(m, n), *v, *v, P)
+            size = C.c_size_t()
+            assert lib.mrl_layer_norm_grad_bytes(d, C.addressof(size)) == 0, lib.mrl_last_error()
+            assert lib.mrl_layer_norm_grad(d, P, size.value, None) == 0, (m, n, sums, lib.mrl_last_error())
+print("done")
+"""
+
+
+def test_more_rows_than_a_launch_takes(tmp_path):
+    """A launch has fewer than 2^32 threads (the runtime here holds callers to that): millions of long rows, a workgroup of 1024 each, go in several."""
+    run_on_fake_hip(tmp_path, MANY)
