@@ -546,8 +546,9 @@ int32_t mrl_dropout(const mrl_dropout_desc* desc, void* hip_stream);
  *   out = (x - mean) r weight + bias
  * over each of the b * m rows of n elements.  weight and bias are optional (1 and 0).  stats: 2 f32 a
  * row without gaps, (mean, r) of the row, batch after batch: what the gradient needs; optional.  x, weight, bias and out
- * may each be f32 or bf16.  out may be x itself.  A row that holds an infinity or NaN is NaN; where squares of (x - mean)
- * leave f32's range (magnitudes of 1e19 and more) r is 0. */
+ * may each be f32 or bf16.  out may be x itself.  A row that holds an infinity or NaN is NaN, as is one
+ * whose sum of elements or of (x - mean) leaves f32's range (magnitudes of 1e38 / n and more); where only the sum of (x - mean)^2 does (1e19 / sqrt(n) and
+ * more), r is 0 and the row its bias. */
 typedef struct {
   uint32_t b, m, n;              /* b * m, and each size, below 2^31                               */
   float eps;                     /* finite, not negative                                           */

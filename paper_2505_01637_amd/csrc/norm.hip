@@ -39,6 +39,13 @@ __device__ __forceinline__ int64_t start(const RowsOf& x, uint32_t row, uint32_t
   return (int64_t)batch * x.batch + (int64_t)(row - batch * M) * x.ld;
 }
 
+// 1 / sqrt(var + eps), given the mean of the squares of what `rest` is the mean of.  rest^2 is not rounded, nor infinite, by itself: where the squares' sum is, the
+// variance is infinite and this is 0.  NaN stays.
+__device__ __forceinline__ float inverse(float squares, float rest, float eps) {
+  const float var = __builtin_fmaf(-rest, rest, squares);
+  return 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + eps);
+}
+
 template <int CTRL>
 __device__ __forceinline__ float moved(float x) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xF, 0xF, true)); }
 // The sum over sixteen neighbouring lanes, in each of them.
@@ -203,7 +210,7 @@ __global__ __launch_bounds__(kRowThreads) void norm_rows_kernel(const NormRows p
       }
     }
     s = team.sum(s, sums[1]);
-    const float rest = s[0] * one, var = s[1] * one - rest * rest, r = 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + p.eps);       // (NaN stays)
+    const float rest = s[0] * one, r = inverse(s[1] * one, rest, p.eps);
     if (row >= rows) continue;
     if (p.stats && t == 0) {
       p.stats[2 * row] = about + rest;
@@ -230,7 +237,7 @@ __global__ __launch_bounds__(256) void norm_few_kernel(const NormRows p, uint32_
   if (row >= (uint64_t)p.batches * p.M) return;
   float v[8], w[8];
   load8(p.x.data, p.x.bf16, start(p.x, (uint32_t)row, p.M, p.batches), p.N, v);
-  float about = 0.0f, rest = 0.0f, var = 0.0f;
+  float about = 0.0f, rest = 0.0f, squares = 0.0f;
 #pragma unroll
   for (uint32_t e = 0; e < 7; e++) about += e < p.N ? v[e] : 0.0f;
   about /= (float)p.N;
@@ -238,11 +245,10 @@ __global__ __launch_bounds__(256) void norm_few_kernel(const NormRows p, uint32_
   for (uint32_t e = 0; e < 7; e++) {
     const float d = e < p.N ? v[e] - about : 0.0f;
     rest += d;
-    var += d * d;
+    squares += d * d;
   }
   rest /= (float)p.N;
-  var = var / (float)p.N - rest * rest;
-  const float r = 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + p.eps);
+  const float r = inverse(squares / (float)p.N, rest, p.eps);
   if (p.stats) {
     p.stats[2 * row] = about + rest;
     p.stats[2 * row + 1] = r;
@@ -351,7 +357,7 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(const NormRows p, uint32
     }
   });
   s = sum_block(s);
-  const float rest = s[0] / N, var = s[1] / N - rest * rest, r = 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + p.eps);       // (NaN stays)
+  const float rest = s[0] / N, r = inverse(s[1] / N, rest, p.eps);
   if (p.stats && threadIdx.x == 0) {
     p.stats[2 * (uint64_t)row] = about + rest;
     p.stats[2 * (uint64_t)row + 1] = r;

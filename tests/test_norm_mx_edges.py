@@ -1,10 +1,12 @@
 """Layer normalisation and 4-bit operands at the ends of what the calls take: the widest results, the most rows, the largest values, sizes of zero;
 and sums whose order is the same however lhs is given."""
+import numpy as np
 import pytest
 
 from paper_2505_01637_amd import binding as B
 from test_host_part import run_on_fake_hip
-from test_operators import U
+from test_norm import norm_of
+from test_operators import U, _torch, check, f64
 
 gpu = pytest.mark.gpu
 
@@ -119,3 +121,34 @@ print("done")
 def test_more_rows_than_a_launch_takes(tmp_path):
     """A launch has fewer than 2^32 threads (the runtime here holds callers to that): millions of long rows, a workgroup of 1024 each, go in several."""
     run_on_fake_hip(tmp_path, MANY)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [2, 5, 7, 40, 130, 2048, 3000, 16001, 40000])
+def test_rows_of_large_magnitude(n, dtype):
+    """Rows whose squares' sum leaves f32's range: the mean is right (test_norm.py's tolerance), r is 0 and the row its bias; d_x is then the residual.  Magnitudes of
+    both signs and of one, up to 1e38 / n: sums of n of them, and of n differences of two, are below 2^128.  Rows whose own sum leaves it are NaN."""
+    torch, types = _torch()
+    rng = np.random.default_rng(n)
+    magnitude = np.array([1e15, 1e22, 1e27, 1e33, 0.5e38 / n] * 2).clip(max=0.5e38 / n)
+    x = (1 + rng.random((10, n))) * magnitude[:, None]
+    x[5:] *= np.where(rng.random((5, n)) < 0.5, -1, 1)
+    x[:, 0] *= np.where(x[:, 0] < 0, 1, -1)               # (no row of equal elements)
+    x = torch.from_numpy(x).to(types[dtype]).cuda()
+    w, b = (torch.from_numpy(rng.standard_normal(n)).float().cuda() for _ in range(2))
+    out, stats = B.layer_norm(x, w, b, stats=True, dtype=torch.float32)
+    want, mean, r, bound = norm_of(f64(x), f64(w), f64(b))
+    X, c = f64(x), n / 64 + 32
+    check(stats[:, 0], mean, c * U * np.abs(X - mean[:, None]).mean(-1) + (c * U) ** 2 * np.abs(X).mean(-1), "f32", "mean")
+    for i in (0, 5):
+        check(out[i], want[i], bound[i], "f32", i)
+    large = [1, 2, 3, 4, 6, 7, 8, 9]
+    assert (stats[large, 1] == 0).all() and torch.equal(out[large], b.expand(8, n))
+    grad, res = (torch.from_numpy(rng.standard_normal((10, n))).float().cuda() for _ in range(2))
+    dx, dw, _ = B.layer_norm_grad(grad[large], x[large], stats[large], w, b, res[large])
+    assert torch.equal(dx, res[large].to(types[dtype])) and (dw == 0).all()
+    assert torch.equal(B.layer_norm(x, stats=True)[1], stats)
+    if n >= 40:
+        out, stats = B.layer_norm(torch.full((2, n), 1.5e38, device="cuda").to(types[dtype]), w, b, stats=True)
+        assert out.isnan().all() and stats[:, 1].isnan().all()
