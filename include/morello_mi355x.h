@@ -548,7 +548,7 @@ int32_t mrl_dropout(const mrl_dropout_desc* desc, void* hip_stream);
  * row without gaps, (mean, r) of the row, batch after batch: what the gradient needs; optional.  x, weight, bias and out
  * may each be f32 or bf16.  out may be x itself.  A row that holds an infinity or NaN is NaN, as is one
  * whose sum of elements or of (x - mean) leaves f32's range (magnitudes of 1e38 / n and more); where only the sum of (x - mean)^2 does (1e19 / sqrt(n) and
- * more), r is 0 and the row its bias. */
+ * more), r is 0 and the row its bias.  n of 0: nothing is written. */
 typedef struct {
   uint32_t b, m, n;              /* b * m, and each size, below 2^31                               */
   float eps;                     /* finite, not negative                                           */

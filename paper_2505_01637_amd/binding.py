@@ -830,7 +830,7 @@ def _form_norm(key, x, weight, bias, dtype, out):
 
 def layer_norm(x, weight=None, bias=None, *, eps=1e-5, stats=False, dtype=None, out=None, stream=None):
     """(x - mean) r weight + bias over the last dimension, r = 1 / sqrt(variance + eps) (mrl_layer_norm); with stats=True
-    also (mean, r) of every row, float32 of x's leading dimensions by 2, which layer_norm_grad needs: (out, stats).
+    also (mean, r) of every row, float32 of x's leading dimensions by 2, which layer_norm_grad needs: (out, stats).  Rows of no elements have NaN there.
 
     x: m x n or b x m x n, rows at any stride; weight, bias: n elements, 1 and 0 if None; each float32 or bfloat16.
     dtype: out's type (x's if None); out: a tensor to write to, which may be x itself; stream: as for linear."""
@@ -845,6 +845,8 @@ def layer_norm(x, weight=None, bias=None, *, eps=1e-5, stats=False, dtype=None, 
     if out is None:              # (of a tensor without gaps the same again, which takes torch two thirds of the time)
         out = _empty_like(x) if like else x.new_empty(x.shape, dtype=dtype)
     kept = x.new_empty(x.shape[:-1] + (2,), dtype=_float32) if stats else None
+    if stats and not sizes[2]:   # (the library writes nothing; there is no mean of nothing)
+        kept.fill_(float("nan"))
     desc = _NORM.pack(*sizes, eps, x.data_ptr(), *mx, out.data_ptr(), *mo, 0 if weight is None else weight.data_ptr(), *mw,
                       0 if bias is None else bias.data_ptr(), *mb, kept.data_ptr() if stats else 0)
     rc = lib().mrl_layer_norm(desc, _raw_stream(x.get_device()))

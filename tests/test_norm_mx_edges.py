@@ -152,3 +152,14 @@ def test_rows_of_large_magnitude(n, dtype):
     if n >= 40:
         out, stats = B.layer_norm(torch.full((2, n), 1.5e38, device="cuda").to(types[dtype]), w, b, stats=True)
         assert out.isnan().all() and stats[:, 1].isnan().all()
+
+
+@gpu
+@pytest.mark.parametrize("shape", [(4, 0), (2, 3, 0), (0, 0)], ids=str)
+def test_statistics_of_rows_without_elements(shape):
+    """There is no mean of nothing: NaN, as 0 / 0 is, and not what the memory held."""
+    torch, _ = _torch()
+    filled = torch.full((8, 2), 7.0, device="cuda")
+    del filled                                    # (what torch gives out next)
+    out, stats = B.layer_norm(torch.empty(shape, device="cuda"), stats=True)
+    assert out.shape == shape and stats.shape == shape[:-1] + (2,) and stats.isnan().all()
