@@ -163,3 +163,26 @@ def test_statistics_of_rows_without_elements(shape):
     del filled                                    # (what torch gives out next)
     out, stats = B.layer_norm(torch.empty(shape, device="cuda"), stats=True)
     assert out.shape == shape and stats.shape == shape[:-1] + (2,) and stats.isnan().all()
+
+
+def test_workspace_of_a_gradient_without_a_gpu():
+    """Gradients of many rows ask for their blocks' sums (f32, two for each column) and refuse less, none and what is not aligned; of few rows they ask for nothing.
+    Host code: nothing is launched (the addresses are of nothing)."""
+    import ctypes as C
+    P, lib = 1 << 20, B.lib()
+    vector = (P, 0, 0, 1, 0)
+
+    def grad(m, n, dw=vector, db=vector):
+        x, size = (P, 0, 0, n, m * n), C.c_size_t()
+        d = B._NORM_GRAD.pack(1, m, n, 0, *x, *x, *B._ABSENT, *B._ABSENT, *x, *dw, *db, P)
+        assert lib.mrl_layer_norm_grad_bytes(d, C.addressof(size)) == 0
+        return size.value, lambda work, have: lib.mrl_layer_norm_grad(d, work, have, None)
+
+    for m, n, blocks in ((1 << 16, 16, 256), (8192, 2048, 256), (100, 20000, 2), (1 << 16, 5, 1024)):
+        for dw, db in ((vector, vector), (vector, B._ABSENT), (B._ABSENT, vector)):
+            need, run = grad(m, n, dw, db)
+            assert need == blocks * 2 * n * 4
+            assert run(None, 0) == B.E_NOMEM and run(P, need - 1) == B.E_NOMEM and run(P + 2, need) == B.E_INVAL and run(None, need) == B.E_INVAL
+        assert grad(m, n, B._ABSENT, B._ABSENT)[0] == 0
+    for m, n in ((1, 16), (256, 16), (8, 2048), (0, 16), (64, 20000)):
+        assert grad(m, n)[0] == 0
