@@ -41,14 +41,14 @@ __device__ __forceinline__ void store8_past(T* p, const float (&v)[8]) {
 #pragma unroll
   for (uint32_t i = 0; i < sizeof t / 16; i++) store16_past((char*)p + 16 * i, (const char*)t + 16 * i);
 }
-__device__ __forceinline__ void store8_past(void* data, uint32_t is_bf16, int64_t at, const float (&v)[8]) {
-  if (is_bf16) store8_past((bf16*)data + at, v);
-  else store8_past((float*)data + at, v);
-}
-// Whether results of so many bytes go there.  Up to 32 MB they would all lie in the dies' caches at the end, which are written back before the next launch; 256 MB
-// are more than the cache at the memory holds, so nothing is lost to who reads them next; between the two the reader loses more than is gained.  Past and not,
-// alone, and with mx_quantize of the results behind it, in us: layer_norm to 16 MB 9.2 and 10.2, 17.0 and 17.4; to 32 MB 13.7 and 14.5, 23.1 and 23.3; to 64 MB 23.8 and
-// 25, 44 and 40; mx_linear (k = 512) to 16 MB 9.8 and 11.6, 22 and 26; 32 MB 15 and 16.5, 27.8 and 27.1; 128 MB 56 and 59, 87 and 82; 8192 x 2048 x 16384, 256 MB, 210 and 242, 297 and 306.
+// Whether the results of layer_norm and of products go there, by their bytes: 11 to 32 MB, which would all lie in the dies' caches at the end and be written back before the next
+// launch, and 256 MB and more, which the cache at the memory does not hold; between the two the reader loses more than is gained.  Past and not, alone, and with mx_quantize of the
+// results behind it, in us, operands from memory (those that are in a cache gain a little more):
+//   layer_norm, rows of 2048 in bf16:  6 MB  5.7  6.0  10.8 11.3;  11 MB 8.8 9.2  14.8 16.8;  16 MB 11.0 11.6  18.4 18.4;  24 MB 13.9 14.6  22.1 23.0;  32 MB 17.2 17.4  26.8 25.9;
+//                                      64 MB 29.4 27.5  46.3 42.1;  128 MB 48 47  85 73;  256 MB 111 109  177 171;  320 MB 140 140  221 222
+//   mx_linear, k = 512, 4096 columns:  6 MB  7.1  7.3  12.5 12.9;  11 MB 8.6 9.2  15.8 17.0;  16 MB  9.0 10.3  19.9 22.1;  24 MB 12.3 13.5  25.1 25.3;  32 MB 13.9 15.3  28.2 27.3;
+//                                      64 MB 28.5 25.9  45.2 41.9;  128 MB 45 41  76 67;  256 MB 81.5 77.0  145 146;  320 MB 96 96  172 200
+// So at 32 MB a reader loses 3 %, about what the writer gains, and the gain does not end at 11 MB.  8192 x 2048 x 16384 (256 MB, several tiles a workgroup) 210 and 242, 297 and 306.
 constexpr uint64_t kCaches = 32ull << 20, kBeyond = 256ull << 20;
 __device__ __forceinline__ bool goes_past(uint64_t bytes) { return (bytes >= kCaches / 3 && bytes <= kCaches) || bytes >= kBeyond; }
 
