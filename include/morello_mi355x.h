@@ -596,7 +596,7 @@ typedef struct {
   mrl_mx blocks;
 } mrl_mx_desc;
 int32_t mrl_mx_quantize(const mrl_mx_desc* desc, void* hip_stream);        /* x -> blocks */
-int32_t mrl_mx_dequantize(const mrl_mx_desc* desc, void* hip_stream);      /* blocks -> x, row-major (exact in either type) */
+int32_t mrl_mx_dequantize(const mrl_mx_desc* desc, void* hip_stream);      /* blocks -> x, row-major (exact in either type where it holds the value: magnitudes below 2^128) */
 
 /* out = residual + f(lhs rhs + bias), as mrl_linear, of operands in blocks along k: rhs has n lines, lhs m; where lhs is given
  * as a matrix it is quantised by the call as mrl_mx_quantize does.  Products within a block are exact, sums

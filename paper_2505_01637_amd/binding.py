@@ -902,7 +902,8 @@ class MX:
 
     codes: uint8 of (batch,) lines x 64 ceil(k / 128); scales: uint8 of (batch,) ceil(lines / 64) x ceil(k / 128) x 4 x 16 x 4, both
     without gaps.  dim: the dimension that the blocks run along, -1 (the lines are rows: the tensor is lines x k) or -2 (they are
-    columns: k x lines, as linear's rhs).  dtype: the type that the tensor had and is read back in."""
+    columns: k x lines, as linear's rhs).  dtype: the type that the tensor had and is read back in.  The attributes of one that is made stay as they are
+    (what a call comes to is kept by them); the tensors' elements may change."""
     __slots__ = ("codes", "scales", "k", "dim", "dtype", "shape", "_key")
 
     def __init__(self, codes, scales, k, *, dim=-1, dtype=None):

@@ -416,8 +416,8 @@ __device__ __forceinline__ Product results_of(product_ref p) {
 // tile load the first ones of the next, and its results leave meanwhile.
 //
 // 8192-cube 252 us, 4360 TFLOP/s, where the matrix units sustain 7600 on operands like these: they are busy 54 % of its cycles, at 1.9 GHz, shared memory 25 %.  8192 x 2048 x 16384 with GELU
-// 191 us (206 with a workgroup a tile): 109 of products, the results' 268 MB are 52 us of memory's time, the activation takes 31 (160 without it: an exponential and a reciprocal
-// are a quarter of the rate).  Half steps twice as many ahead (64 bytes of a line at a time) took 274 us for the cube where this took 247; the second of two smaller workgroups a
+// from blocks, one behind the other, 202 us: 162 without the activation (an exponential and a reciprocal are a quarter of the rate), 115 without results, whose 268 MB are 52 us of memory's
+// time; a call that puts lhs into blocks before it takes 197 to 203 in all, and 8 % more with a workgroup a tile.  4096 x 16384 x 2048 with f32 results and a residual 77 us, 65 without results.  Half steps twice as many ahead (64 bytes of a line at a time) took 274 us for the cube where this took 247; the second of two smaller workgroups a
 // compute unit started half a tile later, or lines asked for steps before, changed nothing or cost time.
 template <int TM, int TN, int WAVES_M, int WAVES_N, int STAGES>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void mx_tile_kernel(const MxProduct x, uint32_t steps, uint32_t per_split, uint32_t splits, uint32_t first,
@@ -743,7 +743,7 @@ hipError_t launch_mx_dequantize(const MxRows& p, hipStream_t st) {
 }
 
 // How long a kernel takes, in us, as linear.hip's rule has it: a round of workgroups on the 256 compute units, one each or two at once, is `fixed`
-// and a step's time for each step along k.  Measured on products whose tiles are one whole round (or two at once), 2048 and 16384 long along k, replayed in a graph.
+// and a step's time for each step along k.  Measured on products whose tiles are one whole round (or two at once), 2048 and 16384 long along k, replayed in a graph.  (On another card a step takes 3 to 8 % less throughout: 1.65, 0.97, 0.64 and 1.10, 0.36 and 0.50.)
 struct Kernel { uint32_t id, tm, tn; float fixed, one, two; };
 constexpr Kernel kKernels[] = {
     {kFast256, 256, 256, 12, 1.70f, 0},       {kFast256x128, 256, 128, 10.5f, 1.045f, 0}, {kFast128, 128, 128, 8, 0.666f, 1.13f},
